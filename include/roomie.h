@@ -369,6 +369,156 @@ int roomie_selftest_bounded_wait(uint32_t *status /* device */, uint64_t limit_n
 int roomie_profile_enable(int on);
 int roomie_profile_walk_ms(float *total_ms /* host */, uint32_t *launches /* host */);
 
+/* ======================================================================================================
+ * Serving operators: the cache kernels of a resident language model (the paper has no counterpart).
+ *
+ * The models the placement rule distributes over GPUs have to run there, and how many fit is decided by
+ * their caches.  These calls are one serving step over a paged cache of 8-bit keys and values: rotary
+ * positions, quantise-and-append, attention, and the page operations that share, copy, free and pack cache
+ * memory.  roomie_record_* turns the launches of such a step into the kernel table and times
+ * roomie_library_build takes, so that a real step is scored against other residents like any profile.
+ * The conventions at the top of this file hold: device pointers of the caller, nothing allocated, work is
+ * only enqueued.  Data-dependent errors set sticky bits in the cache's `status` word and skip the access.
+ * ==================================================================================================== */
+
+/* sticky bits of roomie_kv_cache.status */
+#define ROOMIE_FLAG_KV_PAGE 16u       /* a page id outside [0, num_pages) where a page was needed; or a page whose
+                                         reference count is not 1 was appended to, or freed below 0        */
+#define ROOMIE_FLAG_KV_SEQUENCE 32u   /* a sequence index, length or row offset outside its range, a child that is
+                                         not empty, a sequence named twice                                   */
+#define ROOMIE_FLAG_KV_NONFINITE 64u  /* append met NaN (stored as 0) or an infinity (stored as the largest code) */
+#define ROOMIE_FLAG_KV_FULL 128u      /* fork or reserve found too few free pages for some request           */
+
+#define ROOMIE_F32 0
+#define ROOMIE_F16 1
+#define ROOMIE_BF16 2
+
+/* Rows of heads: element (token, head, d) lies at data[token*token_stride + head*head_stride + d]
+ * (strides in elements; any element-aligned address is accepted, 16-byte aligned ones are faster). */
+typedef struct roomie_rows {
+    void *data;
+    int32_t type;         /* ROOMIE_F32 / F16 / BF16 */
+    int64_t token_stride;
+    int64_t head_stride;
+} roomie_rows;
+
+/* Rotary positions.  Pair i of a head's first rotary_dim elements - (i, i + rotary_dim/2), or (2i, 2i+1) when
+ * interleaved - is turned by position * frequency[i] turns and scaled by `amplitude`; the other elements are
+ * copied.  A frequency is a 64-bit fixed-point fraction (2^64 = one whole turn per position), so the product with
+ * a position is exact modulo one turn: the angle does not lose bits at long contexts as a float32 product does. */
+typedef struct roomie_rope_table {
+    uint32_t rotary_dim;       /* even, 2 .. head_dim */
+    int32_t interleaved;
+    float amplitude;
+    const uint64_t *frequency; /* device [rotary_dim/2] */
+} roomie_rope_table;
+
+/* Frequencies base^(-2i/rotary_dim) / (2 pi) turns per position, optionally stretched for contexts `factor` times
+ * the trained one: a frequency that makes at most low_turns turns over `context` positions is divided by factor,
+ * one that makes at least high_turns is kept, in between the two are mixed linearly in the number of turns.
+ * factor = 1: plain; factor > 1 with context = 0: all are divided (linear interpolation).
+ * Host arithmetic only.  Errors: INVALID_ARG (odd or zero rotary_dim, base <= 1, factor < 1,
+ * low_turns >= high_turns with a context). */
+int roomie_rope_frequencies(uint32_t rotary_dim, double base, double factor, double context, double low_turns,
+                            double high_turns, uint64_t *frequency_out /* host [rotary_dim/2] */);
+
+/* y = rope(x) for [tokens][heads][head_dim], positions int32 [tokens]; `inverse` turns back (the gradient: the
+ * transpose of the rotation).  x and y have the same type; y may be x (same strides), otherwise they must not overlap.
+ * Angles and products in float32, rounded once.  Errors: INVALID_ARG, CUDA. */
+int roomie_rope(const roomie_rope_table *table /* host */, const roomie_rows *x, const roomie_rows *y, uint32_t tokens,
+                uint32_t heads, uint32_t head_dim, const int32_t *positions, int inverse, void *stream);
+
+#define ROOMIE_KV_E4M3 0 /* 1-4-3 floats, largest 448 */
+#define ROOMIE_KV_INT8 1 /* -127 .. 127               */
+#define ROOMIE_KV_HND 0  /* a page of one layer is [kv_heads][page_tokens][head_dim] */
+#define ROOMIE_KV_NHD 1  /* ... or [page_tokens][kv_heads][head_dim]                 */
+
+/* A paged cache of 8-bit keys and values with a float32 scale for each page and head: value = code * scale.
+ * Host struct of device arrays.  Limits: page_tokens 16, 32, 64 or 128; head_dim a multiple of 16 up to 256;
+ * code pointers and strides multiples of 16 bytes. */
+typedef struct roomie_kv_cache {
+    uint32_t layers, num_pages, page_tokens, kv_heads, head_dim;
+    int32_t format;              /* ROOMIE_KV_E4M3 / INT8 */
+    int32_t layout;              /* ROOMIE_KV_HND / NHD   */
+    uint32_t max_seqs, max_pages; /* shape of the page table */
+    void *k, *v;                 /* codes of layer 0, page 0 */
+    int64_t layer_stride, page_stride; /* bytes, of k and v alike */
+    float *k_scale, *v_scale;    /* [layers][num_pages][kv_heads] */
+    int32_t *refs;               /* [num_pages] sequences that hold the page; 0 = free */
+    int32_t *pages;              /* [max_seqs][max_pages] page ids, -1 past a sequence's end */
+    int32_t *length;             /* [max_seqs] tokens; 0 = no sequence */
+    uint32_t *status;            /* [1] sticky ROOMIE_FLAG_KV_* bits */
+} roomie_kv_cache;
+
+/* Device scratch for the calls below that take a workspace: enough for any of them on this cache.  It must be zeroed
+ * once before its first use; every call leaves it ready for the next.  0 on invalid arguments. */
+size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
+
+/* Writes the keys and values of new tokens into `layer` of the cache.  Sequence i of the call is row seqs[i] of the
+ * page table; its new tokens are rows [q_offset[i], q_offset[i+1]) of k and v (q_offset NULL: row i alone) and take the
+ * LAST positions of length[seqs[i]], which already counts them (roomie_kv_reserve sets it).  With `rope`, keys are
+ * rotated to those positions first, and `q` ([rows][q_heads][head_dim], may be NULL) is rotated to q_out as well.
+ * Each page and head gets the least power of two s with largest |value| / s within the format (a power of two,
+ * so that a scale that has to grow while a page fills moves e4m3 codes without rounding them a second time; int8 pays
+ * up to one bit for it); the scale of a page that holds earlier tokens never shrinks, and its earlier codes are
+ * rescaled when it grows.  Float32 arithmetic on values of any ROOMIE_ type, rounded once to the code (nearest even).
+ * Errors: INVALID_ARG, CUDA. */
+int roomie_kv_append(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs,
+                     const int32_t *q_offset, uint32_t rows, const roomie_rows *k, const roomie_rows *v,
+                     const roomie_rope_table *rope, uint32_t q_heads, const roomie_rows *q, const roomie_rows *q_out,
+                     void *stream);
+
+/* softmax(scale * q k^T) v over the cached tokens of each sequence.  Query row t of a sequence's n rows sits at position
+ * length - n + t and sees the keys at or before it (and within `window` positions, itself included, when window > 0).
+ * Query head h reads key head h / (q_heads / kv_heads).  Softmax statistics and sums are float32; products take q and
+ * the codes as they are, probabilities are rounded to 11 bits.  A row that sees nothing gives 0 and lse = -inf.
+ *   q, out  [rows][q_heads][head_dim], F16 or BF16, the same type
+ *   lse     [rows][q_heads] float32 natural logarithm of the softmax denominator, may be NULL
+ * q_offset NULL: one row per sequence (rows == num_seqs).  Rows outside every sequence are not written.
+ * Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
+int roomie_kv_attention(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs,
+                        const int32_t *q_offset, uint32_t rows, uint32_t q_heads, const roomie_rows *q, float scale,
+                        uint32_t window, const roomie_rows *out, float *lse, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/* Page operations.  They change refs, pages and length, over all layers at once, and are deterministic: a page that is
+ * needed is the lowest free one, requests are served in order.  A request is served when the free pages cover what it
+ * and the requests before it need; the others change nothing and set ROOMIE_FLAG_KV_FULL.
+ *   reserve  sequence seqs[i] gets pages for want[i] tokens (never fewer than it has) and that length;
+ *   fork     child children[i] (empty) becomes a copy of parents[i]: whole pages are shared, a part-filled last page is
+ *            copied, codes and scales; parents are taken as they were before the call;
+ *   free     the sequences become empty; their pages lose a reference;
+ *   copy     page src_pages[i] of src to page dst_pages[i] of dst, codes and scales of all layers (n pairs; the caches
+ *            agree in layers, page_tokens, kv_heads, head_dim, format and layout; no page may be written twice, or both
+ *            read and written); tables and counts are left alone;
+ *   compact  with U pages in use, the i-th used page at or past U moves to the i-th free page before U, so that pages
+ *            [U, num_pages) are free and their memory can be given back.  refs_out and pages_out (same shapes as the
+ *            cache's) receive the new counts and table and may be the cache's own; used_out[1] = U, may be NULL.
+ * Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
+int roomie_kv_reserve(const roomie_kv_cache *cache /* host */, const int32_t *seqs, const int32_t *want, uint32_t n,
+                      void *workspace, size_t workspace_bytes, void *stream);
+int roomie_kv_fork(const roomie_kv_cache *cache /* host */, const int32_t *parents, const int32_t *children, uint32_t n,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int roomie_kv_free(const roomie_kv_cache *cache /* host */, const int32_t *seqs, uint32_t n, void *stream);
+int roomie_kv_copy(const roomie_kv_cache *src /* host */, const int32_t *src_pages, const roomie_kv_cache *dst /* host */,
+                   const int32_t *dst_pages, uint32_t n, void *stream);
+int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out, int32_t *pages_out, int32_t *used_out,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Launches of the serving operators as a profile.  While enabled (capacity > 0), the calling thread's serving calls note
+ * each kernel launch - grid, block, registers, shared memory - and bracket it with CUDA events.  roomie_record_read
+ * synchronises on them, writes at most `capacity` records in launch order, stores their number and forgets them:
+ * grid_blocks .. smem_per_block are the columns of roomie_kernel_table, dur_us and gap_us the times of
+ * roomie_library_build (gap: from the launch's end to the next one's start; 0 for the last).  Launches beyond the enabled
+ * capacity are not noted.  roomie_record_enable(0) destroys the events. */
+typedef struct roomie_launch {
+    char name[32];
+    uint32_t grid_blocks, block_threads, regs_per_thread, smem_per_block;
+    float dur_us, gap_us;
+} roomie_launch;
+int roomie_record_enable(uint32_t capacity);
+int roomie_record_read(roomie_launch *out /* host */, uint32_t capacity, uint32_t *count /* host */);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,7 +4,8 @@ Thin Python binding over ``libroomie.so`` (C ABI declared in ``include/roomie.h`
 argument marshalling only.  Every step of the path - occupancy (Section 3.1, Eq. 1), the
 pairwise alignment walk with median and overlap factor (Section 3.2, Algorithm 1), the
 greedy multi-model estimate and argmin placement (Algorithm 2) - runs in the library's CUDA
-kernels.  PyTorch supplies device memory and streams, nothing else.
+kernels.  PyTorch supplies device memory and streams, nothing else.  ``serving`` binds the operators of a
+resident language model's step (rotary positions, paged 8-bit cache, attention over it, page operations).
 
 There is no CPU fallback: importing this package without the compiled library raises.
 """
@@ -15,3 +16,7 @@ from .roomie import (  # noqa: F401
     selftest_bounded_wait, lib_path, EXPORTS,
 )
 from .shard import partition_pairs, combine_shards, pair_matrix_sharded  # noqa: F401,E402
+from .serving import (  # noqa: F401,E402
+    RopeTable, KVCache, rope_frequencies, rope, kv_append, kv_attention, kv_reserve, kv_fork, kv_free, kv_copy, kv_compact,
+    record_launches, profile_columns,
+)

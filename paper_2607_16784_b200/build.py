@@ -9,7 +9,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libroomie.so")
-SOURCES = ["roomie_api.cu", "roomie_library.cu", "roomie_pairs.cu", "roomie_place.cu", "roomie_optimal.cu"]
+SOURCES = ["roomie_api.cu", "roomie_library.cu", "roomie_pairs.cu", "roomie_place.cu", "roomie_optimal.cu",
+           "roomie_serving.cu", "roomie_kv_append.cu", "roomie_kv_attention.cu", "roomie_kv_pages.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--fmad=true", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
@@ -26,14 +27,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    objs = []
-    for src in SOURCES:
+    objs, running = [], []
+    for src in SOURCES:                                   # one compiler per source, side by side
         obj = os.path.join(CSRC, src.replace(".cu", ".o"))
         cmd = [nvcc, *NVCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             cmd.insert(1, "-Xptxas=-v")
-        subprocess.check_call(cmd)
+        running.append((cmd, subprocess.Popen(cmd)))
         objs.append(obj)
+    failed = [(p.returncode, cmd) for cmd, p in running if p.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(*failed[0])
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([nvcc, "-shared", "-o", tmp, *objs, "-lcudart"])
     os.replace(tmp, LIB)

@@ -1,0 +1,604 @@
+// Attention over the paged 8-bit cache.
+//
+// o_i = sum_j p_ij * vs[page(j)] * v_j / sum_j p_ij,  p_ij = exp(scale * ks[page(j)] * q_i.k_j - max)  over the keys j that row i sees.
+#include "roomie_kv.cuh"
+
+namespace roomie {
+
+struct AttnArgs {
+    KvView c;
+    const int32_t *seqs, *q_offset;
+    uint32_t num_seqs, rows, q_heads, group;     // group = q_heads / kv heads
+    const void* q;
+    void* out;
+    float* lse;
+    long long q_token, q_head, o_token, o_head;
+    float scale_log2;                            // scale * log2(e)
+    uint32_t window;
+    int32_t q_aligned, o_aligned;                // 16-byte rows
+    uint32_t* counters;                          // [blocks] zero between calls
+    float* partial;                              // [blocks][2] of (rows x (DP + 2))
+};
+
+constexpr float kLn2 = 0.693147180559945309417f;
+constexpr int kAttnWarps = 4, kAttnThreads = 32 * kAttnWarps;
+constexpr int kMaxAttnBlocksPerSm = 4;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 16x8x16 product, float16 operands, float32 sums
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// four codes of a word to two float16 pairs, exactly (elements 0,1 and 2,3)
+template <int kFormat> __device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (kFormat == ROOMIE_KV_E4M3) {
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+            : "=r"(lo), "=r"(hi) : "r"(w));
+    } else {
+        // 0x6400 | u is 1024 + u in float16; u = code + 128
+        const uint32_t u = w ^ 0x80808080u, bias = 0x64806480u;                   // 1152
+        const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(reinterpret_cast<const __half2&>(l), reinterpret_cast<const __half2&>(bias));
+        const __half2 y = __hsub2(reinterpret_cast<const __half2&>(h), reinterpret_cast<const __half2&>(bias));
+        lo = reinterpret_cast<const uint32_t&>(x);
+        hi = reinterpret_cast<const uint32_t&>(y);
+    }
+}
+
+// The flat order of the call's work: sequence, key head, row tile, key block.  What one sequence contributes:
+struct SeqWork {
+    KvSeq s;
+    uint32_t first_block, blocks, tiles;     // key blocks [first_block, first_block + blocks), row tiles
+};
+template <int kBlock, int kRows>
+__device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool report) {
+    SeqWork w;
+    w.s = kv_seq(a.c, a.seqs, a.q_offset, a.rows, i, report);
+    w.tiles = (w.s.count * a.group + kRows - 1) / kRows;
+    const int start = (int)w.s.length - (int)w.s.count;                  // negative: leading rows that see nothing
+    const int lowest = a.window ? max(start - (int)a.window + 1, 0) : 0; // first key that some row may see
+    w.first_block = (uint32_t)max(min(lowest, (int)w.s.length), 0) / kBlock;
+    const uint32_t end = (w.s.length + kBlock - 1) / kBlock;
+    w.blocks = max(end > w.first_block ? end - w.first_block : 0u, 1u);  // a sequence without keys still writes its rows
+    return w;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+// Few rows a key head (a decoding step: `group` rows for each new token).  Bound by the bytes of the codes, so every code goes from
+// global memory straight into registers, once, and no shared memory is touched until the end.  The products are taken transposed
+// (S^T = K q^T, o^T = V^T p^T), so that keys and values are the 16-row operand and the 8 rows of a GQA group fill the 8-wide one.
+// The contraction index of a matrix product may be permuted freely, and so may the rows of its result: a lane takes 4 bytes of its
+// own contiguous span of a key for each k-step (lane quarter c of a token holds dims [c*DP/4, +DP/4)), and of a value row the dims
+// [r*DP/8, +DP/8) for its result rows r.  Both are whole 16-byte loads, and a warp's loads cover whole rows.
+//
+// A block walks a contiguous part of the flat order; its warps take the 16*kGroups-key steps in turn and meet at each
+// (sequence, head, tile).  A part that does not hold all of a (sequence, head, tile) leaves its sums in the workspace, and the last
+// part to arrive adds them in order.
+template <int DP, int NT, int kFormat, class T>
+struct FewRows {
+    static constexpr int kGroups = DP > 128 ? 1 : 2;               // 16-key groups a warp step
+    static constexpr int kStep = 16 * kGroups;
+    static constexpr int kBlock = kStep * kAttnWarps;              // keys of a flat unit
+    static constexpr int kRows = 8 * NT;
+    static constexpr int KS = DP / 16;
+    static constexpr int KW = DP / 16;                             // words of a lane's key span
+    static constexpr int VW = DP / 32;                             // words of a lane's value span
+    static constexpr int kPartial = kRows * (DP + 2);              // floats of one partial result
+};
+
+// 4*N bytes at p; `dims` limits them to the head's real size (a multiple of 16)
+template <int N>
+__device__ __forceinline__ void load_span(uint32_t* to, const uint8_t* p, uint32_t first_dim, uint32_t dim, bool on) {
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (on && first_dim + 4 * i < dim)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p + 4 * i));
+            to[i] = x.x; to[i + 1] = x.y; to[i + 2] = x.z; to[i + 3] = x.w;
+        }
+    } else {
+        uint2 x = make_uint2(0, 0);
+        if (on && first_dim < dim)
+            asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
+        to[0] = x.x; to[1] = x.y;
+    }
+}
+
+template <class T> __device__ __forceinline__ float load_elem(const T* p) { return to_f32(*p); }
+
+template <int DP, int NT, int kFormat, class T>
+__global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_rows_kernel(AttnArgs a) {
+    using F = FewRows<DP, NT, kFormat, T>;
+    constexpr int G = F::kGroups, KW = F::KW, VW = F::VW, KS = F::KS;
+    extern __shared__ float sm[];                                  // [warps][rows][DP] sums, then [warps][rows][2] max and total
+    __shared__ unsigned long long sh_sum[kAttnWarps + 1];
+    __shared__ uint32_t sh_at[4];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+    const KvView& kv = a.c;
+
+    // ---- where this block's part begins -------------------------------------------------------------------------------
+    unsigned long long mine = 0;
+    for (uint32_t i = threadIdx.x; i < a.num_seqs; i += kAttnThreads) {
+        const SeqWork w = seq_work<F::kBlock, F::kRows>(a, i, blockIdx.x == 0);
+        mine += (unsigned long long)w.tiles * w.blocks * kv.heads;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if (lane == 0) sh_sum[wid] = mine;
+    __syncthreads();
+    unsigned long long total = 0;
+    for (int w = 0; w < kAttnWarps; ++w) total += sh_sum[w];
+    if (total == 0) return;
+    const unsigned long long parts = total < gridDim.x ? total : gridDim.x;
+    if (blockIdx.x >= parts) return;
+    unsigned long long at = total * blockIdx.x / parts;
+    const unsigned long long end = total * (blockIdx.x + 1) / parts;
+
+    uint32_t seq = 0;                                              // the sequence that holds `at`, and the flat index it begins at
+    unsigned long long seq_first = 0;
+    {
+        unsigned long long before = 0;
+        for (uint32_t base = 0; base < a.num_seqs; base += kAttnThreads) {
+            const uint32_t i = base + threadIdx.x;
+            unsigned long long n = 0;
+            if (i < a.num_seqs) {
+                const SeqWork w = seq_work<F::kBlock, F::kRows>(a, i, false);
+                n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+            }
+            unsigned long long incl = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            __syncthreads();
+            if (lane == 31) sh_sum[wid] = incl;
+            __syncthreads();
+            unsigned long long ahead = before, all = 0;
+            for (int w = 0; w < kAttnWarps; ++w) {
+                if (w < wid) ahead += sh_sum[w];
+                all += sh_sum[w];
+            }
+            const unsigned long long first = ahead + incl - n;
+            if (n && at >= first && at < first + n) {
+                sh_at[0] = i;
+                sh_sum[kAttnWarps] = first;
+            }
+            before += all;
+            if (at < before) break;
+        }
+        __syncthreads();
+        seq = sh_at[0];
+        seq_first = sh_sum[kAttnWarps];
+    }
+
+    while (at < end) {
+        SeqWork w = seq_work<F::kBlock, F::kRows>(a, seq, false);
+        unsigned long long n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+        while (at >= seq_first + n) {                              // sequences without rows contribute nothing
+            seq_first += n;
+            if (++seq >= a.num_seqs) return;                       // lengths changed under the call
+            w = seq_work<F::kBlock, F::kRows>(a, seq, false);
+            n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+        }
+        const unsigned long long inside = at - seq_first;
+        const uint32_t head = (uint32_t)(inside / ((unsigned long long)w.tiles * w.blocks));
+        const uint32_t rest = (uint32_t)(inside - (unsigned long long)head * w.tiles * w.blocks);
+        const uint32_t tile = rest / w.blocks, b0 = rest - tile * w.blocks;
+        const uint32_t b1 = (uint32_t)min((unsigned long long)w.blocks, (unsigned long long)b0 + (end - at));
+        const KvSeq& s = w.s;
+        const int start = (int)s.length - (int)s.count;
+        const uint32_t rows = s.count * a.group - tile * F::kRows;  // of this tile: min(rows, kRows)
+
+        // ---- queries: operand b of S^T; row r of the tile, dims as the lane's keys ---------------------------------------
+        uint32_t qf[NT][KS][2];
+        float qscale[NT][2];
+        int see_hi[NT][2], see_lo[NT][2];                          // row n sees keys [lo, hi)
+        int tile_hi = 0, tile_lo = 0x7fffffff, all_hi = 0x7fffffff, all_lo = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t rr = t * 8 + r;
+            const bool on = rr < rows;
+            const uint32_t row = tile * F::kRows + rr, tok = row / a.group;
+            const T* q = static_cast<const T*>(a.q) + (long long)(s.row + tok) * a.q_token +
+                         (long long)(head * a.group + row - tok * a.group) * a.q_head + c * (DP / 4);
+            float x[DP / 4];
+            float amax = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DP / 4; ++d) x[d] = 0.0f;
+            if (on) {
+                if (a.q_aligned) {
+#pragma unroll
+                    for (int d = 0; d < DP / 4; d += 8)
+                        if (c * (DP / 4) + d < kv.dim) unpack<T>(*reinterpret_cast<const uint4*>(q + d), x + d);
+                } else {
+#pragma unroll
+                    for (int d = 0; d < DP / 4; ++d)
+                        if (c * (DP / 4) + d < kv.dim) x[d] = load_elem(q + d);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DP / 4; ++d) amax = fmaxf(amax, fabsf(x[d]));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            // To float16 with the row's largest magnitude in [1, 2): exact for float16 and bfloat16 queries but for elements below
+            // 2^-14 of it, which lose at most 2^-25 of it.
+            int e = (int)(__float_as_uint(amax) >> 23) - 127;
+            e = max(min(e, 126), -126);
+            const float down = pow2f(-e);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const __half2 lo = __floats2half2_rn(x[4 * i] * down, x[4 * i + 1] * down);
+                const __half2 hi = __floats2half2_rn(x[4 * i + 2] * down, x[4 * i + 3] * down);
+                qf[t][i][0] = reinterpret_cast<const uint32_t&>(lo);
+                qf[t][i][1] = reinterpret_cast<const uint32_t&>(hi);
+            }
+            const float up = pow2f(e) * a.scale_log2;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {                          // rows 2c and 2c+1 are the lane's result columns
+                qscale[t][n] = __shfl_sync(0xffffffffu, up, (2 * c + n) * 4);
+                const uint32_t rc = t * 8 + 2 * c + n;
+                const int pos = start + (int)((tile * F::kRows + rc) / a.group);
+                int hi = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
+                int lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
+                if (lo > hi) lo = hi;
+                see_hi[t][n] = hi;
+                see_lo[t][n] = lo;
+                tile_hi = max(tile_hi, hi);
+                if (rc < rows) {
+                    if (hi > lo) tile_lo = min(tile_lo, lo);
+                    all_hi = min(all_hi, hi);
+                    all_lo = max(all_lo, lo);
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 4; d <<= 1) {
+            tile_hi = max(tile_hi, __shfl_xor_sync(0xffffffffu, tile_hi, d));
+            tile_lo = min(tile_lo, __shfl_xor_sync(0xffffffffu, tile_lo, d));
+            all_hi = min(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, d));
+            all_lo = max(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, d));
+        }
+
+        float o[NT][KS][4];
+        float m[NT][2], l[NT][2];
+        float vref = 0.0f;                                         // o is in units of this value scale
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][i][e] = 0.0f;
+            m[t][0] = m[t][1] = -INFINITY;
+            l[t][0] = l[t][1] = 0.0f;
+        }
+
+        // the warp's steps: keys [k0, k0 + kStep) of this tile's blocks that some row sees
+        const int part_lo = (int)((w.first_block + b0) * F::kBlock), part_hi = (int)min((w.first_block + b1) * F::kBlock, s.length);
+        int lo_key = max(part_lo, tile_lo / F::kStep * F::kStep), hi_key = min(part_hi, tile_hi);
+        if (lo_key >= hi_key) lo_key = hi_key = 0;
+        const int32_t* table = kv.pages + (size_t)s.slot * kv.max_pages;
+        const uint32_t row_step = kv.token_step;
+        const long long head_off = (long long)head * kv.head_step;
+
+        uint32_t kr[G][2][KW], vr[G][4][VW];
+        int32_t page[G], next_page[G];
+        auto get_pages = [&](int k0, int32_t* to) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int k = k0 + 16 * g;
+                int32_t id = -1;
+                if (k < hi_key) {
+                    id = __ldg(table + (k >> kv.page_shift));
+                    if ((uint32_t)id >= kv.num_pages) {
+                        if (lane == 0) kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
+                        id = -1;
+                    }
+                }
+                to[g] = id;
+            }
+        };
+        auto get_keys = [&](int k0, const int32_t* pg) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int k = k0 + 16 * g;
+                const uint8_t* p = kv.k + (long long)pg[g] * kv.page_stride + head_off + (k & (kv.page_tokens - 1)) * row_step + c * (DP / 4);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    load_span<KW>(kr[g][h], p + (r + 8 * h) * row_step, c * (DP / 4), kv.dim, pg[g] >= 0 && k + r + 8 * h < hi_key);
+            }
+        };
+        int k0 = lo_key + ((wid - lo_key / F::kStep) & (kAttnWarps - 1)) * F::kStep;   // warp w takes steps w mod 4
+        get_pages(k0, page);
+        get_keys(k0, page);
+        for (; k0 < hi_key; k0 += F::kBlock) {
+            float ks[G], vs[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {                          // values of this step, on their way while S is worked out
+                const int k = k0 + 16 * g;
+                const uint8_t* p = kv.v + (long long)page[g] * kv.page_stride + head_off + (k & (kv.page_tokens - 1)) * row_step + r * (DP / 8);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int tok = 2 * c + (h & 1) + 8 * (h >> 1);
+                    load_span<VW>(vr[g][h], p + tok * row_step, r * (DP / 8), kv.dim, page[g] >= 0 && k + tok < hi_key && k + tok >= tile_lo);
+                }
+                ks[g] = vs[g] = 0.0f;
+                if (page[g] >= 0) {
+                    ks[g] = __ldg(kv.k_scale + (size_t)page[g] * kv.heads + head);
+                    vs[g] = __ldg(kv.v_scale + (size_t)page[g] * kv.heads + head);
+                }
+            }
+            get_pages(k0 + F::kBlock, next_page);
+            float sc[G][NT][4];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[g][t][e] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    uint32_t a0, a1, a2, a3;
+                    codes_to_f16<kFormat>(kr[g][0][i], a0, a2);
+                    codes_to_f16<kFormat>(kr[g][1][i], a1, a3);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma16816(sc[g][t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
+                }
+            }
+            get_keys(k0 + F::kBlock, next_page);
+
+            // softmax over the step: sc[e] is key r + 8*(e >> 1) of the group, row 2c + (e & 1)
+            bool whole = k0 >= all_lo && k0 + F::kStep <= all_hi;
+#pragma unroll
+            for (int g = 0; g < G; ++g) whole = whole && page[g] >= 0;
+            float vmax = vref;
+#pragma unroll
+            for (int g = 0; g < G; ++g) vmax = fmaxf(vmax, vs[g]);
+            const float inv_vref = vmax > 0.0f ? __fdividef(1.0f, vmax) : 0.0f;
+            bool moved = vmax != vref;
+            float old_m[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float f = qscale[t][n] * ks[g];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float& x = sc[g][t][2 * h + n];
+                            x *= f;
+                            if (!whole) {
+                                const int k = k0 + 16 * g + 8 * h + r;
+                                if (k >= see_hi[t][n] || k < see_lo[t][n] || page[g] < 0) x = -INFINITY;
+                            }
+                            mx = fmaxf(mx, x);
+                        }
+                    }
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    old_m[t][n] = m[t][n];
+                    if (mx > m[t][n]) { m[t][n] = mx; moved = true; }
+                }
+            if (__any_sync(0xffffffffu, moved)) {
+                const float v = vref * inv_vref;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const float f = old_m[t][n] == -INFINITY ? 0.0f : exp2_fast(old_m[t][n] - m[t][n]);
+                        l[t][n] *= f;
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) {
+                            o[t][i][n] *= f * v;
+                            o[t][i][n + 2] *= f * v;
+                        }
+                    }
+                vref = vmax;
+            }
+            // probabilities; p * vs / vref <= 1 is rounded to float16 (11 bits) for the product with the codes, the total is not
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float f = vs[g] * inv_vref;
+                uint32_t pb[NT][2];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float m0 = m[t][0] == -INFINITY ? 0.0f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.0f : m[t][1];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float p0 = exp2_fast(sc[g][t][2 * h] - m0), p1 = exp2_fast(sc[g][t][2 * h + 1] - m1);
+                        l[t][0] += p0;
+                        l[t][1] += p1;
+                        const __half2 x = __floats2half2_rn(p0 * f, p1 * f);
+                        pb[t][h] = transpose8x8(reinterpret_cast<const uint32_t&>(x));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < VW; ++j) {
+                    uint32_t a0[4], a1[4];                         // [result-row pair of the word's four dims]
+                    codes_to_f16<kFormat>(__byte_perm(vr[g][0][j], vr[g][1][j], 0x5140), a0[0], a0[1]);
+                    codes_to_f16<kFormat>(__byte_perm(vr[g][0][j], vr[g][1][j], 0x7362), a0[2], a0[3]);
+                    codes_to_f16<kFormat>(__byte_perm(vr[g][2][j], vr[g][3][j], 0x5140), a1[0], a1[1]);
+                    codes_to_f16<kFormat>(__byte_perm(vr[g][2][j], vr[g][3][j], 0x7362), a1[2], a1[3]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        mma16816(o[t][2 * j], a0[0], a0[1], a1[0], a1[1], pb[t][0], pb[t][1]);
+                        mma16816(o[t][2 * j + 1], a0[2], a0[3], a1[2], a1[3], pb[t][0], pb[t][1]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) page[g] = next_page[g];
+        }
+
+        // ---- the warps meet --------------------------------------------------------------------------------------------
+        float* sm_ml = sm + kAttnWarps * F::kRows * DP;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[t][n] += __shfl_xor_sync(0xffffffffu, l[t][n], d);
+                const int row = t * 8 + 2 * c + n;
+                if (r == 0) {
+                    sm_ml[(wid * F::kRows + row) * 2] = m[t][n];
+                    sm_ml[(wid * F::kRows + row) * 2 + 1] = l[t][n];
+                }
+                float* to = sm + (size_t)(wid * F::kRows + row) * DP + r * (DP / 8);
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    to[2 * i] = o[t][i][n] * vref;
+                    to[2 * i + 1] = o[t][i][n + 2] * vref;
+                }
+            }
+        __syncthreads();
+
+        const unsigned long long item = at - b0, item_end = item + w.blocks;
+        const bool complete = b0 == 0 && b1 == w.blocks;
+        const uint32_t n_rows = min(rows, (uint32_t)F::kRows);
+        auto put = [&](uint32_t row, uint32_t d, float mx, float sum, float value) {
+            const uint32_t rr = tile * F::kRows + row, tok = rr / a.group, h = head * a.group + rr - tok * a.group;
+            if (d < kv.dim)
+                (static_cast<T*>(a.out) + (long long)(s.row + tok) * a.o_token + (long long)h * a.o_head)[d] =
+                    from_f32<T>(sum > 0.0f ? value / sum : sum == 0.0f ? 0.0f : sum);
+            if (a.lse && d == 0) a.lse[(size_t)(s.row + tok) * a.q_heads + h] = sum > 0.0f ? (mx + log2f(sum)) * kLn2 : sum == 0.0f ? -INFINITY : sum;
+        };
+        float* part = a.partial + ((size_t)blockIdx.x * 2 + (b0 == 0 ? 1 : 0)) * F::kPartial;
+        for (uint32_t x = threadIdx.x; x < n_rows * DP; x += kAttnThreads) {
+            const uint32_t row = x / DP, d = x - row * DP;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < kAttnWarps; ++v) mx = fmaxf(mx, sm_ml[(v * F::kRows + row) * 2]);
+            float sum = 0.0f, value = 0.0f;
+#pragma unroll
+            for (int v = 0; v < kAttnWarps; ++v) {
+                const float mv = sm_ml[(v * F::kRows + row) * 2];
+                const float f = mv == -INFINITY ? 0.0f : exp2f(mv - mx);
+                sum += f * sm_ml[(v * F::kRows + row) * 2 + 1];
+                value += f * sm[(size_t)(v * F::kRows + row) * DP + d];
+            }
+            if (complete) {
+                put(row, d, mx, sum, value);
+            } else {
+                part[row * DP + d] = value;
+                if (d == 0) {
+                    part[F::kRows * DP + 2 * row] = mx;
+                    part[F::kRows * DP + 2 * row + 1] = sum;
+                }
+            }
+        }
+        if (!complete) {
+            // the parts that share this item are consecutive blocks: first holds its first unit, last its last
+            const uint32_t first = (uint32_t)(((item + 1) * parts - 1) / total), last = (uint32_t)((item_end * parts - 1) / total);
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const uint32_t before = atomicAdd(a.counters + first, 1u);
+                sh_at[1] = before == last - first;
+                if (before == last - first) a.counters[first] = 0;
+            }
+            __syncthreads();
+            if (sh_at[1]) {
+                __threadfence();
+                for (uint32_t x = threadIdx.x; x < n_rows * DP; x += kAttnThreads) {
+                    const uint32_t row = x / DP, d = x - row * DP;
+                    float mx = -INFINITY, sum = 0.0f, value = 0.0f;
+                    for (uint32_t b = first; b <= last; ++b) {
+                        const float* p = a.partial + ((size_t)b * 2 + (b == first ? 1 : 0)) * F::kPartial;
+                        const float mb = __ldcg(p + F::kRows * DP + 2 * row), lb = __ldcg(p + F::kRows * DP + 2 * row + 1), vb = __ldcg(p + row * DP + d);
+                        const float to = fmaxf(mx, mb);
+                        const float f0 = mx == -INFINITY ? 0.0f : exp2f(mx - to), f1 = mb == -INFINITY ? 0.0f : exp2f(mb - to);
+                        sum = sum * f0 + lb * f1;
+                        value = value * f0 + vb * f1;
+                        mx = to;
+                    }
+                    put(row, d, mx, sum, value);
+                }
+            }
+        }
+        __syncthreads();
+        at += b1 - b0;
+    }
+}
+
+size_t kv_attention_bytes(const roomie_kv_cache* c) {
+    const uint32_t dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
+    const size_t bytes = blocks * sizeof(uint32_t) + 256 + blocks * 2 * (16 * (size_t)(dp + 2)) * sizeof(float);
+    return (bytes + 255) / 256 * 256;
+}
+
+template <int DP, int NT, int kFormat, class T>
+static int launch_few(const AttnArgs& a, cudaStream_t st) {
+    using F = FewRows<DP, NT, kFormat, T>;
+    const uint32_t per_sm = DP > 128 || NT > 1 ? 2 : 3;
+    const size_t smem = (size_t)kAttnWarps * F::kRows * (DP + 2) * sizeof(float);
+    return launch("kv_attention", few_rows_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * per_sm), dim3(kAttnThreads), smem, st,
+                  false, a);
+}
+template <int DP, int kFormat, class T>
+static int launch_rows(const AttnArgs& a, bool eight, cudaStream_t st) {
+    return eight ? launch_few<DP, 1, kFormat, T>(a, st) : launch_few<DP, 2, kFormat, T>(a, st);
+}
+template <int kFormat, class T>
+static int launch_dim(const AttnArgs& a, bool eight, cudaStream_t st) {
+    if (a.c.dim <= 64) return launch_rows<64, kFormat, T>(a, eight, st);
+    if (a.c.dim <= 128) return launch_rows<128, kFormat, T>(a, eight, st);
+    return launch_rows<256, kFormat, T>(a, eight, st);
+}
+template <class T>
+static int launch_format(const AttnArgs& a, bool eight, cudaStream_t st) {
+    return a.c.format == ROOMIE_KV_E4M3 ? launch_dim<ROOMIE_KV_E4M3, T>(a, eight, st) : launch_dim<ROOMIE_KV_INT8, T>(a, eight, st);
+}
+
+}  // namespace roomie
+
+using namespace roomie;
+
+extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer, const int32_t* seqs, uint32_t num_seqs,
+                                   const int32_t* q_offset, uint32_t rows, uint32_t q_heads, const roomie_rows* q, float scale,
+                                   uint32_t window, const roomie_rows* out, float* lse, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+    if (kv_check(cache) != ROOMIE_OK || layer >= cache->layers || !rows_valid(q) || !rows_valid(out) || q->type != out->type ||
+        q->type == ROOMIE_F32 || q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !(scale < INFINITY) ||
+        window > 0x7fffffffu)
+        return ROOMIE_ERR_INVALID_ARG;
+    if (num_seqs == 0 || rows == 0) return ROOMIE_OK;
+    if (!seqs || (!q_offset && rows != num_seqs) || num_seqs > 0x3fffffffu || (unsigned long long)rows * q_heads > 0x3fffffffull)
+        return ROOMIE_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ROOMIE_ERR_INVALID_ARG;
+    if (workspace_bytes < roomie_kv_workspace_bytes(cache)) return ROOMIE_ERR_CAPACITY;
+    AttnArgs a = {};
+    a.c = kv_view(cache, layer);
+    a.seqs = seqs; a.q_offset = q_offset; a.num_seqs = num_seqs; a.rows = rows;
+    a.q_heads = q_heads; a.group = q_heads / cache->kv_heads;
+    a.q = q->data; a.out = out->data; a.lse = lse;
+    a.q_token = q->token_stride; a.q_head = q->head_stride; a.o_token = out->token_stride; a.o_head = out->head_stride;
+    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.window = window;
+    a.q_aligned = rows_aligned16(*q, rows, q_heads);
+    a.o_aligned = rows_aligned16(*out, rows, q_heads);
+    a.counters = static_cast<uint32_t*>(workspace);
+    const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
+    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (blocks * sizeof(uint32_t) + 255) / 256 * 256);
+    const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;      // rows a sequence and key head, on average
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return q->type == ROOMIE_F16 ? launch_format<__half>(a, eight, st) : launch_format<__nv_bfloat16>(a, eight, st);
+}

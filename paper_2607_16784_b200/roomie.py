@@ -22,6 +22,9 @@ EXPORTS = [
     "roomie_multi_estimate", "roomie_place", "roomie_place_batch", "roomie_optimal_workspace_bytes",
     "roomie_optimal_assignment", "roomie_assignment_cost", "roomie_strerror", "roomie_last_cuda_error",
     "roomie_launch_count", "roomie_reset_launch_count", "roomie_profile_enable", "roomie_profile_walk_ms",
+    "roomie_rope_frequencies", "roomie_rope", "roomie_kv_workspace_bytes", "roomie_kv_append", "roomie_kv_attention",
+    "roomie_kv_reserve", "roomie_kv_fork", "roomie_kv_free", "roomie_kv_copy", "roomie_kv_compact",
+    "roomie_record_enable", "roomie_record_read",
 ]
 
 
@@ -67,6 +70,20 @@ def _load():
                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     dll.roomie_place_batch.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
                                        C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    p, u32 = C.c_void_p, C.c_uint32
+    dll.roomie_rope_frequencies.argtypes = [u32] + [C.c_double] * 5 + [p]
+    dll.roomie_rope.argtypes = [p, p, p, u32, u32, u32, p, C.c_int, p]
+    dll.roomie_kv_workspace_bytes.restype = C.c_size_t
+    dll.roomie_kv_workspace_bytes.argtypes = [p]
+    dll.roomie_kv_append.argtypes = [p, u32, p, u32, p, u32, p, p, p, u32, p, p, p]
+    dll.roomie_kv_attention.argtypes = [p, u32, p, u32, p, u32, u32, p, C.c_float, u32, p, p, p, C.c_size_t, p]
+    dll.roomie_kv_reserve.argtypes = [p, p, p, u32, p, C.c_size_t, p]
+    dll.roomie_kv_fork.argtypes = [p, p, p, u32, p, C.c_size_t, p]
+    dll.roomie_kv_free.argtypes = [p, p, u32, p]
+    dll.roomie_kv_copy.argtypes = [p, p, p, p, u32, p]
+    dll.roomie_kv_compact.argtypes = [p, p, p, p, p, C.c_size_t, p]
+    dll.roomie_record_enable.argtypes = [u32]
+    dll.roomie_record_read.argtypes = [p, u32, p]
     return dll
 
 
