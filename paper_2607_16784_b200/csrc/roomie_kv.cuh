@@ -46,13 +46,14 @@ __device__ __forceinline__ KvSeq kv_seq(const KvView& c, const int32_t* seqs, co
     return s;
 }
 
-// least power of two s with amax / s <= 448 (e4m3) or 127 (int8), within 2^-100 .. 2^120: from the bits of amax
+// least power of two s with amax / s <= 448 (e4m3) or 127 (int8), from 2^-100 (values below 2^-101 of
+// which are as good as zero) to 2^122 (the largest float needs no more): from the bits of amax
 __device__ __forceinline__ int kv_scale_exponent(float amax, int32_t format) {
     const uint32_t bits = __float_as_uint(amax);
     const int e = (int)(bits >> 23) - 126;                                // amax = m * 2^e, m in [1/2, 1)
     const uint32_t m = bits & 0x7fffffu;
     int x = format == ROOMIE_KV_E4M3 ? e - 9 + (m > 0x600000u) : e - 7 + (m > 0x7e0000u);   // 448 = 0.875 * 2^9
-    return x < -100 ? -100 : x > 120 ? 120 : x;
+    return x < -100 ? -100 : x > 122 ? 122 : x;
 }
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 

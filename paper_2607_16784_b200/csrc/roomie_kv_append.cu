@@ -272,14 +272,15 @@ extern "C" int roomie_kv_append(const roomie_kv_cache* cache, uint32_t layer, co
                                 const int32_t* q_offset, uint32_t rows, const roomie_rows* k, const roomie_rows* v,
                                 const roomie_rope_table* rope, uint32_t q_heads, const roomie_rows* q, const roomie_rows* q_out,
                                 void* stream) {
-    if (kv_check(cache) != ROOMIE_OK || layer >= cache->layers || !rows_valid(k) || !rows_valid(v) || k->type != v->type)
+    if (kv_check(cache) != ROOMIE_OK || layer >= cache->layers) return ROOMIE_ERR_INVALID_ARG;
+    if (num_seqs == 0 || rows == 0) return ROOMIE_OK;
+    if (!rows_valid(k) || !rows_valid(v) || k->type != v->type)
         return ROOMIE_ERR_INVALID_ARG;
     if (rope && !rope_table_valid(rope, cache->head_dim)) return ROOMIE_ERR_INVALID_ARG;
     if ((q != nullptr) != (q_out != nullptr)) return ROOMIE_ERR_INVALID_ARG;
     if (q && (!rope || q_heads == 0 || !rows_valid(q) || !rows_valid(q_out) || q->type != q_out->type || q->type != k->type ||
               (q->data == q_out->data && (q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride))))
         return ROOMIE_ERR_INVALID_ARG;
-    if (num_seqs == 0 || rows == 0) return ROOMIE_OK;
     if (!seqs || (!q_offset && rows != num_seqs) || rows > 0x3fffffffu || num_seqs > 0x3fffffffu ||
         (q && (unsigned long long)rows * q_heads > 0x7fffffffull))
         return ROOMIE_ERR_INVALID_ARG;

@@ -576,11 +576,11 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
                                    const int32_t* q_offset, uint32_t rows, uint32_t q_heads, const roomie_rows* q, float scale,
                                    uint32_t window, const roomie_rows* out, float* lse, void* workspace, size_t workspace_bytes,
                                    void* stream) {
-    if (kv_check(cache) != ROOMIE_OK || layer >= cache->layers || !rows_valid(q) || !rows_valid(out) || q->type != out->type ||
-        q->type == ROOMIE_F32 || q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) || !(scale < INFINITY) ||
-        window > 0x7fffffffu)
+    if (kv_check(cache) != ROOMIE_OK || layer >= cache->layers || q_heads == 0 || q_heads % cache->kv_heads || !(scale > 0.0f) ||
+        !(scale < INFINITY) || window > 0x7fffffffu)
         return ROOMIE_ERR_INVALID_ARG;
     if (num_seqs == 0 || rows == 0) return ROOMIE_OK;
+    if (!rows_valid(q) || !rows_valid(out) || q->type != out->type || q->type == ROOMIE_F32) return ROOMIE_ERR_INVALID_ARG;
     if (!seqs || (!q_offset && rows != num_seqs) || num_seqs > 0x3fffffffu || (unsigned long long)rows * q_heads > 0x3fffffffull)
         return ROOMIE_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ROOMIE_ERR_INVALID_ARG;
