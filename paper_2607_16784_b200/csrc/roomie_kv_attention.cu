@@ -1,62 +1,11 @@
 // Attention over the paged 8-bit cache.
 //
 // o_i = sum_j p_ij * vs[page(j)] * v_j / sum_j p_ij,  p_ij = exp(scale * ks[page(j)] * q_i.k_j - max)  over the keys j that row i sees.
-#include "roomie_kv.cuh"
+#include "roomie_kv_attention.cuh"
 
 namespace roomie {
 
-struct AttnArgs {
-    KvView c;
-    const int32_t *seqs, *q_offset;
-    uint32_t num_seqs, rows, q_heads, group;     // group = q_heads / kv heads
-    const void* q;
-    void* out;
-    float* lse;
-    long long q_token, q_head, o_token, o_head;
-    float scale_log2;                            // scale * log2(e)
-    uint32_t window;
-    int32_t q_aligned, o_aligned;                // 16-byte rows
-    uint32_t* counters;                          // [blocks] zero between calls
-    float* partial;                              // [blocks][2] of (rows x (DP + 2))
-};
-
-constexpr float kLn2 = 0.693147180559945309417f;
 constexpr int kAttnWarps = 4, kAttnThreads = 32 * kAttnWarps;
-constexpr int kMaxAttnBlocksPerSm = 4;
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// 16x8x16 product, float16 operands, float32 sums
-__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-
-// four codes of a word to two float16 pairs, exactly (elements 0,1 and 2,3)
-template <int kFormat> __device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    if constexpr (kFormat == ROOMIE_KV_E4M3) {
-        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-            : "=r"(lo), "=r"(hi) : "r"(w));
-    } else {
-        // 0x6400 | u is 1024 + u in float16; u = code + 128
-        const uint32_t u = w ^ 0x80808080u, bias = 0x64806480u;                   // 1152
-        const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
-        const __half2 x = __hsub2(reinterpret_cast<const __half2&>(l), reinterpret_cast<const __half2&>(bias));
-        const __half2 y = __hsub2(reinterpret_cast<const __half2&>(h), reinterpret_cast<const __half2&>(bias));
-        lo = reinterpret_cast<const uint32_t&>(x);
-        hi = reinterpret_cast<const uint32_t&>(y);
-    }
-}
 
 // The flat order of the call's work: sequence, key head, row tile, key block.  What one sequence contributes:
 struct SeqWork {
@@ -541,7 +490,8 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
 size_t kv_attention_bytes(const roomie_kv_cache* c) {
     const uint32_t dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
-    const size_t bytes = blocks * sizeof(uint32_t) + 256 + blocks * 2 * (16 * (size_t)(dp + 2)) * sizeof(float);
+    const size_t few = blocks * 2 * (16 * (size_t)(dp + 2)) * sizeof(float), many = prompt_partial_bytes(c->head_dim);
+    const size_t bytes = blocks * sizeof(uint32_t) + 256 + (few > many ? few : many);
     return (bytes + 255) / 256 * 256;
 }
 
@@ -600,5 +550,6 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
     a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (blocks * sizeof(uint32_t) + 255) / 256 * 256);
     const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;      // rows a sequence and key head, on average
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((unsigned long long)rows * a.group > 32ull * num_seqs) return launch_prompt(a, q->type == ROOMIE_F16, st);
     return q->type == ROOMIE_F16 ? launch_format<__half>(a, eight, st) : launch_format<__nv_bfloat16>(a, eight, st);
 }

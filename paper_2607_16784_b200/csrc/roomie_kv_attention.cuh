@@ -1,0 +1,63 @@
+// What the attention kernels over the paged 8-bit cache share.
+#pragma once
+#include "roomie_kv.cuh"
+
+namespace roomie {
+
+struct AttnArgs {
+    KvView c;
+    const int32_t *seqs, *q_offset;
+    uint32_t num_seqs, rows, q_heads, group;     // group = q_heads / kv heads
+    const void* q;
+    void* out;
+    float* lse;
+    long long q_token, q_head, o_token, o_head;
+    float scale_log2;                            // scale * log2(e)
+    uint32_t window;
+    int32_t q_aligned, o_aligned;                // 16-byte rows
+    uint32_t* counters;                          // [blocks] zero between calls
+    float* partial;                              // [blocks][2] of (rows x (DP + 2))
+};
+
+constexpr float kLn2 = 0.693147180559945309417f;
+constexpr int kMaxAttnBlocksPerSm = 4;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// 16x8x16 product, float16 operands, float32 sums
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// four codes of a word to two float16 pairs, exactly (elements 0,1 and 2,3)
+template <int kFormat> __device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (kFormat == ROOMIE_KV_E4M3) {
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+            : "=r"(lo), "=r"(hi) : "r"(w));
+    } else {
+        // 0x6400 | u is 1024 + u in float16; u = code + 128
+        const uint32_t u = w ^ 0x80808080u, bias = 0x64806480u;                   // 1152
+        const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(reinterpret_cast<const __half2&>(l), reinterpret_cast<const __half2&>(bias));
+        const __half2 y = __hsub2(reinterpret_cast<const __half2&>(h), reinterpret_cast<const __half2&>(bias));
+        lo = reinterpret_cast<const uint32_t&>(x);
+        hi = reinterpret_cast<const uint32_t&>(y);
+    }
+}
+
+// roomie_kv_prompt.cu: many rows a sequence, on the tensor cores' own memory
+int launch_prompt(const AttnArgs& a, bool half, cudaStream_t st);
+size_t prompt_partial_bytes(uint32_t dim);
+
+}  // namespace roomie
