@@ -7,7 +7,8 @@
 //   softmax          a thread owns a row: reads S, writes the probabilities as float16 over the columns it has read
 //   o += p V         p from tensor memory, V from shared memory, o in tensor memory
 // Warpgroups 0 and 1 are the softmax of tiles 0 and 1, so that one tile's softmax overlaps the other's products; warpgroup 2
-// turns codes into float16 operands (the scales stay out of them); one thread of warpgroup 3 issues the products.
+// turns codes into float16 operands (the scales stay out of them); in warpgroup 3 one thread issues the products and one warp
+// looks up pages and scales, some steps ahead.
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
 // Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M the running maximum of s + log2 vs, is what multiplies
@@ -228,10 +229,13 @@ template <int kRows> __device__ bool walk_start(const AttnArgs& a, Walk& w, unsi
 }
 
 // ---- shared state -----------------------------------------------------------------------------------------------------------
+constexpr int kRing = 8;                            // steps whose pages and scales are looked up ahead
 struct PromptShared {
-    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], scales[4], join[2], drain;
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], look_full[kRing], look_free[kRing], join[2],
+        drain;
     unsigned long long walk[20];
-    float ks[4][8], lvs[4][8], ivs[4][8];           // of 16 keys each: key scale, log2 and inverse of the value scale
+    int32_t page[kRing][8];                         // of 16 keys each: page (-1: none), key scale, log2 and inverse of the value scale
+    float ks[kRing][8], lvs[kRing][8], ivs[kRing][8];
     float q_scale[2][256];                          // of a row, segments in turn: 2^e of its float16 form times scale * log2(e)
     uint32_t tmem, last, failed;
 };
@@ -319,27 +323,15 @@ __device__ void feed(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w)
         mbar_arrive(&sh.q_full);
         ++seg;
 
-        const int32_t* table = kv.pages + (size_t)s.p.s.slot * kv.max_pages;
         const long long head_off = (long long)s.head * kv.head_step + 16 * unit;
         const int hi_key = (int)min((s.first + s.count) * kKeys, s.p.s.length);
-        auto page_at = [&](int key) {
-            int32_t id = -1;
-            if (key < hi_key) {
-                id = __ldg(table + (key >> kv.page_shift));
-                if ((uint32_t)id >= kv.num_pages) {
-                    kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
-                    id = -1;
-                }
-            }
-            return id;
-        };
-        auto get = [&](const uint8_t* base, uint32_t block, uint4* to) {
+        auto get = [&](const uint8_t* base, uint32_t block, uint32_t ring, uint4* to) {
 #pragma unroll
             for (int e = 0; e < kUnits; ++e) {
                 const int key = (int)(block * kKeys + row0 + e * kRowStep);
-                const int32_t id = page_at(key);
+                const int32_t id = sh.page[ring][(row0 + e * kRowStep) >> 4];
                 to[e] = make_uint4(0, 0, 0, 0);
-                if (id >= 0 && inside)
+                if (id >= 0 && inside && key < hi_key)
                     asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(to[e].x), "=r"(to[e].y), "=r"(to[e].z), "=r"(to[e].w)
                                  : "l"(base + (long long)id * kv.page_stride + head_off + (long long)(key & (kv.page_tokens - 1)) * kv.token_step));
             }
@@ -358,12 +350,53 @@ __device__ void feed(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w)
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         };
-        get(kv.k, s.first + s.b0, kr);
-        get(kv.v, s.first + s.b0, vr);
+        if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
+        get(kv.k, s.first + s.b0, step % kRing, kr);
+        get(kv.v, s.first + s.b0, step % kRing, vr);
         for (uint32_t b = s.b0; b < s.b1; ++b, ++step) {
-            const uint32_t stage = step % P::kStages, turn = step / P::kStages, ring = step & 3;
-            if (tid < 8) {                                       // scales of this step's eight groups of 16 keys
-                const int32_t id = page_at((int)((s.first + b) * kKeys + 16 * tid));
+            const uint32_t stage = step % P::kStages, turn = step / P::kStages, ring = (step + 1) % kRing;
+            const bool more = b + 1 < s.b1;
+            if (turn && !warp_wait(&sh.k_empty[stage], (turn - 1) & 1, sh)) return;
+            put(sk + stage * P::kOperand, kr);
+            mbar_arrive(&sh.k_full[stage]);
+            if (more) {
+                if (!warp_wait(&sh.look_full[ring], ((step + 1) / kRing) & 1, sh)) return;
+                get(kv.k, s.first + b + 1, ring, kr);
+            }
+            if (turn && !warp_wait(&sh.v_empty[stage], (turn - 1) & 1, sh)) return;
+            put(sv + stage * P::kOperand, vr);
+            mbar_arrive(&sh.v_full[stage]);
+            if (more) get(kv.v, s.first + b + 1, ring, vr);
+        }
+    }
+}
+
+// ---- warpgroup 3: one warp looks up pages and scales, four steps at a time ------------------------------------------------------
+template <int DP>
+__device__ void look_up(const AttnArgs& a, PromptShared& sh, Walk w) {
+    using P = Prompt<DP>;
+    const KvView& kv = a.c;
+    const uint32_t lane = threadIdx.x & 31, group = lane & 7;
+    uint32_t step = 0;
+    Segment s;
+    while (next_segment<P::kRows>(a, w, s)) {
+        const int32_t* table = kv.pages + (size_t)s.p.s.slot * kv.max_pages;
+        const int hi_key = (int)min((s.first + s.count) * kKeys, s.p.s.length);
+        const uint32_t n = s.b1 - s.b0;
+        for (uint32_t j0 = 0; j0 < n; j0 += 4) {
+            const uint32_t j = j0 + (lane >> 3), x = step + j, last = step + min(j0 + 4, n) - 1;
+            // products end in order: when the last slot of these four is free, all are
+            if (last >= kRing && !warp_wait(&sh.look_free[last % kRing], (last / kRing - 1) & 1, sh)) return;
+            if (j < n) {
+                const int key = (int)((s.first + s.b0 + j) * kKeys + 16 * group);
+                int32_t id = -1;
+                if (key < hi_key) {
+                    id = __ldg(table + (key >> kv.page_shift));
+                    if ((uint32_t)id >= kv.num_pages) {
+                        kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
+                        id = -1;
+                    }
+                }
                 float ks = 0.0f, lvs = -INFINITY, ivs = 0.0f;    // keys that are not there weigh nothing
                 if (id >= 0) {
                     ks = __ldg(kv.k_scale + (size_t)id * kv.heads + s.head);
@@ -371,20 +404,16 @@ __device__ void feed(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w)
                     lvs = log2f(vs);
                     ivs = __fdiv_rn(1.0f, vs);
                 }
-                sh.ks[ring][tid] = ks;
-                sh.lvs[ring][tid] = lvs;
-                sh.ivs[ring][tid] = ivs;
-                mbar_arrive(&sh.scales[ring]);
+                const uint32_t ring = x % kRing;
+                sh.page[ring][group] = id;
+                sh.ks[ring][group] = ks;
+                sh.lvs[ring][group] = lvs;
+                sh.ivs[ring][group] = ivs;
+                mbar_arrive(&sh.look_full[ring]);
             }
-            if (turn && !warp_wait(&sh.k_empty[stage], (turn - 1) & 1, sh)) return;
-            put(sk + stage * P::kOperand, kr);
-            mbar_arrive(&sh.k_full[stage]);
-            if (b + 1 < s.b1) get(kv.k, s.first + b + 1, kr);
-            if (turn && !warp_wait(&sh.v_empty[stage], (turn - 1) & 1, sh)) return;
-            put(sv + stage * P::kOperand, vr);
-            mbar_arrive(&sh.v_full[stage]);
-            if (b + 1 < s.b1) get(kv.v, s.first + b + 1, vr);
+            __syncwarp();
         }
+        step += n;
     }
 }
 
@@ -427,7 +456,10 @@ __device__ void issue(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w
                     tc_commit(&sh.s_full[t]);
                 }
             }
-            if (j) tc_commit(&sh.v_empty[old_stage]);
+            if (j) {
+                tc_commit(&sh.v_empty[old_stage]);
+                tc_commit(&sh.look_free[old % kRing]);
+            }
             if (j < n) tc_commit(&sh.k_empty[stage]);
             if (j + 1 == n) tc_commit(&sh.q_empty);
         }
@@ -452,8 +484,8 @@ __device__ void softmax(const AttnArgs& a, PromptShared& sh, Walk w) {
         float m = -INFINITY, l = 0.0f, q = 0.0f;
         for (uint32_t j = 0; on && j < n; ++j) {
             const int k0 = (int)((s.first + s.b0 + j) * kKeys);
-            const uint32_t ring = (step + j) & 3;
-            if (!warp_wait(&sh.scales[ring], ((step + j) >> 2) & 1, sh) || !warp_wait(&sh.s_full[t], s_turn & 1, sh)) return;
+            const uint32_t ring = (step + j) % kRing;
+            if (!warp_wait(&sh.look_full[ring], ((step + j) / kRing) & 1, sh) || !warp_wait(&sh.s_full[t], s_turn & 1, sh)) return;
             ++s_turn;
             tc_fence_after();
             if (j == 0) q = sh.q_scale[seg & 1][t * 128 + r];
@@ -653,7 +685,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
             mbar_init(&sh.p_full[i], 128);
             mbar_init(&sh.o_full[i], 1);
         }
-        for (int i = 0; i < 4; ++i) mbar_init(&sh.scales[i], 8);
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&sh.look_full[i], 8);
+            mbar_init(&sh.look_free[i], 1);
+        }
         mbar_init(&sh.join[0], 128 * P::kTiles);
         mbar_init(&sh.join[1], 1);
         mbar_init(&sh.drain, 1);
@@ -667,6 +702,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
         softmax<DP, T>(a, sh, w);
     } else if (wid >= 8 && wid < 12) {
         feed<DP, kFormat, T>(a, sh, smem, w);
+    } else if (wid == 13) {
+        look_up<DP>(a, sh, w);
     } else if (threadIdx.x == 12 * 32) {
         issue<DP>(a, sh, smem, w);
         tc_commit(&sh.drain);                                    // whatever was issued has ended before the memory is given back
