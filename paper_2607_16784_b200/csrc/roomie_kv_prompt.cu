@@ -1,14 +1,14 @@
 // Attention over the paged 8-bit cache for many query rows a sequence (prompt chunks): matrix products on the fifth-generation
 // tensor cores, accumulators in tensor memory.
 //
-// A block (512 threads, one an SM) takes kTiles tiles of 128 rows of one key head - a row is one (token, query head) of the
+// A block (640 threads, one an SM) takes kTiles tiles of 128 rows of one key head - a row is one (token, query head) of the
 // group - through the keys 128 at a time:
 //   S = q K^T        both operands in shared memory, float16; S in tensor memory
 //   softmax          a thread owns a row: reads S, writes the probabilities as float16 over the columns it has read
 //   o += p V         p from tensor memory, V from shared memory, o in tensor memory
-// Warpgroups 0 and 1 are the softmax of tiles 0 and 1, so that one tile's softmax overlaps the other's products; warpgroup 2
-// turns codes into float16 operands (the scales stay out of them); in warpgroup 3 one thread issues the products and one warp
-// looks up pages and scales, some steps ahead.
+// Warpgroups 0 and 1 are the softmax of tiles 0 and 1, so that one tile's softmax overlaps the other's products; warpgroups 2 and 3
+// turn the codes of keys and of values into float16 operands (the scales stay out of them); in warpgroup 4 one warp issues the
+// products and one looks up pages and scales, some steps ahead.
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
 // Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M the running maximum of s + log2 vs, is what multiplies
@@ -51,6 +51,12 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* x) {
           "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
         : "r"(at));
 }
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]),
+                   "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+                 : "r"(at));
+}
 __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* x) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
@@ -84,6 +90,9 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lbo) {
 __host__ __device__ constexpr uint32_t instruction(uint32_t n, bool columns_contiguous) {
     return 1u << 4 | (columns_contiguous ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
 }
+
+template <int kN> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
+template <int kN> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN)); }
 
 // ---- shape ------------------------------------------------------------------------------------------------------------------
 constexpr int kKeys = 128;                          // keys of a step
@@ -172,9 +181,9 @@ template <int kRows> __device__ __forceinline__ bool next_segment(const AttnArgs
     return true;
 }
 
-constexpr int kPromptThreads = 512;
+constexpr int kPromptThreads = 640;
 
-template <int kRows> __device__ bool walk_start(const AttnArgs& a, Walk& w, unsigned long long* sh) {
+template <int kRows> __device__ __forceinline__ bool walk_start(const AttnArgs& a, Walk& w, unsigned long long* sh) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     unsigned long long mine = 0;
     for (uint32_t i = wid; i < a.num_seqs; i += kPromptThreads / 32)
@@ -214,7 +223,7 @@ template <int kRows> __device__ bool walk_start(const AttnArgs& a, Walk& w, unsi
                 }
                 const unsigned long long f = ahead + incl - c;
                 if (c && rest >= f && rest < f + c) {
-                    sh[16] = i; sh[17] = head; sh[18] = t; sh[19] = rest - f;
+                    sh[20] = i; sh[21] = head; sh[22] = t; sh[23] = rest - f;
                 }
                 ahead += __shfl_sync(0xffffffffu, incl, 31);
                 if (rest < ahead) break;
@@ -224,38 +233,45 @@ template <int kRows> __device__ bool walk_start(const AttnArgs& a, Walk& w, unsi
         if (w.at < before) break;
     }
     __syncthreads();
-    w.seq = (uint32_t)sh[16]; w.head = (uint32_t)sh[17]; w.tile = (uint32_t)sh[18]; w.block = (uint32_t)sh[19];
+    w.seq = (uint32_t)sh[20]; w.head = (uint32_t)sh[21]; w.tile = (uint32_t)sh[22]; w.block = (uint32_t)sh[23];
     return true;
 }
 
 // ---- shared state -----------------------------------------------------------------------------------------------------------
 constexpr int kRing = 8;                            // steps whose pages and scales are looked up ahead
+constexpr int kSegments = 16;                       // segments ahead: at most one a step, and the one before may still be written out
+struct SegInfo {                                    // a segment as the other warps need it; steps = 0: there are no more
+    uint32_t steps, rows, row0, first_row, head, key0, end_key, length, b0, count;
+    int32_t start;                                  // position of the sequence's first row
+    unsigned long long item;
+};
 struct PromptShared {
-    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], look_full[kRing], look_free[kRing], join[2],
-        drain;
-    unsigned long long walk[20];
-    int32_t page[kRing][8];                         // of 16 keys each: page (-1: none), key scale, log2 and inverse of the value scale
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], look_full[kRing],
+        look_free[kRing], join[2], drain;
+    unsigned long long walk[24];
+    long long at[kRing][8];                         // of 16 keys each: bytes from the pool's start to them (-1: none), key scale, log2
+                                                    // and inverse of the value scale
     float ks[kRing][8], lvs[kRing][8], ivs[kRing][8];
+    SegInfo seg[kSegments];
     float q_scale[2][256];                          // of a row, segments in turn: 2^e of its float16 form times scale * log2(e)
     uint32_t tmem, last, failed;
 };
 
-// A wait that runs out (1 s) ends the block: the flag makes its other waits give up too.
-__device__ __forceinline__ bool wait_on(uint64_t* bar, uint32_t parity, PromptShared& sh) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_ns();
-    for (uint32_t spin = 0; spin < kWaitSpins; ++spin) {
-        if (mbar_try_wait(bar, parity)) return true;
+// By a whole warp, with one answer.  The instruction itself suspends the warp for up to the hint (20 us); a wait that runs out after
+// 2^16 of them (about a second) ends the block: the flag makes its other waits give up too.  Kept to a few instructions: the roles'
+// loops have to fit the instruction caches together.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, PromptShared& sh) {
+    const uint32_t at = smem_addr(bar);
+#pragma unroll 1
+    for (uint32_t spin = 0; spin < 65536u; ++spin) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(at), "r"(parity) : "memory");
+        if (__all_sync(0xffffffffu, ok != 0)) return true;
         if (*reinterpret_cast<volatile uint32_t*>(&sh.failed)) return false;
-        if (global_ns() - t0 > kWaitNs) break;
     }
     *reinterpret_cast<volatile uint32_t*>(&sh.failed) = 1u;
     return false;
-}
-
-// The same by a whole warp, with one answer.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, PromptShared& sh) {
-    return __all_sync(0xffffffffu, wait_on(bar, parity, sh));
 }
 
 // 16 codes to two 16-byte chunks of float16
@@ -266,131 +282,151 @@ template <int kFormat> __device__ __forceinline__ void widen(const uint4& c, uin
     codes_to_f16<kFormat>(c.w, y.z, y.w);
 }
 
-// ---- warpgroup 2: operands ----------------------------------------------------------------------------------------------------
-template <int DP, int kFormat, class T>
-__device__ void feed(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w) {
+// ---- warpgroups 2 and 3: operands ------------------------------------------------------------------------------------------------
+// The call's rows [r0, r1) of the segment's tile, as float16 with the row's largest magnitude in [1, 2) (see few_rows_kernel).
+template <int DP, class T>
+__device__ __forceinline__ void feed_queries(const AttnArgs& a, PromptShared& sh, uint8_t* sq, const SegInfo& s, uint32_t which, uint32_t r0,
+                                             uint32_t r1) {
     using P = Prompt<DP>;
-    constexpr int kUnits = 128 * (DP / 16) / 128;                // 16-code units a thread of a 128-key operand: DP / 16
-    constexpr int kPerRow = DP / 16;
-    const uint32_t tid = threadIdx.x & 127;
-    const KvView& kv = a.c;
-    uint8_t* sq = smem;
-    uint8_t* sk = smem + P::kTiles * P::kOperand;
-    uint8_t* sv = sk + P::kStages * P::kOperand;
-    const uint32_t unit = tid % kPerRow, row0 = tid / kPerRow;   // unit e: key row0 + e * (128 / kPerRow), codes [16 * unit, +16)
-    constexpr int kRowStep = 128 / kPerRow;
-    const uint32_t slab = unit / 4, chunk = (unit & 3) * 2;
-    const bool inside = 16 * unit < kv.dim;
-    uint32_t step = 0, seg = 0;
-    Segment s;
-    uint4 kr[kUnits], vr[kUnits];
-    while (next_segment<P::kRows>(a, w, s)) {
-        // queries: lanes of a row side by side, 8 elements each
-        if (seg && !warp_wait(&sh.q_empty, (seg - 1) & 1, sh)) return;
-        constexpr int kLanes = DP / 8;
-        for (uint32_t r = tid / kLanes; r < (uint32_t)P::kRows; r += 128 / kLanes) {
-            const uint32_t c = tid % kLanes;
-            float x[8];
+    constexpr int kLanes = DP / 8, kPass = 128 / kLanes, kBatch = DP > 64 ? 4 : 2;   // lanes of a row side by side, 8 elements each
+    const uint32_t tid = threadIdx.x & 127, c = tid % kLanes;
+    for (r0 += tid / kLanes; r0 < r1; r0 += kPass * kBatch) {
+        uint4 raw[kBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-            if (r < s.rows && 8 * c < kv.dim) {
-                const uint32_t row = s.tile * P::kRows + r, tok = row / a.group;
-                const T* q = static_cast<const T*>(a.q) + (long long)(s.p.s.row + tok) * a.q_token +
+        for (int i = 0; i < kBatch; ++i) {                       // a batch of rows on their way together
+            const uint32_t r = r0 + i * kPass;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (r < s.rows && 8 * c < a.c.dim) {
+                const uint32_t row = s.first_row + r, tok = row / a.group;
+                const T* q = static_cast<const T*>(a.q) + (long long)(s.row0 + tok) * a.q_token +
                              (long long)(s.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
                 if (a.q_aligned) {
-                    unpack<T>(*reinterpret_cast<const uint4*>(q), x);
+                    raw[i] = *reinterpret_cast<const uint4*>(q);
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = to_f32(q[i]);
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(q);
+                    raw[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                                        h[6] | (uint32_t)h[7] << 16);
                 }
             }
-            float amax = 0.0f;
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i]));
+        for (int i = 0; i < kBatch; ++i) {
+            const uint32_t r = r0 + i * kPass;
+            float x[8], amax = 0.0f;
+            unpack<T>(raw[i], x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(x[k]));
 #pragma unroll
             for (int d = 1; d < kLanes; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-            int e = (int)(__float_as_uint(amax) >> 23) - 127;    // the row's largest magnitude in [1, 2): see few_rows_kernel
+            int e = (int)(__float_as_uint(amax) >> 23) - 127;
             e = max(min(e, 126), -126);
             const float down = pow2f(-e);
             __half2 h[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(x[2 * i] * down, x[2 * i + 1] * down);
+            for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(x[2 * k] * down, x[2 * k + 1] * down);
             uint8_t* to = sq + (r >> 7) * P::kOperand + (c >> 3) * P::kSlab + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
             *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(h);
-            if (c == 0) sh.q_scale[seg & 1][r] = pow2f(e) * a.scale_log2;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(&sh.q_full);
-        ++seg;
-
-        const long long head_off = (long long)s.head * kv.head_step + 16 * unit;
-        const int hi_key = (int)min((s.first + s.count) * kKeys, s.p.s.length);
-        auto get = [&](const uint8_t* base, uint32_t block, uint32_t ring, uint4* to) {
-#pragma unroll
-            for (int e = 0; e < kUnits; ++e) {
-                const int key = (int)(block * kKeys + row0 + e * kRowStep);
-                const int32_t id = sh.page[ring][(row0 + e * kRowStep) >> 4];
-                to[e] = make_uint4(0, 0, 0, 0);
-                if (id >= 0 && inside && key < hi_key)
-                    asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(to[e].x), "=r"(to[e].y), "=r"(to[e].z), "=r"(to[e].w)
-                                 : "l"(base + (long long)id * kv.page_stride + head_off + (long long)(key & (kv.page_tokens - 1)) * kv.token_step));
-            }
-        };
-        auto put = [&](uint8_t* base, const uint4* from) {
-#pragma unroll
-            for (int e = 0; e < kUnits; ++e) {
-                const uint32_t row = row0 + e * kRowStep;
-                uint4 x, y;
-                widen<kFormat>(from[e], x, y);
-                uint8_t* to = base + slab * P::kSlab + row * 128;
-                // the odd slabs store their second chunk first: the eight lanes of a store then hit different banks
-                const bool swap = slab & 1;
-                *reinterpret_cast<uint4*>(to + (((chunk + swap) ^ (row & 7)) << 4)) = swap ? y : x;
-                *reinterpret_cast<uint4*>(to + (((chunk + !swap) ^ (row & 7)) << 4)) = swap ? x : y;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        };
-        if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
-        get(kv.k, s.first + s.b0, step % kRing, kr);
-        get(kv.v, s.first + s.b0, step % kRing, vr);
-        for (uint32_t b = s.b0; b < s.b1; ++b, ++step) {
-            const uint32_t stage = step % P::kStages, turn = step / P::kStages, ring = (step + 1) % kRing;
-            const bool more = b + 1 < s.b1;
-            if (turn && !warp_wait(&sh.k_empty[stage], (turn - 1) & 1, sh)) return;
-            put(sk + stage * P::kOperand, kr);
-            mbar_arrive(&sh.k_full[stage]);
-            if (more) {
-                if (!warp_wait(&sh.look_full[ring], ((step + 1) / kRing) & 1, sh)) return;
-                get(kv.k, s.first + b + 1, ring, kr);
-            }
-            if (turn && !warp_wait(&sh.v_empty[stage], (turn - 1) & 1, sh)) return;
-            put(sv + stage * P::kOperand, vr);
-            mbar_arrive(&sh.v_full[stage]);
-            if (more) get(kv.v, s.first + b + 1, ring, vr);
+            if (c == 0) sh.q_scale[which][r] = pow2f(e) * a.scale_log2;
         }
     }
 }
 
-// ---- warpgroup 3: one warp looks up pages and scales, four steps at a time ------------------------------------------------------
+template <int DP, int kFormat, class T>
+__device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_t* smem, const bool keys) {
+    using P = Prompt<DP>;
+    constexpr int kPerRow = DP / 16;                             // 16-code units of a key
+    constexpr int kUnits = kPerRow;                              // a thread's, of the 128 keys
+    constexpr int kRowStep = 128 / kPerRow;                      // unit e: key row0 + e * kRowStep, codes [16 * unit, +16)
+    const uint32_t tid = threadIdx.x & 127;
+    uint8_t* operands = smem + (P::kTiles + (keys ? 0 : P::kStages)) * P::kOperand;
+    uint64_t* full = keys ? sh.k_full : sh.v_full;
+    uint64_t* empty = keys ? sh.k_empty : sh.v_empty;
+    const uint32_t unit = tid % kPerRow, row0 = tid / kPerRow;
+    const bool inside = 16 * unit < a.c.dim;
+    // Where in an operand unit 0 goes; row0 + e * kRowStep keeps row & 7 (kRowStep is a multiple of 8).  The odd slabs store their
+    // second chunk first: the eight lanes of a store then hit different banks.
+    const uint32_t slab = unit / 4, swap = slab & 1, chunk = (unit & 3) * 2;
+    uint8_t* to0 = operands + slab * P::kSlab + row0 * 128 + (((chunk + swap) ^ (row0 & 7)) << 4);
+    const uint32_t to1 = (((chunk + 1 - swap) ^ (row0 & 7)) << 4) - (((chunk + swap) ^ (row0 & 7)) << 4);
+    uint32_t step = 0;
+    for (uint32_t seg = 0;; ++seg) {
+        if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
+        const SegInfo& s = sh.seg[seg % kSegments];
+        const uint32_t n = s.steps;
+        if (n == 0) return;
+        const uint8_t* pool = (keys ? a.c.k : a.c.v) + (long long)s.head * a.c.head_step + 16 * unit + (long long)(row0 & 15) * a.c.token_step;
+        int left = (int)s.end_key - (int)s.key0 - (int)row0;     // keys there from this thread's first on
+        uint4 c[kUnits];
+        auto get = [&](uint32_t x) {
+            const uint32_t ring = x % kRing;
+#pragma unroll
+            for (int e = 0; e < kUnits; ++e) {
+                const long long at = sh.at[ring][(row0 + e * kRowStep) >> 4];
+                c[e] = make_uint4(0, 0, 0, 0);
+                if (at >= 0 && inside && e * kRowStep < left)
+                    asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[e].x), "=r"(c[e].y), "=r"(c[e].z), "=r"(c[e].w)
+                                 : "l"(pool + at + (kRowStep < 16 && (e & 1) ? 8 * a.c.token_step : 0u)));
+            }
+        };
+        get(step);
+        if (seg && !warp_wait(&sh.q_empty, (seg - 1) & 1, sh)) return;
+        feed_queries<DP, T>(a, sh, smem, s, seg & 1, keys ? 0 : P::kRows / 2, keys ? P::kRows / 2 : P::kRows);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(&sh.q_full);
+        for (uint32_t j = 0; j < n; ++j) {
+            const uint32_t stage = step % P::kStages, turn = step / P::kStages;
+            if (turn && !warp_wait(&empty[stage], (turn - 1) & 1, sh)) return;
+#pragma unroll
+            for (int e = 0; e < kUnits; ++e) {
+                uint4 x, y;
+                widen<kFormat>(c[e], x, y);
+                uint8_t* to = to0 + stage * P::kOperand + e * kRowStep * 128;
+                *reinterpret_cast<uint4*>(to) = swap ? y : x;
+                *reinterpret_cast<uint4*>(to + to1) = swap ? x : y;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&full[stage]);
+            ++step;
+            left -= kKeys;
+            if (j + 1 < n) {
+                if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
+                get(step);
+            }
+        }
+    }
+}
+
+// ---- warpgroup 4: one warp looks up pages and scales, four steps at a time ------------------------------------------------------
 template <int DP>
-__device__ void look_up(const AttnArgs& a, PromptShared& sh, Walk w) {
+__device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Walk w) {
     using P = Prompt<DP>;
     const KvView& kv = a.c;
     const uint32_t lane = threadIdx.x & 31, group = lane & 7;
-    uint32_t step = 0;
-    Segment s;
-    while (next_segment<P::kRows>(a, w, s)) {
-        const int32_t* table = kv.pages + (size_t)s.p.s.slot * kv.max_pages;
-        const int hi_key = (int)min((s.first + s.count) * kKeys, s.p.s.length);
-        const uint32_t n = s.b1 - s.b0;
+    uint32_t step = 0, seg = 0;
+    for (;; ++seg) {
+        Segment s;
+        const bool more = next_segment<P::kRows>(a, w, s);
+        const int32_t* table = kv.pages + (more ? (size_t)s.p.s.slot * kv.max_pages : 0);
+        const uint32_t n = more ? s.b1 - s.b0 : 1u;              // the end takes a step of its own
+        const uint32_t end_key = more ? min((s.first + s.count) * kKeys, s.p.s.length) : 0u;
         for (uint32_t j0 = 0; j0 < n; j0 += 4) {
             const uint32_t j = j0 + (lane >> 3), x = step + j, last = step + min(j0 + 4, n) - 1;
             // products end in order: when the last slot of these four is free, all are
             if (last >= kRing && !warp_wait(&sh.look_free[last % kRing], (last / kRing - 1) & 1, sh)) return;
+            if (j0 == 0) {
+                if (lane == 0) {
+                    SegInfo& o = sh.seg[seg % kSegments];
+                    o.steps = more ? n : 0u;
+                    o.rows = s.rows; o.row0 = s.p.s.row; o.first_row = s.tile * P::kRows; o.head = s.head;
+                    o.key0 = (s.first + s.b0) * kKeys; o.end_key = end_key; o.length = s.p.s.length;
+                    o.b0 = s.b0; o.count = s.count; o.start = s.p.start; o.item = s.item;
+                }
+                __syncwarp();
+            }
             if (j < n) {
-                const int key = (int)((s.first + s.b0 + j) * kKeys + 16 * group);
+                const uint32_t key = more ? (s.first + s.b0 + j) * kKeys + 16 * group : 0u;
                 int32_t id = -1;
-                if (key < hi_key) {
+                if (key < end_key) {
                     id = __ldg(table + (key >> kv.page_shift));
                     if ((uint32_t)id >= kv.num_pages) {
                         kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
@@ -405,7 +441,7 @@ __device__ void look_up(const AttnArgs& a, PromptShared& sh, Walk w) {
                     ivs = __fdiv_rn(1.0f, vs);
                 }
                 const uint32_t ring = x % kRing;
-                sh.page[ring][group] = id;
+                sh.at[ring][group] = id < 0 ? -1ll : (long long)id * kv.page_stride + (long long)(key & (kv.page_tokens - 1)) * kv.token_step;
                 sh.ks[ring][group] = ks;
                 sh.lvs[ring][group] = lvs;
                 sh.ivs[ring][group] = ivs;
@@ -413,169 +449,253 @@ __device__ void look_up(const AttnArgs& a, PromptShared& sh, Walk w) {
             }
             __syncwarp();
         }
+        if (!more) return;
         step += n;
     }
 }
 
-// ---- warpgroup 3: one thread issues the products --------------------------------------------------------------------------------
+// ---- warpgroup 4: one warp issues the products -----------------------------------------------------------------------------------
+// The whole warp goes through the loop, so that operands stay in uniform registers; one elected lane issues.  (A single thread's
+// branch around all of it took 280 cycles an instruction, where one has 64.)
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
 template <int DP>
-__device__ void issue(const AttnArgs& a, PromptShared& sh, uint8_t* smem, Walk w) {
+__device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem) {
     using P = Prompt<DP>;
     const uint32_t sq = smem_addr(smem), sk = sq + P::kTiles * P::kOperand, sv = sk + P::kStages * P::kOperand;
-    const uint32_t tm = sh.tmem;
+    const uint64_t q0 = operand(sq, 16), k0 = operand(sk, 16), v0 = operand(sv, P::kSlab);
+    const uint32_t tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
     constexpr uint32_t kS = instruction(kKeys, false), kO = instruction(DP, true);
-    uint32_t step = 0, seg = 0, p_turn[2] = {0, 0};
-    Segment s;
-    while (next_segment<P::kRows>(a, w, s)) {
-        const uint32_t tiles = s.rows > 128 ? 2 : 1, n = s.b1 - s.b0;
-        if (!wait_on(&sh.q_full, seg & 1, sh)) return;
+    uint32_t step = 0;
+    for (uint32_t seg = 0;; ++seg) {
+        if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
+        const uint32_t n = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].steps, 0);
+        const bool two = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].rows, 0) > 128;
+        if (n == 0 || !warp_wait(&sh.q_full, seg & 1, sh)) return;
         tc_fence_after();
-        ++seg;
         for (uint32_t j = 0; j <= n; ++j) {                      // S of step j, o of step j - 1
-            const uint32_t stage = (step + j) % P::kStages, turn = (step + j) / P::kStages;
-            const uint32_t old = j ? step + j - 1 : 0, old_stage = old % P::kStages, old_turn = old / P::kStages;
-            if (j < n && !wait_on(&sh.k_full[stage], turn & 1, sh)) return;
-            if (j && !wait_on(&sh.v_full[old_stage], old_turn & 1, sh)) return;
-            for (uint32_t t = 0; t < tiles; ++t) {
+            const uint32_t now = step + j, stage = now % P::kStages, old = now - 1, old_stage = old % P::kStages;
+            if (j < n && !warp_wait(&sh.k_full[stage], (now / P::kStages) & 1, sh)) return;
+            if (j && !warp_wait(&sh.v_full[old_stage], (old / P::kStages) & 1, sh)) return;
+            const uint64_t k = k0 + stage * (P::kOperand >> 4), v = v0 + old_stage * (P::kOperand >> 4);
+#pragma unroll 1
+            for (int t = 0; t < P::kTiles; ++t) {
                 const uint32_t s_at = tm + t * 128, o_at = tm + P::kTiles * 128 + t * DP;
-                if (j) {
-                    if (!wait_on(&sh.p_full[t], p_turn[t] & 1, sh)) return;
-                    ++p_turn[t];
-                    tc_fence_after();
+                if (j && !warp_wait(&sh.p_full[t], old & 1, sh)) return;
+                const bool on = t == 0 || two;                   // a tile without rows only keeps step
+                tc_fence_after();
+                if (elected()) {
+                    if (on && j) {
 #pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i)
-                        mma_ts(o_at, s_at + 8 * i, operand(sv + old_stage * P::kOperand + i * 2048, P::kSlab), kO, j > 1 || i > 0);
-                    tc_commit(&sh.o_full[t]);
-                }
-                if (j < n) {
-#pragma unroll
-                    for (int i = 0; i < DP / 16; ++i) {
-                        const uint32_t off = (i / 4) * P::kSlab + (i % 4) * 32;
-                        mma_ss(s_at, operand(sq + t * P::kOperand + off, 16), operand(sk + stage * P::kOperand + off, 16), kS, i > 0);
+                        for (int i = 0; i < kKeys / 16; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, j > 1 || i > 0);
+                        tc_commit(&sh.o_full[t]);
                     }
-                    tc_commit(&sh.s_full[t]);
+                    if (on && j < n) {
+#pragma unroll
+                        for (int i = 0; i < DP / 16; ++i) {
+                            const uint32_t off = ((i / 4) * P::kSlab + (i % 4) * 32) >> 4;
+                            mma_ss(s_at, q0 + (t * P::kOperand >> 4) + off, k + off, kS, i > 0);
+                        }
+                    }
+                    if (j < n) tc_commit(&sh.s_full[t]);
                 }
+                __syncwarp();
             }
-            if (j) {
-                tc_commit(&sh.v_empty[old_stage]);
-                tc_commit(&sh.look_free[old % kRing]);
+            if (elected()) {
+                if (j) {
+                    tc_commit(&sh.v_empty[old_stage]);
+                    tc_commit(&sh.look_free[old % kRing]);
+                }
+                if (j < n) tc_commit(&sh.k_empty[stage]);
+                if (j + 1 == n) tc_commit(&sh.q_empty);
             }
-            if (j < n) tc_commit(&sh.k_empty[stage]);
-            if (j + 1 == n) tc_commit(&sh.q_empty);
+            __syncwarp();
         }
         step += n;
     }
 }
 
+// ---- one row's share of a step -----------------------------------------------------------------------------------------------------
+// two float32 at a time
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void split(uint64_t p, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// 2^x for two x of at most 2^7, on the multiply-add units: x = n + f with |f| <= 1/2 (n by adding 1.5 * 2^23, whose last place is one),
+// 2^f by a polynomial of degree 4 (own least-squares fit of the relative error, 2.6e-6: 2^-6 of what the rounding to float16 does),
+// n into the exponent's bits.  The special-function unit gives 4 exponentials a cycle and scheduler; a step's 2 * 128 * 128 would take
+// it as long as all the step's matrix products.
+__device__ __forceinline__ void exp2_poly(uint64_t x, float& u, float& v) {
+    float a, b;
+    split(x, a, b);
+    x = pair(fmaxf(a, -126.0f), fmaxf(b, -126.0f));
+    const uint64_t magic = pair(12582912.0f, 12582912.0f), un_magic = pair(-12582912.0f, -12582912.0f), minus = pair(-1.0f, -1.0f);
+    const uint64_t t = add2(x, magic);
+    const uint64_t f = fma2(add2(t, un_magic), minus, x);
+    uint64_t p = fma2(f, pair(0.009570100344717503f, 0.009570100344717503f), pair(0.05591785907745361f, 0.05591785907745361f));
+    p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
+    p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
+    p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
+    float ta, tb, pa, pb;
+    split(t, ta, tb);
+    split(p, pa, pb);
+    u = __uint_as_float(__float_as_uint(pa) + (__float_as_uint(ta) << 23));
+    v = __uint_as_float(__float_as_uint(pb) + (__float_as_uint(tb) << 23));
+}
+
+// The row's largest exponent, f * S + log2 vs, among the keys it sees.  kCut: some key of the step is hidden from some row of the warp.
+// The two forms are apart so that the usual one has no branch between its elements (with one, each exponential waits for the one
+// before: 5100 cycles a step instead of 2500, measured); the loops are kept short because the roles share the instruction caches
+// (unrolled over the whole step, a third of all stalls were for instructions).
+template <bool kCut>
+__device__ __forceinline__ float row_top(uint32_t s_at, const PromptShared& sh, uint32_t ring, float q, int k0, int lo, int hi) {
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        uint32_t x[32];
+        tmem_load32(s_at + 32 * c, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int k = k0 + 32 * c + 16 * g + e;
+                mx = fmaxf(mx, !kCut || (k < hi && k >= lo) ? __uint_as_float(x[16 * g + e]) : -INFINITY);
+            }
+            const float v = fmaf(mx, q * sh.ks[ring][2 * c + g], sh.lvs[ring][2 * c + g]);
+            top = fmaxf(top, kCut && mx == -INFINITY ? -INFINITY : v);
+        }
+    }
+    return top;
+}
+// Writes the weights exp2(f * S + log2 vs - base) as float16 over the columns of S that have been read; returns the softmax total's
+// share.  Hidden keys weigh exactly nothing.
+template <bool kCut>
+__device__ __forceinline__ float row_weights(uint32_t s_at, const PromptShared& sh, uint32_t ring, float q, float base, int k0, int lo,
+                                             int hi) {
+    float total = 0.0f;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        uint32_t x[32], p[16];
+        tmem_load32(s_at + 32 * c, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const float f = q * sh.ks[ring][2 * c + g], off = sh.lvs[ring][2 * c + g] - base;
+            const uint64_t f2 = pair(f, f), off2 = pair(off, off);
+            uint64_t sum = 0;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                float u, v;
+                split(fma2(pair(x[16 * g + e], x[16 * g + e + 1]), f2, off2), u, v);
+                if (kCut) {
+                    const int k = k0 + 32 * c + 16 * g + e;
+                    u = k < hi && k >= lo ? u : -INFINITY;
+                    v = k + 1 < hi && k + 1 >= lo ? v : -INFINITY;
+                }
+                u = exp2_fast(u);
+                v = exp2_fast(v);
+                sum = add2(sum, pair(u, v));
+                const __half2 h = __floats2half2_rn(u, v);
+                p[8 * g + e / 2] = reinterpret_cast<const uint32_t&>(h);
+            }
+            float even, odd;
+            split(sum, even, odd);
+            total = fmaf(even + odd, sh.ivs[ring][2 * c + g], total);
+        }
+        tmem_store16(s_at + 16 * c, p);
+    }
+    return total;
+}
+
 // ---- warpgroups 0 and 1: softmax, and the end of a segment ------------------------------------------------------------------------
 template <int DP, class T>
-__device__ void softmax(const AttnArgs& a, PromptShared& sh, Walk w) {
+__device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, unsigned long long total_blocks, unsigned long long parts) {
     using P = Prompt<DP>;
     const uint32_t t = threadIdx.x >> 7, r = threadIdx.x & 127;  // tile, row
     const uint32_t lanes = (threadIdx.x & 96) << 16;             // this warp's quarter of the tensor memory's lanes
     const uint32_t s_at = sh.tmem + t * 128 + lanes, o_at = sh.tmem + P::kTiles * 128 + t * DP + lanes;
-    uint32_t step = 0, s_turn = 0, o_turn = 0, seg = 0, joins = 0;
-    Segment s;
-    while (next_segment<P::kRows>(a, w, s)) {
-        const uint32_t n = s.b1 - s.b0, row = s.tile * P::kRows + t * 128 + r;
+    uint32_t step = 0, o_turn = 0, joins = 0;
+    for (uint32_t seg = 0;; ++seg) {
+        if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
+        const SegInfo& s = sh.seg[seg % kSegments];
+        const uint32_t n = s.steps;
+        if (n == 0) return;
         const bool on = t * 128 < s.rows, mine = t * 128 + r < s.rows;
-        const int tok = (int)(row / a.group), pos = s.p.start + tok;
-        const int hi = mine ? max(min(pos + 1, (int)s.p.s.length), 0) : 0, lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
+        int hi = 0, lo = 0;
+        if (mine) {
+            const int pos = s.start + (int)((s.first_row + t * 128 + r) / a.group);
+            hi = max(min(pos + 1, (int)s.length), 0);
+            lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
+        }
         float m = -INFINITY, l = 0.0f, q = 0.0f;
-        for (uint32_t j = 0; on && j < n; ++j) {
-            const int k0 = (int)((s.first + s.b0 + j) * kKeys);
-            const uint32_t ring = (step + j) % kRing;
-            if (!warp_wait(&sh.look_full[ring], ((step + j) / kRing) & 1, sh) || !warp_wait(&sh.s_full[t], s_turn & 1, sh)) return;
-            ++s_turn;
+        int k0 = (int)s.key0;
+        for (uint32_t j = 0; j < n; ++j, ++step, k0 += kKeys) {
+            const uint32_t ring = step % kRing;
+            if (j && !warp_wait(&sh.look_full[ring], (step / kRing) & 1, sh)) return;
+            if (!warp_wait(&sh.s_full[t], step & 1, sh)) return;
+            if (!on) {
+                mbar_arrive(&sh.p_full[t]);
+                continue;
+            }
             tc_fence_after();
             if (j == 0) q = sh.q_scale[seg & 1][t * 128 + r];
             const bool cut = __any_sync(0xffffffffu, k0 < lo || k0 + kKeys > hi);
-            uint32_t x[32];
-            float top = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tmem_load32(s_at + 32 * c, x);
-                tmem_wait_ld();
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    float mx = -INFINITY;
-                    if (cut) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int k = k0 + 32 * c + 16 * g + e;
-                            mx = fmaxf(mx, k < hi && k >= lo ? __uint_as_float(x[16 * g + e]) : -INFINITY);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, __uint_as_float(x[16 * g + e]));
-                    }
-                    const float v = fmaf(mx, q * sh.ks[ring][2 * c + g], sh.lvs[ring][2 * c + g]);
-                    top = fmaxf(top, mx == -INFINITY ? -INFINITY : v);
-                }
-            }
-            // The sums are taken against an old maximum while the new one is at most 2^8 above it: probabilities then stay below
-            // 2^8, far from float16's end, and o is rescaled in tensor memory only now and then.
-            const bool far = top > m + 8.0f || m == -INFINITY;
-            if (__any_sync(0xffffffffu, far && top > m)) {
+            // The weights are taken against an old maximum while the new one is at most 2^8 above it: they then stay far from float16's
+            // end, and o is rescaled in tensor memory only now and then.
+            const float top = cut ? row_top<true>(s_at, sh, ring, q, k0, lo, hi) : row_top<false>(s_at, sh, ring, q, k0, lo, hi);
+            if (__any_sync(0xffffffffu, top > m + 8.0f || (m == -INFINITY && top > m))) {
                 const float to = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_fast(m - to);
                 m = to;
                 l *= f;
                 if (j) {
                     if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
                     tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < DP / 32; ++c) {
-                        tmem_load32(o_at + 32 * c, x);
+                        uint32_t y[32];
+                        tmem_load32(o_at + 32 * c, y);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-                        tmem_store32(o_at + 32 * c, x);
+                        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                        tmem_store32(o_at + 32 * c, y);
                     }
-                    tmem_wait_st();
                 }
             }
             ++o_turn;
             const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tmem_load32(s_at + 32 * c, x);
-                tmem_wait_ld();
-                uint32_t p[16];
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const float f = q * sh.ks[ring][2 * c + g], off = sh.lvs[ring][2 * c + g] - base;
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2) {
-                        float u = fmaf(__uint_as_float(x[16 * g + e]), f, off), v = fmaf(__uint_as_float(x[16 * g + e + 1]), f, off);
-                        if (cut) {
-                            const int k = k0 + 32 * c + 16 * g + e;
-                            u = k < hi && k >= lo ? u : -INFINITY;
-                            v = k + 1 < hi && k + 1 >= lo ? v : -INFINITY;
-                        }
-                        u = exp2_fast(u);
-                        v = exp2_fast(v);
-                        sum += u + v;
-                        const __half2 h = __floats2half2_rn(u, v);
-                        p[8 * g + e / 2] = reinterpret_cast<const uint32_t&>(h);
-                    }
-                    l = fmaf(sum, sh.ivs[ring][2 * c + g], l);
-                }
-                tmem_store16(s_at + 16 * c, p);
-            }
+            l += cut ? row_weights<true>(s_at, sh, ring, q, base, k0, lo, hi) : row_weights<false>(s_at, sh, ring, q, base, k0, lo, hi);
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&sh.p_full[t]);
         }
-        step += n;
-        ++seg;
 
         // ---- the end of a segment: rows go out, or wait in the workspace for their other parts ---------------------------------
-        const bool complete = s.b0 == 0 && s.b1 == s.count;
-        const uint32_t h = s.head * a.group + row - (uint32_t)tok * a.group;
-        T* out = static_cast<T*>(a.out) + (long long)(s.p.s.row + tok) * a.o_token + (long long)h * a.o_head;
+        const bool complete = s.b0 == 0 && n == s.count;
+        const uint32_t row = s.first_row + t * 128 + r, tok = row / a.group, h = s.head * a.group + row - tok * a.group;
+        T* out = static_cast<T*>(a.out) + (long long)(s.row0 + tok) * a.o_token + (long long)h * a.o_head;
         auto put_lse = [&](float mx, float sum) {
-            if (a.lse) a.lse[(size_t)(s.p.s.row + tok) * a.q_heads + h] = sum > 0.0f ? (mx + log2f(sum)) * kLn2 : sum == 0.0f ? -INFINITY : sum;
+            if (a.lse) a.lse[(size_t)(s.row0 + tok) * a.q_heads + h] = sum > 0.0f ? (mx + log2f(sum)) * kLn2 : sum == 0.0f ? -INFINITY : sum;
         };
         auto put8 = [&](int d, const float* v) {                 // eight elements of the row
             if (d >= (int)a.c.dim) return;
@@ -592,7 +712,7 @@ __device__ void softmax(const AttnArgs& a, PromptShared& sh, Walk w) {
             if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
             tc_fence_after();
             const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 uint32_t x[32];
                 tmem_load32(o_at + 32 * c, x);
@@ -619,8 +739,8 @@ __device__ void softmax(const AttnArgs& a, PromptShared& sh, Walk w) {
             tc_fence_before();
         }
         if (!complete) {
-            const uint32_t first = (uint32_t)(((s.item + 1) * w.parts - 1) / w.total);
-            const uint32_t last = (uint32_t)(((s.item + s.count) * w.parts - 1) / w.total);
+            const uint32_t first = (uint32_t)(((s.item + 1) * parts - 1) / total_blocks);
+            const uint32_t last = (uint32_t)(((s.item + s.count) * parts - 1) / total_blocks);
             __threadfence();
             mbar_arrive(&sh.join[0]);
             if (threadIdx.x < 32) {
@@ -644,19 +764,23 @@ __device__ void softmax(const AttnArgs& a, PromptShared& sh, Walk w) {
                     mx = to;
                 }
                 const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : sum == 0.0f ? 0.0f : sum;
-                for (int d = 0; d < (int)a.c.dim; d += 8) {
-                    float v[8] = {};
+#pragma unroll 1
+                for (int d = 0; d < DP; d += 32) {
+                    float v[32] = {};
                     for (uint32_t b = first; b <= last; ++b) {
                         const float* pp = a.partial + ((size_t)b * 2 + (b == first ? 1 : 0)) * P::kPartial;
                         const float mb = __ldcg(pp + (size_t)P::kRows * DP + 2 * pr);
+                        float4 x[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = __ldcg(reinterpret_cast<const float4*>(pp + ((size_t)(d / 4 + i) * P::kRows + pr) * 4));
                         const float f = mb == -INFINITY ? 0.0f : exp2f(mb - mx) * inv;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(pp + ((size_t)(d / 4 + i) * P::kRows + pr) * 4));
-                            v[4 * i] += f * x.x; v[4 * i + 1] += f * x.y; v[4 * i + 2] += f * x.z; v[4 * i + 3] += f * x.w;
+                        for (int i = 0; i < 8; ++i) {
+                            v[4 * i] += f * x[i].x; v[4 * i + 1] += f * x[i].y; v[4 * i + 2] += f * x[i].z; v[4 * i + 3] += f * x[i].w;
                         }
                     }
-                    put8(d, v);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) put8(d + e, v + e);
                 }
                 put_lse(mx, sum);
             }
@@ -674,7 +798,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
     if (!walk_start<P::kRows>(a, w, sh.walk)) return;            // the same answer in all threads
     const uint32_t wid = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        mbar_init(&sh.q_full, 128);
+        mbar_init(&sh.q_full, 256);
         mbar_init(&sh.q_empty, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.k_full[i], 128);
@@ -694,27 +818,42 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
         mbar_init(&sh.drain, 1);
         sh.failed = 0;
     }
-    if (wid == 12) tmem_alloc(&sh.tmem, 512);
+    if (wid == 16) tmem_alloc(&sh.tmem, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (wid < 4 * P::kTiles) {
-        softmax<DP, T>(a, sh, w);
-    } else if (wid >= 8 && wid < 12) {
-        feed<DP, kFormat, T>(a, sh, smem, w);
-    } else if (wid == 13) {
-        look_up<DP>(a, sh, w);
-    } else if (threadIdx.x == 12 * 32) {
-        issue<DP>(a, sh, smem, w);
-        tc_commit(&sh.drain);                                    // whatever was issued has ended before the memory is given back
-        wait_on(&sh.drain, 0, sh);
+    // 640 threads are launched with 96 registers each; the warpgroups' shares below add up to 5 * 96.
+    if (wid < 4) {
+        registers_up<128>();
+        softmax<DP, T>(a, sh, w.total, w.parts);
+    } else if (wid < 8) {
+        if constexpr (P::kTiles == 2) {
+            registers_up<128>();
+            softmax<DP, T>(a, sh, w.total, w.parts);
+        } else {
+            registers_down<40>();
+        }
+    } else if (wid < 16) {
+        if constexpr (P::kTiles == 2) registers_down<80>();
+        else registers_up<112>();
+        feed<DP, kFormat, T>(a, sh, smem, wid < 12);
+    } else {
+        registers_down<64>();
+        if (wid == 16) {
+            issue<DP>(sh, smem);
+            if (elected()) tc_commit(&sh.drain);                 // whatever was issued has ended before the memory is given back
+            __syncwarp();
+            warp_wait(&sh.drain, 0, sh);
+        } else if (wid == 17) {
+            look_up<DP>(a, sh, w);
+        }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (threadIdx.x == 0 && sh.failed) kv_flag(a.c.status, ROOMIE_FLAG_WAIT_TIMEOUT);
-    if (wid == 12) tmem_free(sh.tmem, 512);
+    if (wid == 16) tmem_free(sh.tmem, 512);
 }
 
 size_t prompt_partial_bytes(uint32_t dim) {
