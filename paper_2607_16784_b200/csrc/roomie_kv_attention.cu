@@ -539,6 +539,7 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
     a.c = kv_view(cache, layer);
     a.seqs = seqs; a.q_offset = q_offset; a.num_seqs = num_seqs; a.rows = rows;
     a.q_heads = q_heads; a.group = q_heads / cache->kv_heads;
+    a.group_inverse = a.group > 1 ? ~0ull / a.group + 1 : 0;
     a.q = q->data; a.out = out->data; a.lse = lse;
     a.q_token = q->token_stride; a.q_head = q->head_stride; a.o_token = out->token_stride; a.o_head = out->head_stride;
     a.scale_log2 = scale * 1.44269504088896340736f;

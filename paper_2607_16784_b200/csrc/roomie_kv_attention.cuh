@@ -8,6 +8,7 @@ struct AttnArgs {
     KvView c;
     const int32_t *seqs, *q_offset;
     uint32_t num_seqs, rows, q_heads, group;     // group = q_heads / kv heads
+    unsigned long long group_inverse;            // 2^64 / group + 1, 0 for a group of 1
     const void* q;
     void* out;
     float* lse;

@@ -108,6 +108,10 @@ template <int DP> struct Prompt {
 };
 
 // ---- the flat order of the work: sequence, key head, row tile, key block -----------------------------------------------------
+// row / group by the host's 2^64 / group + 1 (exact for 32 bits; group 1 has 0 there)
+__device__ __forceinline__ uint32_t token_of(const AttnArgs& a, uint32_t row) {
+    return a.group_inverse ? (uint32_t)__umul64hi(row, a.group_inverse) : row;
+}
 struct PromptSeq {
     KvSeq s;
     uint32_t rows, tiles;                           // rows a key head
@@ -126,8 +130,8 @@ struct Blocks {
 };
 template <int kRows> __device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const PromptSeq& p, uint32_t tile) {
     const uint32_t last_row = min((tile + 1) * kRows, p.rows) - 1;
-    const int hi = max(min((int)p.s.length, p.start + (int)(last_row / a.group) + 1), 0);
-    const int lo = a.window ? min(max(p.start + (int)(tile * kRows / a.group) - (int)a.window + 1, 0), hi) : 0;
+    const int hi = max(min((int)p.s.length, p.start + (int)token_of(a, last_row) + 1), 0);
+    const int lo = a.window ? min(max(p.start + (int)token_of(a, tile * kRows) - (int)a.window + 1, 0), hi) : 0;
     Blocks b;
     b.first = (uint32_t)lo / kKeys;
     const uint32_t end = ((uint32_t)hi + kKeys - 1) / kKeys;
@@ -288,7 +292,7 @@ template <int DP, class T>
 __device__ __forceinline__ void feed_queries(const AttnArgs& a, PromptShared& sh, uint8_t* sq, const SegInfo& s, uint32_t which, uint32_t r0,
                                              uint32_t r1) {
     using P = Prompt<DP>;
-    constexpr int kLanes = DP / 8, kPass = 128 / kLanes, kBatch = DP > 64 ? 4 : 2;   // lanes of a row side by side, 8 elements each
+    constexpr int kLanes = DP / 8, kPass = 128 / kLanes, kBatch = 8;   // lanes of a row side by side, 8 elements each
     const uint32_t tid = threadIdx.x & 127, c = tid % kLanes;
     for (r0 += tid / kLanes; r0 < r1; r0 += kPass * kBatch) {
         uint4 raw[kBatch];
@@ -297,7 +301,7 @@ __device__ __forceinline__ void feed_queries(const AttnArgs& a, PromptShared& sh
             const uint32_t r = r0 + i * kPass;
             raw[i] = make_uint4(0, 0, 0, 0);
             if (r < s.rows && 8 * c < a.c.dim) {
-                const uint32_t row = s.first_row + r, tok = row / a.group;
+                const uint32_t row = s.first_row + r, tok = token_of(a, row);
                 const T* q = static_cast<const T*>(a.q) + (long long)(s.row0 + tok) * a.q_token +
                              (long long)(s.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
                 if (a.q_aligned) {
@@ -368,11 +372,11 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
                                  : "l"(pool + at + (kRowStep < 16 && (e & 1) ? 8 * a.c.token_step : 0u)));
             }
         };
-        get(step);
         if (seg && !warp_wait(&sh.q_empty, (seg - 1) & 1, sh)) return;
         feed_queries<DP, T>(a, sh, smem, s, seg & 1, keys ? 0 : P::kRows / 2, keys ? P::kRows / 2 : P::kRows);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sh.q_full);
+        get(step);
         for (uint32_t j = 0; j < n; ++j) {
             const uint32_t stage = step % P::kStages, turn = step / P::kStages;
             if (turn && !warp_wait(&empty[stage], (turn - 1) & 1, sh)) return;
@@ -540,92 +544,90 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
-// 2^x for two x of at most 2^7, on the multiply-add units: x = n + f with |f| <= 1/2 (n by adding 1.5 * 2^23, whose last place is one),
-// 2^f by a polynomial of degree 4 (own least-squares fit of the relative error, 2.6e-6: 2^-6 of what the rounding to float16 does),
-// n into the exponent's bits.  The special-function unit gives 4 exponentials a cycle and scheduler; a step's 2 * 128 * 128 would take
-// it as long as all the step's matrix products.
-__device__ __forceinline__ void exp2_poly(uint64_t x, float& u, float& v) {
-    float a, b;
-    split(x, a, b);
-    x = pair(fmaxf(a, -126.0f), fmaxf(b, -126.0f));
-    const uint64_t magic = pair(12582912.0f, 12582912.0f), un_magic = pair(-12582912.0f, -12582912.0f), minus = pair(-1.0f, -1.0f);
-    const uint64_t t = add2(x, magic);
-    const uint64_t f = fma2(add2(t, un_magic), minus, x);
-    uint64_t p = fma2(f, pair(0.009570100344717503f, 0.009570100344717503f), pair(0.05591785907745361f, 0.05591785907745361f));
-    p = fma2(p, f, pair(0.240247443318367f, 0.240247443318367f));
-    p = fma2(p, f, pair(0.6931217908859253f, 0.6931217908859253f));
-    p = fma2(p, f, pair(0.9999992847442627f, 0.9999992847442627f));
-    float ta, tb, pa, pb;
-    split(t, ta, tb);
-    split(p, pa, pb);
-    u = __uint_as_float(__float_as_uint(pa) + (__float_as_uint(ta) << 23));
-    v = __uint_as_float(__float_as_uint(pb) + (__float_as_uint(tb) << 23));
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
-// The row's largest exponent, f * S + log2 vs, among the keys it sees.  kCut: some key of the step is hidden from some row of the warp.
-// The two forms are apart so that the usual one has no branch between its elements (with one, each exponential waits for the one
-// before: 5100 cycles a step instead of 2500, measured); the loops are kept short because the roles share the instruction caches
-// (unrolled over the whole step, a third of all stalls were for instructions).
+// 32 columns of the row: x becomes the exponents f_g * S + off_g (hidden keys -inf), the result is the largest.
+// kCut: some key of the step is hidden from some row of the warp.  The two forms are apart so that the usual one has no branch between
+// its elements (with one, each exponential waits for the one before: 5100 cycles a step instead of 2500, measured).
 template <bool kCut>
-__device__ __forceinline__ float row_top(uint32_t s_at, const PromptShared& sh, uint32_t ring, float q, int k0, int lo, int hi) {
-    float top = -INFINITY;
-#pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-        uint32_t x[32];
-        tmem_load32(s_at + 32 * c, x);
-        tmem_wait_ld();
+__device__ __forceinline__ float exponents32(uint32_t* x, const float* ks, const float* lvs, float q, float base, int k0, int lo, int hi) {
+    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            float mx = -INFINITY;
+    for (int g = 0; g < 2; ++g) {
+        const float f = q * ks[g], off = lvs[g] - base;
+        const uint64_t f2 = pair(f, f), off2 = pair(off, off);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int k = k0 + 32 * c + 16 * g + e;
-                mx = fmaxf(mx, !kCut || (k < hi && k >= lo) ? __uint_as_float(x[16 * g + e]) : -INFINITY);
+        for (int e = 16 * g; e < 16 * g + 16; e += 2) {
+            float u, v;
+            split(fma2(pair(x[e], x[e + 1]), f2, off2), u, v);
+            if (kCut) {
+                u = k0 + e < hi && k0 + e >= lo ? u : -INFINITY;
+                v = k0 + e + 1 < hi && k0 + e + 1 >= lo ? v : -INFINITY;
             }
-            const float v = fmaf(mx, q * sh.ks[ring][2 * c + g], sh.lvs[ring][2 * c + g]);
-            top = fmaxf(top, kCut && mx == -INFINITY ? -INFINITY : v);
+            top[g] = max3(top[g], u, v);
+            x[e] = __float_as_uint(u);
+            x[e + 1] = __float_as_uint(v);
         }
     }
-    return top;
+    return fmaxf(top[0], top[1]);
 }
-// Writes the weights exp2(f * S + log2 vs - base) as float16 over the columns of S that have been read; returns the softmax total's
-// share.  Hidden keys weigh exactly nothing.
+
+// One step of a row, 32 keys at a time: the weights exp2(f * S + log2 vs - m) go as float16 over the columns of S that have been read.
+// They are taken against an old maximum m while the new one is at most 2^8 above it, far from float16's end.  Past that m - a whole
+// number - moves up: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor for o.
+// The loop is kept short because the roles share the instruction caches (unrolled over the whole step, a third of all stalls were for
+// instructions).
 template <bool kCut>
-__device__ __forceinline__ float row_weights(uint32_t s_at, const PromptShared& sh, uint32_t ring, float q, float base, int k0, int lo,
-                                             int hi) {
-    float total = 0.0f;
+__device__ __forceinline__ void row_step(uint32_t s_at, const float* ks, const float* lvs, const float* ivs, float q, int k0, int lo, int hi,
+                                         float& m, float& l, float& moved) {
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
         uint32_t x[32], p[16];
         tmem_load32(s_at + 32 * c, x);
         tmem_wait_ld();
+        const float top = exponents32<kCut>(x, ks + 2 * c, lvs + 2 * c, q, m == -INFINITY ? 0.0f : m, k0 + 32 * c, lo, hi);
+        if (__any_sync(0xffffffffu, top > 8.0f || (m == -INFINITY && top > m))) {
+            const bool none = m == -INFINITY;                    // no key so far: there is nothing to multiply
+            const float up = none ? (top > m ? ceilf(top) : 0.0f) : fmaxf(ceilf(top), 0.0f), f = none ? 1.0f : exp2_fast(-up);
+            if (!none || top > m) m = (none ? 0.0f : m) + up;
+            l *= f;
+            moved *= f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) - up);
+            const __half2 f2 = __float2half2_rn(f);
+#pragma unroll 1
+            for (int b = 0; b < c; ++b) {                        // weights already written
+                tmem_wait_st();
+                tmem_load16(s_at + 16 * b, p);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const __half2 w = __hmul2(reinterpret_cast<const __half2&>(p[e]), f2);
+                    p[e] = reinterpret_cast<const uint32_t&>(w);
+                }
+                tmem_store16(s_at + 16 * b, p);
+            }
+        }
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const float f = q * sh.ks[ring][2 * c + g], off = sh.lvs[ring][2 * c + g] - base;
-            const uint64_t f2 = pair(f, f), off2 = pair(off, off);
             uint64_t sum = 0;
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                float u, v;
-                split(fma2(pair(x[16 * g + e], x[16 * g + e + 1]), f2, off2), u, v);
-                if (kCut) {
-                    const int k = k0 + 32 * c + 16 * g + e;
-                    u = k < hi && k >= lo ? u : -INFINITY;
-                    v = k + 1 < hi && k + 1 >= lo ? v : -INFINITY;
-                }
-                u = exp2_fast(u);
-                v = exp2_fast(v);
+                const float u = exp2_fast(__uint_as_float(x[16 * g + e])), v = exp2_fast(__uint_as_float(x[16 * g + e + 1]));
                 sum = add2(sum, pair(u, v));
                 const __half2 h = __floats2half2_rn(u, v);
                 p[8 * g + e / 2] = reinterpret_cast<const uint32_t&>(h);
             }
             float even, odd;
             split(sum, even, odd);
-            total = fmaf(even + odd, sh.ivs[ring][2 * c + g], total);
+            l = fmaf(even + odd, ivs[2 * c + g], l);
         }
         tmem_store16(s_at + 16 * c, p);
     }
-    return total;
 }
 
 // ---- warpgroups 0 and 1: softmax, and the end of a segment ------------------------------------------------------------------------
@@ -644,7 +646,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         const bool on = t * 128 < s.rows, mine = t * 128 + r < s.rows;
         int hi = 0, lo = 0;
         if (mine) {
-            const int pos = s.start + (int)((s.first_row + t * 128 + r) / a.group);
+            const int pos = s.start + (int)token_of(a, s.first_row + t * 128 + r);
             hi = max(min(pos + 1, (int)s.length), 0);
             lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
         }
@@ -661,30 +663,23 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             tc_fence_after();
             if (j == 0) q = sh.q_scale[seg & 1][t * 128 + r];
             const bool cut = __any_sync(0xffffffffu, k0 < lo || k0 + kKeys > hi);
-            // The weights are taken against an old maximum while the new one is at most 2^8 above it: they then stay far from float16's
-            // end, and o is rescaled in tensor memory only now and then.
-            const float top = cut ? row_top<true>(s_at, sh, ring, q, k0, lo, hi) : row_top<false>(s_at, sh, ring, q, k0, lo, hi);
-            if (__any_sync(0xffffffffu, top > m + 8.0f || (m == -INFINITY && top > m))) {
-                const float to = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_fast(m - to);
-                m = to;
-                l *= f;
-                if (j) {
-                    if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
-                    tc_fence_after();
+            float moved = 1.0f;
+            if (cut) row_step<true>(s_at, sh.ks[ring], sh.lvs[ring], sh.ivs[ring], q, k0, lo, hi, m, l, moved);
+            else row_step<false>(s_at, sh.ks[ring], sh.lvs[ring], sh.ivs[ring], q, k0, lo, hi, m, l, moved);
+            if (j && __any_sync(0xffffffffu, moved != 1.0f)) {   // o of the steps before
+                if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
+                tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t y[32];
-                        tmem_load32(o_at + 32 * c, y);
-                        tmem_wait_ld();
+                for (int c = 0; c < DP / 32; ++c) {
+                    uint32_t y[32];
+                    tmem_load32(o_at + 32 * c, y);
+                    tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-                        tmem_store32(o_at + 32 * c, y);
-                    }
+                    for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * moved);
+                    tmem_store32(o_at + 32 * c, y);
                 }
             }
             ++o_turn;
-            const float base = m == -INFINITY ? 0.0f : m;
-            l += cut ? row_weights<true>(s_at, sh, ring, q, base, k0, lo, hi) : row_weights<false>(s_at, sh, ring, q, base, k0, lo, hi);
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&sh.p_full[t]);
@@ -692,7 +687,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
 
         // ---- the end of a segment: rows go out, or wait in the workspace for their other parts ---------------------------------
         const bool complete = s.b0 == 0 && n == s.count;
-        const uint32_t row = s.first_row + t * 128 + r, tok = row / a.group, h = s.head * a.group + row - tok * a.group;
+        const uint32_t row = s.first_row + t * 128 + r, tok = token_of(a, row), h = s.head * a.group + row - tok * a.group;
         T* out = static_cast<T*>(a.out) + (long long)(s.row0 + tok) * a.o_token + (long long)h * a.o_head;
         auto put_lse = [&](float mx, float sum) {
             if (a.lse) a.lse[(size_t)(s.row0 + tok) * a.q_heads + h] = sum > 0.0f ? (mx + log2f(sum)) * kLn2 : sum == 0.0f ? -INFINITY : sum;
