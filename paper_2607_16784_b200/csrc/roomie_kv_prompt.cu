@@ -2,11 +2,13 @@
 // tensor cores, accumulators in tensor memory.
 //
 // A block (640 threads, one an SM) takes kTiles tiles of 128 rows of one key head - a row is one (token, query head) of the
-// group - through the keys 128 at a time:
-//   S = q K^T        both operands in shared memory, float16; S in tensor memory
+// group - through the keys 128 at a time, in two halves of 64:
+//   S = q K^T        both operands in shared memory, float16; S in tensor memory, 64 columns a half
 //   softmax          a thread owns a row: reads S, writes the probabilities as float16 over the columns it has read
 //   o += p V         p from tensor memory, V from shared memory, o in tensor memory
-// Warpgroups 0 and 1 are the softmax of tiles 0 and 1, so that one tile's softmax overlaps the other's products; warpgroups 2 and 3
+// While a tile's softmax is at one half, its products for the other half run (o for the half before, then S for the half after), and
+// warpgroups 0 and 1 are the softmax of tiles 0 and 1.  (With halves of 128 keys the softmax waited for its own products: 4750 cycles a
+// step of 128 keys and two tiles, where the products alone take 2048.)  Warpgroups 2 and 3
 // turn the codes of keys and of values into float16 operands (the scales stay out of them); in warpgroup 4 one warp issues the
 // products and one looks up pages and scales, some steps ahead.
 //
@@ -250,7 +252,7 @@ struct SegInfo {                                    // a segment as the other wa
     unsigned long long item;
 };
 struct PromptShared {
-    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], look_full[kRing],
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_full[2], look_full[kRing],
         look_free[kRing], join[2], drain;
     unsigned long long walk[24];
     long long at[kRing][8];                         // of 16 keys each: bytes from the pool's start to them (-1: none), key scale, log2
@@ -292,46 +294,48 @@ template <int DP, class T>
 __device__ __forceinline__ void feed_queries(const AttnArgs& a, PromptShared& sh, uint8_t* sq, const SegInfo& s, uint32_t which, uint32_t r0,
                                              uint32_t r1) {
     using P = Prompt<DP>;
-    constexpr int kLanes = DP / 8, kPass = 128 / kLanes, kBatch = 8;   // lanes of a row side by side, 8 elements each
+    constexpr int kLanes = DP / 8, kPass = 128 / kLanes;         // lanes of a row side by side, 8 elements each
     const uint32_t tid = threadIdx.x & 127, c = tid % kLanes;
-    for (r0 += tid / kLanes; r0 < r1; r0 += kPass * kBatch) {
-        uint4 raw[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {                       // a batch of rows on their way together
-            const uint32_t r = r0 + i * kPass;
-            raw[i] = make_uint4(0, 0, 0, 0);
-            if (r < s.rows && 8 * c < a.c.dim) {
-                const uint32_t row = s.first_row + r, tok = token_of(a, row);
-                const T* q = static_cast<const T*>(a.q) + (long long)(s.row0 + tok) * a.q_token +
-                             (long long)(s.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
-                if (a.q_aligned) {
-                    raw[i] = *reinterpret_cast<const uint4*>(q);
-                } else {
-                    const unsigned short* h = reinterpret_cast<const unsigned short*>(q);
-                    raw[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                                        h[6] | (uint32_t)h[7] << 16);
-                }
-            }
+    r0 += tid / kLanes;
+    uint8_t* to0 = sq + (c >> 3) * P::kSlab + (((c & 7) ^ (r0 & 7)) << 4);         // kPass is a multiple of 8, or r & 7 moves with it
+    auto place = [&](uint32_t r) {
+        return kPass % 8 == 0 ? to0 + (r >> 7) * P::kOperand + (r & 127) * 128
+                              : sq + (c >> 3) * P::kSlab + (r >> 7) * P::kOperand + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+    };
+#pragma unroll 1
+    for (uint32_t r = r0; r < r1; r += kPass) {                  // as they come, all on their way together
+        const uint32_t row = s.first_row + r, tok = token_of(a, row);
+        const bool there = r < s.rows && 8 * c < a.c.dim;
+        const T* q = static_cast<const T*>(a.q);
+        if (there) q += (long long)(s.row0 + tok) * a.q_token + (long long)(s.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
+        if (a.q_aligned) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(place(r))), "l"(q), "r"(there ? 16u : 0u) : "memory");
+        } else {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(q);
+            if (there)
+                x = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+            *reinterpret_cast<uint4*>(place(r)) = x;
         }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+    for (uint32_t r = r0; r < r1; r += kPass) {                  // each thread its own pieces
+        uint4* at = reinterpret_cast<uint4*>(place(r));
+        float x[8], amax = 0.0f;
+        unpack<T>(*at, x);
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const uint32_t r = r0 + i * kPass;
-            float x[8], amax = 0.0f;
-            unpack<T>(raw[i], x);
+        for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(x[k]));
 #pragma unroll
-            for (int k = 0; k < 8; ++k) amax = fmaxf(amax, fabsf(x[k]));
+        for (int d = 1; d < kLanes; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+        int e = (int)(__float_as_uint(amax) >> 23) - 127;
+        e = max(min(e, 126), -126);
+        const float down = pow2f(-e);
+        __half2 h[4];
 #pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-            int e = (int)(__float_as_uint(amax) >> 23) - 127;
-            e = max(min(e, 126), -126);
-            const float down = pow2f(-e);
-            __half2 h[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(x[2 * k] * down, x[2 * k + 1] * down);
-            uint8_t* to = sq + (r >> 7) * P::kOperand + (c >> 3) * P::kSlab + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(h);
-            if (c == 0) sh.q_scale[which][r] = pow2f(e) * a.scale_log2;
-        }
+        for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(x[2 * k] * down, x[2 * k + 1] * down);
+        *at = *reinterpret_cast<const uint4*>(h);
+        if (c == 0) sh.q_scale[which][r] = pow2f(e) * a.scale_log2;
     }
 }
 
@@ -472,49 +476,60 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem) {
     const uint32_t sq = smem_addr(smem), sk = sq + P::kTiles * P::kOperand, sv = sk + P::kStages * P::kOperand;
     const uint64_t q0 = operand(sq, 16), k0 = operand(sk, 16), v0 = operand(sv, P::kSlab);
     const uint32_t tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
-    constexpr uint32_t kS = instruction(kKeys, false), kO = instruction(DP, true);
+    constexpr uint32_t kS = instruction(kKeys / 2, false), kO = instruction(DP, true);
     uint32_t step = 0;
     for (uint32_t seg = 0;; ++seg) {
         if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
         const uint32_t n = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].steps, 0);
         const bool two = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].rows, 0) > 128;
-        if (n == 0 || !warp_wait(&sh.q_full, seg & 1, sh)) return;
+        if (n == 0 || !warp_wait(&sh.q_full, seg & 1, sh) || !warp_wait(&sh.k_full[step % P::kStages], (step / P::kStages) & 1, sh)) return;
         tc_fence_after();
-        for (uint32_t j = 0; j <= n; ++j) {                      // S of step j, o of step j - 1
-            const uint32_t now = step + j, stage = now % P::kStages, old = now - 1, old_stage = old % P::kStages;
-            if (j < n && !warp_wait(&sh.k_full[stage], (now / P::kStages) & 1, sh)) return;
-            if (j && !warp_wait(&sh.v_full[old_stage], (old / P::kStages) & 1, sh)) return;
-            const uint64_t k = k0 + stage * (P::kOperand >> 4), v = v0 + old_stage * (P::kOperand >> 4);
+        // Half h: o of half h - 2, then S of half h into the columns that held its p.  A tile without rows only keeps step.
+        const uint32_t halves = 2 * n;
+#pragma unroll 1
+        for (uint32_t h = 0; h < halves + 2; ++h) {
+            const uint32_t next = step + h / 2, stage = next % P::kStages;                   // keys of half h
+            const uint32_t now = next - 1, old_stage = now % P::kStages, side = h & 1;       // values of half h - 2
+            if (h >= 2 && side == 0 && !warp_wait(&sh.v_full[old_stage], (now / P::kStages) & 1, sh)) return;
+            const uint64_t k = k0 + ((stage * P::kOperand + side * 8192) >> 4), v = v0 + ((old_stage * P::kOperand + side * 8192) >> 4);
 #pragma unroll 1
             for (int t = 0; t < P::kTiles; ++t) {
-                const uint32_t s_at = tm + t * 128, o_at = tm + P::kTiles * 128 + t * DP;
-                if (j && !warp_wait(&sh.p_full[t], old & 1, sh)) return;
-                const bool on = t == 0 || two;                   // a tile without rows only keeps step
-                tc_fence_after();
-                if (elected()) {
-                    if (on && j) {
+                const uint32_t s_at = tm + t * 128 + side * 64, o_at = tm + P::kTiles * 128 + t * DP;
+                const bool on = t == 0 || two;
+                if (h >= 2) {
+                    if (!warp_wait(&sh.p_full[t][side], now & 1, sh)) return;
+                    tc_fence_after();
+                    if (on && elected()) {
 #pragma unroll
-                        for (int i = 0; i < kKeys / 16; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, j > 1 || i > 0);
+                        for (int i = 0; i < kKeys / 32; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, h > 2 || i > 0);
                         tc_commit(&sh.o_full[t]);
                     }
-                    if (on && j < n) {
-#pragma unroll
-                        for (int i = 0; i < DP / 16; ++i) {
-                            const uint32_t off = ((i / 4) * P::kSlab + (i % 4) * 32) >> 4;
-                            mma_ss(s_at, q0 + (t * P::kOperand >> 4) + off, k + off, kS, i > 0);
-                        }
+                    __syncwarp();
+                }
+                if (h < halves) {
+                    if (h >= 2 && side == 0 && t == 0) {
+                        if (!warp_wait(&sh.k_full[stage], (next / P::kStages) & 1, sh)) return;
+                        tc_fence_after();
                     }
-                    if (j < n) tc_commit(&sh.s_full[t]);
+                    if (elected()) {
+                        if (on)
+#pragma unroll
+                            for (int i = 0; i < DP / 16; ++i) {
+                                const uint32_t off = ((i / 4) * P::kSlab + (i % 4) * 32) >> 4;
+                                mma_ss(s_at, q0 + (t * P::kOperand >> 4) + off, k + off, kS, i > 0);
+                            }
+                        tc_commit(&sh.s_full[t][side]);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
-            if (elected()) {
-                if (j) {
+            if (side == 1 && elected()) {
+                if (h >= 2) {
                     tc_commit(&sh.v_empty[old_stage]);
-                    tc_commit(&sh.look_free[old % kRing]);
+                    tc_commit(&sh.look_free[now % kRing]);
                 }
-                if (j < n) tc_commit(&sh.k_empty[stage]);
-                if (j + 1 == n) tc_commit(&sh.q_empty);
+                if (h < halves) tc_commit(&sh.k_empty[stage]);
+                if (h + 1 == halves) tc_commit(&sh.q_empty);
             }
             __syncwarp();
         }
@@ -550,82 +565,88 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// 32 columns of the row: x becomes the exponents f_g * S + off_g (hidden keys -inf), the result is the largest.
-// kCut: some key of the step is hidden from some row of the warp.  The two forms are apart so that the usual one has no branch between
-// its elements (with one, each exponential waits for the one before: 5100 cycles a step instead of 2500, measured).
-template <bool kCut>
-__device__ __forceinline__ float exponents32(uint32_t* x, const float* ks, const float* lvs, float q, float base, int k0, int lo, int hi) {
-    float top[2] = {-INFINITY, -INFINITY};
+// 2^x of 32 columns, as float16 pairs; the result is their share of the softmax total.
+__device__ __forceinline__ float weights32(const uint32_t* x, uint32_t* p, const float* ivs) {
+    float total = 0.0f;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-        const float f = q * ks[g], off = lvs[g] - base;
-        const uint64_t f2 = pair(f, f), off2 = pair(off, off);
+        uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int e = 16 * g; e < 16 * g + 16; e += 2) {
+        for (int e = 0; e < 16; e += 2) {
+            const float u = exp2_fast(__uint_as_float(x[16 * g + e])), v = exp2_fast(__uint_as_float(x[16 * g + e + 1]));
+            sum[(e / 2) & 1] = add2(sum[(e / 2) & 1], pair(u, v));
+            const __half2 h = __floats2half2_rn(u, v);
+            p[8 * g + e / 2] = reinterpret_cast<const uint32_t&>(h);
+        }
+        float even, odd;
+        split(add2(sum[0], sum[1]), even, odd);
+        total = fmaf(even + odd, ivs[g], total);
+    }
+    return total;
+}
+
+// Half a step of a row, 64 keys, 32 at a time: the weights exp2(f * S + log2 vs - m) go as float16 over the columns of S that have been
+// read.  They are taken against an old maximum m while the new one is at most 2^8 above it, far from float16's end.  Past that m - a
+// whole number - moves up: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor
+// for o.  cut: some key is hidden from some row of the warp; hidden ones weigh exactly nothing.  No branch stands between the elements
+// (with one, each exponential waits for the one before), and the loop is kept short because the roles share the instruction caches
+// (unrolled over a whole step, a third of all stalls were for instructions).
+__device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const float* lvs, const float* ivs, float q, bool cut, int k0, int lo,
+                                         int hi, float& m, float& l, float& moved) {
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+        uint32_t x[32], p[16];
+        tmem_load32(s_at + 32 * c, x);
+        const float base = m == -INFINITY ? 0.0f : m;
+        const float fa = q * ks[2 * c], fb = q * ks[2 * c + 1], oa = lvs[2 * c] - base, ob = lvs[2 * c + 1] - base;
+        const uint64_t f2[2] = {pair(fa, fa), pair(fb, fb)}, off2[2] = {pair(oa, oa), pair(ob, ob)};
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
             float u, v;
-            split(fma2(pair(x[e], x[e + 1]), f2, off2), u, v);
-            if (kCut) {
-                u = k0 + e < hi && k0 + e >= lo ? u : -INFINITY;
-                v = k0 + e + 1 < hi && k0 + e + 1 >= lo ? v : -INFINITY;
-            }
-            top[g] = max3(top[g], u, v);
+            split(fma2(pair(x[e], x[e + 1]), f2[e / 16], off2[e / 16]), u, v);
             x[e] = __float_as_uint(u);
             x[e + 1] = __float_as_uint(v);
         }
-    }
-    return fmaxf(top[0], top[1]);
-}
-
-// One step of a row, 32 keys at a time: the weights exp2(f * S + log2 vs - m) go as float16 over the columns of S that have been read.
-// They are taken against an old maximum m while the new one is at most 2^8 above it, far from float16's end.  Past that m - a whole
-// number - moves up: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor for o.
-// The loop is kept short because the roles share the instruction caches (unrolled over the whole step, a third of all stalls were for
-// instructions).
-template <bool kCut>
-__device__ __forceinline__ void row_step(uint32_t s_at, const float* ks, const float* lvs, const float* ivs, float q, int k0, int lo, int hi,
-                                         float& m, float& l, float& moved) {
-#pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-        uint32_t x[32], p[16];
-        tmem_load32(s_at + 32 * c, x);
-        tmem_wait_ld();
-        const float top = exponents32<kCut>(x, ks + 2 * c, lvs + 2 * c, q, m == -INFINITY ? 0.0f : m, k0 + 32 * c, lo, hi);
-        if (__any_sync(0xffffffffu, top > 8.0f || (m == -INFINITY && top > m))) {
+        if (cut) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                const int k = k0 + 32 * c + e;
+                if (k >= hi || k < lo) x[e] = 0xff800000u;       // -inf
+            }
+        }
+        float top[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top[i] = fmaxf(__uint_as_float(x[8 * i]), __uint_as_float(x[8 * i + 1]));
+#pragma unroll
+            for (int e = 2; e < 8; e += 2) top[i] = max3(top[i], __uint_as_float(x[8 * i + e]), __uint_as_float(x[8 * i + e + 1]));
+        }
+        const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float total = weights32(x, p, ivs + 2 * c);
+        if (__any_sync(0xffffffffu, high > 8.0f || (m == -INFINITY && high > m))) {
             const bool none = m == -INFINITY;                    // no key so far: there is nothing to multiply
-            const float up = none ? (top > m ? ceilf(top) : 0.0f) : fmaxf(ceilf(top), 0.0f), f = none ? 1.0f : exp2_fast(-up);
-            if (!none || top > m) m = (none ? 0.0f : m) + up;
+            const float up = none ? (high > m ? ceilf(high) : 0.0f) : fmaxf(ceilf(high), 0.0f), f = none ? 1.0f : exp2_fast(-up);
+            if (!none || high > m) m = base + up;
             l *= f;
             moved *= f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) - up);
-            const __half2 f2 = __float2half2_rn(f);
-#pragma unroll 1
-            for (int b = 0; b < c; ++b) {                        // weights already written
+            if (c) {                                             // weights already written
+                const __half2 f2h = __float2half2_rn(f);
                 tmem_wait_st();
-                tmem_load16(s_at + 16 * b, p);
+                tmem_load16(s_at, p);
                 tmem_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const __half2 w = __hmul2(reinterpret_cast<const __half2&>(p[e]), f2);
+                    const __half2 w = __hmul2(reinterpret_cast<const __half2&>(p[e]), f2h);
                     p[e] = reinterpret_cast<const uint32_t&>(w);
                 }
-                tmem_store16(s_at + 16 * b, p);
+                tmem_store16(s_at, p);
             }
+            total = weights32(x, p, ivs + 2 * c);
         }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            uint64_t sum = 0;
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const float u = exp2_fast(__uint_as_float(x[16 * g + e])), v = exp2_fast(__uint_as_float(x[16 * g + e + 1]));
-                sum = add2(sum, pair(u, v));
-                const __half2 h = __floats2half2_rn(u, v);
-                p[8 * g + e / 2] = reinterpret_cast<const uint32_t&>(h);
-            }
-            float even, odd;
-            split(sum, even, odd);
-            l = fmaf(even + odd, ivs[2 * c + g], l);
-        }
+        l += total;
         tmem_store16(s_at + 16 * c, p);
     }
 }
@@ -652,21 +673,21 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         }
         float m = -INFINITY, l = 0.0f, q = 0.0f;
         int k0 = (int)s.key0;
-        for (uint32_t j = 0; j < n; ++j, ++step, k0 += kKeys) {
-            const uint32_t ring = step % kRing;
-            if (j && !warp_wait(&sh.look_full[ring], (step / kRing) & 1, sh)) return;
-            if (!warp_wait(&sh.s_full[t], step & 1, sh)) return;
+        for (uint32_t h = 0; h < 2 * n; ++h, k0 += kKeys / 2) {
+            const uint32_t side = h & 1, ring = step % kRing;
+            if (h && !side && !warp_wait(&sh.look_full[ring], (step / kRing) & 1, sh)) return;
+            if (!warp_wait(&sh.s_full[t][side], step & 1, sh)) return;
+            step += side;
             if (!on) {
-                mbar_arrive(&sh.p_full[t]);
+                mbar_arrive(&sh.p_full[t][side]);
                 continue;
             }
             tc_fence_after();
-            if (j == 0) q = sh.q_scale[seg & 1][t * 128 + r];
-            const bool cut = __any_sync(0xffffffffu, k0 < lo || k0 + kKeys > hi);
+            if (h == 0) q = sh.q_scale[seg & 1][t * 128 + r];
+            const bool cut = __any_sync(0xffffffffu, k0 < lo || k0 + kKeys / 2 > hi);
             float moved = 1.0f;
-            if (cut) row_step<true>(s_at, sh.ks[ring], sh.lvs[ring], sh.ivs[ring], q, k0, lo, hi, m, l, moved);
-            else row_step<false>(s_at, sh.ks[ring], sh.lvs[ring], sh.ivs[ring], q, k0, lo, hi, m, l, moved);
-            if (j && __any_sync(0xffffffffu, moved != 1.0f)) {   // o of the steps before
+            row_half(s_at + 64 * side, sh.ks[ring] + 4 * side, sh.lvs[ring] + 4 * side, sh.ivs[ring] + 4 * side, q, cut, k0, lo, hi, m, l, moved);
+            if (h && __any_sync(0xffffffffu, moved != 1.0f)) {   // o of the halves before
                 if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
                 tc_fence_after();
 #pragma unroll 1
@@ -682,7 +703,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             ++o_turn;
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&sh.p_full[t]);
+            mbar_arrive(&sh.p_full[t][side]);
         }
 
         // ---- the end of a segment: rows go out, or wait in the workspace for their other parts ---------------------------------
@@ -800,8 +821,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
             mbar_init(&sh.v_full[i], 128);
             mbar_init(&sh.k_empty[i], 1);
             mbar_init(&sh.v_empty[i], 1);
-            mbar_init(&sh.s_full[i], 1);
-            mbar_init(&sh.p_full[i], 128);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(&sh.s_full[i][h], 1);
+                mbar_init(&sh.p_full[i][h], 128);
+            }
             mbar_init(&sh.o_full[i], 1);
         }
         for (int i = 0; i < kRing; ++i) {
