@@ -9,8 +9,8 @@
 // While a tile's softmax is at one half, its products for the other half run (o for the half before, then S for the half after), and
 // warpgroups 0 and 1 are the softmax of tiles 0 and 1.  (With halves of 128 keys the softmax waited for its own products: 4750 cycles a
 // step of 128 keys and two tiles, where the products alone take 2048.)  Warpgroups 2 and 3
-// turn the codes of keys and of values into float16 operands (the scales stay out of them); in warpgroup 4 one warp issues the
-// products and one looks up pages and scales, some steps ahead.
+// turn the codes of keys and of values into float16 operands (the scales stay out of them); in warpgroup 4 a warp for
+// each tile issues its products and one looks up pages and scales, some steps ahead.
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
 // Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M the running maximum of s + log2 vs, is what multiplies
@@ -33,14 +33,17 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+// Operands in shared memory are given by the low halves of their descriptors; the high half is the same for all (kOperandHigh).
+constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+template <bool kAdd> __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tmov.b64 x, {%1, %4};\n\tmov.b64 y, {%2, %4};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "n"(kOperandHigh), "n"((int)kAdd)
                  : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tmov.b64 y, {%2, %4};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "n"(kOperandHigh),
+                 "r"((uint32_t)add)
                  : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* x) {
@@ -84,10 +87,7 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
 
 // Shared-memory operand: rows of 128 bytes (64 float16), 16-byte chunks exchanged by chunk ^ (row & 7) within groups of 8 rows
 // (1024 bytes apart).  `lbo`: distance of the next 64 columns where the operand's columns are the contiguous direction.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t lbo) {
-    return (uint64_t)((at & 0x3ffffu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)2 << 61;
-}
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t lbo) { return (at & 0x3ffffu) >> 4 | (lbo >> 4) << 16; }
 // float16 operands, float32 accumulator, 128 rows, n columns; `columns_contiguous`: of the second operand
 __host__ __device__ constexpr uint32_t instruction(uint32_t n, bool columns_contiguous) {
     return 1u << 4 | (columns_contiguous ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
@@ -462,26 +462,27 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
     }
 }
 
-// ---- warpgroup 4: one warp issues the products -----------------------------------------------------------------------------------
-// The whole warp goes through the loop, so that operands stay in uniform registers; one elected lane issues.  (A single thread's
-// branch around all of it took 280 cycles an instruction, where one has 64.)
+// ---- warpgroup 4: a warp for each tile issues its products ---------------------------------------------------------------------------
+// The whole warp goes through the loop, so that what does not depend on the lane stays in uniform registers; one elected lane issues.
+// (A single thread's branch around all of it took 280 cycles an instruction, this some 80; the instructions themselves have 32 and 64,
+// so one warp for both tiles was what the step waited for.)
 __device__ __forceinline__ bool elected() {
     uint32_t p;
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
     return p != 0;
 }
 template <int DP>
-__device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem) {
+__device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uint32_t t) {
     using P = Prompt<DP>;
     const uint32_t sq = smem_addr(smem), sk = sq + P::kTiles * P::kOperand, sv = sk + P::kStages * P::kOperand;
-    const uint64_t q0 = operand(sq, 16), k0 = operand(sk, 16), v0 = operand(sv, P::kSlab);
-    const uint32_t tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
+    const uint32_t q = operand(sq + t * P::kOperand, 16), k0 = operand(sk, 16), v0 = operand(sv, P::kSlab);
+    const uint32_t tm = __shfl_sync(0xffffffffu, sh.tmem, 0), s_tile = tm + t * 128, o_at = tm + P::kTiles * 128 + t * DP;
     constexpr uint32_t kS = instruction(kKeys / 2, false), kO = instruction(DP, true);
     uint32_t step = 0;
     for (uint32_t seg = 0;; ++seg) {
         if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
         const uint32_t n = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].steps, 0);
-        const bool two = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].rows, 0) > 128;
+        const bool on = __shfl_sync(0xffffffffu, sh.seg[seg % kSegments].rows, 0) > t * 128;
         if (n == 0 || !warp_wait(&sh.q_full, seg & 1, sh) || !warp_wait(&sh.k_full[step % P::kStages], (step / P::kStages) & 1, sh)) return;
         tc_fence_after();
         // Half h: o of half h - 2, then S of half h into the columns that held its p.  A tile without rows only keeps step.
@@ -490,38 +491,35 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem) {
         for (uint32_t h = 0; h < halves + 2; ++h) {
             const uint32_t next = step + h / 2, stage = next % P::kStages;                   // keys of half h
             const uint32_t now = next - 1, old_stage = now % P::kStages, side = h & 1;       // values of half h - 2
-            if (h >= 2 && side == 0 && !warp_wait(&sh.v_full[old_stage], (now / P::kStages) & 1, sh)) return;
-            const uint64_t k = k0 + ((stage * P::kOperand + side * 8192) >> 4), v = v0 + ((old_stage * P::kOperand + side * 8192) >> 4);
-#pragma unroll 1
-            for (int t = 0; t < P::kTiles; ++t) {
-                const uint32_t s_at = tm + t * 128 + side * 64, o_at = tm + P::kTiles * 128 + t * DP;
-                const bool on = t == 0 || two;
-                if (h >= 2) {
-                    if (!warp_wait(&sh.p_full[t][side], now & 1, sh)) return;
-                    tc_fence_after();
-                    if (on && elected()) {
+            const uint32_t s_at = s_tile + side * 64;
+            if (h >= 2) {
+                if (side == 0 && !warp_wait(&sh.v_full[old_stage], (now / P::kStages) & 1, sh)) return;
+                if (!warp_wait(&sh.p_full[t][side], now & 1, sh)) return;
+                tc_fence_after();
+                const uint32_t v = v0 + ((old_stage * P::kOperand + side * 8192) >> 4);
+                if (on && elected()) {
 #pragma unroll
-                        for (int i = 0; i < kKeys / 32; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, h > 2 || i > 0);
-                        tc_commit(&sh.o_full[t]);
-                    }
-                    __syncwarp();
+                    for (int i = 0; i < kKeys / 32; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, h > 2 || i > 0);
+                    tc_commit(&sh.o_full[t]);
                 }
-                if (h < halves) {
-                    if (h >= 2 && side == 0 && t == 0) {
-                        if (!warp_wait(&sh.k_full[stage], (next / P::kStages) & 1, sh)) return;
-                        tc_fence_after();
-                    }
-                    if (elected()) {
-                        if (on)
+                __syncwarp();
+            }
+            if (h < halves) {
+                if (h >= 2 && side == 0 && !warp_wait(&sh.k_full[stage], (next / P::kStages) & 1, sh)) return;
+                tc_fence_after();
+                const uint32_t k = k0 + ((stage * P::kOperand + side * 8192) >> 4);
+                if (elected()) {
+                    if (on) {
+                        mma_ss<false>(s_at, q, k, kS);
 #pragma unroll
-                            for (int i = 0; i < DP / 16; ++i) {
-                                const uint32_t off = ((i / 4) * P::kSlab + (i % 4) * 32) >> 4;
-                                mma_ss(s_at, q0 + (t * P::kOperand >> 4) + off, k + off, kS, i > 0);
-                            }
-                        tc_commit(&sh.s_full[t][side]);
+                        for (int i = 1; i < DP / 16; ++i) {
+                            const uint32_t off = ((i / 4) * P::kSlab + (i % 4) * 32) >> 4;
+                            mma_ss<true>(s_at, q + off, k + off, kS);
+                        }
                     }
-                    __syncwarp();
+                    tc_commit(&sh.s_full[t][side]);
                 }
+                __syncwarp();
             }
             if (side == 1 && elected()) {
                 if (h >= 2) {
@@ -815,12 +813,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
     const uint32_t wid = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         mbar_init(&sh.q_full, 256);
-        mbar_init(&sh.q_empty, 1);
+        mbar_init(&sh.q_empty, P::kTiles);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.k_full[i], 128);
             mbar_init(&sh.v_full[i], 128);
-            mbar_init(&sh.k_empty[i], 1);
-            mbar_init(&sh.v_empty[i], 1);
+            mbar_init(&sh.k_empty[i], P::kTiles);
+            mbar_init(&sh.v_empty[i], P::kTiles);
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&sh.s_full[i][h], 1);
                 mbar_init(&sh.p_full[i][h], 128);
@@ -829,11 +827,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sh.look_full[i], 8);
-            mbar_init(&sh.look_free[i], 1);
+            mbar_init(&sh.look_free[i], P::kTiles);
         }
         mbar_init(&sh.join[0], 128 * P::kTiles);
         mbar_init(&sh.join[1], 1);
-        mbar_init(&sh.drain, 1);
+        mbar_init(&sh.drain, P::kTiles);
         sh.failed = 0;
     }
     if (wid == 16) tmem_alloc(&sh.tmem, 512);
@@ -857,8 +855,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
         feed<DP, kFormat, T>(a, sh, smem, wid < 12);
     } else {
         registers_down<64>();
-        if (wid == 16) {
-            issue<DP>(sh, smem);
+        if (wid == 16 || (wid == 18 && P::kTiles == 2)) {
+            issue<DP>(sh, smem, wid == 18);
             if (elected()) tc_commit(&sh.drain);                 // whatever was issued has ended before the memory is given back
             __syncwarp();
             warp_wait(&sh.drain, 0, sh);
