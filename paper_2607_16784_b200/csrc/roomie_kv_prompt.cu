@@ -79,7 +79,19 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* x) {
         "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15])
         : "memory");
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The wait names the registers of the load before it: nothing that uses them may be moved in front of it.
+__device__ __forceinline__ void tmem_wait16(uint32_t* x) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]),
+          "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15])::"memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t* x) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]),
+          "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15]),
+          "+r"(x[16]), "+r"(x[17]), "+r"(x[18]), "+r"(x[19]), "+r"(x[20]), "+r"(x[21]), "+r"(x[22]), "+r"(x[23]),
+          "+r"(x[24]), "+r"(x[25]), "+r"(x[26]), "+r"(x[27]), "+r"(x[28]), "+r"(x[29]), "+r"(x[30]), "+r"(x[31])::"memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
@@ -127,6 +139,9 @@ template <int kRows> __device__ __forceinline__ PromptSeq prompt_seq(const AttnA
     p.start = (int)p.s.length - (int)p.s.count;
     return p;
 }
+// A tile's queries, first step and results cost a block about as much time as kTileCost steps: its share of the flat order has so many
+// units in front, which hold no key block.
+constexpr uint32_t kTileCost = 4;
 struct Blocks {
     uint32_t first, count;                          // key blocks that some row of the tile sees, at least one
 };
@@ -141,8 +156,8 @@ template <int kRows> __device__ __forceinline__ Blocks tile_blocks(const AttnArg
     return b;
 }
 template <int kRows> __device__ __forceinline__ unsigned long long seq_blocks(const AttnArgs& a, const PromptSeq& p, int lane) {
-    unsigned long long n = 0;                       // of one key head; by a whole warp
-    for (uint32_t t = lane; t < p.tiles; t += 32) n += tile_blocks<kRows>(a, p, t).count;
+    unsigned long long n = 0;                       // units of one key head; by a whole warp
+    for (uint32_t t = lane; t < p.tiles; t += 32) n += tile_blocks<kRows>(a, p, t).count + kTileCost;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
     return n;
@@ -150,7 +165,7 @@ template <int kRows> __device__ __forceinline__ unsigned long long seq_blocks(co
 
 struct Walk {                                       // where in the flat order a thread is; the same in all threads of the block
     unsigned long long at, end, total, parts;
-    uint32_t seq, head, tile, block;                // block: of the tile, from its first
+    uint32_t seq, head, tile, unit;                 // unit: of the tile
 };
 
 struct Segment {                                    // a run of blocks of one (sequence, head, tile)
@@ -167,16 +182,17 @@ template <int kRows> __device__ __forceinline__ bool next_segment(const AttnArgs
         s.p = prompt_seq<kRows>(a, w.seq, false);
     }
     const Blocks b = tile_blocks<kRows>(a, s.p, w.tile);
+    const uint32_t until = (uint32_t)min((unsigned long long)b.count + kTileCost, (unsigned long long)w.unit + (w.end - w.at));
     s.head = w.head;
     s.tile = w.tile;
     s.first = b.first;
     s.count = b.count;
-    s.b0 = w.block;
-    s.b1 = (uint32_t)min((unsigned long long)b.count, (unsigned long long)w.block + (w.end - w.at));
-    s.item = w.at - w.block;
+    s.b0 = max(w.unit, kTileCost) - kTileCost;
+    s.b1 = max(until, kTileCost) - kTileCost;
+    s.item = w.at - w.unit + kTileCost;
     s.rows = min(s.p.rows - w.tile * kRows, (uint32_t)kRows);
-    w.at += s.b1 - s.b0;
-    w.block = 0;
+    w.at += until - w.unit;
+    w.unit = 0;
     if (++w.tile >= s.p.tiles) {
         w.tile = 0;
         if (++w.head >= a.c.heads) {
@@ -184,7 +200,7 @@ template <int kRows> __device__ __forceinline__ bool next_segment(const AttnArgs
             ++w.seq;
         }
     }
-    return true;
+    return s.b0 < s.b1;                             // a share can end in units without a block, but not begin and go on there
 }
 
 constexpr int kPromptThreads = 640;
@@ -220,7 +236,7 @@ template <int kRows> __device__ __forceinline__ bool walk_start(const AttnArgs& 
             const unsigned long long inside = w.at - first, head = inside / n;
             unsigned long long rest = inside - head * n, ahead = 0;
             for (uint32_t t0 = 0; t0 < p.tiles; t0 += 32) {
-                const uint32_t t = t0 + lane, c = t < p.tiles ? tile_blocks<kRows>(a, p, t).count : 0u;
+                const uint32_t t = t0 + lane, c = t < p.tiles ? tile_blocks<kRows>(a, p, t).count + kTileCost : 0u;
                 unsigned long long incl = c;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
@@ -239,7 +255,7 @@ template <int kRows> __device__ __forceinline__ bool walk_start(const AttnArgs& 
         if (w.at < before) break;
     }
     __syncthreads();
-    w.seq = (uint32_t)sh[20]; w.head = (uint32_t)sh[21]; w.tile = (uint32_t)sh[22]; w.block = (uint32_t)sh[23];
+    w.seq = (uint32_t)sh[20]; w.head = (uint32_t)sh[21]; w.tile = (uint32_t)sh[22]; w.unit = (uint32_t)sh[23];
     return true;
 }
 
@@ -251,8 +267,10 @@ struct SegInfo {                                    // a segment as the other wa
     int32_t start;                                  // position of the sequence's first row
     unsigned long long item;
 };
+// Barriers that are waited for once a half have one for each half of a step: a wait tells only two phases apart, and two halves may be
+// on their way at once.
 struct PromptShared {
-    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_full[2], look_full[kRing],
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_full[2][2], look_full[kRing],
         look_free[kRing], join[2], drain;
     unsigned long long walk[24];
     long long at[kRing][8];                         // of 16 keys each: bytes from the pool's start to them (-1: none), key scale, log2
@@ -497,10 +515,11 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uin
                 if (!warp_wait(&sh.p_full[t][side], now & 1, sh)) return;
                 tc_fence_after();
                 const uint32_t v = v0 + ((old_stage * P::kOperand + side * 8192) >> 4);
-                if (on && elected()) {
+                if (elected()) {
+                    if (on)
 #pragma unroll
-                    for (int i = 0; i < kKeys / 32; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, h > 2 || i > 0);
-                    tc_commit(&sh.o_full[t]);
+                        for (int i = 0; i < kKeys / 32; ++i) mma_ts(o_at, s_at + 8 * i, v + i * (2048 >> 4), kO, h > 2 || i > 0);
+                    tc_commit(&sh.o_full[t][side]);
                 }
                 __syncwarp();
             }
@@ -598,7 +617,7 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
         const float base = m == -INFINITY ? 0.0f : m;
         const float fa = q * ks[2 * c], fb = q * ks[2 * c + 1], oa = lvs[2 * c] - base, ob = lvs[2 * c + 1] - base;
         const uint64_t f2[2] = {pair(fa, fa), pair(fb, fb)}, off2[2] = {pair(oa, oa), pair(ob, ob)};
-        tmem_wait_ld();
+        tmem_wait32(x);
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             float u, v;
@@ -634,7 +653,7 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
                 const __half2 f2h = __float2half2_rn(f);
                 tmem_wait_st();
                 tmem_load16(s_at, p);
-                tmem_wait_ld();
+                tmem_wait16(p);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const __half2 w = __hmul2(reinterpret_cast<const __half2&>(p[e]), f2h);
@@ -656,7 +675,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
     const uint32_t t = threadIdx.x >> 7, r = threadIdx.x & 127;  // tile, row
     const uint32_t lanes = (threadIdx.x & 96) << 16;             // this warp's quarter of the tensor memory's lanes
     const uint32_t s_at = sh.tmem + t * 128 + lanes, o_at = sh.tmem + P::kTiles * 128 + t * DP + lanes;
-    uint32_t step = 0, o_turn = 0, joins = 0;
+    uint32_t step = 0, joins = 0;
     for (uint32_t seg = 0;; ++seg) {
         if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
         const SegInfo& s = sh.seg[seg % kSegments];
@@ -686,19 +705,18 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             float moved = 1.0f;
             row_half(s_at + 64 * side, sh.ks[ring] + 4 * side, sh.lvs[ring] + 4 * side, sh.ivs[ring] + 4 * side, q, cut, k0, lo, hi, m, l, moved);
             if (h && __any_sync(0xffffffffu, moved != 1.0f)) {   // o of the halves before
-                if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
+                if (!warp_wait(&sh.o_full[t][side ^ 1], (step - 1) & 1, sh)) return;
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < DP / 32; ++c) {
                     uint32_t y[32];
                     tmem_load32(o_at + 32 * c, y);
-                    tmem_wait_ld();
+                    tmem_wait32(y);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * moved);
                     tmem_store32(o_at + 32 * c, y);
                 }
             }
-            ++o_turn;
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&sh.p_full[t][side]);
@@ -723,14 +741,14 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         float* part = a.partial + ((size_t)blockIdx.x * 2 + (s.b0 == 0 ? 1 : 0)) * P::kPartial;
         const uint32_t pr = t * 128 + r;
         if (on) {
-            if (!warp_wait(&sh.o_full[t], (o_turn - 1) & 1, sh)) return;
+            if (!warp_wait(&sh.o_full[t][1], (step - 1) & 1, sh)) return;
             tc_fence_after();
             const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 uint32_t x[32];
                 tmem_load32(o_at + 32 * c, x);
-                tmem_wait_ld();
+                tmem_wait32(x);
                 if (complete) {
                     float v[32];
 #pragma unroll
@@ -822,8 +840,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_kernel(AttnArgs a) {
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&sh.s_full[i][h], 1);
                 mbar_init(&sh.p_full[i][h], 128);
+                mbar_init(&sh.o_full[i][h], 1);
             }
-            mbar_init(&sh.o_full[i], 1);
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(&sh.look_full[i], 8);

@@ -277,6 +277,25 @@ def test_attention_long_chunks(torch, rm, dim, page, fmt, layout):
         check_attention(torch, rm, cache, [0, 1, 2, 3], news, q_heads, dtype, window=window, view=view)
 
 
+@pytest.mark.parametrize("dim,kv_heads,group", [(64, 4, 8), (128, 2, 4), (256, 2, 2), (96, 1, 5), (176, 2, 1)])
+def test_attention_prompts_repeat_bit_for_bit(torch, rm, dim, kv_heads, group):
+    """Ragged prompt chunks whose rows' maxima move while products are on their way (keys of growing size): the values are right, and
+    the same call gives the same bits every time."""
+    lengths, news = [1527, 900, 271], [413, 547, 188]
+    cache = make_cache(torch, rm, lengths, page=32, dim=dim, heads=kv_heads, seed=dim)
+    table = cache.pages.cpu().numpy()
+    for s, n in enumerate(lengths):                                  # later pages' keys are larger: up to 2^3 of the first ones
+        for e in range(-(-n // 32)):
+            cache.k_scale[:, table[s, e]] *= 2.0 ** (3 * e * 32 // n)
+    ws = cache.workspace()
+    first = check_attention(torch, rm, cache, [0, 1, 2], news, kv_heads * group, "bf16", workspace=ws, magnitude=0.5)
+    rows = torch.tensor(np.concatenate([[0], np.cumsum(news)]).tolist(), dtype=torch.int32, device="cuda")
+    q = torch.from_numpy(np.random.default_rng(1).normal(size=(sum(news), kv_heads * group, dim)) * 0.5).to(torch.bfloat16).cuda()
+    for _ in range(40):
+        out, lse = rm.kv_attention(cache, [0, 1, 2], q, rows, workspace=ws)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
 def test_attention_split_key_axis_and_order(torch, rm):
     """Few rows over long contexts: the key axis is split over blocks and joined; the same call gives the same bits, and a batch's
     result does not depend on what was in the workspace's sums."""
