@@ -26,16 +26,19 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Few rows a key head (a decoding step: `group` rows for each new token).  Bound by the bytes of the codes, so every code goes from
-// global memory straight into registers, once, and no shared memory is touched until the end.  The products are taken transposed
-// (S^T = K q^T, o^T = V^T p^T), so that keys and values are the 16-row operand and the 8 rows of a GQA group fill the 8-wide one.
-// The contraction index of a matrix product may be permuted freely, and so may the rows of its result: a lane takes 4 bytes of its
+// Few rows a key head (a decoding step: `group` rows for each new token).  Bound by the bytes of the codes.  The products are taken
+// transposed (S^T = K q^T, o^T = V^T p^T), so that keys and values are the 16-row operand and the 8 rows of a GQA group fill the 8-wide
+// one.  The contraction index of a matrix product may be permuted freely, and so may the rows of its result: a lane takes 4 bytes of its
 // own contiguous span of a key for each k-step (lane quarter c of a token holds dims [c*DP/4, +DP/4)), and of a value row the dims
-// [r*DP/8, +DP/8) for its result rows r.  Both are whole 16-byte loads, and a warp's loads cover whole rows.
+// [r*DP/8, +DP/8) for its result rows r: both are whole 16-byte reads of the codes as they are stored.
 //
-// A block walks a contiguous part of the flat order; its warps take the 16*kGroups-key steps in turn and meet at each
-// (sequence, head, tile).  A part that does not hold all of a (sequence, head, tile) leaves its sums in the workspace, and the last
-// part to arrive adds them in order.
+// Every warp works for itself: it has kStages steps of keys and values under way to its own part of shared memory by asynchronous
+// copies (registers alone held half of what the way to DRAM takes: 4.4 TB/s).  A block walks a contiguous part of the flat order; its
+// warps take the 16*kGroups-key steps in turn and meet at each (sequence, head, tile).  A part that does not hold all of a (sequence,
+// head, tile) leaves its sums in the workspace, and the last part to arrive adds them in order.
+//
+// Scales: a page's key scale goes into the factor of the exponent's argument, its value scale vs into the exponent: the weights
+// exp2(s + log2 vs - m), m a maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs.
 template <int DP, int NT, int kFormat, class T>
 struct FewRows {
     static constexpr int kGroups = DP > 128 ? 1 : 2;               // 16-key groups a warp step
@@ -46,23 +49,30 @@ struct FewRows {
     static constexpr int KW = DP / 16;                             // words of a lane's key span
     static constexpr int VW = DP / 32;                             // words of a lane's value span
     static constexpr int kPartial = kRows * (DP + 2);              // floats of one partial result
+    static constexpr int kSide = kStep * DP;                       // bytes of a step's keys
+    static constexpr int kStages = 16384 / (2 * kSide);            // 16 KB a warp: 2 steps, 4 for the smallest heads
+    static constexpr int kRing = kStages * 2 * kSide;
+    static constexpr int kMeet = kAttnWarps * kRows * (DP + 2) * (int)sizeof(float);
+    static constexpr int kSmem = kRing * kAttnWarps > kMeet ? kRing * kAttnWarps : kMeet;
 };
 
-// 4*N bytes at p; `dims` limits them to the head's real size (a multiple of 16)
-template <int N>
-__device__ __forceinline__ void load_span(uint32_t* to, const uint8_t* p, uint32_t first_dim, uint32_t dim, bool on) {
+// Where 16-byte chunk `chunk` of row `row` of a step lies: chunks are exchanged so that neither the keys' reads (8 lanes: two rows, four
+// chunks) nor the values' (four rows, two chunks) meet in a bank.
+template <int DP> __device__ __forceinline__ uint32_t code_at(uint32_t row, uint32_t chunk) {
+    if constexpr (DP >= 128) return row * DP + ((chunk ^ (row & 7)) << 4);
+    const uint32_t line = row >> 1;                                // two rows of 64 bytes
+    return line * 128 + ((((row & 1) * 4 + chunk) ^ ((line & 3) << 1)) << 4);
+}
+// N words from a span that starts at byte `first` of a row
+template <int DP, int N> __device__ __forceinline__ void read_span(uint32_t* to, const uint8_t* side, uint32_t row, uint32_t first) {
     if constexpr (N >= 4) {
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (on && first_dim + 4 * i < dim)
-                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p + 4 * i));
+            const uint4 x = *reinterpret_cast<const uint4*>(side + code_at<DP>(row, first / 16 + i / 4));
             to[i] = x.x; to[i + 1] = x.y; to[i + 2] = x.z; to[i + 3] = x.w;
         }
     } else {
-        uint2 x = make_uint2(0, 0);
-        if (on && first_dim < dim)
-            asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
+        const uint2 x = *reinterpret_cast<const uint2*>(side + code_at<DP>(row, first / 16) + (first & 8));
         to[0] = x.x; to[1] = x.y;
     }
 }
@@ -72,8 +82,8 @@ template <class T> __device__ __forceinline__ float load_elem(const T* p) { retu
 template <int DP, int NT, int kFormat, class T>
 __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_rows_kernel(AttnArgs a) {
     using F = FewRows<DP, NT, kFormat, T>;
-    constexpr int G = F::kGroups, KW = F::KW, VW = F::VW, KS = F::KS;
-    extern __shared__ float sm[];                                  // [warps][rows][DP] sums, then [warps][rows][2] max and total
+    constexpr int G = F::kGroups, KW = F::KW, VW = F::VW, KS = F::KS, kStages = F::kStages;
+    extern __shared__ __align__(1024) float sm[];                  // the warps' steps; then [warps][rows][DP] sums, [warps][rows][2] max and total
     __shared__ unsigned long long sh_sum[kAttnWarps + 1];
     __shared__ uint32_t sh_at[4];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
@@ -225,7 +235,6 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
 
         float o[NT][KS][4];
         float m[NT][2], l[NT][2];
-        float vref = 0.0f;                                         // o is in units of this value scale
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -244,9 +253,14 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
         const uint32_t row_step = kv.token_step;
         const long long head_off = (long long)head * kv.head_step;
 
-        uint32_t kr[G][2][KW], vr[G][4][VW];
-        int32_t page[G], next_page[G];
-        auto get_pages = [&](int k0, int32_t* to) {
+        uint8_t* ring = reinterpret_cast<uint8_t*>(sm) + wid * F::kRing;
+        constexpr int kChunks = DP / 16, kLoads = F::kStep * kChunks / 32;     // 16-byte copies a lane and side
+        const uint32_t chunk = lane % kChunks, row0 = lane / kChunks;          // copy i: row row0 + i * (32 / kChunks)
+        constexpr int kRowsPer = 32 / kChunks;
+        const bool real = 16 * chunk < kv.dim;
+        const long long to_v = kv.v - kv.k;
+        int32_t page[G];                                           // of the step that is copied next
+        auto get_pages = [&](int k0) {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int k = k0 + 16 * g;
@@ -258,143 +272,171 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                         id = -1;
                     }
                 }
-                to[g] = id;
+                page[g] = id;
             }
         };
-        auto get_keys = [&](int k0, const int32_t* pg) {
+        // the scales of a step are fetched with its copies and wait in registers: (key scale, value scale) of stage x, group g
+        float ks_of[kStages][G], vs_of[kStages][G];
+        auto copy_step = [&](int k0, int stage) {
+            const uint32_t to = smem_addr(ring + stage * 2 * F::kSide);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int k = k0 + 16 * g;
-                const uint8_t* p = kv.k + (long long)pg[g] * kv.page_stride + head_off + (k & (kv.page_tokens - 1)) * row_step + c * (DP / 4);
+                const uint8_t* p = kv.k + (long long)max(page[g], 0) * kv.page_stride + head_off + ((k & (kv.page_tokens - 1)) + row0) * row_step + 16 * chunk;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    load_span<KW>(kr[g][h], p + (r + 8 * h) * row_step, c * (DP / 4), kv.dim, pg[g] >= 0 && k + r + 8 * h < hi_key);
+                for (int i = 0; i < kLoads / G; ++i) {
+                    const uint32_t row = 16 * g + row0 + i * kRowsPer;
+                    const int key = k0 + (int)row;
+                    const uint32_t n = page[g] >= 0 && real && key < hi_key && key >= tile_lo ? 16u : 0u;   // the rest becomes zeros
+                    const uint32_t at = to + code_at<DP>(row, chunk);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(p), "r"(n) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + F::kSide), "l"(p + to_v), "r"(n) : "memory");
+                    p += kRowsPer * row_step;
+                }
             }
         };
-        int k0 = lo_key + ((wid - lo_key / F::kStep) & (kAttnWarps - 1)) * F::kStep;   // warp w takes steps w mod 4
-        get_pages(k0, page);
-        get_keys(k0, page);
-        for (; k0 < hi_key; k0 += F::kBlock) {
-            float ks[G], vs[G];
+        auto get_scales = [&](int stage) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) {                          // values of this step, on their way while S is worked out
-                const int k = k0 + 16 * g;
-                const uint8_t* p = kv.v + (long long)page[g] * kv.page_stride + head_off + (k & (kv.page_tokens - 1)) * row_step + r * (DP / 8);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int tok = 2 * c + (h & 1) + 8 * (h >> 1);
-                    load_span<VW>(vr[g][h], p + tok * row_step, r * (DP / 8), kv.dim, page[g] >= 0 && k + tok < hi_key && k + tok >= tile_lo);
-                }
-                ks[g] = vs[g] = 0.0f;
-                if (page[g] >= 0) {
-                    ks[g] = __ldg(kv.k_scale + (size_t)page[g] * kv.heads + head);
-                    vs[g] = __ldg(kv.v_scale + (size_t)page[g] * kv.heads + head);
-                }
-            }
-            get_pages(k0 + F::kBlock, next_page);
-            float sc[G][NT][4];
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[g][t][e] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    uint32_t a0, a1, a2, a3;
-                    codes_to_f16<kFormat>(kr[g][0][i], a0, a2);
-                    codes_to_f16<kFormat>(kr[g][1][i], a1, a3);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) mma16816(sc[g][t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
-                }
-            }
-            get_keys(k0 + F::kBlock, next_page);
-
-            // softmax over the step: sc[e] is key r + 8*(e >> 1) of the group, row 2c + (e & 1)
-            bool whole = k0 >= all_lo && k0 + F::kStep <= all_hi;
-#pragma unroll
-            for (int g = 0; g < G; ++g) whole = whole && page[g] >= 0;
-            float vmax = vref;
-#pragma unroll
-            for (int g = 0; g < G; ++g) vmax = fmaxf(vmax, vs[g]);
-            const float inv_vref = vmax > 0.0f ? __fdividef(1.0f, vmax) : 0.0f;
-            bool moved = vmax != vref;
-            float old_m[NT][2];
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    float mx = -INFINITY;
+            for (int s2 = 0; s2 < kStages; ++s2)
+                if (s2 == stage)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float f = qscale[t][n] * ks[g];
+                        ks_of[s2][g] = 0.0f;
+                        vs_of[s2][g] = -1.0f;                      // no page
+                        if (page[g] >= 0) {
+                            ks_of[s2][g] = __ldg(kv.k_scale + (size_t)page[g] * kv.heads + head);
+                            vs_of[s2][g] = __ldg(kv.v_scale + (size_t)page[g] * kv.heads + head);
+                        }
+                    }
+        };
+        int k0 = lo_key + ((wid - lo_key / F::kStep) & (kAttnWarps - 1)) * F::kStep;   // warp w takes steps w mod 4
+        get_pages(k0);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float& x = sc[g][t][2 * h + n];
-                            x *= f;
-                            if (!whole) {
-                                const int k = k0 + 16 * g + 8 * h + r;
-                                if (k >= see_hi[t][n] || k < see_lo[t][n] || page[g] < 0) x = -INFINITY;
+        for (int i = 0; i < kStages; ++i) {
+            copy_step(k0 + i * F::kBlock, i);
+            get_scales(i);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            get_pages(k0 + (i + 1) * F::kBlock);
+        }
+        while (k0 < hi_key) {
+#pragma unroll
+            for (int stage = 0; stage < kStages; ++stage) {
+                if (k0 >= hi_key) break;
+                asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+                __syncwarp();
+                const uint8_t* side = ring + stage * 2 * F::kSide;
+                float sc[G][NT][4], ivs[G];
+                bool whole = k0 >= all_lo && k0 + F::kStep <= all_hi, high = false;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[g][t][e] = 0.0f;
+                    uint32_t kr[2][KW];
+                    read_span<DP, KW>(kr[0], side, 16 * g + r, c * (DP / 4));
+                    read_span<DP, KW>(kr[1], side, 16 * g + r + 8, c * (DP / 4));
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        codes_to_f16<kFormat>(kr[0][i], a0, a2);
+                        codes_to_f16<kFormat>(kr[1][i], a1, a3);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma16816(sc[g][t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
+                    }
+                }
+                // exponents: sc[e] is key r + 8*(e >> 1) of the group, row 2c + (e & 1)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const float ks = ks_of[stage][g];
+                    float vs = vs_of[stage][g], lvs = -INFINITY;   // a page that is not there weighs nothing
+                    ivs[g] = 0.0f;
+                    if (vs >= 0.0f) {
+                        vs = fmaxf(vs, 7.888609052210118e-31f);    // 2^-100
+                        lvs = log2_fast(vs);
+                        ivs[g] = __fdividef(1.0f, vs);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const float f = qscale[t][n] * ks;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float& x = sc[g][t][2 * h + n];
+                                x = fmaf(x, f, lvs);
+                                if (!whole) {
+                                    const int k = k0 + 16 * g + 8 * h + r;
+                                    if (k >= see_hi[t][n] || k < see_lo[t][n]) x = -INFINITY;
+                                }
+                                high = high || x > m[t][n] + 8.0f;
                             }
-                            mx = fmaxf(mx, x);
                         }
-                    }
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    old_m[t][n] = m[t][n];
-                    if (mx > m[t][n]) { m[t][n] = mx; moved = true; }
                 }
-            if (__any_sync(0xffffffffu, moved)) {
-                const float v = vref * inv_vref;
+                // The maximum is looked for only when some exponent is past 2^8 above the old one: weights stay far from float16's end.
+                if (__any_sync(0xffffffffu, high)) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const float f = old_m[t][n] == -INFINITY ? 0.0f : exp2_fast(old_m[t][n] - m[t][n]);
-                        l[t][n] *= f;
+                        for (int n = 0; n < 2; ++n) {
+                            float mx = m[t][n];
 #pragma unroll
-                        for (int i = 0; i < KS; ++i) {
-                            o[t][i][n] *= f * v;
-                            o[t][i][n + 2] *= f * v;
+                            for (int g = 0; g < G; ++g) mx = fmaxf(mx, fmaxf(sc[g][t][n], sc[g][t][n + 2]));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                            const float f = m[t][n] == -INFINITY ? 0.0f : exp2_fast(m[t][n] - mx);
+                            m[t][n] = mx;
+                            l[t][n] *= f;
+#pragma unroll
+                            for (int i = 0; i < KS; ++i) {
+                                o[t][i][n] *= f;
+                                o[t][i][n + 2] *= f;
+                            }
                         }
-                    }
-                vref = vmax;
-            }
-            // probabilities; p * vs / vref <= 1 is rounded to float16 (11 bits) for the product with the codes, the total is not
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const float f = vs[g] * inv_vref;
-                uint32_t pb[NT][2];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const float m0 = m[t][0] == -INFINITY ? 0.0f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.0f : m[t][1];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float p0 = exp2_fast(sc[g][t][2 * h] - m0), p1 = exp2_fast(sc[g][t][2 * h + 1] - m1);
-                        l[t][0] += p0;
-                        l[t][1] += p1;
-                        const __half2 x = __floats2half2_rn(p0 * f, p1 * f);
-                        pb[t][h] = transpose8x8(reinterpret_cast<const uint32_t&>(x));
-                    }
                 }
+                // weights: rounded to float16 (11 bits) for the product with the codes, not for the total
 #pragma unroll
-                for (int j = 0; j < VW; ++j) {
-                    uint32_t a0[4], a1[4];                         // [result-row pair of the word's four dims]
-                    codes_to_f16<kFormat>(__byte_perm(vr[g][0][j], vr[g][1][j], 0x5140), a0[0], a0[1]);
-                    codes_to_f16<kFormat>(__byte_perm(vr[g][0][j], vr[g][1][j], 0x7362), a0[2], a0[3]);
-                    codes_to_f16<kFormat>(__byte_perm(vr[g][2][j], vr[g][3][j], 0x5140), a1[0], a1[1]);
-                    codes_to_f16<kFormat>(__byte_perm(vr[g][2][j], vr[g][3][j], 0x7362), a1[2], a1[3]);
+                for (int g = 0; g < G; ++g) {
+                    uint32_t pb[NT][2];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        mma16816(o[t][2 * j], a0[0], a0[1], a1[0], a1[1], pb[t][0], pb[t][1]);
-                        mma16816(o[t][2 * j + 1], a0[2], a0[3], a1[2], a1[3], pb[t][0], pb[t][1]);
+                        const float m0 = m[t][0] == -INFINITY ? 0.0f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.0f : m[t][1];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float p0 = exp2_fast(sc[g][t][2 * h] - m0), p1 = exp2_fast(sc[g][t][2 * h + 1] - m1);
+                            l[t][0] = fmaf(p0, ivs[g], l[t][0]);
+                            l[t][1] = fmaf(p1, ivs[g], l[t][1]);
+                            const __half2 x = __floats2half2_rn(p0, p1);
+                            pb[t][h] = transpose8x8(reinterpret_cast<const uint32_t&>(x));
+                        }
+                    }
+                    uint32_t vr[4][VW];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) read_span<DP, VW>(vr[h], side + F::kSide, 16 * g + 2 * c + (h & 1) + 8 * (h >> 1), r * (DP / 8));
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) {
+                        uint32_t a0[4], a1[4];                     // [result-row pair of the word's four dims]
+                        codes_to_f16<kFormat>(__byte_perm(vr[0][j], vr[1][j], 0x5140), a0[0], a0[1]);
+                        codes_to_f16<kFormat>(__byte_perm(vr[0][j], vr[1][j], 0x7362), a0[2], a0[3]);
+                        codes_to_f16<kFormat>(__byte_perm(vr[2][j], vr[3][j], 0x5140), a1[0], a1[1]);
+                        codes_to_f16<kFormat>(__byte_perm(vr[2][j], vr[3][j], 0x7362), a1[2], a1[3]);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma16816(o[t][2 * j], a0[0], a0[1], a1[0], a1[1], pb[t][0], pb[t][1]);
+                            mma16816(o[t][2 * j + 1], a0[2], a0[3], a1[2], a1[3], pb[t][0], pb[t][1]);
+                        }
                     }
                 }
+                __syncwarp();                                      // the stage has been read
+                copy_step(k0 + kStages * F::kBlock, stage);
+                get_scales(stage);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                k0 += F::kBlock;
+                get_pages(k0 + kStages * F::kBlock);
             }
-#pragma unroll
-            for (int g = 0; g < G; ++g) page[g] = next_page[g];
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
 
         // ---- the warps meet --------------------------------------------------------------------------------------------
         float* sm_ml = sm + kAttnWarps * F::kRows * DP;
@@ -413,8 +455,8 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                 float* to = sm + (size_t)(wid * F::kRows + row) * DP + r * (DP / 8);
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
-                    to[2 * i] = o[t][i][n] * vref;
-                    to[2 * i + 1] = o[t][i][n + 2] * vref;
+                    to[2 * i] = o[t][i][n];
+                    to[2 * i + 1] = o[t][i][n + 2];
                 }
             }
         __syncthreads();
@@ -499,9 +541,8 @@ template <int DP, int NT, int kFormat, class T>
 static int launch_few(const AttnArgs& a, cudaStream_t st) {
     using F = FewRows<DP, NT, kFormat, T>;
     const uint32_t per_sm = DP > 128 || NT > 1 ? 2 : 3;
-    const size_t smem = (size_t)kAttnWarps * F::kRows * (DP + 2) * sizeof(float);
-    return launch("kv_attention", few_rows_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * per_sm), dim3(kAttnThreads), smem, st,
-                  false, a);
+    return launch("kv_attention", few_rows_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * per_sm), dim3(kAttnThreads),
+                  F::kSmem, st, false, a);
 }
 template <int DP, int kFormat, class T>
 static int launch_rows(const AttnArgs& a, bool eight, cudaStream_t st) {
