@@ -6,6 +6,7 @@
 namespace roomie {
 
 constexpr int kAttnWarps = 4, kAttnThreads = 32 * kAttnWarps;
+constexpr int kJoin = 20;                                        // parts that one block adds up
 
 // The flat order of the call's work: sequence, key head, row tile, key block.  What one sequence contributes:
 struct SeqWork {
@@ -48,7 +49,7 @@ struct FewRows {
     static constexpr int KS = DP / 16;
     static constexpr int KW = DP / 16;                             // words of a lane's key span
     static constexpr int VW = DP / 32;                             // words of a lane's value span
-    static constexpr int kPartial = kRows * (DP + 2);              // floats of one partial result
+    static constexpr int kPartial = kRows * (DP + 2);              // floats of one partial result, a multiple of 4
     static constexpr int kSide = kStep * DP;                       // bytes of a step's keys
     static constexpr int kStages = 16384 / (2 * kSide);            // 16 KB a warp: 2 steps, 4 for the smallest heads
     static constexpr int kRing = kStages * 2 * kSide;
@@ -86,30 +87,44 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
     extern __shared__ __align__(1024) float sm[];                  // the warps' steps; then [warps][rows][DP] sums, [warps][rows][2] max and total
     __shared__ unsigned long long sh_sum[kAttnWarps + 1];
     __shared__ uint32_t sh_at[4];
+    __shared__ float sm_row[2 * F::kRows];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const KvView& kv = a.c;
 
-    // ---- where this block's part begins -------------------------------------------------------------------------------
-    unsigned long long mine = 0;
+    // ---- where this block's part begins: a scan of the sequences' units, kept from the first pass when they are at most a block's threads
+    unsigned long long mine = 0, own = 0;
     for (uint32_t i = threadIdx.x; i < a.num_seqs; i += kAttnThreads) {
         const SeqWork w = seq_work<F::kBlock, F::kRows>(a, i, blockIdx.x == 0);
-        mine += (unsigned long long)w.tiles * w.blocks * kv.heads;
+        own = (unsigned long long)w.tiles * w.blocks * kv.heads;
+        mine += own;
     }
+    unsigned long long upto = mine;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-    if (lane == 0) sh_sum[wid] = mine;
+    for (int d = 1; d < 32; d <<= 1) {
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += up;
+    }
+    if (lane == 31) sh_sum[wid] = upto;
     __syncthreads();
-    unsigned long long total = 0;
-    for (int w = 0; w < kAttnWarps; ++w) total += sh_sum[w];
+    unsigned long long total = 0, ahead0 = 0;
+    for (int w = 0; w < kAttnWarps; ++w) {
+        if (w < wid) ahead0 += sh_sum[w];
+        total += sh_sum[w];
+    }
     if (total == 0) return;
     const unsigned long long parts = total < gridDim.x ? total : gridDim.x;
     if (blockIdx.x >= parts) return;
     unsigned long long at = total * blockIdx.x / parts;
     const unsigned long long end = total * (blockIdx.x + 1) / parts;
 
-    uint32_t seq = 0;                                              // the sequence that holds `at`, and the flat index it begins at
-    unsigned long long seq_first = 0;
-    {
+    // the sequence that holds `at`, and the flat index it begins at
+    if (a.num_seqs <= kAttnThreads) {
+        const unsigned long long first = ahead0 + upto - own;
+        if (own && at >= first && at < first + own) {
+            sh_at[0] = threadIdx.x;
+            sh_sum[kAttnWarps] = first;
+        }
+    } else {
         unsigned long long before = 0;
         for (uint32_t base = 0; base < a.num_seqs; base += kAttnThreads) {
             const uint32_t i = base + threadIdx.x;
@@ -140,10 +155,10 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             before += all;
             if (at < before) break;
         }
-        __syncthreads();
-        seq = sh_at[0];
-        seq_first = sh_sum[kAttnWarps];
     }
+    __syncthreads();
+    uint32_t seq = sh_at[0];
+    unsigned long long seq_first = sh_sum[kAttnWarps];
 
     while (at < end) {
         SeqWork w = seq_work<F::kBlock, F::kRows>(a, seq, false);
@@ -496,33 +511,74 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             }
         }
         if (!complete) {
-            // the parts that share this item are consecutive blocks: first holds its first unit, last its last
+            // The parts that share this item are consecutive blocks: first holds its first unit, last its last.  With many of them the last
+            // to arrive of each kJoin adds those up, and the last of these the sums: one block alone took 60 us over 444 parts.
             const uint32_t first = (uint32_t)(((item + 1) * parts - 1) / total), last = (uint32_t)((item_end * parts - 1) / total);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const uint32_t before = atomicAdd(a.counters + first, 1u);
-                sh_at[1] = before == last - first;
-                if (before == last - first) a.counters[first] = 0;
-            }
-            __syncthreads();
-            if (sh_at[1]) {
+            const uint32_t count = last - first + 1, groups = (count + kJoin - 1) / kJoin;
+            auto part_of = [&](uint32_t b) { return a.partial + ((size_t)(first + b) * 2 + (b == 0 ? 1 : 0)) * F::kPartial; };
+            auto arrive = [&](uint32_t* counter, uint32_t n) {     // whether this block is the last of n
                 __threadfence();
-                for (uint32_t x = threadIdx.x; x < n_rows * DP; x += kAttnThreads) {
-                    const uint32_t row = x / DP, d = x - row * DP;
-                    float mx = -INFINITY, sum = 0.0f, value = 0.0f;
-                    for (uint32_t b = first; b <= last; ++b) {
-                        const float* p = a.partial + ((size_t)b * 2 + (b == first ? 1 : 0)) * F::kPartial;
-                        const float mb = __ldcg(p + F::kRows * DP + 2 * row), lb = __ldcg(p + F::kRows * DP + 2 * row + 1), vb = __ldcg(p + row * DP + d);
-                        const float to = fmaxf(mx, mb);
-                        const float f0 = mx == -INFINITY ? 0.0f : exp2f(mx - to), f1 = mb == -INFINITY ? 0.0f : exp2f(mb - to);
-                        sum = sum * f0 + lb * f1;
-                        value = value * f0 + vb * f1;
-                        mx = to;
-                    }
-                    put(row, d, mx, sum, value);
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    const uint32_t before = atomicAdd(counter, 1u);
+                    sh_at[1] = before == n - 1;
+                    if (before == n - 1) *counter = 0;
                 }
+                __syncthreads();
+                __threadfence();
+                return sh_at[1] != 0;
+            };
+            // parts b0, b0 + step, ...: n of them, to the results (or into the first)
+            auto join = [&](uint32_t b0, uint32_t step, uint32_t n, bool end) {
+                float* factor = sm;                                // [n][rows]
+                for (uint32_t row = wid; row < n_rows; row += kAttnWarps) {
+                    float mx = -INFINITY, sum = 0.0f;
+                    for (uint32_t b = lane; b < n; b += 32) mx = fmaxf(mx, __ldcg(part_of(b0 + b * step) + F::kRows * DP + 2 * row));
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                    for (uint32_t b = lane; b < n; b += 32) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of(b0 + b * step) + F::kRows * DP + 2 * row));
+                        const float f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - mx);
+                        factor[b * F::kRows + row] = f;
+                        sum += f * ml.y;
+                    }
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    if (lane == 0) {
+                        sm_row[2 * row] = mx;
+                        sm_row[2 * row + 1] = sum;
+                    }
+                }
+                __syncthreads();
+                float* to = part_of(b0);
+                for (uint32_t x = threadIdx.x; x < n_rows * (DP / 4); x += kAttnThreads) {
+                    const uint32_t row = x / (DP / 4), d = 4 * (x - row * (DP / 4));
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+                    for (uint32_t b = 0; b < n; ++b) {             // many loads under way
+                        const float4 y = __ldcg(reinterpret_cast<const float4*>(part_of(b0 + b * step) + row * DP + d));
+                        const float f = factor[b * F::kRows + row];
+                        v.x += f * y.x; v.y += f * y.y; v.z += f * y.z; v.w += f * y.w;
+                    }
+                    const float mx = sm_row[2 * row], sum = sm_row[2 * row + 1];
+                    if (end) {
+                        put(row, d, mx, sum, v.x);
+                        put(row, d + 1, mx, sum, v.y);
+                        put(row, d + 2, mx, sum, v.z);
+                        put(row, d + 3, mx, sum, v.w);
+                    } else {
+                        *reinterpret_cast<float4*>(to + row * DP + d) = v;
+                        if (d == 0) *reinterpret_cast<float2*>(to + F::kRows * DP + 2 * row) = make_float2(mx, sum);
+                    }
+                }
+            };
+            const uint32_t group = (blockIdx.x - first) / kJoin, in_group = min((uint32_t)kJoin, count - group * kJoin);
+            bool go = true;
+            if (groups > 1 && in_group > 1) {                      // (a group of one needs no counter, and the next item may have it)
+                go = arrive(a.counters + gridDim.x + first + group * kJoin, in_group);
+                if (go) join(group * kJoin, 1, in_group, false);
             }
+            if (go && arrive(a.counters + first, groups > 1 ? groups : count)) join(0, groups > 1 ? kJoin : 1, groups > 1 ? groups : count, true);
         }
         __syncthreads();
         at += b1 - b0;
@@ -533,7 +589,7 @@ size_t kv_attention_bytes(const roomie_kv_cache* c) {
     const uint32_t dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
     const size_t few = blocks * 2 * (16 * (size_t)(dp + 2)) * sizeof(float), many = prompt_partial_bytes(c->head_dim);
-    const size_t bytes = blocks * sizeof(uint32_t) + 256 + (few > many ? few : many);
+    const size_t bytes = 2 * blocks * sizeof(uint32_t) + 256 + (few > many ? few : many);
     return (bytes + 255) / 256 * 256;
 }
 
@@ -589,7 +645,7 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
     a.o_aligned = rows_aligned16(*out, rows, q_heads);
     a.counters = static_cast<uint32_t*>(workspace);
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
-    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (blocks * sizeof(uint32_t) + 255) / 256 * 256);
+    a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (2 * blocks * sizeof(uint32_t) + 255) / 256 * 256);
     const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;      // rows a sequence and key head, on average
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if ((unsigned long long)rows * a.group > 32ull * num_seqs) return launch_prompt(a, q->type == ROOMIE_F16, st);

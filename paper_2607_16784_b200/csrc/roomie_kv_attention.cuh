@@ -16,7 +16,7 @@ struct AttnArgs {
     float scale_log2;                            // scale * log2(e)
     uint32_t window;
     int32_t q_aligned, o_aligned;                // 16-byte rows
-    uint32_t* counters;                          // [blocks] zero between calls
+    uint32_t* counters;                          // [2][blocks] zero between calls
     float* partial;                              // [blocks][2] of (rows x (DP + 2))
 };
 
