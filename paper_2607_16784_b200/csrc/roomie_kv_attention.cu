@@ -6,7 +6,7 @@
 namespace roomie {
 
 constexpr int kAttnWarps = 4, kAttnThreads = 32 * kAttnWarps;
-constexpr int kJoin = 20;                                        // parts that one block adds up
+constexpr int kJoin = 32;                                        // parts that one block adds up: a lane each (and at most 32 such groups)
 
 // The flat order of the call's work: sequence, key head, row tile, key block.  What one sequence contributes:
 struct SeqWork {
@@ -532,16 +532,14 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             auto join = [&](uint32_t b0, uint32_t step, uint32_t n, bool end) {
                 float* factor = sm;                                // [n][rows]
                 for (uint32_t row = wid; row < n_rows; row += kAttnWarps) {
-                    float mx = -INFINITY, sum = 0.0f;
-                    for (uint32_t b = lane; b < n; b += 32) mx = fmaxf(mx, __ldcg(part_of(b0 + b * step) + F::kRows * DP + 2 * row));
+                    float2 ml = make_float2(-INFINITY, 0.0f);      // a lane for each part: n <= 32
+                    if (lane < (int)n) ml = __ldcg(reinterpret_cast<const float2*>(part_of(b0 + lane * step) + F::kRows * DP + 2 * row));
+                    float mx = ml.x;
 #pragma unroll
                     for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                    for (uint32_t b = lane; b < n; b += 32) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of(b0 + b * step) + F::kRows * DP + 2 * row));
-                        const float f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - mx);
-                        factor[b * F::kRows + row] = f;
-                        sum += f * ml.y;
-                    }
+                    const float f = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - mx);
+                    if (lane < (int)n) factor[lane * F::kRows + row] = f;
+                    float sum = f * ml.y;
 #pragma unroll
                     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
                     if (lane == 0) {

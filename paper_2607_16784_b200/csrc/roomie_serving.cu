@@ -48,6 +48,21 @@ static void record_drop(uint32_t made) {
     t_rec_cap = t_rec_n = 0;
 }
 
+// ---- large shared memory ---------------------------------------------------------------------------------------------
+// The attribute belongs to a function and a device and only ever grows here; a thread remembers what it has set, because setting it
+// costs as much as half a launch.
+int allow_smem(const void* fn, size_t bytes) {
+    struct Set { const void* fn; int dev; size_t bytes; };
+    static thread_local Set sets[64];
+    int dev = 0;
+    ROOMIE_CUDA_OK(cudaGetDevice(&dev));
+    Set& s = sets[(reinterpret_cast<uintptr_t>(fn) >> 4) % 64];
+    if (s.fn == fn && s.dev == dev && s.bytes >= bytes) return ROOMIE_OK;
+    ROOMIE_CUDA_OK(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    s = {fn, dev, bytes};
+    return ROOMIE_OK;
+}
+
 // ---- rotary positions ------------------------------------------------------------------------------------------------
 struct RopeArgs {
     HeadRows io;

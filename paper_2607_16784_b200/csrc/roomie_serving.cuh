@@ -13,14 +13,18 @@ void record_begin(const char* name, const void* fn, unsigned long long blocks, u
                   cudaStream_t st);
 void record_end(cudaStream_t st);
 
+int allow_smem(const void* fn, size_t bytes);   // more than 48 KB of dynamic shared memory for a kernel
+
 // With `overlap` the kernel may start while the launch before it on the stream drains; it then waits for that launch's
 // results itself (grid_dependency_wait) before it reads or writes anything another kernel touches.
 template <class... KArgs, class... Args>
 int launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool overlap,
            Args... args) {
     const void* fn = reinterpret_cast<const void*>(kernel);
-    if (smem > 48 * 1024)
-        ROOMIE_CUDA_OK(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (smem > 48 * 1024) {
+        const int rc = allow_smem(fn, smem);
+        if (rc != ROOMIE_OK) return rc;
+    }
     const bool rec = record_on();
     if (rec) record_begin(name, fn, (unsigned long long)grid.x * grid.y * grid.z, block.x * block.y * block.z, smem, st);
     cudaLaunchConfig_t cfg = {};

@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import struct
 from contextlib import contextmanager
 
 import numpy as np
@@ -18,8 +19,10 @@ _FORMATS = {"e4m3": 0, "int8": 1}
 _LAYOUTS = {"hnd": 0, "nhd": 1}
 
 
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+# roomie_rows as bytes (data, type, token_stride, head_stride): a step's calls last a few microseconds on the GPU, and building a
+# ctypes structure for each tensor cost as much again on the host
+_pack_rows = struct.Struct("=Qi4xqq").pack
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 class _RopeTable(C.Structure):
@@ -42,9 +45,11 @@ class _Launch(C.Structure):
 
 def _rows(t, what):
     """[tokens, heads, head_dim] with a unit last stride, as the library sees it."""
-    if t.dim() != 3 or t.dtype not in _TYPES or not t.is_cuda or (t.stride(2) != 1 and t.shape[2] > 1):
+    kind = _TYPES.get(t.dtype)
+    stride = t.stride()
+    if kind is None or len(stride) != 3 or not t.is_cuda or (stride[2] != 1 and t.shape[2] > 1):
         raise ValueError(f"{what}: a [tokens, heads, head_dim] CUDA tensor of float32, float16 or bfloat16 whose last dimension is contiguous")
-    return _Rows(t.data_ptr(), _TYPES[t.dtype], t.stride(0), t.stride(1))
+    return _pack_rows(t.data_ptr(), kind, stride[0], stride[1])
 
 
 def _ids(t, what, n=None):
@@ -53,8 +58,8 @@ def _ids(t, what, n=None):
         t = torch.as_tensor(np.asarray(t, dtype=np.int32), device="cuda")
     if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{what}: a contiguous one-dimensional int32 CUDA tensor")
-    if n is not None and t.numel() != n:
-        raise ValueError(f"{what}: {n} entries expected, got {t.numel()}")
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"{what}: {n} entries expected, got {t.shape[0]}")
     return t
 
 
@@ -69,8 +74,8 @@ def _on_stream(call):
     return wrapped
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+def _stream(t):
+    return _raw_stream(t.get_device())
 
 
 def rope_frequencies(rotary_dim, base=10000.0, factor=1.0, context=0, low_turns=1.0, high_turns=4.0):
@@ -110,14 +115,13 @@ def rope(x, positions, table: RopeTable, *, inverse=False, out=None):
     """roomie_rope: x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); `inverse` is the gradient.
     `out` may be x itself.  Returns out."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out: the shape and type of x")
-    cx, cy = _rows(x, "x"), _rows(out, "out")
+    cx = _rows(x, "x")
     n, h, d = x.shape
     positions = _ids(positions, "positions", n)
-    _check(_dll.roomie_rope(table.ref, C.byref(cx), C.byref(cy), n, h, d, positions.data_ptr(), int(inverse), _stream()),
-           "roomie_rope")
+    _check(_dll.roomie_rope(table.ref, cx, _rows(out, "out"), n, h, d, positions.data_ptr(), inverse, _stream(x)), "roomie_rope")
     return out
 
 
@@ -195,10 +199,10 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
     q_offset[i]..q_offset[i+1] of sequence i; None: one row each), rotated when `rope` is given.  With `q` its rotated rows are
     returned (q itself without `rope`)."""
     rows, d = k.shape[0], cache.head_dim
-    if tuple(k.shape) != (rows, cache.kv_heads, d) or k.shape != v.shape or k.dtype != v.dtype:
+    if k.shape[1:] != (cache.kv_heads, d) or k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k, v: [rows, kv_heads, head_dim] of one type")
     seqs = _ids(seqs, "seqs")
-    n = seqs.numel()
+    n = seqs.shape[0]
     if q_offset is not None:
         q_offset = _ids(q_offset, "q_offset", n + 1)
     elif rows != n:
@@ -209,13 +213,13 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
         if q.dim() != 3 or q.shape[0] != rows or q.shape[2] != d or q.dtype != k.dtype:
             raise ValueError("q: [rows, q_heads, head_dim] of k's type")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty_like(q)
         elif q_out.shape != q.shape or q_out.dtype != q.dtype:
             raise ValueError("q_out: the shape and type of q")
         cq, co = _rows(q, "q"), _rows(q_out, "q_out")
-    _check(_dll.roomie_kv_append(cache.ref, layer, seqs.data_ptr(), n, _ptr(q_offset), rows, C.byref(ck), C.byref(cv),
-                                 rope.ref if rope is not None else None, q.shape[1] if turn else 0, C.byref(cq) if turn else None,
-                                 C.byref(co) if turn else None, _stream()), "roomie_kv_append")
+    _check(_dll.roomie_kv_append(cache.ref, layer, seqs.data_ptr(), n, None if q_offset is None else q_offset.data_ptr(), rows, ck, cv,
+                                 rope.ref if rope is not None else None, q.shape[1] if turn else 0, cq if turn else None,
+                                 co if turn else None, _stream(k)), "roomie_kv_append")
     return q_out if turn else q
 
 
@@ -226,24 +230,23 @@ def kv_attention(cache: KVCache, seqs, q, q_offset=None, *, layer=0, scale=None,
     if d != cache.head_dim or heads % cache.kv_heads:
         raise ValueError("q: [rows, q_heads, head_dim] with q_heads a multiple of the cache's kv_heads")
     seqs = _ids(seqs, "seqs")
-    n = seqs.numel()
+    n = seqs.shape[0]
     if q_offset is not None:
         q_offset = _ids(q_offset, "q_offset", n + 1)
     elif rows != n:
         raise ValueError("without q_offset every sequence brings one row")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out: the shape and type of q")
     if lse is None:
-        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+        lse = cache.k_scale.new_empty((rows, heads))
     elif tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse: a contiguous float32 tensor [rows, q_heads]")
     workspace = _scratch(cache, workspace)
-    cq, co = _rows(q, "q"), _rows(out, "out")
-    _check(_dll.roomie_kv_attention(cache.ref, layer, seqs.data_ptr(), n, _ptr(q_offset), rows, heads, C.byref(cq),
-                                    d ** -0.5 if scale is None else scale, window, C.byref(co), lse.data_ptr(),
-                                    workspace.data_ptr(), workspace.numel(), _stream()), "roomie_kv_attention")
+    _check(_dll.roomie_kv_attention(cache.ref, layer, seqs.data_ptr(), n, None if q_offset is None else q_offset.data_ptr(), rows, heads,
+                                    _rows(q, "q"), d ** -0.5 if scale is None else scale, window, _rows(out, "out"), lse.data_ptr(),
+                                    workspace.data_ptr(), workspace.shape[0], _stream(q)), "roomie_kv_attention")
     return out, lse
 
 
@@ -254,7 +257,7 @@ def kv_reserve(cache: KVCache, seqs, want, *, workspace=None):
     want = _ids(want, "want", seqs.numel())
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_reserve(cache.ref, seqs.data_ptr(), want.data_ptr(), seqs.numel(), workspace.data_ptr(), workspace.numel(),
-                                  _stream()), "roomie_kv_reserve")
+                                  _stream(cache.k)), "roomie_kv_reserve")
 
 
 @_on_stream
@@ -264,14 +267,14 @@ def kv_fork(cache: KVCache, parents, children, *, workspace=None):
     children = _ids(children, "children", parents.numel())
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_fork(cache.ref, parents.data_ptr(), children.data_ptr(), parents.numel(), workspace.data_ptr(),
-                               workspace.numel(), _stream()), "roomie_kv_fork")
+                               workspace.numel(), _stream(cache.k)), "roomie_kv_fork")
 
 
 @_on_stream
 def kv_free(cache: KVCache, seqs):
     """roomie_kv_free: the sequences become empty, their pages lose a reference."""
     seqs = _ids(seqs, "seqs")
-    _check(_dll.roomie_kv_free(cache.ref, seqs.data_ptr(), seqs.numel(), _stream()), "roomie_kv_free")
+    _check(_dll.roomie_kv_free(cache.ref, seqs.data_ptr(), seqs.numel(), _stream(cache.k)), "roomie_kv_free")
 
 
 @_on_stream
@@ -279,7 +282,7 @@ def kv_copy(src: KVCache, src_pages, dst: KVCache, dst_pages):
     """roomie_kv_copy: page src_pages[i] of src to page dst_pages[i] of dst, all layers, codes and scales."""
     src_pages = _ids(src_pages, "src_pages")
     dst_pages = _ids(dst_pages, "dst_pages", src_pages.numel())
-    _check(_dll.roomie_kv_copy(src.ref, src_pages.data_ptr(), dst.ref, dst_pages.data_ptr(), src_pages.numel(), _stream()),
+    _check(_dll.roomie_kv_copy(src.ref, src_pages.data_ptr(), dst.ref, dst_pages.data_ptr(), src_pages.numel(), _stream(src.k)),
            "roomie_kv_copy")
 
 
@@ -296,7 +299,7 @@ def kv_compact(cache: KVCache, *, refs_out=None, pages_out=None, used_out=None, 
         _ids(used_out, "used_out", 1)
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_compact(cache.ref, refs_out.data_ptr(), pages_out.data_ptr(), _ptr(used_out), workspace.data_ptr(),
-                                  workspace.numel(), _stream()), "roomie_kv_compact")
+                                  workspace.numel(), _stream(cache.k)), "roomie_kv_compact")
 
 
 @contextmanager
