@@ -13,11 +13,12 @@ struct AppendArgs {
     long long k_token, k_head, v_token, v_head;
     RopeView rope;                 // rot = 0: keys are stored as they come
     HeadRows q;
-    uint32_t q_heads, q_per_block, kv_blocks;
-    int32_t q_in_place;
+    uint32_t q_heads, q_units, q_groups, kv_blocks;
+    unsigned long long q_threads;
 };
 
-constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
+constexpr unsigned long long kApartBytes = 4ull << 20;
+constexpr int kAppendThreads = 512, kAppendWarps = kAppendThreads / 32;
 
 // The `j`-th (sequence, page) in which the call's sequences have new tokens: every thread of the block gets the same answer.
 // false: there are fewer.
@@ -51,53 +52,19 @@ __device__ bool find_page(const AppendArgs& a, uint32_t j, KvSeq& s, uint32_t& p
         }
         const uint32_t first = ahead + incl - n;
         if (n && j >= first && j < first + n) {
-            sh[8] = mine.slot; sh[9] = mine.row; sh[10] = mine.count; sh[11] = mine.start; sh[12] = mine.length;
-            sh[13] = (mine.start >> a.c.page_shift) + (j - first);
+            sh[16] = mine.slot; sh[17] = mine.row; sh[18] = mine.count; sh[19] = mine.start; sh[20] = mine.length;
+            sh[21] = (mine.start >> a.c.page_shift) + (j - first);
         }
         __syncthreads();
         if (j < before + all) {
-            s.slot = sh[8]; s.row = sh[9]; s.count = sh[10]; s.start = sh[11]; s.length = sh[12];
-            page = sh[13];
+            s.slot = sh[16]; s.row = sh[17]; s.count = sh[18]; s.start = sh[19]; s.length = sh[20];
+            page = sh[21];
             return true;
         }
         before += all;
         __syncthreads();
     }
     return false;
-}
-
-// Loads unit `unit` of (row, head) as float32 - rotated pairs first, then the copied part - into x[0..kV) and, for a rotated
-// unit, x[kV..2kV); at[] are the elements they belong at.
-template <class T, int kV, bool kPairs>
-__device__ __forceinline__ bool load_unit(const T* p, uint32_t unit, uint32_t rot, const float2* cs, float* x, uint32_t* at) {
-    const uint32_t half = rot / 2, n_rot = half / kV;
-    using Raw = typename std::conditional<kV == 1, T, uint4>::type;
-    auto get = [](const T* from, float* to) {
-        const Raw r = *reinterpret_cast<const Raw*>(from);
-        if constexpr (kV == 1) to[0] = to_f32(r);
-        else unpack<T>(r, to);
-    };
-    if (unit >= n_rot) {
-        at[0] = rot + (unit - n_rot) * kV;
-        get(p + at[0], x);
-        return false;
-    }
-    at[0] = kPairs ? 2 * unit * kV : unit * kV;
-    at[1] = kPairs ? at[0] + kV : at[0] + half;
-    get(p + at[0], x);
-    get(p + at[1], x + kV);
-    const float2* w = cs + unit * kV;
-    if constexpr (kPairs && kV > 1) {
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {                                    // pairs (2i, 2i+1) of the 2*kV elements
-            const float e = x[2 * i], o = x[2 * i + 1];
-            x[2 * i] = __fsub_rn(__fmul_rn(e, w[i].x), __fmul_rn(o, w[i].y));
-            x[2 * i + 1] = __fadd_rn(__fmul_rn(o, w[i].x), __fmul_rn(e, w[i].y));
-        }
-    } else {
-        rotate_half<kV>(x, x + kV, w);
-    }
-    return true;
 }
 
 template <int kV> __device__ __forceinline__ void store_codes(uint8_t* to, const float* x, float inv, int32_t format) {
@@ -114,18 +81,35 @@ template <int kV> __device__ __forceinline__ void store_codes(uint8_t* to, const
     }
 }
 
-// finite magnitude of a value; NaN becomes 0, an infinity the largest float
-__device__ __forceinline__ float finite(float x, bool& odd) {
-    if (fabsf(x) <= 3.402823466e38f) return x;
-    odd = true;
-    return x != x ? 0.0f : copysignf(3.402823466e38f, x);
+// NaN becomes 0, an infinity the largest float; the result is the largest magnitude.  One multiply-add an element finds both: x * 0 is
+// no number for either.
+template <int kN> __device__ __forceinline__ float finite(float* x, bool& odd) {
+    float most = 0.0f, zero = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        most = fmaxf(most, fabsf(x[i]));
+        zero = fmaf(x[i], 0.0f, zero);
+    }
+    if (zero != 0.0f) {
+        odd = true;
+        most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -3.402823466e38f), 3.402823466e38f);
+            most = fmaxf(most, fabsf(x[i]));
+        }
+    }
+    return most;
 }
 
-// One block writes the new tokens of one page, keys or values, for all heads.  Groups of warps take a head each: a first pass
-// over the head's new tokens finds the largest magnitude, a second one quantises (it reads the tokens again, from L1/L2: a page's
-// tokens of one head are 4 to 64 KB, too much for registers in general).
+// One block writes the new tokens of one page, keys or values, for all heads.  A head's new tokens have to be seen twice, for their
+// largest magnitude and to be quantised: as many warps take a head as hold its tokens in registers, kHold units a thread, and the block
+// takes so many heads at a time.  A thread has the same units of every head, so where they lie and their angles are worked out once.
+// Larger pages (more than 512 units) are read, and turned, again.
+// A row's units: `pairs` pairs of kV elements - the rotated part, or all of a row that is not rotated - then single units of what a
+// partial rotation leaves.
 template <class T, int kV, bool kPairs>
-__device__ void append_page(const AppendArgs& a, uint32_t j, bool keys, float2* cs, uint32_t* sh, float* shf) {
+__device__ void append_page(const AppendArgs& a, uint32_t j, bool keys, uint32_t* sh, float* shf) {
     KvSeq s;
     uint32_t page;
     if (!find_page(a, j, s, page, sh)) return;
@@ -138,130 +122,199 @@ __device__ void append_page(const AppendArgs& a, uint32_t j, bool keys, float2* 
         if (threadIdx.x == 0) kv_flag(c.status, ROOMIE_FLAG_KV_PAGE);
         return;
     }
-    const uint32_t rot = keys ? a.rope.rot : 0, half = rot / 2;
-    for (uint32_t i = threadIdx.x; i < tokens * half; i += kAppendThreads) {
-        const uint32_t t = i / half, p = i - t * half;
-        cs[i] = rope_turn(a.rope.frequency[p], (int32_t)(pos0 + t), a.rope.amplitude);
-    }
     uint8_t* base = (keys ? c.k : c.v) + (long long)id * c.page_stride;
     float* scale = (keys ? c.k_scale : c.v_scale) + (size_t)id * c.heads;
-    const T* x = static_cast<const T*>(keys ? a.k : a.v);
     const long long x_token = keys ? a.k_token : a.v_token, x_head = keys ? a.k_head : a.v_head;
+    const T* x = static_cast<const T*>(keys ? a.k : a.v) + row0 * x_token;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    uint32_t together = 1;                                                // heads at a time: a power of two
-    while (together * 2 <= c.heads && together < kAppendWarps) together *= 2;
-    const uint32_t warps = kAppendWarps / together, group = wid / warps, team = warps * 32;
+    const uint32_t rot = keys ? a.rope.rot : 0;
+    const uint32_t pairs = (rot ? rot : c.dim) / 2 / kV, units = pairs + (rot ? (c.dim - rot) / kV : 0), n = tokens * units;
+    const uint32_t mate = kPairs || !rot ? kV : rot / 2;                  // from a unit to the other of its pair
+    constexpr int kHold = kV == 1 ? 4 : 1;
+    uint32_t warps = 1;                                                   // of a head: a power of two
+    while (warps < kAppendWarps && (warps * 32 * kHold < n || kAppendWarps / warps > c.heads)) warps *= 2;
+    const uint32_t together = kAppendWarps / warps, group = wid / warps, team = warps * 32;
     const uint32_t me = (wid % warps) * 32 + lane;
-    const uint32_t units = half / kV + (c.dim - rot) / kV;
+    const bool once = n <= team * kHold;
+    using Raw = typename std::conditional<kV == 1, T, uint4>::type;
     bool odd = false;
+
+    long long src[kHold];                                                 // elements from x; bytes from the head's part of the page
+    uint32_t dst[kHold];
+    int kind[kHold];                                                      // 0: nothing, 1: a single, 2: a pair
+    float2 w[kHold][kV];
+    Raw ra[kHold], rb[kHold];
+    float y[kHold][2 * kV];
+    auto place = [&](uint32_t i0) {
+#pragma unroll
+        for (int e = 0; e < kHold; ++e) {
+            const uint32_t i = i0 + e * team, t = i / units, u = i - t * units;
+            kind[e] = i >= n ? 0 : u >= pairs ? 1 : 2;
+            const uint32_t at = u >= pairs ? rot + (u - pairs) * kV : mate == kV ? 2 * u * kV : u * kV;
+            src[e] = t * x_token + at;
+            dst[e] = (held + t) * c.token_step + at;
+            if (rot && kind[e] == 2)
+#pragma unroll
+                for (int k = 0; k < kV; ++k) w[e][k] = rope_turn(a.rope.frequency[u * kV + k], (int32_t)(pos0 + t), a.rope.amplitude);
+        }
+    };
+    auto fetch = [&](uint32_t h) {                                        // all loads under way together
+#pragma unroll
+        for (int e = 0; e < kHold; ++e) {
+            const T* p = x + h * x_head + src[e];
+            if (kind[e]) ra[e] = *reinterpret_cast<const Raw*>(p);
+            if (kind[e] == 2) rb[e] = *reinterpret_cast<const Raw*>(p + mate);
+        }
+    };
+    auto widen = [](const Raw& r, float* to) {
+        if constexpr (kV == 1) to[0] = to_f32(r);
+        else unpack<T>(r, to);
+    };
+    auto values = [&]() {                                                 // of what was fetched; the result is their largest magnitude
+        float most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < kHold; ++e) {
+            if (kind[e] == 0) continue;
+            widen(ra[e], y[e]);
+            if (kind[e] == 2) {
+                widen(rb[e], y[e] + kV);
+                if (rot) {
+                    if constexpr (kPairs && kV > 1) {
+#pragma unroll
+                        for (int i = 0; i < kV; ++i) {                    // pairs (2i, 2i+1) of the 2*kV elements
+                            const float p = y[e][2 * i], q = y[e][2 * i + 1];
+                            y[e][2 * i] = __fsub_rn(__fmul_rn(p, w[e][i].x), __fmul_rn(q, w[e][i].y));
+                            y[e][2 * i + 1] = __fadd_rn(__fmul_rn(q, w[e][i].x), __fmul_rn(p, w[e][i].y));
+                        }
+                    } else {
+                        rotate_half<kV>(y[e], y[e] + kV, w[e]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = kV; i < 2 * kV; ++i) y[e][i] = 0.0f;
+            }
+            most = fmaxf(most, finite<2 * kV>(y[e], odd));
+        }
+        return most;
+    };
+
+    place(me);
+    if (once && group < c.heads) fetch(group);
     for (uint32_t h0 = 0; h0 < c.heads; h0 += together) {
         const uint32_t h = h0 + group;
         const bool on = h < c.heads;
-        __syncthreads();                                                  // cs is written; shf is free again
         const float old = on && held ? scale[h] : 0.0f;
         float amax = 0.0f;
-        if (on)
-            for (uint32_t i = me; i < tokens * units; i += team) {
-                const uint32_t t = i / units, u = i - t * units;
-                float y[2 * kV];
-                uint32_t at[2];
-                const bool two = load_unit<T, kV, kPairs>(x + (row0 + t) * x_token + h * x_head, u, rot, cs + (size_t)t * half, y, at);
-#pragma unroll
-                for (int e = 0; e < kV; ++e) amax = fmaxf(amax, fabsf(finite(y[e], odd)));
-                if (two)
-#pragma unroll
-                    for (int e = kV; e < 2 * kV; ++e) amax = fmaxf(amax, fabsf(finite(y[e], odd)));
+        if (on) {
+            if (once) {
+                amax = values();
+            } else {
+                for (uint32_t i0 = me; i0 < n; i0 += kHold * team) {
+                    place(i0);
+                    fetch(h);
+                    amax = fmaxf(amax, values());
+                }
             }
+        }
+        if (once && h + together < c.heads) fetch(h + together);          // on their way while this head is finished
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+        __syncthreads();                                                  // shf is free again, and `old` has been read
         if (lane == 0) shf[wid] = amax;
         __syncthreads();
         if (!on) continue;
-        for (uint32_t w = 0; w < warps; ++w) amax = fmaxf(amax, shf[group * warps + w]);
-        const int e = kv_scale_exponent(amax, c.format);
-        float now = pow2f(e), inv = pow2f(-e);
+        for (uint32_t v = 0; v < warps; ++v) amax = fmaxf(amax, shf[group * warps + v]);
+        const int ex = kv_scale_exponent(amax, c.format);
+        float now = pow2f(ex), inv = pow2f(-ex);
         if (held && old >= now) { now = old; inv = __fdiv_rn(1.0f, old); }
         uint8_t* to = base + h * c.head_step;
         if (held && old < now) {                                          // earlier tokens of the page: to the wider scale
             const float ratio = old * inv;
             for (uint32_t i = me; i < held * (c.dim / 2); i += team) {
                 const uint32_t t = i / (c.dim / 2), d = 2 * (i - t * (c.dim / 2));
-                uint16_t* w = reinterpret_cast<uint16_t*>(to + t * c.token_step + d);
-                const uint32_t code = *w;
-                *w = (uint16_t)kv_codes2(kv_value(code & 0xff, c.format) * ratio, kv_value(code >> 8, c.format) * ratio, c.format);
+                uint16_t* code2 = reinterpret_cast<uint16_t*>(to + t * c.token_step + d);
+                const uint32_t code = *code2;
+                *code2 = (uint16_t)kv_codes2(kv_value(code & 0xff, c.format) * ratio, kv_value(code >> 8, c.format) * ratio, c.format);
             }
         }
         if (me == 0) scale[h] = now;
-        for (uint32_t i = me; i < tokens * units; i += team) {
-            const uint32_t t = i / units, u = i - t * units;
-            float y[2 * kV];
-            uint32_t at[2];
-            const bool two = load_unit<T, kV, kPairs>(x + (row0 + t) * x_token + h * x_head, u, rot, cs + (size_t)t * half, y, at);
-            uint8_t* q = to + (held + t) * c.token_step;
+        for (uint32_t i0 = me; i0 < n; i0 += kHold * team) {
+            if (!once) {
+                place(i0);
+                fetch(h);
+                values();
+            }
 #pragma unroll
-            for (int e2 = 0; e2 < kV; ++e2) y[e2] = finite(y[e2], odd);
-            store_codes<kV>(q + at[0], y, inv, c.format);
-            if (two) {
-#pragma unroll
-                for (int e2 = kV; e2 < 2 * kV; ++e2) y[e2] = finite(y[e2], odd);
-                store_codes<kV>(q + at[1], y + kV, inv, c.format);
+            for (int e = 0; e < kHold; ++e) {
+                if (kind[e] == 0) continue;
+                store_codes<kV>(to + dst[e], y[e], inv, c.format);
+                if (kind[e] == 2) store_codes<kV>(to + dst[e] + mate, y[e] + kV, inv, c.format);
             }
         }
     }
     if (odd) kv_flag(c.status, ROOMIE_FLAG_KV_NONFINITE);
 }
 
-// The queries of q_per_block consecutive rows, rotated to their positions.
+// The queries, rotated to their rows' positions: thread `i` of those that roomie_rope would take.
 template <class T, int kV, bool kPairs>
-__device__ void append_queries(const AppendArgs& a, uint32_t block, float2* cs, int32_t* pos) {
-    const uint32_t first = block * a.q_per_block, tokens = min(a.q_per_block, a.rows - first), half = a.rope.rot / 2;
-    if (threadIdx.x < tokens) {
-        const uint32_t row = first + threadIdx.x;
-        uint32_t i = row;                                                 // the sequence of this row: the last with offset <= row
-        if (a.q_offset) {
-            uint32_t lo = 0, hi = a.num_seqs;
-            while (hi - lo > 1) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (a.q_offset[mid] <= (int32_t)row) lo = mid;
-                else hi = mid;
-            }
-            i = lo;
+__device__ void append_queries(const AppendArgs& a, unsigned long long i) {
+    if (i >= a.q_threads) return;
+    const uint32_t rest = (uint32_t)(i / a.q_units), unit = (uint32_t)(i - (unsigned long long)rest * a.q_units);
+    const uint32_t row = rest / a.q_groups, group = rest - row * a.q_groups;
+    uint32_t s = row;                                                     // the sequence of this row: the last with offset <= row
+    if (a.q_offset) {
+        uint32_t lo = 0, hi = a.num_seqs;
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (a.q_offset[mid] <= (int32_t)row) lo = mid;
+            else hi = mid;
         }
-        int32_t p = -1;
-        if (i < a.num_seqs) {
-            const KvSeq s = kv_seq(a.c, a.seqs, a.q_offset, a.rows, i, false);
-            if (row >= s.row && row < s.row + s.count && s.count <= s.length) p = (int32_t)(s.start + (row - s.row));
-        }
-        pos[threadIdx.x] = p;
+        s = lo;
     }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < tokens * half; i += kAppendThreads) {
-        const uint32_t t = i / half, p = i - t * half;
-        // a row that belongs to no sequence is passed on unturned
-        cs[i] = pos[t] < 0 ? make_float2(1.0f, 0.0f) : rope_turn(a.rope.frequency[p], pos[t], a.rope.amplitude);
+    RopeView rope = a.rope;
+    int32_t position = 0;
+    bool turned = false;
+    if (s < a.num_seqs) {
+        const KvSeq q = kv_seq(a.c, a.seqs, a.q_offset, a.rows, s, false);
+        turned = row >= q.row && row < q.row + q.count && q.count <= q.length;
+        if (turned) position = (int32_t)(q.start + (row - q.row));
     }
-    __syncthreads();
-    rope_block<T, kV, kPairs, kV == 1 ? 1 : 4>(a.q, cs, first, tokens, a.q_heads, a.c.dim, a.rope.rot, a.q_in_place != 0);
+    if (!turned) rope.amplitude = 1.0f;                                   // a row of no sequence is passed on as it is (position 0)
+    rope_heads<T, kV, kPairs, kV == 1 ? 1 : 2>(a.q, rope, row, position, false, unit, group, a.q_groups, a.q_heads);
 }
 
 // Blocks [0, 2 * kv_blocks): page j of the call, keys (even) and values (odd); the rest: queries.  One launch for the three, because
 // a decoding step's share of each is far below a launch's cost.
 template <class T, int kV, bool kPairs>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
-    extern __shared__ float2 cs[];
-    __shared__ uint32_t sh[16];
+__global__ void __launch_bounds__(kAppendThreads, 2) append_kernel(AppendArgs a) {
+    __shared__ uint32_t sh[24];
     __shared__ float shf[kAppendWarps];
-    if (blockIdx.x < 2 * a.kv_blocks) append_page<T, kV, kPairs>(a, blockIdx.x >> 1, (blockIdx.x & 1) == 0, cs, sh, shf);
-    else append_queries<T, kV, kPairs>(a, blockIdx.x - 2 * a.kv_blocks, cs, reinterpret_cast<int32_t*>(sh));
+    grid_dependency_launch();                                             // the queries' kernel needs nothing of this one
+    if (blockIdx.x < 2 * a.kv_blocks) append_page<T, kV, kPairs>(a, blockIdx.x >> 1, (blockIdx.x & 1) == 0, sh, shf);
+    else append_queries<T, kV, kPairs>(a, (unsigned long long)(blockIdx.x - 2 * a.kv_blocks) * kAppendThreads + threadIdx.x);
+}
+
+// The queries alone, with the registers that they need.
+constexpr int kQueryThreads = 128;
+template <class T, int kV, bool kPairs>
+__global__ void __launch_bounds__(kQueryThreads, 8) append_queries_kernel(AppendArgs a) {
+    append_queries<T, kV, kPairs>(a, (unsigned long long)blockIdx.x * kQueryThreads + threadIdx.x);
+    grid_dependency_wait();                                               // it started beside the keys and values; what follows waits for both
 }
 
 template <class T>
-static int launch_append(const AppendArgs& a, bool wide, bool pairs, dim3 grid, size_t smem, cudaStream_t st) {
+static int launch_append(const AppendArgs& a, bool wide, bool pairs, bool apart, cudaStream_t st) {
     constexpr int v = kVecOf<T>;
     void (*k)(AppendArgs);
     if (pairs) k = wide ? append_kernel<T, v, true> : append_kernel<T, 1, true>;
     else k = wide ? append_kernel<T, v, false> : append_kernel<T, 1, false>;
-    return launch("kv_append", k, grid, dim3(kAppendThreads), smem, st, false, a);
+    const unsigned long long beside = apart ? 0 : (a.q_threads + kAppendThreads - 1) / kAppendThreads;
+    const int rc = launch("kv_append", k, dim3((uint32_t)(2 * a.kv_blocks + beside)), dim3(kAppendThreads), 0, st, false, a);
+    if (rc != ROOMIE_OK || !apart) return rc;
+    if (pairs) k = wide ? append_queries_kernel<T, v, true> : append_queries_kernel<T, 1, true>;
+    else k = wide ? append_queries_kernel<T, v, false> : append_queries_kernel<T, 1, false>;
+    return launch("kv_append_queries", k, dim3((uint32_t)((a.q_threads + kQueryThreads - 1) / kQueryThreads)), dim3(kQueryThreads), 0, st, true, a);
 }
 
 }  // namespace roomie
@@ -298,24 +351,22 @@ extern "C" int roomie_kv_append(const roomie_kv_cache* cache, uint32_t layer, co
     unsigned long long blocks = rows / cache->page_tokens + 2ull * num_seqs;
     if (blocks > rows) blocks = rows;
     a.kv_blocks = (uint32_t)blocks;
-    uint32_t q_blocks = 0;
+    unsigned long long q_blocks = 0;
     if (q) {
         a.q = {q->data, q_out->data, q->token_stride, q->head_stride, q_out->token_stride, q_out->head_stride};
         a.q_heads = q_heads;
-        a.q_in_place = q->data == q_out->data;
         wide = wide && rows_aligned16(*q, rows, q_heads) && rows_aligned16(*q_out, rows, q_heads);
-        const uint32_t full = (uint32_t)sm_count() * 8;
-        a.q_per_block = rows / full < 1 ? 1 : rows / full > 8 ? 8 : rows / full;
-        q_blocks = (rows + a.q_per_block - 1) / a.q_per_block;
+        const RopeSplit s = rope_split(rows, q_heads, cache->head_dim, rope->rotary_dim, wide ? 16u / (uint32_t)size_of_type(k->type) : 1u,
+                                       q->data == q_out->data, (uint32_t)sm_count());
+        a.q_units = s.units; a.q_groups = s.groups; a.q_threads = s.threads;
+        q_blocks = (s.threads + kQueryThreads - 1) / kQueryThreads;
     }
-    const uint32_t half = rope ? rope->rotary_dim / 2 : 0;
-    const uint32_t most = cache->page_tokens < rows ? cache->page_tokens : rows;
-    const size_t smem = (size_t)(most > a.q_per_block ? most : a.q_per_block) * half * sizeof(float2);
-    if (smem > 200 * 1024) return ROOMIE_ERR_CAPACITY;
-    const dim3 grid(2 * a.kv_blocks + q_blocks);
+    if (q_blocks + 2ull * a.kv_blocks > 0x7fffffffull) return ROOMIE_ERR_INVALID_ARG;
+    // Many queries go in a launch of their own: beside the keys and values they have too few registers to keep the memory busy
+    const bool apart = q && (unsigned long long)rows * q_heads * cache->head_dim * size_of_type(k->type) >= kApartBytes;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool pairs = rope && rope->interleaved;
-    if (k->type == ROOMIE_F32) return launch_append<float>(a, wide, pairs, grid, smem, st);
-    if (k->type == ROOMIE_F16) return launch_append<__half>(a, wide, pairs, grid, smem, st);
-    return launch_append<__nv_bfloat16>(a, wide, pairs, grid, smem, st);
+    if (k->type == ROOMIE_F32) return launch_append<float>(a, wide, pairs, apart, st);
+    if (k->type == ROOMIE_F16) return launch_append<__half>(a, wide, pairs, apart, st);
+    return launch_append<__nv_bfloat16>(a, wide, pairs, apart, st);
 }

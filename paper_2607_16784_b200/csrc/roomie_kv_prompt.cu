@@ -896,7 +896,7 @@ size_t prompt_partial_bytes(uint32_t dim) {
 }
 
 template <int DP, int kFormat, class T> static int launch_one(const AttnArgs& a, cudaStream_t st) {
-    return launch("kv_attention_prompt", prompt_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count()), dim3(kPromptThreads), Prompt<DP>::kSmem,
+    return launch("kv_attention", prompt_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count()), dim3(kPromptThreads), Prompt<DP>::kSmem,
                   st, false, a);
 }
 template <int kFormat, class T> static int launch_dims(const AttnArgs& a, cudaStream_t st) {

@@ -17,78 +17,86 @@ struct HeadRows {            // element strides
     long long x_token, x_head, y_token, y_head;
 };
 
-// Threads (chunk, row) of a 256-thread block go over the rows (token, head) of `tokens` consecutive tokens from `first`.
-// cs: [tokens][rot/2] cosine and sine, in shared memory.  A unit is kV elements; a row has rot/(2*kV) unit pairs that are
-// rotated and, unless it is done in place, (dim - rot)/kV units that are copied.  kV = 16 bytes, or 1 when some row is not
-// 16-byte aligned or the parts do not divide into such units.
+// What one thread does: unit `unit` of heads head, head + step, ... of one token.  A unit is kV elements; a row has rot/(2*kV) pairs of
+// units that are rotated and, unless it is done in place, (dim - rot)/kV units that are copied.  kV = 16 bytes, or 1 when some row is
+// not 16-byte aligned or the parts do not divide into such units.  The thread works out its own kV cosines and sines (some 25
+// instructions each) once for all its heads: nothing is shared, nobody waits.
 template <class T, int kV, bool kPairs, int kUnroll>
-__device__ __forceinline__ void rope_block(const HeadRows& io, const float2* cs, uint32_t first, uint32_t tokens, uint32_t heads,
-                                           uint32_t dim, uint32_t rot, bool in_place) {
-    const uint32_t half = rot / 2, n_rot = half / kV, n_copy = in_place ? 0 : (dim - rot) / kV, units = n_rot + n_copy;
-    const uint32_t width = units < blockDim.x ? units : blockDim.x, lanes = blockDim.x / width;
-    const uint32_t lane = threadIdx.x / width;
-    if (lane >= lanes) return;
-    const uint32_t rows = tokens * heads;
+__device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& rope, uint32_t token, int32_t position, bool inverse,
+                                           uint32_t unit, uint32_t head, uint32_t step, uint32_t heads) {
+    const uint32_t half = rope.rot / 2, n_rot = half / kV;
     using Raw = typename std::conditional<kV == 1, T, uint4>::type;
-    for (uint32_t unit = threadIdx.x % width; unit < units; unit += width) {
-        const bool turn = unit < n_rot;
-        const uint32_t a = !turn ? rot + (unit - n_rot) * kV : kPairs ? 2 * unit * kV : unit * kV;
-        const uint32_t b = kPairs ? a + kV : a + half;
-        uint32_t tok = lane / heads, head = lane % heads;
-        for (uint32_t row = lane; row < rows; row += lanes * kUnroll) {
-            Raw ra[kUnroll], rb[kUnroll];
-            uint32_t tt[kUnroll], hh[kUnroll];
+    const bool turn = unit < n_rot;
+    const uint32_t a = !turn ? rope.rot + (unit - n_rot) * kV : kPairs ? 2 * unit * kV : unit * kV;
+    const uint32_t b = kPairs ? a + kV : a + half;
+    float2 w[kV];
+    if (turn)
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                tt[u] = tok;
-                hh[u] = head;
-                if (row + u * lanes < rows) {
-                    const T* p = static_cast<const T*>(io.x) + (first + tok) * io.x_token + head * io.x_head;
-                    ra[u] = *reinterpret_cast<const Raw*>(p + a);
-                    if (turn) rb[u] = *reinterpret_cast<const Raw*>(p + b);
-                }
-                head += lanes;
-                while (head >= heads) { head -= heads; ++tok; }
+        for (int i = 0; i < kV; ++i) {
+            w[i] = rope_turn(rope.frequency[unit * kV + i], position, rope.amplitude);
+            if (inverse) w[i].y = -w[i].y;
+        }
+    const T* x = static_cast<const T*>(io.x) + token * io.x_token + head * io.x_head;
+    T* y = static_cast<T*>(io.y) + token * io.y_token + head * io.y_head;
+    for (uint32_t h = head; h < heads; h += step * kUnroll) {
+        Raw ra[kUnroll], rb[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (h + u * step < heads) {
+                const T* p = x + (long long)(u * step) * io.x_head;
+                ra[u] = *reinterpret_cast<const Raw*>(p + a);
+                if (turn) rb[u] = *reinterpret_cast<const Raw*>(p + b);
             }
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                if (row + u * lanes >= rows) break;
-                T* p = static_cast<T*>(io.y) + (first + tt[u]) * io.y_token + hh[u] * io.y_head;
-                if (!turn) {
-                    *reinterpret_cast<Raw*>(p + a) = ra[u];
-                    continue;
-                }
-                const float2* w = cs + (size_t)tt[u] * half + unit * kV;
-                if constexpr (kV == 1) {
-                    const float x = to_f32(ra[u]), y = to_f32(rb[u]);
-                    p[a] = from_f32<T>(__fsub_rn(__fmul_rn(x, w->x), __fmul_rn(y, w->y)));
-                    p[b] = from_f32<T>(__fadd_rn(__fmul_rn(y, w->x), __fmul_rn(x, w->y)));
-                } else {
-                    float xa[kV], xb[kV];
-                    unpack<T>(ra[u], xa);
-                    unpack<T>(rb[u], xb);
-                    if constexpr (kPairs) {
-                        float e[kV], o[kV];
+        for (int u = 0; u < kUnroll; ++u) {
+            if (h + u * step >= heads) break;
+            T* p = y + (long long)(u * step) * io.y_head;
+            if (!turn) {
+                *reinterpret_cast<Raw*>(p + a) = ra[u];
+                continue;
+            }
+            if constexpr (kV == 1) {
+                const float e = to_f32(ra[u]), o = to_f32(rb[u]);
+                p[a] = from_f32<T>(__fsub_rn(__fmul_rn(e, w->x), __fmul_rn(o, w->y)));
+                p[b] = from_f32<T>(__fadd_rn(__fmul_rn(o, w->x), __fmul_rn(e, w->y)));
+            } else {
+                float xa[2 * kV];
+                unpack<T>(ra[u], xa);
+                unpack<T>(rb[u], xa + kV);
+                if constexpr (kPairs) {
 #pragma unroll
-                        for (int i = 0; i < kV / 2; ++i) {
-                            e[i] = xa[2 * i]; o[i] = xa[2 * i + 1];
-                            e[kV / 2 + i] = xb[2 * i]; o[kV / 2 + i] = xb[2 * i + 1];
-                        }
-                        rotate_half<kV>(e, o, w);
-#pragma unroll
-                        for (int i = 0; i < kV / 2; ++i) {
-                            xa[2 * i] = e[i]; xa[2 * i + 1] = o[i];
-                            xb[2 * i] = e[kV / 2 + i]; xb[2 * i + 1] = o[kV / 2 + i];
-                        }
-                    } else {
-                        rotate_half<kV>(xa, xb, w);
+                    for (int i = 0; i < kV; ++i) {                        // pairs (2i, 2i+1) of the 2*kV elements
+                        const float e = xa[2 * i], o = xa[2 * i + 1];
+                        xa[2 * i] = __fsub_rn(__fmul_rn(e, w[i].x), __fmul_rn(o, w[i].y));
+                        xa[2 * i + 1] = __fadd_rn(__fmul_rn(o, w[i].x), __fmul_rn(e, w[i].y));
                     }
-                    *reinterpret_cast<uint4*>(p + a) = pack<T>(xa);
-                    *reinterpret_cast<uint4*>(p + b) = pack<T>(xb);
+                } else {
+                    rotate_half<kV>(xa, xa + kV, w);
                 }
+                *reinterpret_cast<uint4*>(p + a) = pack<T>(xa);
+                *reinterpret_cast<uint4*>(p + b) = pack<T>(xa + kV);
             }
         }
+        x += (long long)(step * kUnroll) * io.x_head;
+        y += (long long)(step * kUnroll) * io.y_head;
     }
+}
+
+// Threads are (token, head group, unit), units fastest.  Enough head groups to fill the GPU's threads twice over (measured: see rope_kernel), as few as that takes otherwise, because
+// each works out its own angles.
+struct RopeSplit {
+    uint32_t units, groups;
+    unsigned long long threads;
+};
+inline RopeSplit rope_split(uint32_t tokens, uint32_t heads, uint32_t dim, uint32_t rot, uint32_t kv, bool in_place, uint32_t sms) {
+    RopeSplit s;
+    s.units = rot / 2 / kv + (in_place ? 0 : (dim - rot) / kv);
+    const unsigned long long one = (unsigned long long)tokens * s.units, fill = 2048ull * sms * 2;
+    unsigned long long g = one ? (fill + one - 1) / one : 1;
+    if (g > heads) g = heads;
+    s.groups = (uint32_t)(g < 1 ? 1 : g);
+    s.threads = one * s.groups;
+    return s;
 }
 
 // The parts of a row divide into units of 16 bytes.

@@ -68,38 +68,35 @@ struct RopeArgs {
     HeadRows io;
     RopeView rope;
     const int32_t* positions;
-    uint32_t tokens, heads, dim, per_block;
-    int32_t inverse, in_place;
+    uint32_t heads, units, groups;
+    unsigned long long threads;
+    int32_t inverse;
 };
 
-// Memory-bound: every element is read and written once.  A block takes `per_block` tokens, works out their rot/2 cosines
-// and sines once into shared memory (about 25 instructions each, shared by all heads of the token) and then streams the
-// heads through registers in 128-bit units.
+constexpr int kRopeThreads = 128;
+
+// Memory-bound: every element is read and written once.
 template <class T, int kV, bool kPairs>
-__global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
-    extern __shared__ float2 cs[];
-    const uint32_t first = blockIdx.x * a.per_block;
-    const uint32_t tokens = min(a.per_block, a.tokens - first);
-    const uint32_t half = a.rope.rot / 2;
-    for (uint32_t i = threadIdx.x; i < tokens * half; i += blockDim.x) {
-        const uint32_t t = i / half, p = i - t * half;
-        float2 w = rope_turn(a.rope.frequency[p], a.positions[first + t], a.rope.amplitude);
-        if (a.inverse) w.y = -w.y;
-        cs[i] = w;
-    }
-    __syncthreads();
-    rope_block<T, kV, kPairs, kV == 1 ? 1 : 4>(a.io, cs, first, tokens, a.heads, a.dim, a.rope.rot, a.in_place != 0);
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_kernel(RopeArgs a) {
+    const unsigned long long i = (unsigned long long)blockIdx.x * kRopeThreads + threadIdx.x;
+    if (i >= a.threads) return;
+    const uint32_t rest = (uint32_t)(i / a.units), unit = (uint32_t)(i - (unsigned long long)rest * a.units);
+    const uint32_t token = rest / a.groups, group = rest - token * a.groups;
+    rope_heads<T, kV, kPairs, kV == 1 ? 1 : 2>(a.io, a.rope, token, a.positions[token], a.inverse != 0, unit, group, a.groups, a.heads);
 }
 
 template <class T>
-static int launch_rope(const RopeArgs& a, bool wide, cudaStream_t st) {
-    const dim3 grid((a.tokens + a.per_block - 1) / a.per_block);
-    const size_t smem = (size_t)a.per_block * (a.rope.rot / 2) * sizeof(float2);
+static int launch_rope(RopeArgs a, uint32_t tokens, uint32_t dim, bool in_place, bool wide, cudaStream_t st) {
     constexpr int v = kVecOf<T>;
+    const RopeSplit s = rope_split(tokens, a.heads, dim, a.rope.rot, wide ? v : 1, in_place, (uint32_t)sm_count());
+    if (s.threads / a.heads > 0xffffffffull) return ROOMIE_ERR_INVALID_ARG;
+    a.units = s.units; a.groups = s.groups; a.threads = s.threads;
+    const unsigned long long blocks = (s.threads + kRopeThreads - 1) / kRopeThreads;
+    if (blocks > 0x7fffffffull) return ROOMIE_ERR_INVALID_ARG;
     void (*k)(RopeArgs);
     if (a.rope.interleaved) k = wide ? rope_kernel<T, v, true> : rope_kernel<T, 1, true>;
     else k = wide ? rope_kernel<T, v, false> : rope_kernel<T, 1, false>;
-    return launch("rope", k, grid, dim3(256), smem, st, false, a);
+    return launch("rope", k, dim3((uint32_t)blocks), dim3(kRopeThreads), 0, st, false, a);
 }
 
 }  // namespace roomie
@@ -130,20 +127,18 @@ extern "C" int roomie_rope(const roomie_rope_table* table, const roomie_rows* x,
     const bool same = x->data == y->data;
     if (same && (x->token_stride != y->token_stride || x->head_stride != y->head_stride)) return ROOMIE_ERR_INVALID_ARG;
     if ((unsigned long long)tokens * heads > 0x7fffffffull) return ROOMIE_ERR_INVALID_ARG;
-    RopeArgs a;
+    RopeArgs a = {};
     a.io = {x->data, y->data, x->token_stride, x->head_stride, y->token_stride, y->head_stride};
     a.rope = {table->frequency, table->rotary_dim, table->interleaved, table->amplitude};
     a.positions = positions;
-    a.tokens = tokens; a.heads = heads; a.dim = head_dim;
-    a.inverse = inverse != 0; a.in_place = same;
-    const uint32_t full = (uint32_t)sm_count() * 8;                       // blocks that fill the GPU
-    a.per_block = tokens / full < 1 ? 1 : tokens / full > 8 ? 8 : tokens / full;
+    a.heads = heads;
+    a.inverse = inverse != 0;
     const bool wide = rope_units_of_16(table->rotary_dim, head_dim, x->type, table->interleaved) &&
                       rows_aligned16(*x, tokens, heads) && rows_aligned16(*y, tokens, heads);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (x->type == ROOMIE_F32) return launch_rope<float>(a, wide, st);
-    if (x->type == ROOMIE_F16) return launch_rope<__half>(a, wide, st);
-    return launch_rope<__nv_bfloat16>(a, wide, st);
+    if (x->type == ROOMIE_F32) return launch_rope<float>(a, tokens, head_dim, same, wide, st);
+    if (x->type == ROOMIE_F16) return launch_rope<__half>(a, tokens, head_dim, same, wide, st);
+    return launch_rope<__nv_bfloat16>(a, tokens, head_dim, same, wide, st);
 }
 
 extern "C" int roomie_record_enable(uint32_t capacity) {
