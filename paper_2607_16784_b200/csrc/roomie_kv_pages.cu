@@ -56,7 +56,8 @@ struct CopyArgs {
     uint32_t* status;
 };
 
-// Bound by memory: each unit is up to 16 KB of one run, 256 threads with four 128-bit loads in flight each.
+// Bound by memory: each unit is up to 16 KB of one run, 256 threads with four 128-bit loads in flight each, past the caches' reuse; up to
+// four times the blocks that fit at once, so that the last ones end together (1.35 GB moved: 221 us, with one round of blocks 242).
 constexpr uint32_t kCopyUnit = 16384;
 __device__ void copy_pages(const CopyArgs& a, unsigned long long worker, unsigned long long workers) {
     const uint32_t n = a.count ? min((uint32_t)max(*a.count, 0), a.n) : a.n;
@@ -78,10 +79,10 @@ __device__ void copy_pages(const CopyArgs& a, unsigned long long worker, unsigne
         uint4 x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (threadIdx.x + e * 256 < vecs) x[e] = s[threadIdx.x + e * 256];
+            if (threadIdx.x + e * 256 < vecs) x[e] = __ldcs(s + threadIdx.x + e * 256);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (threadIdx.x + e * 256 < vecs) d[threadIdx.x + e * 256] = x[e];
+            if (threadIdx.x + e * 256 < vecs) __stcs(d + threadIdx.x + e * 256, x[e]);
         if (part == 0) {
             const float* ss = (side ? a.svs : a.sks) + ((size_t)layer * a.s_pages + from) * a.heads;
             float* ds = (side ? a.dvs : a.dks) + ((size_t)layer * a.d_pages + to) * a.heads;
@@ -105,7 +106,7 @@ static CopyArgs copy_args(const roomie_kv_cache* s, const roomie_kv_cache* d) {
 }
 static uint32_t copy_blocks(const CopyArgs& a, unsigned long long pairs) {
     const unsigned long long units = pairs * a.layers * 2 * ((a.bytes + kCopyUnit - 1) / kCopyUnit);
-    const unsigned long long full = (unsigned long long)sm_count() * 8;
+    const unsigned long long full = (unsigned long long)sm_count() * 32;
     return (uint32_t)(units < 1 ? 1 : units < full ? units : full);
 }
 
@@ -307,6 +308,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(TableView t, co
 // Blocks [0, n): the table row of one child; the rest: the part-filled pages.
 __global__ void __launch_bounds__(256) fork_move_kernel(TableView t, const int32_t* parents, const int32_t* children, uint32_t n,
                                                         const int32_t* ws, CopyArgs copy) {
+    grid_dependency_wait();                                       // the plan; this kernel's start overlaps its end
     if (blockIdx.x >= n) {
         copy_pages(copy, blockIdx.x - n, gridDim.x - n);
         return;
@@ -357,26 +359,45 @@ __global__ void __launch_bounds__(128) free_kernel(TableView t, const int32_t* s
 }
 
 // ---- compact -----------------------------------------------------------------------------------------------------------
+// which of the kScan pages from p0 on are in use
+__device__ __forceinline__ uint32_t used_mask(const int32_t* refs, uint32_t p0, uint32_t num_pages) {
+    uint32_t m = 0;
+    if (p0 < num_pages && num_pages - p0 >= kScan && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+#pragma unroll
+        for (int e = 0; e < kScan / 4; ++e) {
+            const int4 r = *reinterpret_cast<const int4*>(refs + p0 + 4 * e);
+            m |= ((r.x > 0) | (r.y > 0) << 1 | (r.z > 0) << 2 | (r.w > 0) << 3) << (4 * e);
+        }
+    } else {
+        for (int e = 0; e < kScan; ++e)
+            if ((unsigned long long)p0 + e < num_pages && refs[p0 + e] > 0) m |= 1u << e;
+    }
+    return m;
+}
+
 // Workspace: [0] moves, [1] used pages, [2..4) unused, then source, hole, count (num_pages each) and the map of moved pages.
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(TableView t, int32_t* ws, int32_t* used_out) {
     __shared__ uint32_t sh[kPlanWarps];
     const uint32_t P = t.num_pages;
     int32_t *source = ws + 4, *hole = source + P, *count = hole + P, *map = count + P;
     uint32_t mine = 0, used;
-    for (uint32_t p = threadIdx.x; p < P; p += kPlanThreads) mine += t.refs[p] > 0;
+    for (uint32_t base = 0; base < P; base += kPlanThreads * kScan)
+        mine += __popc(used_mask(t.refs, base + threadIdx.x * kScan, P));
     block_exclusive(mine, used, sh);
     uint32_t holes = 0, sources = 0;
-    for (uint32_t base = 0; base < P; base += kPlanThreads) {
-        const uint32_t p = base + threadIdx.x;
-        const int32_t r = p < P ? t.refs[p] : 0;
-        const bool is_hole = p < used && r <= 0, is_source = p < P && p >= used && r > 0;
-        uint32_t all;
-        const uint32_t at = block_exclusive((is_hole ? 1u : 0u) | (is_source ? 1u << 16 : 0u), all, sh);
-        if (p < P && p >= used && !is_source) map[p] = -1;
-        if (is_hole) hole[holes + (at & 0xffffu)] = (int32_t)p;
-        if (is_source) {
-            source[sources + (at >> 16)] = (int32_t)p;
-            count[sources + (at >> 16)] = r;
+    for (uint32_t base = 0; base < P; base += kPlanThreads * kScan) {
+        const uint32_t p0 = base + threadIdx.x * kScan;
+        const uint32_t in_use = used_mask(t.refs, p0, P), there = p0 >= P ? 0u : P - p0 >= kScan ? (1u << kScan) - 1 : (1u << (P - p0)) - 1;
+        const uint32_t below = p0 >= used ? 0u : used - p0 >= kScan ? (1u << kScan) - 1 : (1u << (used - p0)) - 1;
+        uint32_t hole_bits = ~in_use & there & below, source_bits = in_use & ~below, all;
+        const uint32_t at = block_exclusive((uint32_t)__popc(hole_bits) | (uint32_t)__popc(source_bits) << 16, all, sh);
+        uint32_t h = holes + (at & 0xffffu), s = sources + (at >> 16);
+        for (uint32_t rest = there & ~below & ~in_use; rest; rest &= rest - 1) map[p0 + __ffs(rest) - 1] = -1;
+        for (; hole_bits; hole_bits &= hole_bits - 1) hole[h++] = (int32_t)(p0 + __ffs(hole_bits) - 1);
+        for (; source_bits; source_bits &= source_bits - 1) {
+            const uint32_t p = p0 + __ffs(source_bits) - 1;
+            source[s] = (int32_t)p;
+            count[s++] = t.refs[p];
         }
         holes += all & 0xffffu;
         sources += all >> 16;
@@ -392,6 +413,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(TableView t,
 
 __global__ void __launch_bounds__(256) compact_move_kernel(TableView t, const int32_t* ws, int32_t* refs_out, int32_t* pages_out,
                                                            uint32_t table_blocks, CopyArgs copy) {
+    grid_dependency_wait();                                       // the plan; this kernel's start overlaps its end
     if (blockIdx.x >= table_blocks) {
         copy_pages(copy, blockIdx.x - table_blocks, gridDim.x - table_blocks);
         return;
@@ -469,7 +491,7 @@ extern "C" int roomie_kv_fork(const roomie_kv_cache* cache, const int32_t* paren
     if (rc != ROOMIE_OK) return rc;
     CopyArgs copy = copy_args(cache, cache);
     copy.n = n; copy.src = ws + 2 * (size_t)n; copy.dst = ws + 3 * (size_t)n;
-    return launch("kv_fork_move", fork_move_kernel, dim3(n + copy_blocks(copy, n)), dim3(256), 0, st, false, t, parents, children, n,
+    return launch("kv_fork_move", fork_move_kernel, dim3(n + copy_blocks(copy, n)), dim3(256), 0, st, true, t, parents, children, n,
                   ws, copy);
 }
 
@@ -510,5 +532,5 @@ extern "C" int roomie_kv_compact(const roomie_kv_cache* cache, int32_t* refs_out
     const unsigned long long entries = (unsigned long long)cache->max_seqs * cache->max_pages + P;
     const uint32_t table_blocks = (uint32_t)(entries / 1024 < 1 ? 1 : entries / 1024 > 148 ? 148 : entries / 1024);
     return launch("kv_compact_move", compact_move_kernel, dim3(table_blocks + copy_blocks(copy, P / 2 ? P / 2 : 1)), dim3(256), 0, st,
-                  false, t, ws, refs_out, pages_out, table_blocks, copy);
+                  true, t, ws, refs_out, pages_out, table_blocks, copy);
 }

@@ -82,8 +82,9 @@ __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& r
     }
 }
 
-// Threads are (token, head group, unit), units fastest.  Enough head groups to fill the GPU's threads twice over (measured: see rope_kernel), as few as that takes otherwise, because
-// each works out its own angles.
+// Threads are (token, head group, unit), units fastest.  Each works out its own angles, so it should have four heads or more (1000 tokens
+// x 40 heads: 8.3 us, with one head a thread 10.4); up to that, groups enough for twice the GPU's threads (16384 tokens: 61.7 us, with
+// half as many 64.7); and for few tokens, where only latency counts, as many groups as it takes to give every SM 256 threads.
 struct RopeSplit {
     uint32_t units, groups;
     unsigned long long threads;
@@ -91,10 +92,12 @@ struct RopeSplit {
 inline RopeSplit rope_split(uint32_t tokens, uint32_t heads, uint32_t dim, uint32_t rot, uint32_t kv, bool in_place, uint32_t sms) {
     RopeSplit s;
     s.units = rot / 2 / kv + (in_place ? 0 : (dim - rot) / kv);
-    const unsigned long long one = (unsigned long long)tokens * s.units, fill = 2048ull * sms * 2;
-    unsigned long long g = one ? (fill + one - 1) / one : 1;
-    if (g > heads) g = heads;
-    s.groups = (uint32_t)(g < 1 ? 1 : g);
+    const unsigned long long one = (unsigned long long)tokens * s.units;
+    if (one == 0) return {s.units, 1, 0};                                 // in place, and nothing is rotated
+    unsigned long long g = (4096ull * sms + one - 1) / one, few = 256ull * sms / one;
+    if (g > heads / 4) g = heads / 4;
+    if (g < few) g = few;
+    s.groups = (uint32_t)(g < 1 ? 1 : g > heads ? heads : g);
     s.threads = one * s.groups;
     return s;
 }
