@@ -450,8 +450,9 @@ typedef struct roomie_kv_cache {
     uint32_t *status;            /* [1] sticky ROOMIE_FLAG_KV_* bits */
 } roomie_kv_cache;
 
-/* Device scratch for the calls below that take a workspace: enough for any of them on this cache.  It must be zeroed
- * once before its first use; every call leaves it ready for the next.  0 on invalid arguments. */
+/* Device scratch for the calls below that take a workspace: enough for any of them on this cache, 256-byte aligned.  Its first
+ * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them so.  0 on invalid arguments. */
+#define ROOMIE_KV_WORKSPACE_ZEROED 16384u
 size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
 
 /* Writes the keys and values of new tokens into `layer` of the cache.  Sequence i of the call is row seqs[i] of the
@@ -462,6 +463,7 @@ size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
  * so that a scale that has to grow while a page fills moves e4m3 codes without rounding them a second time; int8 pays
  * up to one bit for it); the scale of a page that holds earlier tokens never shrinks, and its earlier codes are
  * rescaled when it grows.  Float32 arithmetic on values of any ROOMIE_ type, rounded once to the code (nearest even).
+ * q_out may be q (same strides).  Rows that belong to no sequence are not stored and their queries are passed on unrotated.
  * Errors: INVALID_ARG, CUDA. */
 int roomie_kv_append(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs,
                      const int32_t *q_offset, uint32_t rows, const roomie_rows *k, const roomie_rows *v,
@@ -472,6 +474,10 @@ int roomie_kv_append(const roomie_kv_cache *cache /* host */, uint32_t layer, co
  * length - n + t and sees the keys at or before it (and within `window` positions, itself included, when window > 0).
  * Query head h reads key head h / (q_heads / kv_heads).  Softmax statistics and sums are float32; products take q and
  * the codes as they are, probabilities are rounded to 11 bits.  A row that sees nothing gives 0 and lse = -inf.
+ * Scales are 0 or more, of any value (a value scale below 2^-100 counts as 2^-100).  What lies behind a sequence's length, in pages
+ * it does not hold, or before every row's window is not read, whatever it holds.  Codes 0x7f and 0xff of e4m3 are NaN, which
+ * roomie_kv_append never writes; a NaN that some row of a tile of rows sees may reach the other rows of that tile.
+ * The result does not depend on timing: the same call gives the same bits.
  *   q, out  [rows][q_heads][head_dim], F16 or BF16, the same type
  *   lse     [rows][q_heads] float32 natural logarithm of the softmax denominator, may be NULL
  * q_offset NULL: one row per sequence (rows == num_seqs).  Rows outside every sequence are not written.

@@ -587,6 +587,7 @@ size_t kv_attention_bytes(const roomie_kv_cache* c) {
     const uint32_t dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
     const size_t few = blocks * 2 * (16 * (size_t)(dp + 2)) * sizeof(float), many = prompt_partial_bytes(c->head_dim);
+    static_assert(2 * 512 * kMaxAttnBlocksPerSm * sizeof(uint32_t) <= ROOMIE_KV_WORKSPACE_ZEROED, "counters of up to 512 SMs");
     const size_t bytes = 2 * blocks * sizeof(uint32_t) + 256 + (few > many ? few : many);
     return (bytes + 255) / 256 * 256;
 }

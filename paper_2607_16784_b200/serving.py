@@ -176,7 +176,9 @@ class KVCache:
 
     def workspace(self):
         """Device scratch for the calls that take one; keep it and pass it to each of them."""
-        return torch.zeros(self._bytes, dtype=torch.uint8, device=self.k.device)
+        scratch = torch.empty(self._bytes, dtype=torch.uint8, device=self.k.device)
+        scratch[:16384].zero_()                          # ROOMIE_KV_WORKSPACE_ZEROED
+        return scratch
 
     def status_flags(self) -> int:
         """Synchronises and returns the sticky ROOMIE_FLAG_KV_* bits."""

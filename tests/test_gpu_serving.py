@@ -788,3 +788,17 @@ def test_serving_step_and_its_profile(torch, rm):
         for _ in range(4):
             rm.kv_free(cache, [0])
     assert len(few) == 2
+
+
+def test_example_runs(torch, rm):
+    """The example's steps: shared pages after the fork, half of them given back, finite results, a GPU for the model."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serving_step.py")
+    spec = importlib.util.spec_from_file_location("serving_step", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    launches, out, gpu = example.main(["--seqs", "3", "--prompt", "130", "--steps", "4", "--beams", "2"])
+    assert torch.isfinite(out).all() and out.shape == (6, 32, 128) and 0 <= gpu < 16
+    assert {"kv_reserve", "kv_append", "kv_attention", "kv_fork_plan", "kv_fork_move", "kv_free", "kv_compact_plan",
+            "kv_compact_move"} <= {r["name"] for r in launches}
