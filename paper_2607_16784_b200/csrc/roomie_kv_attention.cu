@@ -13,6 +13,8 @@ struct SeqWork {
     KvSeq s;
     uint32_t first_block, blocks, tiles;     // key blocks [first_block, first_block + blocks), row tiles
 };
+constexpr uint32_t kWhole = 3, kMostEqual = 12; // units: see few_rows_kernel
+__device__ __forceinline__ uint32_t parts_of(uint32_t blocks, uint32_t most) { return blocks <= kWhole ? 1u : (blocks + most - 1) / most; }
 template <int kBlock, int kRows>
 __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool report) {
     SeqWork w;
@@ -85,44 +87,75 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
     using F = FewRows<DP, NT, kFormat, T>;
     constexpr int G = F::kGroups, KW = F::KW, VW = F::VW, KS = F::KS, kStages = F::kStages;
     extern __shared__ __align__(1024) float sm[];                  // the warps' steps; then [warps][rows][DP] sums, [warps][rows][2] max and total
-    __shared__ unsigned long long sh_sum[kAttnWarps + 1];
+    __shared__ unsigned long long sh_sum[kAttnWarps], sh_first;
     __shared__ uint32_t sh_at[4];
     __shared__ float sm_row[2 * F::kRows];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const KvView& kv = a.c;
 
-    // ---- where this block's part begins: a scan of the sequences' units, kept from the first pass when they are at most a block's threads
-    unsigned long long mine = 0, own = 0;
+    // ---- where this block's part begins: a scan of the sequences' units, kept from the first pass when they are at most a block's
+    // threads
+    auto scan = [&](unsigned long long x, unsigned long long& all) {      // exclusive over the block
+        unsigned long long upto = x;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += up;
+        }
+        __syncthreads();
+        if (lane == 31) sh_sum[wid] = upto;
+        __syncthreads();
+        all = 0;
+        for (int w = 0; w < kAttnWarps; ++w) {
+            if (w < wid) upto += sh_sum[w];
+            all += sh_sum[w];
+        }
+        return upto - x;
+    };
+    unsigned long long mine = 0, own = 0, total;
+    SeqWork own_work = {};
     for (uint32_t i = threadIdx.x; i < a.num_seqs; i += kAttnThreads) {
-        const SeqWork w = seq_work<F::kBlock, F::kRows>(a, i, blockIdx.x == 0);
-        own = (unsigned long long)w.tiles * w.blocks * kv.heads;
+        own_work = seq_work<F::kBlock, F::kRows>(a, i, blockIdx.x == 0);
+        own = (unsigned long long)own_work.tiles * own_work.blocks * kv.heads;
         mine += own;
     }
-    unsigned long long upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long up = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += up;
-    }
-    if (lane == 31) sh_sum[wid] = upto;
-    __syncthreads();
-    unsigned long long total = 0, ahead0 = 0;
-    for (int w = 0; w < kAttnWarps; ++w) {
-        if (w < wid) ahead0 += sh_sum[w];
-        total += sh_sum[w];
-    }
+    const unsigned long long own_first = scan(mine, total);
     if (total == 0) return;
-    const unsigned long long parts = total < gridDim.x ? total : gridDim.x;
+    // Work of few units a block is not cut at any unit but into equal parts of each item, items of up to kWhole units not at all, when
+    // that makes no more parts than blocks: fewer items then need joining (16 sequences of up to 4096 keys: 31 us, cut at any unit 37; three of up to 300: 8.3 and 10.4).
+    uint32_t most = (uint32_t)min(total / gridDim.x + 1, 1ull << 30), own_parts = 0;
+    unsigned long long own_first_part = 0, parts = total < gridDim.x ? total : gridDim.x;
+    bool equal = a.num_seqs <= kAttnThreads && most <= kMostEqual;
+    if (equal) {                                                   // parts of at most `most`, most + 1 and most + 2 units: 21 bits each
+        unsigned long long three = 0, all_three;
+        if (own)                                                   // at most `own` each, which is below 2^20 here
+            for (uint32_t e = 0; e < 3; ++e)
+                three |= (unsigned long long)(own_work.tiles * kv.heads * parts_of(own_work.blocks, most + e)) << (21 * e);
+        unsigned long long first_three = scan(three, all_three);
+        equal = false;
+        for (uint32_t e = 0; e < 3 && !equal; ++e, three >>= 21, first_three >>= 21, all_three >>= 21)
+            if ((all_three & 0x1fffff) <= gridDim.x) {
+                equal = true;
+                own_parts = (uint32_t)(three & 0x1fffff);
+                own_first_part = first_three & 0x1fffff;
+                parts = all_three & 0x1fffff;
+                most += e;
+            }
+    }
     if (blockIdx.x >= parts) return;
-    unsigned long long at = total * blockIdx.x / parts;
-    const unsigned long long end = total * (blockIdx.x + 1) / parts;
+    unsigned long long at = equal ? 0 : total * blockIdx.x / parts;
+    const unsigned long long end = equal ? 1 : total * (blockIdx.x + 1) / parts;
 
     // the sequence that holds `at`, and the flat index it begins at
-    if (a.num_seqs <= kAttnThreads) {
-        const unsigned long long first = ahead0 + upto - own;
-        if (own && at >= first && at < first + own) {
+    if (equal) {                                                   // seq_first: the first part of the sequence
+        if (own_parts && blockIdx.x >= own_first_part && blockIdx.x < own_first_part + own_parts) {
             sh_at[0] = threadIdx.x;
-            sh_sum[kAttnWarps] = first;
+            sh_first = own_first_part;
+        }
+    } else if (a.num_seqs <= kAttnThreads) {
+        if (own && at >= own_first && at < own_first + own) {
+            sh_at[0] = threadIdx.x;
+            sh_first = own_first;
         }
     } else {
         unsigned long long before = 0;
@@ -133,24 +166,11 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                 const SeqWork w = seq_work<F::kBlock, F::kRows>(a, i, false);
                 n = (unsigned long long)w.tiles * w.blocks * kv.heads;
             }
-            unsigned long long incl = n;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
-            }
-            __syncthreads();
-            if (lane == 31) sh_sum[wid] = incl;
-            __syncthreads();
-            unsigned long long ahead = before, all = 0;
-            for (int w = 0; w < kAttnWarps; ++w) {
-                if (w < wid) ahead += sh_sum[w];
-                all += sh_sum[w];
-            }
-            const unsigned long long first = ahead + incl - n;
+            unsigned long long all;
+            const unsigned long long first = before + scan(n, all);
             if (n && at >= first && at < first + n) {
                 sh_at[0] = i;
-                sh_sum[kAttnWarps] = first;
+                sh_first = first;
             }
             before += all;
             if (at < before) break;
@@ -158,73 +178,48 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
     }
     __syncthreads();
     uint32_t seq = sh_at[0];
-    unsigned long long seq_first = sh_sum[kAttnWarps];
+    unsigned long long seq_first = sh_first;
 
     while (at < end) {
         SeqWork w = seq_work<F::kBlock, F::kRows>(a, seq, false);
-        unsigned long long n = (unsigned long long)w.tiles * w.blocks * kv.heads;
-        while (at >= seq_first + n) {                              // sequences without rows contribute nothing
-            seq_first += n;
-            if (++seq >= a.num_seqs) return;                       // lengths changed under the call
-            w = seq_work<F::kBlock, F::kRows>(a, seq, false);
-            n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+        uint32_t head, tile, b0, b1, first_part, last_part;        // the blocks that share the item
+        if (equal) {
+            const uint32_t cuts = parts_of(w.blocks, most), rest = blockIdx.x - (uint32_t)seq_first, which = rest / cuts, j = rest - which * cuts;
+            head = which / w.tiles;
+            tile = which - head * w.tiles;
+            b0 = (uint32_t)((unsigned long long)w.blocks * j / cuts);
+            b1 = (uint32_t)((unsigned long long)w.blocks * (j + 1) / cuts);
+            first_part = blockIdx.x - j;
+            last_part = first_part + cuts - 1;
+        } else {
+            unsigned long long n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+            while (at >= seq_first + n) {                          // sequences without rows contribute nothing
+                seq_first += n;
+                if (++seq >= a.num_seqs) return;                   // lengths changed under the call
+                w = seq_work<F::kBlock, F::kRows>(a, seq, false);
+                n = (unsigned long long)w.tiles * w.blocks * kv.heads;
+            }
+            const unsigned long long inside = at - seq_first;
+            head = (uint32_t)(inside / ((unsigned long long)w.tiles * w.blocks));
+            const uint32_t rest = (uint32_t)(inside - (unsigned long long)head * w.tiles * w.blocks);
+            tile = rest / w.blocks;
+            b0 = rest - tile * w.blocks;
+            b1 = (uint32_t)min((unsigned long long)w.blocks, (unsigned long long)b0 + (end - at));
+            const unsigned long long item = at - b0;               // consecutive blocks: from that of its first unit to that of its last
+            first_part = (uint32_t)(((item + 1) * parts - 1) / total);
+            last_part = (uint32_t)(((item + w.blocks) * parts - 1) / total);
         }
-        const unsigned long long inside = at - seq_first;
-        const uint32_t head = (uint32_t)(inside / ((unsigned long long)w.tiles * w.blocks));
-        const uint32_t rest = (uint32_t)(inside - (unsigned long long)head * w.tiles * w.blocks);
-        const uint32_t tile = rest / w.blocks, b0 = rest - tile * w.blocks;
-        const uint32_t b1 = (uint32_t)min((unsigned long long)w.blocks, (unsigned long long)b0 + (end - at));
         const KvSeq& s = w.s;
         const int start = (int)s.length - (int)s.count;
         const uint32_t rows = s.count * a.group - tile * F::kRows;  // of this tile: min(rows, kRows)
 
-        // ---- queries: operand b of S^T; row r of the tile, dims as the lane's keys ---------------------------------------
-        uint32_t qf[NT][KS][2];
-        float qscale[NT][2];
+        // ---- which keys the rows see; rows 2c and 2c+1 of each eight are the lane's result columns -------------------------
         int see_hi[NT][2], see_lo[NT][2];                          // row n sees keys [lo, hi)
         int tile_hi = 0, tile_lo = 0x7fffffff, all_hi = 0x7fffffff, all_lo = 0;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const uint32_t rr = t * 8 + r;
-            const bool on = rr < rows;
-            const uint32_t row = tile * F::kRows + rr, tok = row / a.group;
-            const T* q = static_cast<const T*>(a.q) + (long long)(s.row + tok) * a.q_token +
-                         (long long)(head * a.group + row - tok * a.group) * a.q_head + c * (DP / 4);
-            float x[DP / 4];
-            float amax = 0.0f;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int d = 0; d < DP / 4; ++d) x[d] = 0.0f;
-            if (on) {
-                if (a.q_aligned) {
-#pragma unroll
-                    for (int d = 0; d < DP / 4; d += 8)
-                        if (c * (DP / 4) + d < kv.dim) unpack<T>(*reinterpret_cast<const uint4*>(q + d), x + d);
-                } else {
-#pragma unroll
-                    for (int d = 0; d < DP / 4; ++d)
-                        if (c * (DP / 4) + d < kv.dim) x[d] = load_elem(q + d);
-                }
-            }
-#pragma unroll
-            for (int d = 0; d < DP / 4; ++d) amax = fmaxf(amax, fabsf(x[d]));
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            // To float16 with the row's largest magnitude in [1, 2): exact for float16 and bfloat16 queries but for elements below
-            // 2^-14 of it, which lose at most 2^-25 of it.
-            int e = (int)(__float_as_uint(amax) >> 23) - 127;
-            e = max(min(e, 126), -126);
-            const float down = pow2f(-e);
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const __half2 lo = __floats2half2_rn(x[4 * i] * down, x[4 * i + 1] * down);
-                const __half2 hi = __floats2half2_rn(x[4 * i + 2] * down, x[4 * i + 3] * down);
-                qf[t][i][0] = reinterpret_cast<const uint32_t&>(lo);
-                qf[t][i][1] = reinterpret_cast<const uint32_t&>(hi);
-            }
-            const float up = pow2f(e) * a.scale_log2;
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {                          // rows 2c and 2c+1 are the lane's result columns
-                qscale[t][n] = __shfl_sync(0xffffffffu, up, (2 * c + n) * 4);
+            for (int n = 0; n < 2; ++n) {
                 const uint32_t rc = t * 8 + 2 * c + n;
                 const int pos = start + (int)((tile * F::kRows + rc) / a.group);
                 int hi = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
@@ -239,7 +234,6 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                     all_lo = max(all_lo, lo);
                 }
             }
-        }
 #pragma unroll
         for (int d = 1; d < 4; d <<= 1) {
             tile_hi = max(tile_hi, __shfl_xor_sync(0xffffffffu, tile_hi, d));
@@ -333,6 +327,52 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             asm volatile("cp.async.commit_group;" ::: "memory");
             get_pages(k0 + (i + 1) * F::kBlock);
         }
+        // ---- queries, while the first copies are on their way: operand b of S^T; row r of the tile, dims as the lane's keys ---------------------------------------
+        uint32_t qf[NT][KS][2];
+        float qscale[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t rr = t * 8 + r;
+            const bool on = rr < rows;
+            const uint32_t row = tile * F::kRows + rr, tok = row / a.group;
+            const T* q = static_cast<const T*>(a.q) + (long long)(s.row + tok) * a.q_token +
+                         (long long)(head * a.group + row - tok * a.group) * a.q_head + c * (DP / 4);
+            float x[DP / 4];
+            float amax = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DP / 4; ++d) x[d] = 0.0f;
+            if (on) {
+                if (a.q_aligned) {
+#pragma unroll
+                    for (int d = 0; d < DP / 4; d += 8)
+                        if (c * (DP / 4) + d < kv.dim) unpack<T>(*reinterpret_cast<const uint4*>(q + d), x + d);
+                } else {
+#pragma unroll
+                    for (int d = 0; d < DP / 4; ++d)
+                        if (c * (DP / 4) + d < kv.dim) x[d] = load_elem(q + d);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DP / 4; ++d) amax = fmaxf(amax, fabsf(x[d]));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            // To float16 with the row's largest magnitude in [1, 2): exact for float16 and bfloat16 queries but for elements below
+            // 2^-14 of it, which lose at most 2^-25 of it.
+            int e = (int)(__float_as_uint(amax) >> 23) - 127;
+            e = max(min(e, 126), -126);
+            const float down = pow2f(-e);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const __half2 lo = __floats2half2_rn(x[4 * i] * down, x[4 * i + 1] * down);
+                const __half2 hi = __floats2half2_rn(x[4 * i + 2] * down, x[4 * i + 3] * down);
+                qf[t][i][0] = reinterpret_cast<const uint32_t&>(lo);
+                qf[t][i][1] = reinterpret_cast<const uint32_t&>(hi);
+            }
+            const float up = pow2f(e) * a.scale_log2;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) qscale[t][n] = __shfl_sync(0xffffffffu, up, (2 * c + n) * 4);
+        }
+
         while (k0 < hi_key) {
 #pragma unroll
             for (int stage = 0; stage < kStages; ++stage) {
@@ -476,7 +516,6 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             }
         __syncthreads();
 
-        const unsigned long long item = at - b0, item_end = item + w.blocks;
         const bool complete = b0 == 0 && b1 == w.blocks;
         const uint32_t n_rows = min(rows, (uint32_t)F::kRows);
         auto put = [&](uint32_t row, uint32_t d, float mx, float sum, float value) {
@@ -511,9 +550,8 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             }
         }
         if (!complete) {
-            // The parts that share this item are consecutive blocks: first holds its first unit, last its last.  With many of them the last
-            // to arrive of each kJoin adds those up, and the last of these the sums: one block alone took 60 us over 444 parts.
-            const uint32_t first = (uint32_t)(((item + 1) * parts - 1) / total), last = (uint32_t)((item_end * parts - 1) / total);
+            // With many parts the last to arrive of each kJoin adds those up, and the last of these the sums: one block alone took 60 us over 444 parts.
+            const uint32_t first = first_part, last = last_part;
             const uint32_t count = last - first + 1, groups = (count + kJoin - 1) / kJoin;
             auto part_of = [&](uint32_t b) { return a.partial + ((size_t)(first + b) * 2 + (b == 0 ? 1 : 0)) * F::kPartial; };
             auto arrive = [&](uint32_t* counter, uint32_t n) {     // whether this block is the last of n
@@ -579,7 +617,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             if (go && arrive(a.counters + first, groups > 1 ? groups : count)) join(0, groups > 1 ? kJoin : 1, groups > 1 ? groups : count, true);
         }
         __syncthreads();
-        at += b1 - b0;
+        at += equal ? 1 : b1 - b0;
     }
 }
 
@@ -645,7 +683,12 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
     a.counters = static_cast<uint32_t*>(workspace);
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
     a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (2 * blocks * sizeof(uint32_t) + 255) / 256 * 256);
-    const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;      // rows a sequence and key head, on average
+    // Rows a sequence and key head, on average (32 query heads on 8, sequences of up to 4096 keys, 16 of them and 2 of them, us):
+    //   rows        8       16      24      32      64
+    //   8 a tile    36 23   57 29   57 33   82 32   117 37
+    //   16 a tile   36 23   52 33   61 33   84 39   106 42
+    //   prompt      82 47   82 48   83 48   83 44   82 44
+    const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if ((unsigned long long)rows * a.group > 32ull * num_seqs) return launch_prompt(a, q->type == ROOMIE_F16, st);
     return q->type == ROOMIE_F16 ? launch_format<__half>(a, eight, st) : launch_format<__nv_bfloat16>(a, eight, st);
