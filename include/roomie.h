@@ -381,7 +381,7 @@ int roomie_profile_walk_ms(float *total_ms /* host */, uint32_t *launches /* hos
  * only enqueued.  Data-dependent errors set sticky bits in the cache's `status` word and skip the access.
  * ==================================================================================================== */
 
-/* sticky bits of roomie_kv_cache.status */
+/* sticky bits of roomie_kv_cache.status (beside ROOMIE_FLAG_WAIT_TIMEOUT) */
 #define ROOMIE_FLAG_KV_PAGE 16u       /* a page id outside [0, num_pages) where a page was needed; or a page whose
                                          reference count is not 1 was appended to, or freed below 0        */
 #define ROOMIE_FLAG_KV_SEQUENCE 32u   /* a sequence index, length or row offset outside its range, a child that is
@@ -451,7 +451,8 @@ typedef struct roomie_kv_cache {
 } roomie_kv_cache;
 
 /* Device scratch for the calls below that take a workspace: enough for any of them on this cache, 256-byte aligned.  Its first
- * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them so.  0 on invalid arguments. */
+ * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them so, unless ROOMIE_FLAG_WAIT_TIMEOUT shows up in the
+ * cache's status: zero them again then.  0 on invalid arguments. */
 #define ROOMIE_KV_WORKSPACE_ZEROED 16384u
 size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
 

@@ -6,11 +6,17 @@
 //   S = q K^T        both operands in shared memory, float16; S in tensor memory, 64 columns a half
 //   softmax          a thread owns a row: reads S, writes the probabilities as float16 over the columns it has read
 //   o += p V         p from tensor memory, V from shared memory, o in tensor memory
-// While a tile's softmax is at one half, its products for the other half run (o for the half before, then S for the half after), and
-// warpgroups 0 and 1 are the softmax of tiles 0 and 1.  (With halves of 128 keys the softmax waited for its own products: 4750 cycles a
-// step of 128 keys and two tiles, where the products alone take 2048.)  Warpgroups 2 and 3
-// turn the codes of keys and of values into float16 operands (the scales stay out of them); in warpgroup 4 a warp for
-// each tile issues its products and one looks up pages and scales, some steps ahead.
+// While a tile's softmax is at one half, its products for the other half run (o for the half before, then S for the half after).
+// Warpgroups 0 and 1 are the softmax of tiles 0 and 1, warpgroups 2 and 3 turn the codes of keys and of values into float16 operands
+// (the scales stay out of them); in warpgroup 4 a warp for each tile issues its products and one looks up pages and scales, some steps
+// ahead.  The flat order of all (sequence, head, tile, key block) is cut into one equal share a block.
+//
+// What bounds it: chunks of 1024 tokens over up to 8192 (32 query heads on 8, 128 dims) take 407 us, 798 TFLOP/s of the 1666 that a
+// plain matrix product reaches.  A step of 128 keys and two tiles takes some 4400 cycles, where the products have 2048, the
+// exponentials as many on the special-function units, and the operands' way through shared memory 2600: none of them is full, the
+// chain product - softmax - product of a tile is what is left, and tensor memory (512 columns: two S and two o) has no room for a third
+// tile to hide it behind.  Tried and slower: a quarter of the exponentials as polynomials (465 us against 464), tiles that take turns
+// at the softmax (544 against 475), two threads a row (538 against 487).
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
 // Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M the running maximum of s + log2 vs, is what multiplies
@@ -524,6 +530,9 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uin
                 __syncwarp();
             }
             if (h < halves) {
+                // S takes the columns that p was read from: products of different shapes are not counted on to end in order (head sizes to
+                // 128: no cost; 256, with one tile: 11 %)
+                if (h >= 2 && !warp_wait(&sh.o_full[t][side], now & 1, sh)) return;
                 if (h >= 2 && side == 0 && !warp_wait(&sh.k_full[stage], (next / P::kStages) & 1, sh)) return;
                 tc_fence_after();
                 const uint32_t k = k0 + ((stage * P::kOperand + side * 8192) >> 4);
@@ -759,7 +768,8 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4*>(part + ((size_t)(8 * c + e / 4) * P::kRows + pr) * 4) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                        *reinterpret_cast<uint4*>(part + ((size_t)(8 * c + e / 4) * P::kRows + pr) * 4) =
+                            make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 }
             }
             if (complete) {

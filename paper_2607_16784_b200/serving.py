@@ -187,7 +187,7 @@ class KVCache:
     def check(self):
         f = self.status_flags()
         if f:
-            names = [n for b, n in ((16, "KV_PAGE"), (32, "KV_SEQUENCE"), (64, "KV_NONFINITE"), (128, "KV_FULL")) if f & b]
+            names = [n for b, n in ((8, "WAIT_TIMEOUT"), (16, "KV_PAGE"), (32, "KV_SEQUENCE"), (64, "KV_NONFINITE"), (128, "KV_FULL")) if f & b]
             raise RoomieError("cache status flags set: " + "|".join(names))
 
 

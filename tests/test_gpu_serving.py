@@ -310,6 +310,52 @@ def test_attention_split_key_axis_and_order(torch, rm):
     check_attention(torch, rm, cache, [1, 0], [3, 2], 4, "bf16", workspace=ws)
 
 
+@pytest.mark.parametrize("most_new,count", [(1, 300), (3, 150), (40, 50)])
+def test_attention_many_sequences(torch, rm, most_new, count):
+    """More sequences than a block has threads (or warps), of very different lengths, some empty, some without new rows."""
+    rng = np.random.default_rng(count)
+    lengths = [int(x) for x in np.where(rng.random(count) < 0.1, 0, np.exp(rng.uniform(0, np.log(900), count)).astype(int))]
+    news = [1] * count if most_new == 1 else [int(x) for x in rng.integers(0, most_new + 1, count)]
+    cache = make_cache(torch, rm, lengths, page=16, dim=64, heads=1, seed=count)
+    ws = cache.workspace()
+    order = [int(s) for s in rng.permutation(count)]
+    for _ in range(2):
+        check_attention(torch, rm, cache, order, [news[s] for s in order], 4, "f16", workspace=ws, offsets=most_new > 1)
+
+
+@pytest.mark.parametrize("seqs,length", [(1, 40000), (1, 700), (2, 130), (7, 2600), (40, 390)])
+def test_attention_cuts_of_the_key_axis(torch, rm, seqs, length):
+    """Items left whole, cut into equal parts, cut at any unit and joined in one and in two levels."""
+    cache = make_cache(torch, rm, [max(1, length - 37 * s) for s in range(seqs)], page=64, dim=128, heads=1, seed=seqs)
+    ws = cache.workspace()
+    for q_heads in (8, 16):
+        for window in (0, length // 2):
+            check_attention(torch, rm, cache, list(range(seqs)), [1] * seqs, q_heads, "f16", workspace=ws, window=window)
+
+
+def test_append_many_sequences(torch, rm):
+    """More sequences than a block has threads; some bring nothing."""
+    rng = np.random.default_rng(8)
+    count = 700
+    lengths = [int(x) for x in rng.integers(1, 40, count)]
+    news = [int(min(n, x)) for n, x in zip(lengths, rng.integers(0, 4, count))]
+    cache = make_cache(torch, rm, lengths, page=16, dim=16, heads=1, seed=3, garbage=False)
+    check_append(torch, rm, cache, list(range(count)), news, rope=rm.RopeTable(16), q_heads=2)
+    assert cache.status_flags() == 0
+
+
+def test_append_many_queries(torch, rm):
+    """Enough query bytes for a launch of their own, in place and not, rows of no sequence passed on."""
+    cache = make_cache(torch, rm, [1500, 700], page=64, dim=128, heads=2, seed=6, garbage=False)
+    check_append(torch, rm, cache, [0, 1], [1400, 650], rope=rm.RopeTable(128), q_heads=16)
+    table, ids = rm.RopeTable(128, amplitude=2.0), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    k, q = torch.randn((2060, 2, 128), device="cuda").half(), torch.randn((2060, 16, 128), device="cuda").half()
+    rows = torch.tensor([5, 1400, 2050], dtype=torch.int32, device="cuda")                # five rows before, ten behind
+    want = rm.kv_append(cache, ids, k, k, rows, rope=table, q=q)
+    assert torch.equal(want[:5], q[:5]) and torch.equal(want[2050:], q[2050:]) and not torch.equal(want[5], q[5])
+    assert rm.kv_append(cache, ids, k, k, rows, rope=table, q=q, q_out=q) is q and torch.equal(q, want)
+
+
 def test_attention_extremes(torch, rm):
     """Large and tiny queries (float16 operands are normalised a row), peaked and flat softmax, zero queries, a given scale."""
     cache = make_cache(torch, rm, [200, 90], page=32, dim=64, seed=9)
