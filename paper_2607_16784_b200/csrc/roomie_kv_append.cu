@@ -272,7 +272,6 @@ __device__ void append_queries(const AppendArgs& a, unsigned long long i) {
         }
         s = lo;
     }
-    RopeView rope = a.rope;
     int32_t position = 0;
     bool turned = false;
     if (s < a.num_seqs) {
@@ -280,8 +279,7 @@ __device__ void append_queries(const AppendArgs& a, unsigned long long i) {
         turned = row >= q.row && row < q.row + q.count && q.count <= q.length;
         if (turned) position = (int32_t)(q.start + (row - q.row));
     }
-    if (!turned) rope.amplitude = 1.0f;                                   // a row of no sequence is passed on as it is (position 0)
-    rope_heads<T, kV, kPairs, kV == 1 ? 1 : 2>(a.q, rope, row, position, false, unit, group, a.q_groups, a.q_heads);
+    rope_heads<T, kV, kPairs, kV == 1 ? 1 : 2>(a.q, a.rope, row, position, false, unit, group, a.q_groups, a.q_heads, !turned);
 }
 
 // Blocks [0, 2 * kv_blocks): page j of the call, keys (even) and values (odd); the rest: queries.  One launch for the three, because

@@ -20,10 +20,10 @@ struct HeadRows {            // element strides
 // What one thread does: unit `unit` of heads head, head + step, ... of one token.  A unit is kV elements; a row has rot/(2*kV) pairs of
 // units that are rotated and, unless it is done in place, (dim - rot)/kV units that are copied.  kV = 16 bytes, or 1 when some row is
 // not 16-byte aligned or the parts do not divide into such units.  The thread works out its own kV cosines and sines (some 25
-// instructions each) once for all its heads: nothing is shared, nobody waits.
+// instructions each) once for all its heads: nothing is shared, nobody waits.  `as_is`: the row is copied, infinities and all.
 template <class T, int kV, bool kPairs, int kUnroll>
 __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& rope, uint32_t token, int32_t position, bool inverse,
-                                           uint32_t unit, uint32_t head, uint32_t step, uint32_t heads) {
+                                           uint32_t unit, uint32_t head, uint32_t step, uint32_t heads, bool as_is = false) {
     const uint32_t half = rope.rot / 2, n_rot = half / kV;
     using Raw = typename std::conditional<kV == 1, T, uint4>::type;
     const bool turn = unit < n_rot;
@@ -51,8 +51,9 @@ __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& r
         for (int u = 0; u < kUnroll; ++u) {
             if (h + u * step >= heads) break;
             T* p = y + (long long)(u * step) * io.y_head;
-            if (!turn) {
+            if (!turn || as_is) {
                 *reinterpret_cast<Raw*>(p + a) = ra[u];
+                if (turn) *reinterpret_cast<Raw*>(p + b) = rb[u];
                 continue;
             }
             if constexpr (kV == 1) {

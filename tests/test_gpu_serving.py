@@ -356,6 +356,21 @@ def test_append_many_queries(torch, rm):
     assert rm.kv_append(cache, ids, k, k, rows, rope=table, q=q, q_out=q) is q and torch.equal(q, want)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("turned", [64, 6])
+def test_append_passes_rows_of_no_sequence_on(torch, rm, interleaved, turned):
+    """Bit for bit, infinities, NaN and negative zeros too."""
+    dim = 64
+    cache = make_cache(torch, rm, [20], page=16, dim=dim, heads=1, seed=2, garbage=False)
+    table, ids = rm.RopeTable(turned, interleaved=interleaved), torch.tensor([0], dtype=torch.int32, device="cuda")
+    k, q = torch.ones((6, 1, dim), device="cuda").half(), torch.randn((6, 4, dim), device="cuda").half()
+    q[0, :, ::3], q[5, :, 1::3], q[5, 0, 0], q[0, 1, 2] = float("inf"), -float("inf"), float("nan"), -0.0
+    got = rm.kv_append(cache, ids, k, k, torch.tensor([1, 4], dtype=torch.int32, device="cuda"), rope=table, q=q)
+    for row in (0, 4, 5):
+        assert torch.equal(got[row].view(torch.int16), q[row].view(torch.int16))
+    assert torch.isfinite(got[1:4]).all() and cache.status_flags() == 0
+
+
 def test_attention_extremes(torch, rm):
     """Large and tiny queries (float16 operands are normalised a row), peaked and flat softmax, zero queries, a given scale."""
     cache = make_cache(torch, rm, [200, 90], page=32, dim=64, seed=9)
