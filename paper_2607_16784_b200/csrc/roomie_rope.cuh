@@ -20,10 +20,10 @@ struct HeadRows {            // element strides
 // What one thread does: unit `unit` of heads head, head + step, ... of one token.  A unit is kV elements; a row has rot/(2*kV) pairs of
 // units that are rotated and, unless it is done in place, (dim - rot)/kV units that are copied.  kV = 16 bytes, or 1 when some row is
 // not 16-byte aligned or the parts do not divide into such units.  The thread works out its own kV cosines and sines (some 25
-// instructions each) once for all its heads: nothing is shared, nobody waits.  `as_is`: the row is copied, infinities and all.
+// instructions each) once for all its heads: nothing is shared, nobody waits.
 template <class T, int kV, bool kPairs, int kUnroll>
 __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& rope, uint32_t token, int32_t position, bool inverse,
-                                           uint32_t unit, uint32_t head, uint32_t step, uint32_t heads, bool as_is = false) {
+                                           uint32_t unit, uint32_t head, uint32_t step, uint32_t heads) {
     const uint32_t half = rope.rot / 2, n_rot = half / kV;
     using Raw = typename std::conditional<kV == 1, T, uint4>::type;
     const bool turn = unit < n_rot;
@@ -51,9 +51,8 @@ __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& r
         for (int u = 0; u < kUnroll; ++u) {
             if (h + u * step >= heads) break;
             T* p = y + (long long)(u * step) * io.y_head;
-            if (!turn || as_is) {
+            if (!turn) {
                 *reinterpret_cast<Raw*>(p + a) = ra[u];
-                if (turn) *reinterpret_cast<Raw*>(p + b) = rb[u];
                 continue;
             }
             if constexpr (kV == 1) {
@@ -80,6 +79,23 @@ __device__ __forceinline__ void rope_heads(const HeadRows& io, const RopeView& r
         }
         x += (long long)(step * kUnroll) * io.x_head;
         y += (long long)(step * kUnroll) * io.y_head;
+    }
+}
+
+// The same units passed on as they are, infinities and all.
+template <class T, int kV, bool kPairs>
+__device__ __forceinline__ void rope_copy(const HeadRows& io, const RopeView& rope, uint32_t token, uint32_t unit, uint32_t head, uint32_t step,
+                                       uint32_t heads) {
+    const uint32_t half = rope.rot / 2, n_rot = half / kV;
+    using Raw = typename std::conditional<kV == 1, T, uint4>::type;
+    const bool turn = unit < n_rot;
+    const uint32_t a = !turn ? rope.rot + (unit - n_rot) * kV : kPairs ? 2 * unit * kV : unit * kV;
+    const uint32_t b = kPairs ? a + kV : a + half;
+    for (uint32_t h = head; h < heads; h += step) {
+        const T* x = static_cast<const T*>(io.x) + token * io.x_token + h * io.x_head;
+        T* y = static_cast<T*>(io.y) + token * io.y_token + h * io.y_head;
+        *reinterpret_cast<Raw*>(y + a) = *reinterpret_cast<const Raw*>(x + a);
+        if (turn) *reinterpret_cast<Raw*>(y + b) = *reinterpret_cast<const Raw*>(x + b);
     }
 }
 
