@@ -451,8 +451,8 @@ typedef struct roomie_kv_cache {
 } roomie_kv_cache;
 
 /* Device scratch for the calls below that take a workspace: enough for any of them on this cache, 256-byte aligned.  Its first
- * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them so, unless ROOMIE_FLAG_WAIT_TIMEOUT shows up in the
- * cache's status: zero them again then.  0 on invalid arguments. */
+ * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them
+ * so, unless ROOMIE_FLAG_WAIT_TIMEOUT shows up in the cache's status: zero them again then.  0 on invalid arguments. */
 #define ROOMIE_KV_WORKSPACE_ZEROED 16384u
 size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
 
@@ -464,7 +464,7 @@ size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
  * so that a scale that has to grow while a page fills moves e4m3 codes without rounding them a second time; int8 pays
  * up to one bit for it); the scale of a page that holds earlier tokens never shrinks, and its earlier codes are
  * rescaled when it grows.  Float32 arithmetic on values of any ROOMIE_ type, rounded once to the code (nearest even).
- * q_out may be q (same strides).  Rows that belong to no sequence are not stored and their queries are passed on unrotated.
+ * q_out may be q (same strides).  A call names a row of the page table once.  Rows that belong to no sequence are not stored and their queries are passed on unrotated.
  * Errors: INVALID_ARG, CUDA. */
 int roomie_kv_append(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs,
                      const int32_t *q_offset, uint32_t rows, const roomie_rows *k, const roomie_rows *v,

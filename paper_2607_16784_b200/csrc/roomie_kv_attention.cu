@@ -36,9 +36,10 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
 // [r*DP/8, +DP/8) for its result rows r: both are whole 16-byte reads of the codes as they are stored.
 //
 // Every warp works for itself: it has kStages steps of keys and values under way to its own part of shared memory by asynchronous
-// copies (64 sequences of up to 16384 tokens in int8: 232 us, 5650 GB/s; with one step ahead in registers 297).  A block walks a contiguous part of the flat order; its
-// warps take the 16*kGroups-key steps in turn and meet at each (sequence, head, tile).  A part that does not hold all of a (sequence,
-// head, tile) leaves its sums in the workspace, and the last part to arrive adds them in order.
+// copies (64 sequences of up to 16384 tokens in int8, 1.31 GB: 231 to 258 us by how the lengths fall, 5650 to 5090 GB/s; with one
+// step ahead in registers 297 where this takes 231).  A block walks a contiguous part of the flat order; its warps take the
+// 16*kGroups-key steps in turn and meet at each (sequence, head, tile).  A part that does not hold all of a (sequence, head, tile)
+// leaves its sums in the workspace, and the last part to arrive adds them in order.
 //
 // Scales: a page's key scale goes into the factor of the exponent's argument, its value scale vs into the exponent: the weights
 // exp2(s + log2 vs - m), m a maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs.

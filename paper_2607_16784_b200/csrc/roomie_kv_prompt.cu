@@ -11,7 +11,7 @@
 // (the scales stay out of them); in warpgroup 4 a warp for each tile issues its products and one looks up pages and scales, some steps
 // ahead.  The flat order of all (sequence, head, tile, key block) is cut into one equal share a block.
 //
-// What bounds it: chunks of 1024 tokens over up to 8192 (32 query heads on 8, 128 dims) take 407 us, 798 TFLOP/s of the 1666 that a
+// What bounds it: chunks of 1024 tokens over up to 8192 (32 query heads on 8, 128 dims) take 405 us, 801 TFLOP/s of the 1666 that a
 // plain matrix product reaches.  A step of 128 keys and two tiles takes some 4400 cycles, where the products have 2048, the
 // exponentials as many on the special-function units, and the operands' way through shared memory 2600: none of them is full, the
 // chain product - softmax - product of a tile is what is left, and tensor memory (512 columns: two S and two o) has no room for a third
