@@ -530,9 +530,9 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uin
                 __syncwarp();
             }
             if (h < halves) {
-                // S takes the columns that p was read from: products of different shapes are not counted on to end in order (head sizes to
-                // 128: no cost; 256, with one tile: 11 %)
-                if (h >= 2 && !warp_wait(&sh.o_full[t][side], now & 1, sh)) return;
+                // S takes the columns that p was read from, by a segment's first halves the last step's of the segment before: products of
+                // different shapes are not counted on to end in order (head sizes to 128: no cost; 256, with one tile: 11 %)
+                if (next && !warp_wait(&sh.o_full[t][side], now & 1, sh)) return;
                 if (h >= 2 && side == 0 && !warp_wait(&sh.k_full[stage], (next / P::kStages) & 1, sh)) return;
                 tc_fence_after();
                 const uint32_t k = k0 + ((stage * P::kOperand + side * 8192) >> 4);

@@ -296,6 +296,24 @@ def test_attention_prompts_repeat_bit_for_bit(torch, rm, dim, kv_heads, group):
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
 
 
+@pytest.mark.parametrize("dim,kv_heads,group", [(64, 4, 8), (128, 4, 8), (256, 3, 4)])
+def test_attention_prompts_of_many_short_segments(torch, rm, dim, kv_heads, group):
+    """Three or four (sequence, head, tile) segments of one to three steps for each block of the prompt kernel: where one ends and the
+    next begins, the next one's logits take the columns that the last products of the one before read."""
+    rng = np.random.default_rng(dim)
+    lengths = [int(x) for x in rng.integers(20, 300, 160)]
+    news = [int(min(n, x)) for n, x in zip(lengths, rng.integers(9, 30, 160))]
+    cache = make_cache(torch, rm, lengths, page=16, dim=dim, heads=kv_heads, seed=dim)
+    ws = cache.workspace()
+    first = check_attention(torch, rm, cache, list(range(160)), news, kv_heads * group, "bf16", workspace=ws)
+    rows = torch.tensor(np.concatenate([[0], np.cumsum(news)]).tolist(), dtype=torch.int32, device="cuda")
+    q = torch.from_numpy(np.random.default_rng(1).normal(size=(sum(news), kv_heads * group, dim))).to(torch.bfloat16).cuda()
+    ids = torch.arange(160, dtype=torch.int32, device="cuda")
+    for _ in range(40):
+        out, lse = rm.kv_attention(cache, ids, q, rows, workspace=ws)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
 def test_attention_split_key_axis_and_order(torch, rm):
     """Few rows over long contexts: the key axis is split over blocks and joined; the same call gives the same bits, and a batch's
     result does not depend on what was in the workspace's sums."""
