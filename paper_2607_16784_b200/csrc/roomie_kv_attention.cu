@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             for (int g = 0; g < G; ++g) {
                 const int k = k0 + 16 * g;
                 int32_t id = -1;
-                if (k < hi_key) {
+                if (k < hi_key && k + 16 > tile_lo) {
                     id = __ldg(table + (k >> kv.page_shift));
                     if ((uint32_t)id >= kv.num_pages) {
                         if (lane == 0) kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);

@@ -150,6 +150,7 @@ template <int kRows> __device__ __forceinline__ PromptSeq prompt_seq(const AttnA
 constexpr uint32_t kTileCost = 4;
 struct Blocks {
     uint32_t first, count;                          // key blocks that some row of the tile sees, at least one
+    uint32_t lo, hi;                                // no row sees a key outside [lo, hi)
 };
 template <int kRows> __device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const PromptSeq& p, uint32_t tile) {
     const uint32_t last_row = min((tile + 1) * kRows, p.rows) - 1;
@@ -159,6 +160,8 @@ template <int kRows> __device__ __forceinline__ Blocks tile_blocks(const AttnArg
     b.first = (uint32_t)lo / kKeys;
     const uint32_t end = ((uint32_t)hi + kKeys - 1) / kKeys;
     b.count = end > b.first ? end - b.first : 1u;
+    b.lo = (uint32_t)lo;
+    b.hi = (uint32_t)hi;
     return b;
 }
 template <int kRows> __device__ __forceinline__ unsigned long long seq_blocks(const AttnArgs& a, const PromptSeq& p, int lane) {
@@ -177,6 +180,7 @@ struct Walk {                                       // where in the flat order a
 struct Segment {                                    // a run of blocks of one (sequence, head, tile)
     PromptSeq p;
     uint32_t head, tile, first, count, b0, b1;      // blocks first + [b0, b1) of count
+    uint32_t lo, hi;                                // keys that some row sees
     unsigned long long item;                        // flat index of the tile's first block
     uint32_t rows;                                  // of the tile
 };
@@ -193,6 +197,8 @@ template <int kRows> __device__ __forceinline__ bool next_segment(const AttnArgs
     s.tile = w.tile;
     s.first = b.first;
     s.count = b.count;
+    s.lo = b.lo;
+    s.hi = b.hi;
     s.b0 = max(w.unit, kTileCost) - kTileCost;
     s.b1 = max(until, kTileCost) - kTileCost;
     s.item = w.at - w.unit + kTileCost;
@@ -269,7 +275,7 @@ template <int kRows> __device__ __forceinline__ bool walk_start(const AttnArgs& 
 constexpr int kRing = 8;                            // steps whose pages and scales are looked up ahead
 constexpr int kSegments = 16;                       // segments ahead: at most one a step, and the one before may still be written out
 struct SegInfo {                                    // a segment as the other warps need it; steps = 0: there are no more
-    uint32_t steps, rows, row0, first_row, head, key0, end_key, length, b0, count;
+    uint32_t steps, rows, row0, first_row, head, key0, low_key, end_key, length, b0, count;   // keys outside [low, end) are not read
     int32_t start;                                  // position of the sequence's first row
     unsigned long long item;
 };
@@ -388,6 +394,7 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
         if (n == 0) return;
         const uint8_t* pool = (keys ? a.c.k : a.c.v) + (long long)s.head * a.c.head_step + 16 * unit + (long long)(row0 & 15) * a.c.token_step;
         int left = (int)s.end_key - (int)s.key0 - (int)row0;     // keys there from this thread's first on
+        int skip = (int)s.low_key - (int)s.key0 - (int)row0;     // and of them in front of every row's window (the first step only)
         uint4 c[kUnits];
         auto get = [&](uint32_t x) {
             const uint32_t ring = x % kRing;
@@ -395,7 +402,7 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
             for (int e = 0; e < kUnits; ++e) {
                 const long long at = sh.at[ring][(row0 + e * kRowStep) >> 4];
                 c[e] = make_uint4(0, 0, 0, 0);
-                if (at >= 0 && inside && e * kRowStep < left)
+                if (at >= 0 && inside && e * kRowStep < left && e * kRowStep >= skip)
                     asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[e].x), "=r"(c[e].y), "=r"(c[e].z), "=r"(c[e].w)
                                  : "l"(pool + at + (kRowStep < 16 && (e & 1) ? 8 * a.c.token_step : 0u)));
             }
@@ -420,6 +427,7 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
             mbar_arrive(&full[stage]);
             ++step;
             left -= kKeys;
+            skip -= kKeys;
             if (j + 1 < n) {
                 if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
                 get(step);
@@ -440,7 +448,7 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
         const bool more = next_segment<P::kRows>(a, w, s);
         const int32_t* table = kv.pages + (more ? (size_t)s.p.s.slot * kv.max_pages : 0);
         const uint32_t n = more ? s.b1 - s.b0 : 1u;              // the end takes a step of its own
-        const uint32_t end_key = more ? min((s.first + s.count) * kKeys, s.p.s.length) : 0u;
+        const uint32_t low_key = more ? s.lo : 0u, end_key = more ? s.hi : 0u;
         for (uint32_t j0 = 0; j0 < n; j0 += 4) {
             const uint32_t j = j0 + (lane >> 3), x = step + j, last = step + min(j0 + 4, n) - 1;
             // products end in order: when the last slot of these four is free, all are
@@ -450,7 +458,7 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
                     SegInfo& o = sh.seg[seg % kSegments];
                     o.steps = more ? n : 0u;
                     o.rows = s.rows; o.row0 = s.p.s.row; o.first_row = s.tile * P::kRows; o.head = s.head;
-                    o.key0 = (s.first + s.b0) * kKeys; o.end_key = end_key; o.length = s.p.s.length;
+                    o.key0 = (s.first + s.b0) * kKeys; o.low_key = low_key; o.end_key = end_key; o.length = s.p.s.length;
                     o.b0 = s.b0; o.count = s.count; o.start = s.p.start; o.item = s.item;
                 }
                 __syncwarp();
@@ -458,7 +466,7 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
             if (j < n) {
                 const uint32_t key = more ? (s.first + s.b0 + j) * kKeys + 16 * group : 0u;
                 int32_t id = -1;
-                if (key < end_key) {
+                if (key < end_key && key + 16 > low_key) {
                     id = __ldg(table + (key >> kv.page_shift));
                     if ((uint32_t)id >= kv.num_pages) {
                         kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);

@@ -447,6 +447,48 @@ def test_attention_offsets_past_32_bits(torch, rm):
     assert int(used) == small.num_pages and torch.equal(big.k[:, :small.num_pages], small.k) and big.status_flags() == 0
 
 
+@pytest.mark.parametrize("page,dim,layout", [(16, 64, "hnd"), (16, 128, "nhd"), (32, 256, "hnd"), (64, 128, "hnd"), (128, 64, "nhd")])
+@pytest.mark.parametrize("news", [(1, 1, 1), (3, 5, 2), (547, 70, 129)])
+def test_attention_reads_nothing_before_the_windows(torch, rm, page, dim, layout, news):
+    """What lies before every row's window may be anything: NaN codes, pages given up (-1), NaN and infinite scales of the pages before.
+    The results are those of the whole cache, bit for bit, and nothing is reported."""
+    lengths, window = [900, 333, 701], 150
+    cache = make_cache(torch, rm, lengths, page=page, dim=dim, layout=layout, seed=page + dim)
+    ids = torch.arange(3, dtype=torch.int32, device="cuda")
+    rows = torch.tensor(np.concatenate([[0], np.cumsum(news)]).tolist(), dtype=torch.int32, device="cuda")
+    q = torch.from_numpy(np.random.default_rng(2).normal(size=(sum(news), 8, dim))).to(torch.bfloat16).cuda()
+    ws = cache.workspace()
+    check_attention(torch, rm, cache, [0, 1, 2], list(news), 8, "bf16", window=window, workspace=ws)
+    want, want_lse = rm.kv_attention(cache, ids, q, rows, window=window, workspace=ws)
+    table = cache.pages.cpu().numpy()
+    for s, (n, new) in enumerate(zip(lengths, news)):
+        first = max(0, n - new - window + 1)                           # the first key that the first row sees
+        for e in range(-(-first // page)):
+            ends = min(first - e * page, page)                         # keys of this page before it
+            at = int(table[s, e])
+            for codes, nan in ((cache.k, 0x7F), (cache.v, 0xFF)):
+                (codes[0, at, :, :ends] if layout == "hnd" else codes[0, at, :ends]).fill_(nan)
+            if ends == page and e % 3 and (e + 1) * page + page <= first:
+                cache.k_scale[0, at], cache.v_scale[0, at] = (float("nan"), float("inf")) if e % 3 == 1 else (float("-inf"), float("nan"))
+            elif ends == page:                                         # every third, and the last one
+                cache.pages[s, e] = -1
+    got, lse = rm.kv_attention(cache, ids, q, rows, window=window, workspace=ws)
+    assert cache.status_flags() == 0
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_attention_reads_nothing_that_no_row_of_a_tile_sees(torch, rm, page):
+    """A NaN in the last token's value reaches rows of that token's tile only: the first 512 rows end before it, in the same 128 keys."""
+    cache = make_cache(torch, rm, [880], page=page, dim=128, heads=1, seed=4)
+    rows = torch.tensor([0, 530], dtype=torch.int32, device="cuda")
+    q = torch.randn((530, 1, 128), device="cuda").to(torch.bfloat16)
+    want, want_lse = rm.kv_attention(cache, [0], q, rows)
+    cache.v[0, int(cache.pages[0, 879 // page]), 0, 879 % page] = 0x7F
+    got, lse = rm.kv_attention(cache, [0], q, rows)
+    assert torch.equal(got[:512], want[:512]) and torch.equal(lse[:512], want_lse[:512]) and torch.isnan(got[529]).all()
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
