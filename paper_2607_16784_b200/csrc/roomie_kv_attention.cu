@@ -42,7 +42,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
 // leaves its sums in the workspace, and the last part to arrive adds them in order.
 //
 // Scales: a page's key scale goes into the factor of the exponent's argument, its value scale vs into the exponent: the weights
-// exp2(s + log2 vs - m), m a maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs.
+// exp2(s + log2 vs - m), m near the maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs.
 template <int DP, int NT, int kFormat, class T>
 struct FewRows {
     static constexpr int kGroups = DP > 128 ? 1 : 2;               // 16-key groups a warp step
@@ -427,22 +427,23 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                                     const int k = k0 + 16 * g + 8 * h + r;
                                     if (k >= see_hi[t][n] || k < see_lo[t][n]) x = -INFINITY;
                                 }
-                                high = high || x > m[t][n] + 8.0f;
+                                high = high || x > m[t][n] + kAbove;
                             }
                         }
                 }
-                // The maximum is looked for only when some exponent is past 2^8 above the old one: weights stay far from float16's end.
+                // The maximum is looked for only when some exponent is more than kAbove over the reference m.
                 if (__any_sync(0xffffffffu, high)) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int n = 0; n < 2; ++n) {
-                            float mx = m[t][n];
+                            float mx = -INFINITY;
 #pragma unroll
                             for (int g = 0; g < G; ++g) mx = fmaxf(mx, fmaxf(sc[g][t][n], sc[g][t][n + 2]));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                            mx = fmaxf(mx - kBelow, m[t][n]);
                             const float f = m[t][n] == -INFINITY ? 0.0f : exp2_fast(m[t][n] - mx);
                             m[t][n] = mx;
                             l[t][n] *= f;

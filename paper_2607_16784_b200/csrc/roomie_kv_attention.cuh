@@ -23,6 +23,13 @@ struct AttnArgs {
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr int kMaxAttnBlocksPerSm = 4;
 
+// Weights are float16 for the product with the codes.  They are taken against a reference that moves, to kBelow under the largest
+// exponent so far, only when some exponent is more than kAbove over it: the largest weight then lies in 2^7 .. 2^15, below float16's end at
+// 65504, and every weight down to 2^-21 of the largest keeps its 11 bits (with a reference at the largest itself: down to 2^-14, and a
+// long flat tail behind one leading key lost 1 %).  A running maximum that is moved lazily is a published variation of the one-pass
+// softmax (Milakov and Gimelshein, 2018).
+constexpr float kAbove = 15.0f, kBelow = 7.0f;
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

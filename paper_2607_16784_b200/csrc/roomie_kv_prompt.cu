@@ -19,7 +19,7 @@
 // at the softmax (544 against 475), two threads a row (538 against 487).
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
-// Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M the running maximum of s + log2 vs, is what multiplies
+// Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M near the running maximum of s + log2 vs, is what multiplies
 // V's codes, and the softmax total sum exp2(s - M) is the sum of each page's w times 1 / vs.  So neither costs an instruction an
 // element, and the operands stay exact.
 #include "roomie_kv_attention.cuh"
@@ -620,8 +620,8 @@ __device__ __forceinline__ float weights32(const uint32_t* x, uint32_t* p, const
 }
 
 // Half a step of a row, 64 keys, 32 at a time: the weights exp2(f * S + log2 vs - m) go as float16 over the columns of S that have been
-// read.  They are taken against an old maximum m while the new one is at most 2^8 above it, far from float16's end.  Past that m - a
-// whole number - moves up: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor
+// read.  They are taken against an old reference m while no exponent is more than kAbove over it.  Past that m - a
+// whole number - moves up to kBelow under the new maximum: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor
 // for o.  cut: some key is hidden from some row of the warp; hidden ones weigh exactly nothing.  No branch stands between the elements
 // (with one, each exponential waits for the one before), and the loop is kept short because the roles share the instruction caches
 // (unrolled over a whole step, a third of all stalls were for instructions).
@@ -658,9 +658,9 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
         }
         const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float total = weights32(x, p, ivs + 2 * c);
-        if (__any_sync(0xffffffffu, high > 8.0f || (m == -INFINITY && high > m))) {
+        if (__any_sync(0xffffffffu, high > kAbove || (m == -INFINITY && high > m))) {
             const bool none = m == -INFINITY;                    // no key so far: there is nothing to multiply
-            const float up = none ? (high > m ? ceilf(high) : 0.0f) : fmaxf(ceilf(high), 0.0f), f = none ? 1.0f : exp2_fast(-up);
+            const float up = none ? (high > m ? ceilf(high) - kBelow : 0.0f) : fmaxf(ceilf(high) - kBelow, 0.0f), f = none ? 1.0f : exp2_fast(-up);
             if (!none || high > m) m = base + up;
             l *= f;
             moved *= f;

@@ -489,6 +489,46 @@ def test_attention_reads_nothing_that_no_row_of_a_tile_sees(torch, rm, page):
     assert torch.equal(got[:512], want[:512]) and torch.equal(lse[:512], want_lse[:512]) and torch.isnan(got[529]).all()
 
 
+def flat_cache(torch, rm, lengths, *, page=16, dim=64, heads=1, fmt="e4m3", value_scales=(1.0,), seed=0):
+    """Keys of zeros, so that all logits are equal; the value scales of a sequence's pages in turn, for each head another first."""
+    cache = make_cache(torch, rm, lengths, page=page, dim=dim, heads=heads, fmt=fmt, seed=seed)
+    cache.k.zero_()
+    cache.k_scale.fill_(1.0)
+    table = cache.pages.cpu().numpy()
+    for s, n in enumerate(lengths):
+        for e in range(-(-n // page)):
+            for h in range(heads):
+                cache.v_scale[0, int(table[s, e]), h] = value_scales[(e + h) % len(value_scales)]
+    return cache
+
+
+@pytest.mark.parametrize("at", [0, 31, 700, 1899])
+@pytest.mark.parametrize("news", [1, 3, 40])
+@pytest.mark.parametrize("dtype,fmt", [("f16", "e4m3"), ("bf16", "int8")])
+def test_attention_one_leading_key_and_a_flat_tail(torch, rm, at, news, dtype, fmt):
+    """One key whose weight is 2^19.4 times each other's, with a value of nothing: the result is the sum of the many small weights, each of
+    them to 11 bits all the same.  Work enough (64 sequences, on the same pages) that a key axis is not cut."""
+    length, seqs, heads, dim = 2048, 64, 8, 64
+    cache = flat_cache(torch, rm, [length] + [0] * (seqs - 1), page=64, dim=dim, heads=heads, fmt=fmt, value_scales=(0.0107,), seed=3)
+    cache.pages[1:], cache.length[1:] = cache.pages[0].clone(), length
+    cache.v.bitwise_and_(0x7F)                                          # no sums that cancel
+    cache.v.masked_fill_(cache.v == 0x7F, 0x40)
+    p = int(cache.pages[0, at // 64])
+    cache.k[0, p, :, at % 64], cache.v[0, p, :, at % 64] = 0x38 if fmt == "e4m3" else 1, 0        # 1 in each dimension
+    q = torch.full((seqs * news, 2 * heads, dim), 19.4 * float(np.log(2.0)) / dim, device="cuda").to(dtype_of(torch, dtype))
+    rows = torch.arange(0, seqs * news + 1, news, dtype=torch.int32, device="cuda")
+    got, lse = rm.kv_attention(cache, torch.arange(seqs, dtype=torch.int32, device="cuda"), q, rows, scale=1.0)
+    k, v = cached(cache, 0, 0, "k"), cached(cache, 0, 0, "v")
+    for t in sorted({0, news // 2, news - 1}):
+        want, want_lse, weight = sp.attend(host(q[t:t + 1]), k, v, length - news + t, 1.0, 0)
+        # weights to 11 bits, their sums, and the largest logit (13.4; 68 2^-24 of it each) as in the head of this file
+        p_err = 2 * (68 * 2.0 ** -24 * 13.5 + 2.0 ** -22 + 14 * 2.0 ** -23)
+        bound = (2.0 ** -11 + 2.0 ** -16 + p_err) * weight + U[dtype] * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 0)
+        for s in (0, 5, seqs - 1):
+            assert np.all(np.abs(host(got[s * news + t]) - want[0]) <= bound[0])
+            assert np.all(np.abs(host(lse[s * news + t]) - want_lse[0]) <= p_err + 2.0 ** -20 * 14)
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
