@@ -660,20 +660,20 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
         float total = weights32(x, p, ivs + 2 * c);
         if (__any_sync(0xffffffffu, high > kAbove || (m == -INFINITY && high > m))) {
             const bool none = m == -INFINITY;                    // no key so far: there is nothing to multiply
-            const float up = none ? (high > m ? ceilf(high) - kBelow : 0.0f) : fmaxf(ceilf(high) - kBelow, 0.0f), f = none ? 1.0f : exp2_fast(-up);
+            const float up = none ? (high > m ? floorf(high) - kBelow : 0.0f) : fmaxf(floorf(high) - kBelow, 0.0f), f = none ? 1.0f : exp2_fast(-up);
             if (!none || high > m) m = base + up;
             l *= f;
             moved *= f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) - up);
-            if (c) {                                             // weights already written
-                const __half2 f2h = __float2half2_rn(f);
+            if (c) {                                             // weights already written (f may be below float16's least)
                 tmem_wait_st();
                 tmem_load16(s_at, p);
                 tmem_wait16(p);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const __half2 w = __hmul2(reinterpret_cast<const __half2&>(p[e]), f2h);
+                    const float2 w2 = __half22float2(reinterpret_cast<const __half2&>(p[e]));
+                    const __half2 w = __floats2half2_rn(w2.x * f, w2.y * f);
                     p[e] = reinterpret_cast<const uint32_t&>(w);
                 }
                 tmem_store16(s_at, p);

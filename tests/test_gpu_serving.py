@@ -529,6 +529,36 @@ def test_attention_one_leading_key_and_a_flat_tail(torch, rm, at, news, dtype, f
             assert np.all(np.abs(host(lse[s * news + t]) - want_lse[0]) <= p_err + 2.0 ** -20 * 14)
 
 
+@pytest.mark.parametrize("at", [1867, 1899, 1919])
+@pytest.mark.parametrize("news", [1, 40])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_attention_a_key_that_leads_late(torch, rm, at, news, fmt):
+    """The maximum moves by 2^28 and more at once, in a step's first and later keys: weights that are already taken move with it."""
+    length, seqs, heads, dim = 2048, 64, 8, 64
+    cache = flat_cache(torch, rm, [length] + [0] * (seqs - 1), page=64, dim=dim, heads=heads, fmt=fmt, value_scales=(2.0 ** -6,), seed=3)
+    cache.pages[1:], cache.length[1:] = cache.pages[0].clone(), length
+    cache.k_scale.fill_(1.0 if fmt == "e4m3" else 0.125)
+    low, middle, top = (0, 0x2C, 0x3B) if fmt == "e4m3" else (0, 3, 11)                            # 0, 0.375 and 1.375
+    half = [int(p) for p in cache.pages[0, :length // 64]]
+    cache.k.fill_(middle)
+    cache.k[0, half[0], :, :32] = low                                   # what the first keys set stays, 2^7.5 are not enough to move it
+    cache.v.zero_()
+    where, inside = half[at // 64], at % 64
+    cache.v[0, where, :, :] = 0x38 if fmt == "e4m3" else 1              # only the keys around the leading one have a value, it has none
+    cache.k[0, where, :, inside], cache.v[0, where, :, inside] = top, 0
+    q = torch.full((seqs * news, 2 * heads, dim), 20 * float(np.log(2.0)) / dim, device="cuda").to(torch.bfloat16)
+    rows = torch.arange(0, seqs * news + 1, news, dtype=torch.int32, device="cuda")
+    got, lse = rm.kv_attention(cache, torch.arange(seqs, dtype=torch.int32, device="cuda"), q, rows, scale=1.0)
+    k, v = cached(cache, 0, 0, "k"), cached(cache, 0, 0, "v")
+    for t in sorted({0, news - 1}):
+        want, want_lse, weight = sp.attend(host(q[t:t + 1]), k, v, length - news + t, 1.0, 0)
+        p_err = 2 * (68 * 2.0 ** -24 * 20 + 2.0 ** -22 + 20 * 2.0 ** -23)             # as in the head of this file: the largest logit is 19.1
+        bound = (2.0 ** -11 + 2.0 ** -16 + p_err) * weight + U["bf16"] * np.abs(want) + 1e-30
+        for s in (0, seqs - 1):
+            assert np.all(np.abs(host(got[s * news + t]) - want[0]) <= bound[0])
+            assert np.all(np.abs(host(lse[s * news + t]) - want_lse[0]) <= p_err + 2.0 ** -20 * 20)
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
