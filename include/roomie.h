@@ -476,7 +476,7 @@ int roomie_kv_append(const roomie_kv_cache *cache /* host */, uint32_t layer, co
  * Query head h reads key head h / (q_heads / kv_heads).  Softmax statistics and sums are float32; products take q and
  * the codes as they are; a key's weight - probability times value scale - is rounded to 11 bits, one below 2^-21 of its row's
  * largest to 2^-32 of that.  A row that sees nothing gives 0 and lse = -inf.
- * Scales are 0 or more, of any value (a value scale below 2^-100 counts as 2^-100).  What lies behind a sequence's length, in pages
+ * Scales are 0 or more, finite, of any value (a value scale below 2^-100 counts as 2^-100).  What lies behind a sequence's length, in pages
  * it does not hold, or before every row's window is not read, whatever it holds.  Codes 0x7f and 0xff of e4m3 are NaN, which
  * roomie_kv_append never writes; a NaN that some row of a tile of rows sees may reach the other rows of that tile.
  * The result does not depend on timing: the same call gives the same bits.

@@ -42,7 +42,8 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
 // leaves its sums in the workspace, and the last part to arrive adds them in order.
 //
 // Scales: a page's key scale goes into the factor of the exponent's argument, its value scale vs into the exponent: the weights
-// exp2(s + log2 vs - m), m near the maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs.
+// exp2(s + log2 vs - m), m near the maximum of s + log2 vs, multiply the codes, and the softmax total sums them times 1 / vs
+// (or is summed apart: see kNear).
 template <int DP, int NT, int kFormat, class T>
 struct FewRows {
     static constexpr int kGroups = DP > 128 ? 1 : 2;               // 16-key groups a warp step
@@ -91,6 +92,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
     __shared__ unsigned long long sh_sum[kAttnWarps], sh_first;
     __shared__ uint32_t sh_at[4];
     __shared__ float sm_row[2 * F::kRows];
+    __shared__ float sh_ref[2 * NT][kAttnThreads];                 // reference of a row's total while it is summed apart
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const KvView& kv = a.c;
 
@@ -255,6 +257,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             m[t][0] = m[t][1] = -INFINITY;
             l[t][0] = l[t][1] = 0.0f;
         }
+        bool apart = false;                                        // the totals are; the same in all lanes
 
         // the warp's steps: keys [k0, k0 + kStep) of this tile's blocks that some row sees
         const int part_lo = (int)((w.first_block + b0) * F::kBlock), part_hi = (int)min((w.first_block + b1) * F::kBlock, s.length);
@@ -384,7 +387,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                 __syncwarp();
                 const uint8_t* side = ring + stage * 2 * F::kSide;
                 float sc[G][NT][4], ivs[G];
-                bool whole = k0 >= all_lo && k0 + F::kStep <= all_hi, high = false;
+                bool whole = k0 >= all_lo && k0 + F::kStep <= all_hi, high = apart, wide = false;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
 #pragma unroll
@@ -410,9 +413,10 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                     float vs = vs_of[stage][g], lvs = -INFINITY;   // a page that is not there weighs nothing
                     ivs[g] = 0.0f;
                     if (vs >= 0.0f) {
-                        vs = fmaxf(vs, 7.888609052210118e-31f);    // 2^-100
+                        vs = fmaxf(vs, kLeastScale);
                         lvs = log2_fast(vs);
                         ivs[g] = __fdividef(1.0f, vs);
+                        wide = wide || fabsf(lvs) > kNear;
                     }
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
@@ -431,8 +435,15 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                             }
                         }
                 }
-                // The maximum is looked for only when some exponent is more than kAbove over the reference m.
-                if (__any_sync(0xffffffffu, high)) {
+                // The maximum is looked for only when some exponent is more than kAbove over the reference m, or the totals are summed apart.
+                if (__any_sync(0xffffffffu, high || wide)) {
+                    if (wide && !apart) {
+                        apart = true;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) sh_ref[2 * t + n][threadIdx.x] = m[t][n];
+                    }
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -446,13 +457,40 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                             mx = fmaxf(mx - kBelow, m[t][n]);
                             const float f = m[t][n] == -INFINITY ? 0.0f : exp2_fast(m[t][n] - mx);
                             m[t][n] = mx;
-                            l[t][n] *= f;
+                            if (!apart) l[t][n] *= f;
 #pragma unroll
                             for (int i = 0; i < KS; ++i) {
                                 o[t][i][n] *= f;
                                 o[t][i][n + 2] *= f;
                             }
                         }
+                    if (apart) {
+                        float less[G];                                 // log2 vs
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            less[g] = vs_of[stage][g] >= 0.0f ? log2_fast(fmaxf(vs_of[stage][g], kLeastScale)) : 0.0f;
+                            ivs[g] = 0.0f;
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) {
+                                float ref = sh_ref[2 * t + n][threadIdx.x], mx = -INFINITY;
+#pragma unroll
+                                for (int g = 0; g < G; ++g) mx = fmaxf(mx, fmaxf(sc[g][t][n], sc[g][t][n + 2]) - less[g]);
+                                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                                if (mx > ref + kAbove) {
+                                    if (ref != -INFINITY) l[t][n] *= exp2_fast(ref - (mx - kBelow));
+                                    ref = mx - kBelow;
+                                    sh_ref[2 * t + n][threadIdx.x] = ref;
+                                }
+                                if (ref == -INFINITY) ref = 0.0f;
+#pragma unroll
+                                for (int g = 0; g < G; ++g) l[t][n] += exp2_fast(sc[g][t][n] - less[g] - ref) + exp2_fast(sc[g][t][n + 2] - less[g] - ref);
+                            }
+                    }
                 }
                 // weights: rounded to float16 (11 bits) for the product with the codes, not for the total
 #pragma unroll
@@ -499,6 +537,20 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
 
         // ---- the warps meet --------------------------------------------------------------------------------------------
         float* sm_ml = sm + kAttnWarps * F::kRows * DP;
+        if (apart) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float up;
+                    one_reference(m[t][n], l[t][n], up, sh_ref[2 * t + n][threadIdx.x]);
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        o[t][i][n] *= up;
+                        o[t][i][n + 2] *= up;
+                    }
+                }
+        }
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < NT; ++t)

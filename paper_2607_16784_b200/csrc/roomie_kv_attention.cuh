@@ -30,6 +30,24 @@ constexpr int kMaxAttnBlocksPerSm = 4;
 // softmax (Milakov and Gimelshein, 2018).
 constexpr float kAbove = 15.0f, kBelow = 7.0f;
 
+// The softmax total is the weights' sum with each page's value scale divided out again.  That holds while all value scales met are
+// within 2^-kNear .. 2^kNear: the largest probability's weight is then above 2^-57 and its share of the total above 2^-25, far from float32's
+// end.  From the first page with another scale on, a row's total is summed apart, from exponents without log2 vs, against a reference of
+// its own that moves in the same way; a page of zeros, which append gives 2^-100, would drop out of it beside a large one.  At the end both
+// go to one reference between the two, where each is within float32.
+constexpr float kNear = 32.0f;
+constexpr float kLeastScale = 7.888609052210118e-31f;   // 2^-100: a value scale below counts as this
+
+// sums against m (o) and ref (l): o *= up, l and m become those of one reference
+__device__ __forceinline__ void one_reference(float& m, float& l, float& up, float ref) {
+    up = 1.0f;
+    if (m == -INFINITY) return;                         // no key
+    const float d = floorf(0.5f * (m - ref));
+    up = exp2f(d);
+    l *= exp2f(ref - m + d);
+    m -= d;
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -21,7 +21,7 @@
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
 // Its value scale vs goes into the exponent: w = exp2(s + log2 vs - M), M near the running maximum of s + log2 vs, is what multiplies
 // V's codes, and the softmax total sum exp2(s - M) is the sum of each page's w times 1 / vs.  So neither costs an instruction an
-// element, and the operands stay exact.
+// element, and the operands stay exact.  (Value scales beyond kNear: the total is summed apart.)
 #include "roomie_kv_attention.cuh"
 
 namespace roomie {
@@ -288,6 +288,8 @@ struct PromptShared {
     long long at[kRing][8];                         // of 16 keys each: bytes from the pool's start to them (-1: none), key scale, log2
                                                     // and inverse of the value scale
     float ks[kRing][8], lvs[kRing][8], ivs[kRing][8];
+    __align__(4) uint8_t wide[kRing][8];            // the value scale is beyond kNear
+    float l_ref[256];                               // reference of a row's total while it is summed apart
     SegInfo seg[kSegments];
     float q_scale[2][256];                          // of a row, segments in turn: 2^e of its float16 form times scale * log2(e)
     uint32_t tmem, last, failed;
@@ -394,9 +396,9 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
         if (n == 0) return;
         const uint8_t* pool = (keys ? a.c.k : a.c.v) + (long long)s.head * a.c.head_step + 16 * unit + (long long)(row0 & 15) * a.c.token_step;
         int left = (int)s.end_key - (int)s.key0 - (int)row0;     // keys there from this thread's first on
-        int skip = (int)s.low_key - (int)s.key0 - (int)row0;     // and of them in front of every row's window (the first step only)
+        const int skip = (int)s.low_key - (int)s.key0 - (int)row0;   // and of them in front of every row's window: of the first step only
         uint4 c[kUnits];
-        auto get = [&](uint32_t x) {
+        auto get = [&](uint32_t x, int skip) {
             const uint32_t ring = x % kRing;
 #pragma unroll
             for (int e = 0; e < kUnits; ++e) {
@@ -411,7 +413,7 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
         feed_queries<DP, T>(a, sh, smem, s, seg & 1, keys ? 0 : P::kRows / 2, keys ? P::kRows / 2 : P::kRows);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&sh.q_full);
-        get(step);
+        get(step, skip);
         for (uint32_t j = 0; j < n; ++j) {
             const uint32_t stage = step % P::kStages, turn = step / P::kStages;
             if (turn && !warp_wait(&empty[stage], (turn - 1) & 1, sh)) return;
@@ -427,10 +429,9 @@ __device__ __forceinline__ void feed(const AttnArgs& a, PromptShared& sh, uint8_
             mbar_arrive(&full[stage]);
             ++step;
             left -= kKeys;
-            skip -= kKeys;
             if (j + 1 < n) {
                 if (!warp_wait(&sh.look_full[step % kRing], (step / kRing) & 1, sh)) return;
-                get(step);
+                get(step, 0);
             }
         }
     }
@@ -476,7 +477,7 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
                 float ks = 0.0f, lvs = -INFINITY, ivs = 0.0f;    // keys that are not there weigh nothing
                 if (id >= 0) {
                     ks = __ldg(kv.k_scale + (size_t)id * kv.heads + s.head);
-                    const float vs = fmaxf(__ldg(kv.v_scale + (size_t)id * kv.heads + s.head), 7.888609052210118e-31f);   // 2^-100
+                    const float vs = fmaxf(__ldg(kv.v_scale + (size_t)id * kv.heads + s.head), kLeastScale);
                     lvs = log2f(vs);
                     ivs = __fdiv_rn(1.0f, vs);
                 }
@@ -485,6 +486,7 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
                 sh.ks[ring][group] = ks;
                 sh.lvs[ring][group] = lvs;
                 sh.ivs[ring][group] = ivs;
+                sh.wide[ring][group] = id >= 0 && fabsf(lvs) > kNear;
                 mbar_arrive(&sh.look_full[ring]);
             }
             __syncwarp();
@@ -619,6 +621,23 @@ __device__ __forceinline__ float weights32(const uint32_t* x, uint32_t* p, const
     return total;
 }
 
+// The same columns' share of a total that is summed apart: x holds s + log2 vs - base.
+__device__ __forceinline__ float total_apart(const uint32_t* x, const float* lvs, float base, float& ref_at, float& l) {
+    float add[2], ref = ref_at, top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) add[g] = base - (lvs[g] == -INFINITY ? 0.0f : lvs[g]);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(x[e]) + add[e / 16]);
+    if (top > ref + kAbove) {
+        if (ref != -INFINITY) l *= exp2_fast(ref - (top - kBelow));
+        ref_at = ref = top - kBelow;
+    }
+    if (ref == -INFINITY) ref = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) total += exp2_fast(__uint_as_float(x[e]) + add[e / 16] - ref);
+    return total;
+}
+
 // Half a step of a row, 64 keys, 32 at a time: the weights exp2(f * S + log2 vs - m) go as float16 over the columns of S that have been
 // read.  They are taken against an old reference m while no exponent is more than kAbove over it.  Past that m - a
 // whole number - moves up to kBelow under the new maximum: the weights already written, o and the total are multiplied by a power of two.  `moved` collects that factor
@@ -626,7 +645,7 @@ __device__ __forceinline__ float weights32(const uint32_t* x, uint32_t* p, const
 // (with one, each exponential waits for the one before), and the loop is kept short because the roles share the instruction caches
 // (unrolled over a whole step, a third of all stalls were for instructions).
 __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const float* lvs, const float* ivs, float q, bool cut, int k0, int lo,
-                                         int hi, float& m, float& l, float& moved) {
+                                         int hi, bool apart, float& ref, float& m, float& l, float& moved) {
 #pragma unroll 1
     for (int c = 0; c < 2; ++c) {
         uint32_t x[32], p[16];
@@ -658,11 +677,11 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
         }
         const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         float total = weights32(x, p, ivs + 2 * c);
-        if (__any_sync(0xffffffffu, high > kAbove || (m == -INFINITY && high > m))) {
+        if (__any_sync(0xffffffffu, apart || high > kAbove || (m == -INFINITY && high > m))) {
             const bool none = m == -INFINITY;                    // no key so far: there is nothing to multiply
             const float up = none ? (high > m ? floorf(high) - kBelow : 0.0f) : fmaxf(floorf(high) - kBelow, 0.0f), f = none ? 1.0f : exp2_fast(-up);
             if (!none || high > m) m = base + up;
-            l *= f;
+            if (!apart) l *= f;
             moved *= f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) - up);
@@ -679,6 +698,7 @@ __device__ __forceinline__ void row_half(uint32_t s_at, const float* ks, const f
                 tmem_store16(s_at, p);
             }
             total = weights32(x, p, ivs + 2 * c);
+            if (apart) total = total_apart(x, lvs + 2 * c, m == -INFINITY ? 0.0f : m, ref, l);
         }
         l += total;
         tmem_store16(s_at + 16 * c, p);
@@ -706,6 +726,8 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
         }
         float m = -INFINITY, l = 0.0f, q = 0.0f;
+        float& l_ref = sh.l_ref[t * 128 + r];
+        bool apart = false;
         int k0 = (int)s.key0;
         for (uint32_t h = 0; h < 2 * n; ++h, k0 += kKeys / 2) {
             const uint32_t side = h & 1, ring = step % kRing;
@@ -720,7 +742,11 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             if (h == 0) q = sh.q_scale[seg & 1][t * 128 + r];
             const bool cut = __any_sync(0xffffffffu, k0 < lo || k0 + kKeys / 2 > hi);
             float moved = 1.0f;
-            row_half(s_at + 64 * side, sh.ks[ring] + 4 * side, sh.lvs[ring] + 4 * side, sh.ivs[ring] + 4 * side, q, cut, k0, lo, hi, m, l, moved);
+            const bool wide = *reinterpret_cast<const uint32_t*>(sh.wide[ring] + 4 * side) != 0;
+            if (wide && !apart) l_ref = m;
+            apart = apart || wide;
+            row_half(s_at + 64 * side, sh.ks[ring] + 4 * side, sh.lvs[ring] + 4 * side, sh.ivs[ring] + 4 * side, q, cut, k0, lo, hi, apart,
+                     l_ref, m, l, moved);
             if (h && __any_sync(0xffffffffu, moved != 1.0f)) {   // o of the halves before
                 if (!warp_wait(&sh.o_full[t][side ^ 1], (step - 1) & 1, sh)) return;
                 tc_fence_after();
@@ -739,6 +765,8 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
             mbar_arrive(&sh.p_full[t][side]);
         }
 
+        float up = 1.0f;
+        if (apart) one_reference(m, l, up, l_ref);
         // ---- the end of a segment: rows go out, or wait in the workspace for their other parts ---------------------------------
         const bool complete = s.b0 == 0 && n == s.count;
         const uint32_t row = s.first_row + t * 128 + r, tok = token_of(a, row), h = s.head * a.group + row - tok * a.group;
@@ -760,7 +788,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         if (on) {
             if (!warp_wait(&sh.o_full[t][1], (step - 1) & 1, sh)) return;
             tc_fence_after();
-            const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
+            const float inv = l > 0.0f ? __fdiv_rn(up, l) : l == 0.0f ? 0.0f : l;
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 uint32_t x[32];
@@ -774,6 +802,8 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) put8(32 * c + e, v + e);
                 } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * up);
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
                         *reinterpret_cast<uint4*>(part + ((size_t)(8 * c + e / 4) * P::kRows + pr) * 4) =

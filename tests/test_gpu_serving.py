@@ -559,6 +559,68 @@ def test_attention_a_key_that_leads_late(torch, rm, at, news, fmt):
             assert np.all(np.abs(host(lse[s * news + t]) - want_lse[0]) <= p_err + 2.0 ** -20 * 20)
 
 
+def check_scaled(torch, rm, cache, seqs, news, q_heads, window=0, workspace=None):
+    """As check_attention, with what lies under a weight's 11 bits: 2^-32 of the row's largest weight (probability times value scale) for
+    each key, times its code.  Where page scales differ by 2^20 and more that is what a small result beside large ones is left with."""
+    rng = np.random.default_rng(1)
+    rows, d = sum(news), cache.head_dim
+    q = torch.from_numpy(rng.normal(size=(rows, q_heads, d))).to(torch.bfloat16).cuda()
+    offset = torch.tensor(np.concatenate([[0], np.cumsum(news)]).tolist(), dtype=torch.int32, device="cuda")
+    got, lse = rm.kv_attention(cache, torch.tensor(seqs, dtype=torch.int32, device="cuda"), q, offset, window=window, workspace=workspace)
+    gq, go, gl, group, scale = host(q), host(got), host(lse), q_heads // cache.kv_heads, d ** -0.5
+    at = 0
+    for s, n in zip(seqs, news):
+        k, v = cached(cache, 0, s, "k"), cached(cache, 0, s, "v")
+        ids = cache.pages[s].cpu().numpy()[:-(-len(k) // cache.page_tokens)]
+        page_scale = np.maximum(cache.v_scale[0].cpu().numpy().astype(np.float64)[ids], 2.0 ** -100)
+        vs = np.repeat(page_scale, cache.page_tokens, 0)[:len(k)]                                    # [length, kv_heads]
+        codes = np.abs(v) / vs[..., None]
+        want, want_lse, weight = sp.attend(gq[at:at + n], k, v, len(k) - n, scale, window)
+        mass = scale * np.abs(gq[at:at + n]).max() * np.abs(k).sum(-1).max()
+        p_err = 2 * ((d + 4) * 2.0 ** -24 * mass + 2.0 ** -22 + 2.0 ** -22 + (np.abs(want_lse).max() + mass) * 2.0 ** -23)
+        for t in range(n):
+            pos = len(k) - n + t
+            lo, hi = max(0, pos - window + 1) if window else 0, pos + 1
+            for j in range(q_heads):
+                g = j // group
+                p = np.exp(scale * (k[lo:hi, g] @ gq[at + t, j]) - want_lse[t, j])
+                floor = 2.0 ** -32 * (p * vs[lo:hi, g]).max() * codes[lo:hi, g].sum(0)
+                bound = (2.0 ** -11 + 2.0 ** -16 + p_err) * weight[t, j] + floor + U["bf16"] * np.abs(want[t, j]) + 1e-30
+                # 127 * 2^122 is past float32: where the values' magnitudes add up to its end, infinity is right as well
+                past = np.maximum(np.abs(want[t, j]), weight[t, j]) + bound > 3.3895e38
+                assert np.all((np.abs(go[at + t, j] - want[t, j]) <= bound) | (past & (go[at + t, j] * np.sign(want[t, j]) > 3.3e38))), (s, t, j)
+        assert np.all(np.abs(gl[at:at + n] - want_lse) <= p_err + 2.0 ** -20 * np.maximum(1, np.abs(want_lse).max()))
+        at += n
+    assert cache.status_flags() == 0
+    return got, lse
+
+
+@pytest.mark.parametrize("scales", [(2.0 ** 30, 2.0 ** -100), (2.0 ** -100, 1.0, 0.0, 2.0 ** 30), (0.0, 0.0, 0.0, 2.0 ** -6), (2.0 ** 122, 0.01, 2.0 ** -100),
+                                    (0.0, 2.0 ** 122), (2.0 ** -100,), (3.0e-31, 7.0e-20, 5.0e-3, 11.0, 6.0e25), (2.0 ** 127,), (1.5 * 2.0 ** 126, 1.0)])
+@pytest.mark.parametrize("news", [(1, 1, 1), (2, 5, 3), (70, 45, 129)])
+@pytest.mark.parametrize("fmt,dim", [("e4m3", 128), ("int8", 64), ("e4m3", 256)])
+def test_attention_of_widely_different_value_scales(torch, rm, scales, news, fmt, dim):
+    """Every key counts in the softmax total, whatever its page's value scale is: pages of zeros (append gives them 2^-100) and scale 0
+    beside large ones, equal and different logits."""
+    lengths = [2300, 150, 400]
+    cache = flat_cache(torch, rm, lengths, dim=dim, heads=2, fmt=fmt, value_scales=scales, seed=dim)
+    if max(scales) >= 2.0 ** 126:                                       # values stay within float32
+        cache.v.bitwise_and_(0x83 if fmt == "int8" else 0x9F)
+        cache.v.masked_fill_(cache.v == (0x80 if fmt == "e4m3" else 0x83), 0)
+        if fmt == "int8":
+            cache.v.bitwise_and_(0x01)
+    check_scaled(torch, rm, cache, [0, 1, 2], list(news), 4)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cache.k.copy_(torch.randint(0, 0x38 if fmt == "e4m3" else 40, cache.k.shape, generator=gen, device="cuda", dtype=torch.uint8))
+    check_scaled(torch, rm, cache, [0, 1, 2], list(news), 4)
+    check_scaled(torch, rm, cache, [2, 0], [news[2], news[0]], 4, window=333)
+    ws = cache.workspace()                                              # the same bits again
+    rows = torch.tensor([0, news[1], news[1] + news[0]], dtype=torch.int32, device="cuda")
+    q = torch.randn((news[1] + news[0], 16, dim), generator=gen, device="cuda").to(torch.bfloat16)
+    a, b = (rm.kv_attention(cache, [1, 0], q, rows, workspace=ws) for _ in range(2))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
