@@ -21,7 +21,7 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
     w.s = kv_seq(a.c, a.seqs, a.q_offset, a.rows, i, report);
     w.tiles = (w.s.count * a.group + kRows - 1) / kRows;
     const int start = (int)w.s.length - (int)w.s.count;                  // negative: leading rows that see nothing
-    const int lowest = a.window ? max(start - (int)a.window + 1, 0) : 0; // first key that some row may see
+    const int lowest = a.window ? first_seen(start, a.window) : 0;        // first key that some row may see
     w.first_block = (uint32_t)max(min(lowest, (int)w.s.length), 0) / kBlock;
     const uint32_t end = (w.s.length + kBlock - 1) / kBlock;
     w.blocks = max(end > w.first_block ? end - w.first_block : 0u, 1u);  // a sequence without keys still writes its rows
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
                 const uint32_t rc = t * 8 + 2 * c + n;
                 const int pos = start + (int)((tile * F::kRows + rc) / a.group);
                 int hi = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
-                int lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
+                int lo = a.window ? first_seen(pos, a.window) : 0;
                 if (lo > hi) lo = hi;
                 see_hi[t][n] = hi;
                 see_lo[t][n] = lo;

@@ -48,6 +48,9 @@ __device__ __forceinline__ void one_reference(float& m, float& l, float& up, flo
     m -= d;
 }
 
+// The first key that a row at `position` sees.  Rows may lie before the sequence, and a window be as wide as its type: neither wraps here.
+__device__ __forceinline__ int first_seen(int position, uint32_t window) { return max(max(position + 1, 0) - (int)window, 0); }
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

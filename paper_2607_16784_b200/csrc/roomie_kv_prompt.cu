@@ -155,7 +155,7 @@ struct Blocks {
 template <int kRows> __device__ __forceinline__ Blocks tile_blocks(const AttnArgs& a, const PromptSeq& p, uint32_t tile) {
     const uint32_t last_row = min((tile + 1) * kRows, p.rows) - 1;
     const int hi = max(min((int)p.s.length, p.start + (int)token_of(a, last_row) + 1), 0);
-    const int lo = a.window ? min(max(p.start + (int)token_of(a, tile * kRows) - (int)a.window + 1, 0), hi) : 0;
+    const int lo = a.window ? min(first_seen(p.start + (int)token_of(a, tile * kRows), a.window), hi) : 0;
     Blocks b;
     b.first = (uint32_t)lo / kKeys;
     const uint32_t end = ((uint32_t)hi + kKeys - 1) / kKeys;
@@ -723,7 +723,7 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         if (mine) {
             const int pos = s.start + (int)token_of(a, s.first_row + t * 128 + r);
             hi = max(min(pos + 1, (int)s.length), 0);
-            lo = a.window ? max(pos + 1 - (int)a.window, 0) : 0;
+            lo = a.window ? first_seen(pos, a.window) : 0;
         }
         float m = -INFINITY, l = 0.0f, q = 0.0f;
         float& l_ref = sh.l_ref[t * 128 + r];

@@ -621,6 +621,19 @@ def test_attention_of_widely_different_value_scales(torch, rm, scales, news, fmt
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("most", [(1 << 31) - 1, (1 << 31) - 100, 1 << 30])
+@pytest.mark.parametrize("idle", [0, 40])
+def test_attention_more_rows_than_tokens_and_an_endless_window(torch, rm, most, idle):
+    """A window as wide as its type beside rows that lie before the sequence: as without a window, in both kernels (idle sequences decide
+    which one runs)."""
+    lengths, news = [200, 450] + [5] * idle, [210, 453] + [0] * idle
+    cache = make_cache(torch, rm, lengths, page=16, dim=64, heads=1, seed=7)
+    order = list(range(2 + idle))
+    want = check_attention(torch, rm, cache, order, news, 1, "bf16")
+    got = check_attention(torch, rm, cache, order, news, 1, "bf16", window=most)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
