@@ -840,7 +840,8 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
                 for (uint32_t b = first; b <= last; ++b) {
                     const float* pp = a.partial + ((size_t)b * 2 + (b == first ? 1 : 0)) * P::kPartial + (size_t)P::kRows * DP + 2 * pr;
                     const float mb = __ldcg(pp), lb = __ldcg(pp + 1), to = fmaxf(mx, mb);
-                    sum = (mx == -INFINITY ? 0.0f : sum * exp2f(mx - to)) + (mb == -INFINITY ? 0.0f : lb * exp2f(mb - to));
+                    // a part without keys has a total of 0, one of a query that is no number NaN: neither has a maximum
+                    sum = (mx == -INFINITY ? sum : sum * exp2f(mx - to)) + (mb == -INFINITY ? lb : lb * exp2f(mb - to));
                     mx = to;
                 }
                 const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : sum == 0.0f ? 0.0f : sum;

@@ -634,6 +634,21 @@ def test_attention_more_rows_than_tokens_and_an_endless_window(torch, rm, most, 
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("news", [1, 4, 40, 300])
+def test_attention_of_a_nan_query_is_nan(torch, rm, news):
+    """One query head of one row is NaN: that row is NaN, whether its keys are cut into parts or not, and no other one changes."""
+    for length in (330, 9000):
+        cache = make_cache(torch, rm, [length], page=64, dim=128, heads=1, seed=8)
+        rows = torch.tensor([0, news], dtype=torch.int32, device="cuda")
+        q = torch.randn((news, 2, 128), device="cuda").to(torch.bfloat16)
+        want, want_lse = (t.clone() for t in rm.kv_attention(cache, [0], q, rows))
+        q[news // 2, 1, 5] = float("nan")
+        want[news // 2, 1], want_lse[news // 2, 1] = float("nan"), float("nan")
+        got, lse = rm.kv_attention(cache, [0], q, rows)
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
+        assert torch.equal(lse.isnan(), want_lse.isnan()) and torch.equal(lse.nan_to_num(), want_lse.nan_to_num())
+
+
 def test_attention_bad_tables_are_reported(torch, rm):
     """Page ids, lengths and offsets that do not exist set status bits and read nothing."""
     def fresh():
