@@ -612,15 +612,9 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
             const uint32_t count = last - first + 1, groups = (count + kJoin - 1) / kJoin;
             auto part_of = [&](uint32_t b) { return a.partial + ((size_t)(first + b) * 2 + (b == 0 ? 1 : 0)) * F::kPartial; };
             auto arrive = [&](uint32_t* counter, uint32_t n) {     // whether this block is the last of n
-                __threadfence();
                 __syncthreads();
-                if (threadIdx.x == 0) {
-                    const uint32_t before = atomicAdd(counter, 1u);
-                    sh_at[1] = before == n - 1;
-                    if (before == n - 1) *counter = 0;
-                }
+                if (threadIdx.x == 0) sh_at[1] = count_part(counter, n) == n - 1;
                 __syncthreads();
-                __threadfence();
                 return sh_at[1] != 0;
             };
             // parts b0, b0 + step, ...: n of them, to the results (or into the first)

@@ -63,6 +63,17 @@ __device__ __forceinline__ float log2_fast(float x) {
     return y;
 }
 
+// One thread counts its block's part, one of n, after a barrier at which all its threads met; the last one leaves the counter zero.  Both
+// fences are this thread's: the first stands between the barrier and the count, so that what every thread wrote comes before it, the second
+// between the count and the barrier behind which the other parts are read.
+__device__ __forceinline__ uint32_t count_part(uint32_t* counter, uint32_t n) {
+    __threadfence();
+    const uint32_t before = atomicAdd(counter, 1u);
+    if (before == n - 1) *counter = 0;
+    __threadfence();
+    return before;
+}
+
 // 16x8x16 product, float16 operands, float32 sums
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -821,21 +821,18 @@ __device__ __forceinline__ void softmax(const AttnArgs& a, PromptShared& sh, uns
         if (!complete) {
             const uint32_t first = (uint32_t)(((s.item + 1) * parts - 1) / total_blocks);
             const uint32_t last = (uint32_t)(((s.item + s.count) * parts - 1) / total_blocks);
-            __threadfence();
             mbar_arrive(&sh.join[0]);
             if (threadIdx.x < 32) {
                 if (!warp_wait(&sh.join[0], joins & 1, sh)) return;
                 if (threadIdx.x == 0) {
-                    const uint32_t before = atomicAdd(a.counters + first, 1u);
+                    const uint32_t before = count_part(a.counters + first, last - first + 1);
                     sh.last = before == last - first;
-                    if (before == last - first) a.counters[first] = 0;
                     mbar_arrive(&sh.join[1]);
                 }
             }
             if (!warp_wait(&sh.join[1], joins & 1, sh)) return;
             ++joins;
             if (sh.last && mine) {
-                __threadfence();
                 float mx = -INFINITY, sum = 0.0f;
                 for (uint32_t b = first; b <= last; ++b) {
                     const float* pp = a.partial + ((size_t)b * 2 + (b == first ? 1 : 0)) * P::kPartial + (size_t)P::kRows * DP + 2 * pr;
