@@ -63,6 +63,19 @@ def _ids(t, what, n=None):
     return t
 
 
+def _here(index, *tensors):
+    """The library launches on the current device: a cache's or a table's (`index`) and the tensors (None: not given) have to be on it."""
+    device = torch.cuda.current_device()
+    if index == device:
+        for t in tensors:
+            if t is not None and t.get_device() != device:
+                index = t.get_device()
+                break
+        else:
+            return
+    raise ValueError(f"all tensors of a call live on the current CUDA device ({device}), got one on {index}")
+
+
 def _on_stream(call):
     """With stream= given, what the binding itself allocates or copies is ordered on that stream too."""
     @functools.wraps(call)
@@ -105,7 +118,7 @@ class RopeTable:
 
     def _set(self, frequency, interleaved, amplitude):
         self.frequency, self.interleaved, self.amplitude = frequency, bool(interleaved), float(amplitude)
-        self.rotary_dim = 2 * frequency.numel()
+        self.rotary_dim, self.index = 2 * frequency.numel(), frequency.get_device()
         self.c = _RopeTable(self.rotary_dim, int(self.interleaved), self.amplitude, frequency.data_ptr())
         self.ref = C.byref(self.c)
 
@@ -114,13 +127,14 @@ class RopeTable:
 def rope(x, positions, table: RopeTable, *, inverse=False, out=None):
     """roomie_rope: x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); `inverse` is the gradient.
     `out` may be x itself.  Returns out."""
+    cx = _rows(x, "x")
+    n, h, d = x.shape
+    positions = _ids(positions, "positions", n)
+    _here(table.index, x, out, positions)
     if out is None:
         out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out: the shape and type of x")
-    cx = _rows(x, "x")
-    n, h, d = x.shape
-    positions = _ids(positions, "positions", n)
     _check(_dll.roomie_rope(table.ref, cx, _rows(out, "out"), n, h, d, positions.data_ptr(), inverse, _stream(x)), "roomie_rope")
     return out
 
@@ -159,18 +173,20 @@ class KVCache:
                                (pages, tuple(pages.shape), torch.int32)):
             if tuple(t.shape) != shape or t.dtype != kind or not t.is_contiguous():
                 raise ValueError(f"a contiguous {kind} tensor of shape {shape} expected, got {t.dtype} {tuple(t.shape)}")
-        if not all(t.is_cuda for t in (k, v, k_scale, v_scale, refs, pages, length)):
-            raise ValueError("the cache's tensors live on a CUDA device")
+        if not all(t.is_cuda and t.device == k.device for t in (k, v, k_scale, v_scale, refs, pages, length)):
+            raise ValueError("the cache's tensors live on one CUDA device")
         self.k, self.v, self.k_scale, self.v_scale, self.refs, self.pages, self.length = k, v, k_scale, v_scale, refs, pages, length
         self.fmt, self.layout = fmt, layout
         self.layers, self.num_pages, self.page_tokens, self.kv_heads, self.head_dim = layers, num_pages, tokens, heads, dim
         self.max_seqs, self.max_pages = pages.shape
+        self.index = k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.c = _KVCache(layers, num_pages, tokens, heads, dim, _FORMATS[fmt], _LAYOUTS[layout], self.max_seqs, self.max_pages,
                           k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k_scale.data_ptr(), v_scale.data_ptr(),
                           refs.data_ptr(), pages.data_ptr(), length.data_ptr(), self.status.data_ptr())
         self.ref = C.byref(self.c)
-        self._bytes = int(_dll.roomie_kv_workspace_bytes(self.ref))
+        with torch.cuda.device(k.device):                # the size follows the device's number of SMs
+            self._bytes = int(_dll.roomie_kv_workspace_bytes(self.ref))
         if self._bytes == 0:
             raise ValueError("cache shape outside the library's limits (page_tokens 16..128, head_dim a multiple of 16 up to 256)")
 
@@ -209,6 +225,9 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
         q_offset = _ids(q_offset, "q_offset", n + 1)
     elif rows != n:
         raise ValueError("without q_offset every sequence brings one row")
+    _here(cache.index, seqs, q_offset, k, v, q, q_out)
+    if rope is not None and rope.index != cache.index:
+        raise ValueError("rope: a table on the cache's device")
     ck, cv = _rows(k, "k"), _rows(v, "v")
     turn = rope is not None and q is not None
     if turn:
@@ -237,6 +256,7 @@ def kv_attention(cache: KVCache, seqs, q, q_offset=None, *, layer=0, scale=None,
         q_offset = _ids(q_offset, "q_offset", n + 1)
     elif rows != n:
         raise ValueError("without q_offset every sequence brings one row")
+    _here(cache.index, seqs, q_offset, q, out, lse, workspace)
     if out is None:
         out = torch.empty_like(q)
     elif out.shape != q.shape or out.dtype != q.dtype:
@@ -257,6 +277,7 @@ def kv_reserve(cache: KVCache, seqs, want, *, workspace=None):
     """roomie_kv_reserve: sequences get pages for `want` tokens and that length."""
     seqs = _ids(seqs, "seqs")
     want = _ids(want, "want", seqs.numel())
+    _here(cache.index, seqs, want, workspace)
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_reserve(cache.ref, seqs.data_ptr(), want.data_ptr(), seqs.numel(), workspace.data_ptr(), workspace.numel(),
                                   _stream(cache.k)), "roomie_kv_reserve")
@@ -267,6 +288,7 @@ def kv_fork(cache: KVCache, parents, children, *, workspace=None):
     """roomie_kv_fork: children become copies of parents; whole pages shared, part-filled last pages copied."""
     parents = _ids(parents, "parents")
     children = _ids(children, "children", parents.numel())
+    _here(cache.index, parents, children, workspace)
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_fork(cache.ref, parents.data_ptr(), children.data_ptr(), parents.numel(), workspace.data_ptr(),
                                workspace.numel(), _stream(cache.k)), "roomie_kv_fork")
@@ -276,6 +298,7 @@ def kv_fork(cache: KVCache, parents, children, *, workspace=None):
 def kv_free(cache: KVCache, seqs):
     """roomie_kv_free: the sequences become empty, their pages lose a reference."""
     seqs = _ids(seqs, "seqs")
+    _here(cache.index, seqs)
     _check(_dll.roomie_kv_free(cache.ref, seqs.data_ptr(), seqs.numel(), _stream(cache.k)), "roomie_kv_free")
 
 
@@ -284,6 +307,7 @@ def kv_copy(src: KVCache, src_pages, dst: KVCache, dst_pages):
     """roomie_kv_copy: page src_pages[i] of src to page dst_pages[i] of dst, all layers, codes and scales."""
     src_pages = _ids(src_pages, "src_pages")
     dst_pages = _ids(dst_pages, "dst_pages", src_pages.numel())
+    _here(src.index, dst.k, src_pages, dst_pages)
     _check(_dll.roomie_kv_copy(src.ref, src_pages.data_ptr(), dst.ref, dst_pages.data_ptr(), src_pages.numel(), _stream(src.k)),
            "roomie_kv_copy")
 
@@ -299,6 +323,7 @@ def kv_compact(cache: KVCache, *, refs_out=None, pages_out=None, used_out=None, 
             raise ValueError("refs_out, pages_out: the shape and type of the cache's refs and pages")
     if used_out is not None:
         _ids(used_out, "used_out", 1)
+    _here(cache.index, refs_out, pages_out, used_out, workspace)
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_compact(cache.ref, refs_out.data_ptr(), pages_out.data_ptr(), _ptr(used_out), workspace.data_ptr(),
                                   workspace.numel(), _stream(cache.k)), "roomie_kv_compact")

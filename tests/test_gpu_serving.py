@@ -1038,6 +1038,24 @@ def test_other_streams_and_graphs(torch, rm):
     assert torch.equal(out, step())
 
 
+def test_tensors_of_another_device_are_refused(torch, rm, monkeypatch):
+    """Every call looks at the current device before it launches anything (here it is told of another one)."""
+    cache = make_cache(torch, rm, [30, 20], page=16, dim=32, garbage=False)
+    ws, table, ids = cache.workspace(), rm.RopeTable(32), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    k, out = torch.zeros((2, 2, 32), device="cuda").half(), torch.zeros((2, 2, 32), device="cuda").half()
+    lse = torch.zeros((2, 2), device="cuda")
+    before = [t.clone() for t in (cache.k, cache.v, cache.refs, cache.pages, cache.length)]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 7)
+    for call in (lambda: rm.rope(k, ids, table, out=out), lambda: rm.kv_append(cache, ids, k, k, rope=table, q=k, q_out=out),
+                 lambda: rm.kv_attention(cache, ids, k, out=out, lse=lse, workspace=ws), lambda: rm.kv_reserve(cache, ids, ids, workspace=ws),
+                 lambda: rm.kv_fork(cache, ids, ids, workspace=ws), lambda: rm.kv_free(cache, ids), lambda: rm.kv_copy(cache, ids, cache, ids),
+                 lambda: rm.kv_compact(cache, workspace=ws)):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
+    monkeypatch.undo()
+    assert all(torch.equal(a, b) for a, b in zip(before, (cache.k, cache.v, cache.refs, cache.pages, cache.length)))
+
+
 def test_serving_step_and_its_profile(torch, rm):
     """Reserve, append, attend, fork and free as one path; its launches become a profile that the model scores."""
     import roomie_synth as rs

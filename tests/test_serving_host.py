@@ -112,6 +112,19 @@ def test_page_refusals():
     assert dll.roomie_kv_compact(ref, FAKE, FAKE, None, FAKE, need - 256, None) == -4
 
 
+def test_tensors_of_a_call_live_on_the_current_device(monkeypatch):
+    class Tensor:
+        def __init__(self, device):
+            self.device = device
+        def get_device(self):
+            return self.device
+    monkeypatch.setattr(serving.torch.cuda, "current_device", lambda: 1)
+    serving._here(1, Tensor(1), None, Tensor(1))
+    for bad in ((0,), (0, Tensor(1)), (1, Tensor(1), Tensor(0)), (1, None, Tensor(-1))):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            serving._here(*bad)
+
+
 def test_record_without_launches():
     count = C.c_uint32(7)
     assert dll.roomie_record_enable(0) == 0
