@@ -126,7 +126,11 @@ class RopeTable:
 @_on_stream
 def rope(x, positions, table: RopeTable, *, inverse=False, out=None):
     """roomie_rope: x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); `inverse` is the gradient.
-    `out` may be x itself.  Returns out."""
+    `out` may be x itself.  Returns out.  Without `out` the call is differentiable in x."""
+    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+        if out is not None:
+            raise ValueError("out: not where a gradient is wanted")
+        return _Turn.apply(x, _ids(positions, "positions"), table, inverse)
     cx = _rows(x, "x")
     n, h, d = x.shape
     positions = _ids(positions, "positions", n)
@@ -137,6 +141,21 @@ def rope(x, positions, table: RopeTable, *, inverse=False, out=None):
         raise ValueError("out: the shape and type of x")
     _check(_dll.roomie_rope(table.ref, cx, _rows(out, "out"), n, h, d, positions.data_ptr(), inverse, _stream(x)), "roomie_rope")
     return out
+
+
+class _Turn(torch.autograd.Function):
+    """The rotation where a gradient is wanted: the gradient is the turn back, which can be differentiated again."""
+
+    @staticmethod
+    def forward(ctx, x, positions, table, inverse):
+        ctx.save_for_backward(positions)
+        ctx.table, ctx.inverse = table, inverse
+        return rope(x, positions, table, inverse=inverse)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, = ctx.saved_tensors
+        return rope(grad if grad.stride(2) == 1 else grad.contiguous(), positions, ctx.table, inverse=not ctx.inverse), None, None, None
 
 
 class KVCache:
@@ -215,7 +234,7 @@ def _scratch(cache, workspace):
 def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeTable | None = None, q=None, q_out=None):
     """roomie_kv_append: rows of k, v [rows, kv_heads, head_dim] become the last tokens of sequences `seqs` (rows
     q_offset[i]..q_offset[i+1] of sequence i; None: one row each), rotated when `rope` is given.  With `q` its rotated rows are
-    returned (q itself without `rope`)."""
+    returned (q itself without `rope`).  For serving: no gradient passes through."""
     rows, d = k.shape[0], cache.head_dim
     if k.shape[1:] != (cache.kv_heads, d) or k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k, v: [rows, kv_heads, head_dim] of one type")
@@ -246,7 +265,8 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
 
 @_on_stream
 def kv_attention(cache: KVCache, seqs, q, q_offset=None, *, layer=0, scale=None, window=0, out=None, lse=None, workspace=None):
-    """roomie_kv_attention: q [rows, q_heads, head_dim] over the cached tokens of `seqs`.  Returns (out, lse)."""
+    """roomie_kv_attention: q [rows, q_heads, head_dim] over the cached tokens of `seqs`.  Returns (out, lse); rows of no sequence are
+    not written.  For serving: no gradient passes through."""
     rows, heads, d = q.shape
     if d != cache.head_dim or heads % cache.kv_heads:
         raise ValueError("q: [rows, q_heads, head_dim] with q_heads a multiple of the cache's kv_heads")

@@ -106,6 +106,38 @@ def test_rope_gradient_is_the_transpose_and_the_difference(torch, rm):
             assert abs(slope - float(grad[at])) < 2 * 8e-6 * 5 / h
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_rope_is_differentiable(torch, rm, interleaved, dtype):
+    """The gradient that autograd finds is the turn back, of ordinary, broadcast and strided inputs and of gradients with zero strides; a second
+    derivative; and where no gradient can pass the call says so."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    table = rm.RopeTable(32, interleaved=interleaved, amplitude=1.5)
+    new = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(dtype_of(torch, dtype))
+    p = torch.tensor([3, 0, 70001, 12], dtype=torch.int32, device="cuda")
+    for inverse in (False, True):
+        x, g = new(4, 5, 48).requires_grad_(), new(4, 5, 48)
+        y = rm.rope(x, p, table, inverse=inverse)
+        assert torch.equal(y, rm.rope(x.detach(), p, table, inverse=inverse))
+        y.backward(g)
+        assert torch.equal(x.grad, rm.rope(g, p, table, inverse=not inverse))
+    one = new(4, 1, 48).requires_grad_()                               # one head shared by all
+    rm.rope(one.expand(4, 5, 48), p, table).backward(g)
+    turned = host(rm.rope(g, p, table, inverse=True))
+    assert np.all(np.abs(host(one.grad)[:, 0] - turned.sum(1)) <= 6 * U[dtype] * np.abs(turned).sum(1) + 1e-30)
+    x = new(4, 5, 48).requires_grad_()
+    rm.rope(x, p.tolist(), table).sum().backward()                     # a gradient with strides of zero
+    assert torch.equal(x.grad, rm.rope(torch.ones_like(x), p, table, inverse=True))
+    w = new(4, 5, 48).requires_grad_()                                 # of (w . turn back g) by g: the turn of w
+    grad, = torch.autograd.grad(rm.rope(x, p, table), x, w, create_graph=True)
+    again, = torch.autograd.grad(grad, w, g)
+    assert torch.equal(again, rm.rope(g, p, table))
+    with pytest.raises(ValueError, match="gradient"):
+        rm.rope(x, p, table, out=torch.empty_like(g))
+    with torch.no_grad():
+        assert not rm.rope(x, p, table, out=torch.empty_like(g)).requires_grad and not rm.rope(x, p, table).requires_grad
+
+
 def test_rope_stretched_frequencies(torch, rm):
     """By parts: slow frequencies divided, fast ones kept, a mix between; without a context all divided."""
     plain, all_slow = rm.rope_frequencies(64), rm.rope_frequencies(64, factor=8.0)
