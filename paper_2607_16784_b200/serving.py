@@ -234,7 +234,7 @@ def _scratch(cache, workspace):
 def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeTable | None = None, q=None, q_out=None):
     """roomie_kv_append: rows of k, v [rows, kv_heads, head_dim] become the last tokens of sequences `seqs` (rows
     q_offset[i]..q_offset[i+1] of sequence i; None: one row each), rotated when `rope` is given.  With `q` its rotated rows are
-    returned (q itself without `rope`).  For serving: no gradient passes through."""
+    returned in q_out (q itself, or its copy in q_out, without `rope`).  For serving: no gradient passes through."""
     rows, d = k.shape[0], cache.head_dim
     if k.shape[1:] != (cache.kv_heads, d) or k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k, v: [rows, kv_heads, head_dim] of one type")
@@ -249,17 +249,23 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
         raise ValueError("rope: a table on the cache's device")
     ck, cv = _rows(k, "k"), _rows(v, "v")
     turn = rope is not None and q is not None
-    if turn:
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out: without q there is nothing to write")
+    elif turn or q_out is not None:
         if q.dim() != 3 or q.shape[0] != rows or q.shape[2] != d or q.dtype != k.dtype:
             raise ValueError("q: [rows, q_heads, head_dim] of k's type")
+        if q_out is not None and (q_out.shape != q.shape or q_out.dtype != q.dtype):
+            raise ValueError("q_out: the shape and type of q")
+    if turn:
         if q_out is None:
             q_out = torch.empty_like(q)
-        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
-            raise ValueError("q_out: the shape and type of q")
         cq, co = _rows(q, "q"), _rows(q_out, "q_out")
     _check(_dll.roomie_kv_append(cache.ref, layer, seqs.data_ptr(), n, None if q_offset is None else q_offset.data_ptr(), rows, ck, cv,
                                  rope.ref if rope is not None else None, q.shape[1] if turn else 0, cq if turn else None,
                                  co if turn else None, _stream(k)), "roomie_kv_append")
+    if not turn and q_out is not None:
+        return q_out.copy_(q)
     return q_out if turn else q
 
 

@@ -406,6 +406,20 @@ def test_append_many_queries(torch, rm):
     assert rm.kv_append(cache, ids, k, k, rows, rope=table, q=q, q_out=q) is q and torch.equal(q, want)
 
 
+def test_append_without_rope_fills_q_out(torch, rm):
+    """Where nothing turns the queries, q_out is their copy; without q there is nothing to write."""
+    cache = make_cache(torch, rm, [20, 30], page=16, dim=32, garbage=False)
+    k, q = torch.randn((2, 2, 32), device="cuda").half(), torch.randn((2, 4, 32), device="cuda").half()
+    assert rm.kv_append(cache, [0, 1], k, k, q=q) is q and rm.kv_append(cache, [0, 1], k, k) is None
+    wide = torch.zeros((2, 6, 32), device="cuda").half()
+    out = wide[:, 1:5]
+    assert rm.kv_append(cache, [0, 1], k, k, q=q, q_out=out) is out and torch.equal(out, q) and not wide[:, 0].any() and not wide[:, 5].any()
+    assert rm.kv_append(cache, [0, 1], k, k, q=q, q_out=q) is q and torch.equal(out, q)
+    for bad in (dict(q_out=out), dict(q=q, q_out=out[:1]), dict(q=q, q_out=out.float()), dict(q=q[:1], q_out=out[:1])):
+        with pytest.raises(ValueError):
+            rm.kv_append(cache, [0, 1], k, k, **bad)
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("turned", [64, 6])
 def test_append_passes_rows_of_no_sequence_on(torch, rm, interleaved, turned):
