@@ -125,6 +125,19 @@ def test_tensors_of_a_call_live_on_the_current_device(monkeypatch):
             serving._here(*bad)
 
 
+def test_binding_needs_no_private_name(monkeypatch):
+    """Without torch's short way to a stream the binding is imported all the same and asks the public one."""
+    import importlib.util
+    from types import SimpleNamespace
+    if hasattr(serving.torch._C, "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(serving.torch._C, "_cuda_getCurrentRawStream")
+    spec = importlib.util.spec_from_file_location(serving.__name__ + "_again", serving.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    monkeypatch.setattr(again.torch.cuda, "current_stream", lambda device: SimpleNamespace(cuda_stream=40 + device))
+    assert again._stream(SimpleNamespace(get_device=lambda: 2)) == 42
+
+
 def test_record_without_launches():
     count = C.c_uint32(7)
     assert dll.roomie_record_enable(0) == 0
