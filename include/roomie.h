@@ -394,7 +394,8 @@ int roomie_profile_walk_ms(float *total_ms /* host */, uint32_t *launches /* hos
 #define ROOMIE_BF16 2
 
 /* Rows of heads: element (token, head, d) lies at data[token*token_stride + head*head_stride + d]
- * (strides in elements; any element-aligned address is accepted, 16-byte aligned ones are faster). */
+ * (strides in elements; any element-aligned address is accepted, 16-byte aligned ones are faster).  Inputs may have strides of 0;
+ * rows of an output share no element: strides of head_dim or more. */
 typedef struct roomie_rows {
     void *data;
     int32_t type;         /* ROOMIE_F32 / F16 / BF16 */

@@ -332,6 +332,7 @@ extern "C" int roomie_kv_append(const roomie_kv_cache* cache, uint32_t layer, co
     if (rope && !rope_table_valid(rope, cache->head_dim)) return ROOMIE_ERR_INVALID_ARG;
     if ((q != nullptr) != (q_out != nullptr)) return ROOMIE_ERR_INVALID_ARG;
     if (q && (!rope || q_heads == 0 || !rows_valid(q) || !rows_valid(q_out) || q->type != q_out->type || q->type != k->type ||
+              !rows_apart(*q_out, rows, q_heads, cache->head_dim) ||
               (q->data == q_out->data && (q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride))))
         return ROOMIE_ERR_INVALID_ARG;
     if (!seqs || (!q_offset && rows != num_seqs) || rows > 0x3fffffffu || num_seqs > 0x3fffffffu ||

@@ -715,7 +715,8 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
         !(scale < INFINITY) || window > 0x7fffffffu)
         return ROOMIE_ERR_INVALID_ARG;
     if (num_seqs == 0 || rows == 0) return ROOMIE_OK;
-    if (!rows_valid(q) || !rows_valid(out) || q->type != out->type || q->type == ROOMIE_F32) return ROOMIE_ERR_INVALID_ARG;
+    if (!rows_valid(q) || !rows_valid(out) || q->type != out->type || q->type == ROOMIE_F32 || !rows_apart(*out, rows, q_heads, cache->head_dim))
+        return ROOMIE_ERR_INVALID_ARG;
     if (!seqs || (!q_offset && rows != num_seqs) || num_seqs > 0x3fffffffu || (unsigned long long)rows * q_heads > 0x3fffffffull)
         return ROOMIE_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ROOMIE_ERR_INVALID_ARG;

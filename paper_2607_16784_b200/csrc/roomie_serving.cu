@@ -123,7 +123,7 @@ extern "C" int roomie_rope(const roomie_rope_table* table, const roomie_rows* x,
                            uint32_t heads, uint32_t head_dim, const int32_t* positions, int inverse, void* stream) {
     if (!rope_table_valid(table, head_dim) || head_dim > 1024) return ROOMIE_ERR_INVALID_ARG;
     if (tokens == 0 || heads == 0) return ROOMIE_OK;
-    if (!rows_valid(x) || !rows_valid(y) || x->type != y->type || !positions) return ROOMIE_ERR_INVALID_ARG;
+    if (!rows_valid(x) || !rows_valid(y) || x->type != y->type || !positions || !rows_apart(*y, tokens, heads, head_dim)) return ROOMIE_ERR_INVALID_ARG;
     const bool same = x->data == y->data;
     if (same && (x->token_stride != y->token_stride || x->head_stride != y->head_stride)) return ROOMIE_ERR_INVALID_ARG;
     if ((unsigned long long)tokens * heads > 0x7fffffffull) return ROOMIE_ERR_INVALID_ARG;

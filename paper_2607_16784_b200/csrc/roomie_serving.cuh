@@ -78,6 +78,12 @@ inline bool rows_aligned16(const roomie_rows& r, uint32_t tokens, uint32_t heads
     return (reinterpret_cast<uintptr_t>(r.data) & 15u) == 0 && (tokens <= 1 || (r.token_stride * e) % 16 == 0) &&
            (heads <= 1 || (r.head_stride * e) % 16 == 0);
 }
+// no two rows of an output share an element (a stride of 0, or below a row's length: several threads would write it, and one that is
+// turned in place would be turned more than once)
+inline bool rows_apart(const roomie_rows& r, uint32_t tokens, uint32_t heads, uint32_t dim) {
+    const long long d = dim;
+    return (tokens <= 1 || r.token_stride >= d || r.token_stride <= -d) && (heads <= 1 || r.head_stride >= d || r.head_stride <= -d);
+}
 inline bool rows_valid(const roomie_rows* r) {
     return r && r->data && known_type(r->type) && (reinterpret_cast<uintptr_t>(r->data) % size_of_type(r->type)) == 0;
 }

@@ -4,6 +4,7 @@ import math
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2607_16784_b200 as rm
 from paper_2607_16784_b200 import roomie, serving
@@ -136,6 +137,25 @@ def test_binding_needs_no_private_name(monkeypatch):
     spec.loader.exec_module(again)
     monkeypatch.setattr(again.torch.cuda, "current_stream", lambda device: SimpleNamespace(cuda_stream=40 + device))
     assert again._stream(SimpleNamespace(get_device=lambda: 2)) == 42
+
+
+def test_outputs_whose_rows_share_elements_are_refused():
+    """Strides of 0 and below a row's length, of rope's, append's and attention's outputs; one token or one head has no such stride."""
+    c, t, need = cache(), table(), size()
+    def turn(out, tokens=4, heads=4):
+        return dll.roomie_rope(C.byref(t), rows(), out, tokens, heads, 128, FAKE, 0, None)
+    def append(out, heads=8):
+        return dll.roomie_kv_append(C.byref(c), 0, FAKE, 2, None, 2, rows(), rows(), C.byref(t), heads, rows(FAKE + 4096), out, None)
+    def attend(out, heads=8):
+        return dll.roomie_kv_attention(C.byref(c), 0, FAKE, 2, None, 2, heads, rows(), 0.1, 0, out, None, FAKE, need, None)
+    for call in (turn, append, attend):
+        for bad in (dict(token=0), dict(head=0), dict(token=127), dict(head=64), dict(token=-100), dict(token=0, head=0)):
+            assert call(rows(FAKE + (1 << 20), **bad)) == -1, (call, bad)
+    assert turn(rows(FAKE, token=0, head=0)) == -1                     # in place on a broadcast input: it would be turned several times
+    if not torch.cuda.is_available():                                  # accepted: only the launch finds no device
+        for good in (turn(rows(FAKE + (1 << 20), token=0), tokens=1), turn(rows(FAKE + (1 << 20), head=0), heads=1),
+                     turn(rows(FAKE + (1 << 20), token=-512, head=128)), turn(rows(FAKE + (1 << 20), token=128, head=512))):
+            assert good == -3
 
 
 def test_record_without_launches():
