@@ -113,30 +113,30 @@ static uint32_t copy_blocks(const CopyArgs& a, unsigned long long pairs) {
 // ---- a block's view of the free pages ----------------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
 
-// exclusive prefix sum over the block of one value a thread; `total` for all.  sh: kPlanWarps + 1 words.
-__device__ __forceinline__ uint32_t block_exclusive(uint32_t x, uint32_t& total, uint32_t* sh) {
+// exclusive prefix sum over the block of one value a thread; `total` for all.  sh: kPlanWarps values.
+template <class V> __device__ __forceinline__ V block_exclusive(V x, V& total, V* sh) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    uint32_t incl = x;
+    V incl = x;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t up = __shfl_up_sync(0xffffffffu, incl, d);
+        const V up = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += up;
     }
     __syncthreads();
     if (lane == 31) sh[wid] = incl;
     __syncthreads();
     if (wid == 0) {
-        uint32_t w = sh[lane];
+        V w = sh[lane];
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const uint32_t up = __shfl_up_sync(0xffffffffu, w, d);
+            const V up = __shfl_up_sync(0xffffffffu, w, d);
             if (lane >= d) w += up;
         }
         sh[lane] = w;
     }
     __syncthreads();
     total = sh[kPlanWarps - 1];
-    return (wid ? sh[wid - 1] : 0u) + incl - x;
+    return (wid ? sh[wid - 1] : V(0)) + incl - x;
 }
 
 // Writes the lowest `want` free pages to list, ascending; returns how many there are.
@@ -157,7 +157,7 @@ __device__ uint32_t lowest_free(const int32_t* refs, uint32_t num_pages, uint32_
                 if (p0 + e < num_pages && refs[p0 + e] == 0) free |= 1u << e;
         }
         uint32_t all;
-        uint32_t at = found + block_exclusive(__popc(free), all, sh);
+        uint32_t at = found + block_exclusive((uint32_t)__popc(free), all, sh);
         while (free && at < want) {
             list[at++] = (int32_t)(p0 + __ffs(free) - 1);
             free &= free - 1;
@@ -184,18 +184,20 @@ __device__ __forceinline__ uint32_t pages_of(const TableView& t, uint32_t tokens
 }
 
 // One block.  need[i] = pages request i wants (0 for one that is refused, with state[i] = -1); afterwards first[i] is where its
-// pages begin in list, and the return value is how many of list exist.
+// pages begin in list, and the return value is how many of list exist.  Sums are 64 bits wide: what is asked for may be any multiple of
+// what there is.
 __device__ uint32_t serve(const TableView& t, uint32_t n, const int32_t* need, int32_t* first, int32_t* list, uint32_t limit, uint32_t* sh) {
-    uint32_t carry = 0;
+    __shared__ unsigned long long sums[kPlanWarps];
+    unsigned long long carry = 0;
     for (uint32_t base = 0; base < n; base += kPlanThreads) {
         const uint32_t i = base + threadIdx.x;
-        uint32_t all;
-        const uint32_t x = i < n ? (uint32_t)need[i] : 0u;
-        const uint32_t at = block_exclusive(x, all, sh);
-        if (i < n) first[i] = (int32_t)min(carry + at, 0x7fffffffu);
-        carry = min(carry + all, 0x3fffffffu);
+        unsigned long long all;
+        const unsigned long long x = i < n ? (uint32_t)need[i] : 0u;
+        const unsigned long long at = carry + block_exclusive(x, all, sums);
+        if (i < n) first[i] = (int32_t)min(at, 0x7fffffffull);
+        carry += all;
     }
-    return lowest_free(t.refs, t.num_pages, min(carry, limit), list, sh);
+    return lowest_free(t.refs, t.num_pages, (uint32_t)min(carry, (unsigned long long)limit), list, sh);
 }
 
 // Workspace of n requests: need, first (n words each), the list of free pages (num_pages), refused (n).

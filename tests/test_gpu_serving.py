@@ -1010,6 +1010,16 @@ def test_pages_run_out_in_order(torch, rm):
     b.fork([0, 1, 0, 1], [4, 5, 6, 7], flags=FLAG_FULL)              # two pages are left
 
 
+def test_pages_asked_for_add_up_past_32_bits(torch, rm):
+    """1024 requests of 2^22 pages each, together 2^32, and a small one behind them: none is served."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 17 GB of device memory for the page table")
+    cache = rm.KVCache(8, 16, 1, 16, 1026, 1 << 22)
+    rm.kv_reserve(cache, list(range(1025)), [16 << 22] * 1024 + [16])
+    assert cache.status_flags() == FLAG_FULL
+    assert not cache.refs.any() and not cache.length.any() and (cache.pages[:, 0] == -1).all()
+
+
 def test_pages_refusals_on_the_device(torch, rm):
     b = Both(torch, rm, 10, 16, 6, 3)
     b.reserve([0, 1], [20, 30])
