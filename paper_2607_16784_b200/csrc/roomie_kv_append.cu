@@ -17,7 +17,6 @@ struct AppendArgs {
     unsigned long long q_threads;
 };
 
-constexpr unsigned long long kApartBytes = 4ull << 20;
 constexpr int kAppendThreads = 512, kAppendWarps = kAppendThreads / 32;
 
 // The `j`-th (sequence, page) in which the call's sequences have new tokens: every thread of the block gets the same answer.
@@ -279,42 +278,34 @@ __device__ void append_queries(const AppendArgs& a, unsigned long long i) {
         turned = row >= q.row && row < q.row + q.count && q.count <= q.length;
         if (turned) position = (int32_t)(q.start + (row - q.row));
     }
-    // a row of no sequence; a loop of its own, because a condition in the other costs 1.3 us of 89 (17000 tokens)
+    // a row of no sequence; a loop of its own, because a condition in the other costs 1.3 us of the 50 that 17000 rows of queries alone take
     if (!turned) return rope_copy<T, kV, kPairs>(a.q, a.rope, row, unit, group, a.q_groups, a.q_heads);
     rope_heads<T, kV, kPairs, kV == 1 ? 1 : 2>(a.q, a.rope, row, position, false, unit, group, a.q_groups, a.q_heads);
 }
 
-// Blocks [0, 2 * kv_blocks): page j of the call, keys (even) and values (odd); the rest: queries.  One launch for the three, because
-// a decoding step's share of each is far below a launch's cost.
+// Blocks [0, 2 * kv_blocks): page j of the call, keys (even) and values (odd); the rest: queries.  One launch for the three: a decoding
+// step's share of each is far below a launch's cost (64 sequences: 13.5 us a call, with the queries in a launch of their own 15.4), and for
+// many rows the two would follow each other, because two blocks of keys and values take all of an SM's registers (us, one launch and two;
+// 32 query heads on 8, 128 dims, bfloat16, with the queries' MB):
+//   rows       512 (4)      2048 (16)    4096 (32)    8192 (64)    17000 (133)
+//              18.9 20.5    20.9 24.7    26.7 30.9    45.0 47.1    84.8 87.7
+// (Other heads and types: as many rows as leave the last wave of blocks short lose 2 to 18 % by it, 12000 rows win up to 22 %.)
 template <class T, int kV, bool kPairs>
 __global__ void __launch_bounds__(kAppendThreads, 2) append_kernel(AppendArgs a) {
     __shared__ uint32_t sh[24];
     __shared__ float shf[kAppendWarps];
-    grid_dependency_launch();                                             // the queries' kernel needs nothing of this one
     if (blockIdx.x < 2 * a.kv_blocks) append_page<T, kV, kPairs>(a, blockIdx.x >> 1, (blockIdx.x & 1) == 0, sh, shf);
     else append_queries<T, kV, kPairs>(a, (unsigned long long)(blockIdx.x - 2 * a.kv_blocks) * kAppendThreads + threadIdx.x);
 }
 
-// The queries alone, with the registers that they need.
-constexpr int kQueryThreads = 128;
-template <class T, int kV, bool kPairs>
-__global__ void __launch_bounds__(kQueryThreads, 8) append_queries_kernel(AppendArgs a) {
-    append_queries<T, kV, kPairs>(a, (unsigned long long)blockIdx.x * kQueryThreads + threadIdx.x);
-    grid_dependency_wait();                                               // it started beside the keys and values; what follows waits for both
-}
-
 template <class T>
-static int launch_append(const AppendArgs& a, bool wide, bool pairs, bool apart, cudaStream_t st) {
+static int launch_append(const AppendArgs& a, bool wide, bool pairs, cudaStream_t st) {
     constexpr int v = kVecOf<T>;
     void (*k)(AppendArgs);
     if (pairs) k = wide ? append_kernel<T, v, true> : append_kernel<T, 1, true>;
     else k = wide ? append_kernel<T, v, false> : append_kernel<T, 1, false>;
-    const unsigned long long beside = apart ? 0 : (a.q_threads + kAppendThreads - 1) / kAppendThreads;
-    const int rc = launch("kv_append", k, dim3((uint32_t)(2 * a.kv_blocks + beside)), dim3(kAppendThreads), 0, st, false, a);
-    if (rc != ROOMIE_OK || !apart) return rc;
-    if (pairs) k = wide ? append_queries_kernel<T, v, true> : append_queries_kernel<T, 1, true>;
-    else k = wide ? append_queries_kernel<T, v, false> : append_queries_kernel<T, 1, false>;
-    return launch("kv_append_queries", k, dim3((uint32_t)((a.q_threads + kQueryThreads - 1) / kQueryThreads)), dim3(kQueryThreads), 0, st, true, a);
+    const unsigned long long queries = (a.q_threads + kAppendThreads - 1) / kAppendThreads;
+    return launch("kv_append", k, dim3((uint32_t)(2 * a.kv_blocks + queries)), dim3(kAppendThreads), 0, st, false, a);
 }
 
 }  // namespace roomie
@@ -360,14 +351,12 @@ extern "C" int roomie_kv_append(const roomie_kv_cache* cache, uint32_t layer, co
         const RopeSplit s = rope_split(rows, q_heads, cache->head_dim, rope->rotary_dim, wide ? 16u / (uint32_t)size_of_type(k->type) : 1u,
                                        q->data == q_out->data, (uint32_t)sm_count());
         a.q_units = s.units; a.q_groups = s.groups; a.q_threads = s.threads;
-        q_blocks = (s.threads + kQueryThreads - 1) / kQueryThreads;
+        q_blocks = (s.threads + kAppendThreads - 1) / kAppendThreads;
     }
     if (q_blocks + 2ull * a.kv_blocks > 0x7fffffffull) return ROOMIE_ERR_INVALID_ARG;
-    // Many queries go in a launch of their own: beside the keys and values they have too few registers to keep the memory busy
-    const bool apart = q && (unsigned long long)rows * q_heads * cache->head_dim * size_of_type(k->type) >= kApartBytes;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool pairs = rope && rope->interleaved;
-    if (k->type == ROOMIE_F32) return launch_append<float>(a, wide, pairs, apart, st);
-    if (k->type == ROOMIE_F16) return launch_append<__half>(a, wide, pairs, apart, st);
-    return launch_append<__nv_bfloat16>(a, wide, pairs, apart, st);
+    if (k->type == ROOMIE_F32) return launch_append<float>(a, wide, pairs, st);
+    if (k->type == ROOMIE_F16) return launch_append<__half>(a, wide, pairs, st);
+    return launch_append<__nv_bfloat16>(a, wide, pairs, st);
 }

@@ -44,7 +44,6 @@ int launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, si
 }
 
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_dependency_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- element types --------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float to_f32(float x) { return x; }

@@ -420,6 +420,17 @@ def test_append_without_rope_fills_q_out(torch, rm):
             rm.kv_append(cache, [0, 1], k, k, **bad)
 
 
+def test_append_is_one_launch(torch, rm):
+    """However many queries there are."""
+    table = rm.RopeTable(128)
+    for rows in (2, 2000):
+        cache = make_cache(torch, rm, [rows // 2, rows // 2], page=64, dim=128, heads=2, garbage=False)
+        k, q = torch.randn((rows, 2, 128), device="cuda").half(), torch.randn((rows, 16, 128), device="cuda").half()
+        with rm.record_launches() as launches:
+            rm.kv_append(cache, [0, 1], k, k, [0, rows // 2, rows], rope=table, q=q)
+        assert [r["name"] for r in launches] == ["kv_append"]
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("turned", [64, 6])
 def test_append_passes_rows_of_no_sequence_on(torch, rm, interleaved, turned):
