@@ -4,7 +4,8 @@
 
 One attention layer's worth of the model's serving operators runs as it would be used: prompts are reserved, rotated, quantised into the
 cache and attended to; some sequences are forked and decode on their own; the losers are freed and the pool is compacted.  The launches
-are recorded on the way.  Their configurations and isolated durations become one more profile beside a library of synthetic residents,
+are recorded on the way (the cache operators' own: a model's projections and other products come from other libraries).  Their
+configurations and isolated durations become one more profile beside a library of synthetic residents,
 the pairwise interference of all of them is evaluated, and the model is placed on the GPU of a small cluster where it is disturbed and
 disturbs least."""
 from __future__ import annotations

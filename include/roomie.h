@@ -13,9 +13,10 @@
  * General conventions
  *   - Every data pointer is a DEVICE pointer owned by the caller unless its comment says
  *     "host".  The library never allocates or frees device memory and keeps no pointer after a
- *     call returns; scratch space is passed in as `workspace`.  Two documented exceptions:
+ *     call returns; scratch space is passed in as `workspace`.  Three documented exceptions:
  *     roomie_pair_interference_static works in a fixed array inside the library image instead
- *     of a workspace, and roomie_profile_enable creates CUDA events (host-side objects).  On the
+ *     of a workspace, and roomie_profile_enable and roomie_record_enable create CUDA events (host-side
+ *     objects; the latter keeps its records in host memory until it is called with 0).  On the
  *     host, the size arithmetic of the pair calls keeps two small per-thread vectors.
  *   - Calls only enqueue work on `stream` (a cudaStream_t passed as void*, NULL = default
  *     stream) and return without synchronising, except where a comment says otherwise.
@@ -375,8 +376,9 @@ int roomie_profile_walk_ms(float *total_ms /* host */, uint32_t *launches /* hos
  * The models the placement rule distributes over GPUs have to run there, and how many fit is decided by
  * their caches.  These calls are one serving step over a paged cache of 8-bit keys and values: rotary
  * positions, quantise-and-append, attention, and the page operations that share, copy, free and pack cache
- * memory.  roomie_record_* turns the launches of such a step into the kernel table and times
- * roomie_library_build takes, so that a real step is scored against other residents like any profile.
+ * memory.  roomie_record_* turns the launches of these calls into the kernel table and times
+ * roomie_library_build takes, so that the cache's share of a step is scored against other residents like any
+ * profile (a model's projections and other products are launches of other libraries and are not recorded).
  * The conventions at the top of this file hold: device pointers of the caller, nothing allocated, work is
  * only enqueued.  Data-dependent errors set sticky bits in the cache's `status` word and skip the access.
  * ==================================================================================================== */
@@ -452,8 +454,9 @@ typedef struct roomie_kv_cache {
 } roomie_kv_cache;
 
 /* Device scratch for the calls below that take a workspace: enough for any of them on this cache, 256-byte aligned.  Its first
- * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use; every call leaves them
- * so, unless ROOMIE_FLAG_WAIT_TIMEOUT shows up in the cache's status: zero them again then.  0 on invalid arguments. */
+ * ROOMIE_KV_WORKSPACE_ZEROED bytes must be zeroed once before its first use.  The calls leave those of them zero that have to be
+ * (counters) and write over the others; only if ROOMIE_FLAG_WAIT_TIMEOUT shows up in the cache's status they have to be zeroed again.
+ * 0 on invalid arguments. */
 #define ROOMIE_KV_WORKSPACE_ZEROED 16384u
 size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
 
@@ -462,8 +465,8 @@ size_t roomie_kv_workspace_bytes(const roomie_kv_cache *cache /* host */);
  * LAST positions of length[seqs[i]], which already counts them (roomie_kv_reserve sets it).  With `rope`, keys are
  * rotated to those positions first, and `q` ([rows][q_heads][head_dim], may be NULL) is rotated to q_out as well.
  * Each page and head gets the least power of two s with largest |value| / s within the format (a power of two,
- * so that a scale that has to grow while a page fills moves e4m3 codes without rounding them a second time; int8 pays
- * up to one bit for it); the scale of a page that holds earlier tokens never shrinks, and its earlier codes are
+ * so that a scale that has to grow while a page fills moves e4m3 codes without rounding them a second time, but for those that fall
+ * below the format's least normal value, 2^-6; int8 pays up to one bit for it); the scale of a page that holds earlier tokens never shrinks, and its earlier codes are
  * rescaled when it grows.  Float32 arithmetic on values of any ROOMIE_ type, rounded once to the code (nearest even).
  * q_out may be q (same strides).  A call names a row of the page table once.  Rows that belong to no sequence are not stored and their queries are passed on unrotated.
  * Errors: INVALID_ARG, CUDA. */

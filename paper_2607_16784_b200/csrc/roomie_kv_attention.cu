@@ -36,8 +36,8 @@ __device__ __forceinline__ SeqWork seq_work(const AttnArgs& a, uint32_t i, bool 
 // [r*DP/8, +DP/8) for its result rows r: both are whole 16-byte reads of the codes as they are stored.
 //
 // Every warp works for itself: it has kStages steps of keys and values under way to its own part of shared memory by asynchronous
-// copies (64 sequences of up to 16384 tokens in int8, 1.31 GB: 231 to 258 us by how the lengths fall, 5650 to 5090 GB/s; with one
-// step ahead in registers 297 where this takes 231).  A block walks a contiguous part of the flat order; its warps take the
+// copies (64 sequences of up to 16384 tokens in int8, 1.31 GB: 247 to 264 us from run to run, 5300 to 4960 GB/s; with one step ahead in
+// registers 297).  A block walks a contiguous part of the flat order; its warps take the
 // 16*kGroups-key steps in turn and meet at each (sequence, head, tile).  A part that does not hold all of a (sequence, head, tile)
 // leaves its sums in the workspace, and the last part to arrive adds them in order.
 //
@@ -125,8 +125,12 @@ __global__ void __launch_bounds__(kAttnThreads, DP > 128 || NT > 1 ? 2 : 3) few_
     const unsigned long long own_first = scan(mine, total);
     if (total == 0) return;
     // Work of few units a block is not cut at any unit but into equal parts of each item, items of up to kWhole units not at all, when
-    // that makes no more parts than blocks: fewer items then need joining (16 sequences of up to 4096 keys: 31 us, cut at any unit 37;
-    // three of up to 300: 8.3 and 10.4).
+    // that makes no more parts than blocks: fewer items then need joining.  Device times, us, equal parts where they fit and any cut (32
+    // query heads on 8, 128 dims, page 64; units a block by `most`):
+    //   sequences x keys   3 x 300    2 x 8192   16 x 4096  4 x 16384  | 64 x 2048  2 x 65536  64 x 4096  2 x 131072
+    //   units a block      1          2          7          7          | 14         14         28         28
+    //                      10.9 11.2  20.1 26.7  31.8 35.9  37.7 43.6  | 56.0 55.1  50.6 55.2  82.1 80.6  79.4 84.6
+    // Above kMostEqual units many items lose by it and few gain.
     uint32_t most = (uint32_t)min(total / gridDim.x + 1, 1ull << 30), own_parts = 0;
     unsigned long long own_first_part = 0, parts = total < gridDim.x ? total : gridDim.x;
     bool equal = a.num_seqs <= kAttnThreads && most <= kMostEqual;
@@ -735,7 +739,8 @@ extern "C" int roomie_kv_attention(const roomie_kv_cache* cache, uint32_t layer,
     a.counters = static_cast<uint32_t*>(workspace);
     const size_t blocks = (size_t)sm_count() * kMaxAttnBlocksPerSm;
     a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + (2 * blocks * sizeof(uint32_t) + 255) / 256 * 256);
-    // Rows a sequence and key head, on average (32 query heads on 8, sequences of up to 4096 keys, 16 of them and 2 of them, us):
+    // Which kernel, and how many rows a tile.  Measured on calls whose sequences bring alike; one that mixes single tokens with a chunk goes by
+    // its average.  Rows a sequence and key head (32 query heads on 8, sequences of up to 4096 keys, 16 of them and 2 of them, us):
     //   rows        8       16      24      32      64
     //   8 a tile    36 23   57 29   57 33   82 32   117 37
     //   16 a tile   36 23   52 33   61 33   84 39   106 42

@@ -92,7 +92,7 @@ template <int kFormat> __device__ __forceinline__ void codes_to_f16(uint32_t w, 
         asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
             : "=r"(lo), "=r"(hi) : "r"(w));
     } else {
-        // 0x6400 | u is 1024 + u in float16; u = code + 128
+        // 0x6400 | u is 1024 + u in float16; u = code + 128 (a published conversion: Kim, Henry, Fahim and Awadalla, 2022)
         const uint32_t u = w ^ 0x80808080u, bias = 0x64806480u;                   // 1152
         const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
         const __half2 x = __hsub2(reinterpret_cast<const __half2&>(l), reinterpret_cast<const __half2&>(bias));

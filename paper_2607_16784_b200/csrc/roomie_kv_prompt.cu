@@ -11,11 +11,12 @@
 // (the scales stay out of them); in warpgroup 4 a warp for each tile issues its products and one looks up pages and scales, some steps
 // ahead.  The flat order of all (sequence, head, tile, key block) is cut into one equal share a block.
 //
-// What bounds it: chunks of 1024 tokens over up to 8192 (32 query heads on 8, 128 dims) take 405 us, 801 TFLOP/s of the 1666 that a
-// plain matrix product reaches.  A step of 128 keys and two tiles takes some 4400 cycles, where the products have 2048, the
-// exponentials as many on the special-function units, and the operands' way through shared memory 2600: none of them is full, the
-// chain product - softmax - product of a tile is what is left, and tensor memory (512 columns: two S and two o) has no room for a third
-// tile to hide it behind.  Tried and slower: a quarter of the exponentials as polynomials (465 us against 464), tiles that take turns
+// What bounds it: chunks of 1024 tokens over up to 8192 (32 query heads on 8, 128 dims) take 415 us, 783 TFLOP/s of the 1666 that a
+// plain matrix product reaches (heads of 64: 356 us, 456 TFLOP/s; of 256: 938 us, 692).  A step of 128 keys and two tiles takes some 4500
+// cycles.  The products are 2048 of tensor work, but 2560 as they are fed: a 16-deep step of S, 64 columns wide, reads 6 KB of operands
+// from shared memory, 48 cycles of it for 32 of work.  The exponentials take some 2048 on the special-function units, the operands' way
+// through shared memory 2600.  None of them is full (tensor pipe 38 %); the chain product - softmax - product of a tile, with the loads from
+// tensor memory waited for one after the other, is what is left.  Tensor memory (512 columns: two S and two o) holds no third tile.  Tried and slower: a quarter of the exponentials as polynomials (465 us against 464), tiles that take turns
 // at the softmax (544 against 475), two threads a row (538 against 487).
 //
 // Scales.  A page's key scale multiplies 16 or more neighbouring columns of S: it goes into the factor of the exponent's argument.
@@ -146,7 +147,12 @@ template <int kRows> __device__ __forceinline__ PromptSeq prompt_seq(const AttnA
     return p;
 }
 // A tile's queries, first step and results cost a block about as much time as kTileCost steps: its share of the flat order has so many
-// units in front, which hold no key block.
+// units in front, which hold no key block.  Device times, us, by that number (32 query heads on 8; tokens a chunk over context):
+//        16 x 64/1024  2 x 512/4096  2048/2048  4 x 1024/8192  4 x 512/8192, heads of 256
+//   0    60.0          93.5          117.6      485.6          462
+//   2    53.0          84.1          89.3       485.6          445
+//   4    53.1          83.4          83.1       484.3          450
+//   8    49.5          90.0          90.4       482.4          467
 constexpr uint32_t kTileCost = 4;
 struct Blocks {
     uint32_t first, count;                          // key blocks that some row of the tile sees, at least one
