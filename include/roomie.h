@@ -431,6 +431,25 @@ int roomie_rope_frequencies(uint32_t rotary_dim, double base, double factor, dou
 int roomie_rope(const roomie_rope_table *table /* host */, const roomie_rows *x, const roomie_rows *y, uint32_t tokens,
                 uint32_t heads, uint32_t head_dim, const int32_t *positions, int inverse, void *stream);
 
+/* Norms of queries and keys for each head with their rotary positions, in one pass: y = rope(x * r * weight) with
+ * r = (mean(x^2) + eps)^(-1/2) over a head's head_dim elements (at most 256).  q and k have one type and `tokens` rows each; a side with 0 heads
+ * is left out.  Weights [head_dim] of weight_type, NULL: ones.  table NULL: no rotation (positions may be NULL then).  Float32
+ * arithmetic, rounded once; rows of any finite magnitude.  An output may be its input (same strides), otherwise they must not overlap.
+ * Since the positions are given, this also serves a cache whose lengths are no longer positions (roomie_kv_evict): append then takes no `rope`.
+ * Errors: INVALID_ARG, CUDA. */
+int roomie_qk_norm_rope(const roomie_rope_table *table /* host */, float eps, uint32_t tokens, uint32_t head_dim, const int32_t *positions,
+                        int32_t weight_type, uint32_t q_heads, const roomie_rows *q, const void *q_weight, const roomie_rows *q_out,
+                        uint32_t k_heads, const roomie_rows *k, const void *k_weight, const roomie_rows *k_out, void *stream);
+
+/* Its gradients: of gradients gq, gk of the results to dq, dk (which overlap nothing else) and to the weights, dq_weight and dk_weight of
+ * weight_type (NULL: not wanted).  The weights' sums are float32, in an order that depends on the shapes alone.  workspace: the bytes that
+ * roomie_qk_norm_rope_workspace_bytes tells, 4-byte aligned, nothing in it is kept.  Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
+size_t roomie_qk_norm_rope_workspace_bytes(uint32_t head_dim);
+int roomie_qk_norm_rope_grad(const roomie_rope_table *table /* host */, float eps, uint32_t tokens, uint32_t head_dim, const int32_t *positions,
+                             int32_t weight_type, uint32_t q_heads, const roomie_rows *q, const void *q_weight, const roomie_rows *gq,
+                             const roomie_rows *dq, void *dq_weight, uint32_t k_heads, const roomie_rows *k, const void *k_weight,
+                             const roomie_rows *gk, const roomie_rows *dk, void *dk_weight, void *workspace, size_t workspace_bytes, void *stream);
+
 #define ROOMIE_KV_E4M3 0 /* 1-4-3 floats, largest 448 */
 #define ROOMIE_KV_INT8 1 /* -127 .. 127               */
 #define ROOMIE_KV_HND 0  /* a page of one layer is [kv_heads][page_tokens][head_dim] */

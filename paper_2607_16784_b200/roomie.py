@@ -22,7 +22,8 @@ EXPORTS = [
     "roomie_multi_estimate", "roomie_place", "roomie_place_batch", "roomie_optimal_workspace_bytes",
     "roomie_optimal_assignment", "roomie_assignment_cost", "roomie_strerror", "roomie_last_cuda_error",
     "roomie_launch_count", "roomie_reset_launch_count", "roomie_profile_enable", "roomie_profile_walk_ms",
-    "roomie_rope_frequencies", "roomie_rope", "roomie_kv_workspace_bytes", "roomie_kv_append", "roomie_kv_attention",
+    "roomie_rope_frequencies", "roomie_rope", "roomie_qk_norm_rope", "roomie_qk_norm_rope_grad", "roomie_qk_norm_rope_workspace_bytes",
+    "roomie_kv_workspace_bytes", "roomie_kv_append", "roomie_kv_attention",
     "roomie_kv_reserve", "roomie_kv_fork", "roomie_kv_free", "roomie_kv_copy", "roomie_kv_compact",
     "roomie_record_enable", "roomie_record_read",
 ]
@@ -73,6 +74,11 @@ def _load():
     p, u32 = C.c_void_p, C.c_uint32
     dll.roomie_rope_frequencies.argtypes = [u32] + [C.c_double] * 5 + [p]
     dll.roomie_rope.argtypes = [p, p, p, u32, u32, u32, p, C.c_int, p]
+    norm = [p, C.c_float, u32, u32, p, C.c_int32]
+    dll.roomie_qk_norm_rope.argtypes = norm + 2 * [u32, p, p, p] + [p]
+    dll.roomie_qk_norm_rope_grad.argtypes = norm + 2 * [u32, p, p, p, p, p] + [p, C.c_size_t, p]
+    dll.roomie_qk_norm_rope_workspace_bytes.restype = C.c_size_t
+    dll.roomie_qk_norm_rope_workspace_bytes.argtypes = [u32]
     dll.roomie_kv_workspace_bytes.restype = C.c_size_t
     dll.roomie_kv_workspace_bytes.argtypes = [p]
     dll.roomie_kv_append.argtypes = [p, u32, p, u32, p, u32, p, p, p, u32, p, p, p]

@@ -159,6 +159,85 @@ class _Turn(torch.autograd.Function):
         return rope(grad if grad.stride(2) == 1 else grad.contiguous(), positions, ctx.table, inverse=not ctx.inverse), None, None, None
 
 
+def _head_weight(w, dim, like, what):
+    """(pointer, type) of a weight [head_dim], or of none."""
+    if w is None:
+        return None, like
+    kind = _TYPES.get(w.dtype)
+    if kind is None or tuple(w.shape) != (dim,) or not w.is_contiguous() or not w.is_cuda or (like is not None and kind != like):
+        raise ValueError(f"{what}: contiguous CUDA tensors [head_dim] of one type, float32, float16 or bfloat16")
+    return w.data_ptr(), kind
+
+
+def _norm_sides(q, k, q_weight, k_weight, positions, table, *others):
+    """What both directions check: (tokens, head_dim, positions, type of the weights, [(heads, weight)] of the sides)."""
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
+        raise ValueError("q, k: [tokens, heads, head_dim] of one type")
+    if k is None and k_weight is not None:
+        raise ValueError("k_weight: without k there is nothing to scale")
+    n, _, d = q.shape
+    qw, kind = _head_weight(q_weight, d, None, "q_weight, k_weight")
+    kw, kind = _head_weight(k_weight, d, kind, "q_weight, k_weight")
+    if table is not None:
+        positions = _ids(positions, "positions", n)
+    _here(q.get_device() if table is None else table.index, q, k, q_weight, k_weight, positions if table is not None else None, *others)
+    return n, d, positions.data_ptr() if table is not None else None, kind or 0, (q.shape[1], qw), (0 if k is None else k.shape[1], kw)
+
+
+def _norm_out(x, out, what):
+    if x is None:
+        if out is not None:
+            raise ValueError(f"{what}: without its input there is nothing to write")
+        return None
+    if out is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError(f"{what}: the shape and type of its input")
+    return out
+
+
+@_on_stream
+def qk_norm_rope(q, k, positions, table: RopeTable | None, q_weight=None, k_weight=None, *, eps=1e-6, q_out=None, k_out=None):
+    """roomie_qk_norm_rope: q and k [tokens, heads, head_dim] (k may be None), each head divided by its root mean square, times its weight
+    [head_dim] (None: ones), turned to `positions` (int32 [tokens]; table None: not turned).  Outputs may be the inputs.  Returns
+    (q_out, k_out).  Without outputs given the call is differentiable, once, in q, k and the weights."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight, q_out, k_out)):
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out, k_out: not where a gradient is wanted")
+        if table is not None:
+            positions = _ids(positions, "positions")
+        return _NormTurn.apply(q, k, positions if table is not None else None, table, q_weight, k_weight, eps)
+    n, d, at, kind, (hq, qw), (hk, kw) = _norm_sides(q, k, q_weight, k_weight, positions, table, q_out, k_out)
+    q_out, k_out = _norm_out(q, q_out, "q_out"), _norm_out(k, k_out, "k_out")
+    _check(_dll.roomie_qk_norm_rope(table.ref if table is not None else None, eps, n, d, at, kind, hq, _rows(q, "q"), qw, _rows(q_out, "q_out"), hk,
+                                    _rows(k, "k") if hk else None, kw, _rows(k_out, "k_out") if hk else None, _stream(q)), "roomie_qk_norm_rope")
+    return q_out, k_out
+
+
+class _NormTurn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, table, q_weight, k_weight, eps):
+        ctx.save_for_backward(q, k, positions, q_weight, k_weight)
+        ctx.table, ctx.eps = table, eps
+        return qk_norm_rope(q, k, positions, table, q_weight, k_weight, eps=eps)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gq, gk):
+        q, k, positions, q_weight, k_weight = ctx.saved_tensors
+        unit = lambda g: g if g is None or g.stride(2) == 1 else g.clone(memory_format=torch.contiguous_format)
+        gq, gk = unit(gq), unit(gk) if k is not None else None
+        n, d, at, kind, (hq, qw), (hk, kw) = _norm_sides(q, k, q_weight, k_weight, positions, ctx.table, gq, gk)
+        dq, dk = _norm_out(q, None, "q"), _norm_out(k, None, "k")
+        dqw, dkw = (torch.empty_like(w) if w is not None and need else None for w, need in ((q_weight, ctx.needs_input_grad[4]), (k_weight, ctx.needs_input_grad[5])))
+        scratch = torch.empty(int(_dll.roomie_qk_norm_rope_workspace_bytes(d)), dtype=torch.uint8, device=q.device)
+        _check(_dll.roomie_qk_norm_rope_grad(ctx.table.ref if ctx.table is not None else None, ctx.eps, n, d, at, kind, hq, _rows(q, "q"), qw, _rows(gq, "gq"),
+                                             _rows(dq, "dq"), _ptr(dqw), hk, _rows(k, "k") if hk else None, kw, _rows(gk, "gk") if hk else None,
+                                             _rows(dk, "dk") if hk else None, _ptr(dkw), scratch.data_ptr(), scratch.numel(), _stream(q)),
+               "roomie_qk_norm_rope_grad")
+        return dq, dk, None, None, dqw, dkw, None
+
+
 class KVCache:
     """A paged cache of 8-bit keys and values (roomie_kv_cache): codes k, v [layers, num_pages, ...], a float32 scale for each
     page and head, reference counts, the page table and the sequences' lengths, all device tensors."""

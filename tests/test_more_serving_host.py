@@ -1,0 +1,45 @@
+"""The host side of the operators of a search step and a bounded cache: size queries and refusals answer without a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_16784_b200 as rm
+from paper_2607_16784_b200 import roomie, serving
+
+dll = roomie._dll
+FAKE = 0x7F0000000000                                                  # never dereferenced
+
+
+def rows(data=FAKE, kind=2, token=4 * 128, head=128):
+    return serving._pack_rows(data or 0, kind, token, head)
+
+
+def table(rot=128, frequency=FAKE):
+    return serving._RopeTable(rot, 0, 1.0, frequency)
+
+
+def test_norm_refusals():
+    def call(t=table(), eps=1e-6, tokens=4, dim=128, positions=FAKE, kind=0, hq=4, q=rows(), wq=FAKE, qo=rows(FAKE + (1 << 20)), hk=2, k=rows(FAKE + (1 << 21)), wk=None,
+             ko=rows(FAKE + (1 << 22))):
+        return dll.roomie_qk_norm_rope(C.byref(t) if t is not None else None, eps, tokens, dim, positions, kind, hq, q, wq, qo, hk, k, wk, ko, None)
+    for bad in (dict(t=table(0)), dict(t=table(7)), dict(t=table(130)), dict(t=table(frequency=None)), dict(eps=0.0), dict(eps=-1e-6), dict(eps=float("nan")),
+                dict(eps=float("inf")), dict(dim=0), dict(dim=257, t=None), dict(dim=64), dict(positions=None), dict(kind=3), dict(kind=-1), dict(wq=FAKE + 2), dict(wq=FAKE + 1, kind=2),
+                dict(q=None), dict(q=rows(None)), dict(q=rows(kind=5)), dict(q=rows(FAKE + 1)), dict(qo=None), dict(qo=rows(FAKE + (1 << 20), kind=1)), dict(k=rows(kind=1)),
+                dict(k=None), dict(ko=rows(FAKE + (1 << 22), token=0)), dict(ko=rows(FAKE + (1 << 22), head=64)), dict(qo=rows(token=1024)), dict(qo=rows(head=256)),
+                dict(tokens=1 << 29)):
+        assert call(**bad) == -1, bad
+    assert call(tokens=0) == 0 and call(hq=0, hk=0) == 0 and call(tokens=0, t=None, positions=None) == 0
+
+
+def test_norm_gradient_refusals():
+    room = dll.roomie_qk_norm_rope_workspace_bytes(128)
+    assert room > 0 and dll.roomie_qk_norm_rope_workspace_bytes(0) == 0 and dll.roomie_qk_norm_rope_workspace_bytes(257) == 0
+    far = [rows(FAKE + (i << 20)) for i in range(6)]
+    def call(q=far[0], gq=far[1], dq=far[2], dwq=FAKE, k=far[3], gk=far[4], dk=far[5], dwk=None, ws=FAKE, room=room, hk=2, kind=0):
+        return dll.roomie_qk_norm_rope_grad(C.byref(table()), 1e-6, 4, 128, FAKE, kind, 4, q, FAKE, gq, dq, dwq, hk, k, None, gk, dk, dwk, ws, room, None)
+    for bad in (dict(q=None), dict(gq=None), dict(dq=None), dict(gq=rows(kind=1)), dict(dk=rows(kind=0)), dict(dq=rows(token=0)), dict(dk=rows(head=1)), dict(dwq=FAKE + 2),
+                dict(dwk=FAKE + 1, kind=1), dict(ws=None), dict(ws=FAKE + 2), dict(kind=7)):
+        assert call(**bad) == -1, bad
+    assert call(room=room - 1) == -4
