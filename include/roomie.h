@@ -536,6 +536,20 @@ int roomie_kv_copy(const roomie_kv_cache *src /* host */, const int32_t *src_pag
 int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out, int32_t *pages_out, int32_t *used_out,
                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* One step of beam search: of each request's beams * vocab continuations the `num` with the largest scores[r][b] + logit[v] - log sum exp(logit),
+ * in order, equal ones by (beam, token).  logits: element (r, b, v) at r * request_stride + b * beam_stride + v (strides in elements, any
+ * alignment of the rows); scores, ended [requests][beams]; outputs [requests][num]: the score rounded to float32, the row r * beams + b it comes from
+ * (what roomie_kv_reorder takes) and its token; -infinity, -1, -1 where there are fewer candidates.
+ *   A logit of -infinity is no candidate.  A beam whose score is not finite, or whose row holds NaN or +infinity, or nothing above -infinity, has none.
+ *   A beam with ended != 0 (ended may be NULL) has one: itself, with its score and the token `pad`; its logits are not read.
+ * Sums of exponentials are float32 over a thread's 8 to 64 logits and a block's threads, 64 bits from there on; scores are compared in 64 bits.
+ * Limits: beams 1..256, vocab 1..2^24, num 1..128, requests * beams <= 65535.  workspace: roomie_beam_workspace_bytes of the same shape (0 where
+ * it is outside these limits), 256-byte aligned, nothing in it is kept.  Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
+size_t roomie_beam_workspace_bytes(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type);
+int roomie_beam_select(const void *logits, int32_t type, int64_t request_stride, int64_t beam_stride, uint32_t requests, uint32_t beams,
+                       uint32_t vocab, const float *scores, const uint8_t *ended, uint32_t pad, uint32_t num, float *scores_out,
+                       int32_t *parent_out, int32_t *token_out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Launches of the serving operators as a profile.  While enabled (capacity > 0), the calling thread's serving calls note
  * each kernel launch - grid, block, registers, shared memory - and bracket it with CUDA events.  roomie_record_read
  * synchronises on them, writes at most `capacity` records in launch order, stores their number and forgets them:

@@ -1,0 +1,413 @@
+// Beam search's selection: the best continuations of a request over its beams and the vocabulary.
+//
+//   c[b, v] = score[b] + logit[b, v] - log sum_u exp(logit[b, u]),  the `num` largest over (b, v), equal ones in the order of (b, v)
+//
+// Two launches.  rows_kernel: a block takes a part of a row that its threads hold in registers: the part's maximum and sum of exponentials, and
+// its `num` best logits in order.  pick_kernel: a block for each request adds the parts' sums up in 64 bits and picks from their lists.
+#include "roomie_serving.cuh"
+
+namespace roomie {
+
+struct BeamArgs {
+    const void* logits;
+    long long request_stride, beam_stride;          // elements
+    const float* scores;
+    const uint8_t* ended;
+    uint32_t requests, beams, vocab, num, pad, splits;
+    unsigned long long* keys;                       // [rows][splits][num]
+    float2* sums;                                   // [rows][splits] of maximum, sum of exp(x - maximum)
+    float* scores_out;
+    int32_t *parent_out, *token_out;
+};
+
+// A candidate as one number: the larger is the better.  The logit's bits in the order of their values above the token's complement; 0: none.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);                    // -0 counts as 0
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+__device__ __forceinline__ unsigned long long candidate(float x, uint32_t token) { return (unsigned long long)ordered(x) << 32 | (uint32_t)~token; }
+
+constexpr int kBeamThreads = 256, kBeamWarps = kBeamThreads / 32, kMostNum = 128;
+constexpr int kList = 1024;                         // candidates that a block looks at closely
+
+// sorts R numbers a lane, descending over (register, lane)
+template <int R> __device__ __forceinline__ void sort_warp(unsigned long long* x) {
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+    for (int size = 2; size <= 32 * R; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step > 0; step /= 2) {
+            if (step >= 32) {
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+                    if (!(i & (step / 32))) {
+                        const int j = i | (step / 32);
+                        const bool up = (i * 32) & size;
+                        if ((x[i] < x[j]) != up) {
+                            const unsigned long long t = x[i];
+                            x[i] = x[j];
+                            x[j] = t;
+                        }
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const unsigned long long other = __shfl_xor_sync(0xffffffffu, x[i], step);
+                    const bool up = ((i * 32 + lane) & size) != 0, low = !(lane & step);
+                    x[i] = (low != up) == (x[i] > other) ? x[i] : other;
+                }
+            }
+        }
+}
+
+// The `num` largest of the numbers that each thread offers, in order, to out[0, num); 0 where there are fewer.  offer(bound, put) calls put for
+// each of the thread's numbers that is at least `bound`; best: the thread's largest (0: none).  Numbers other than 0 differ.
+//
+// A bound that leaves few: at least `num` numbers are as large as the num-th of the threads' (or neighbouring threads') largest.  What is above it
+// is listed, and each listed number counts those above it.  Should the list run over, the num-th of the listed ones is a higher bound.
+struct PickShared {
+    unsigned long long best[kMostNum], list[kList], bound;
+    uint32_t count;
+};
+template <class Offer>
+__device__ __forceinline__ void pick_best(PickShared& sh, unsigned long long best, uint32_t num, unsigned long long* out, Offer offer) {
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    // the largest of 2 (up to 128 wanted), or 8 (up to 32) neighbouring threads
+    const uint32_t wide = num <= 32 ? 8u : 2u, groups = kBeamThreads / wide;
+    for (uint32_t d = 1; d < wide; d *= 2) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, d);
+        if (other > best) best = other;
+    }
+    __syncthreads();
+    if ((lane & (wide - 1)) == 0) sh.best[threadIdx.x / wide] = best;
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    if (wid == 0) {
+        if (groups == 32) {
+            unsigned long long x[1] = {sh.best[lane]};
+            sort_warp<1>(x);
+            if (lane == num - 1) sh.bound = x[0];
+        } else {
+            unsigned long long x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = sh.best[32 * i + lane];
+            sort_warp<4>(x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (32 * i + lane == num - 1) sh.bound = x[i];
+        }
+    }
+    __syncthreads();
+    while (true) {
+        const unsigned long long bound = sh.bound > 0 ? sh.bound : 1ull;
+        offer(bound, [&](unsigned long long x) {
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < kList) sh.list[at] = x;
+        });
+        __syncthreads();
+        const uint32_t n = sh.count;
+        if (n <= kList) break;
+        // rank num - 1 of the listed
+        __syncthreads();
+        if (threadIdx.x == 0) sh.count = 0;
+        for (uint32_t i = threadIdx.x; i < kList; i += kBeamThreads) {
+            const unsigned long long x = sh.list[i];
+            uint32_t above = 0;
+            for (uint32_t j = 0; j < kList; ++j) above += sh.list[j] > x;
+            if (above == num - 1) sh.bound = x;
+        }
+        __syncthreads();
+    }
+    const uint32_t n = sh.count;
+    for (uint32_t i = threadIdx.x; i < n; i += kBeamThreads) {
+        const unsigned long long x = sh.list[i];
+        uint32_t above = 0;
+        for (uint32_t j = 0; j < n; ++j) above += sh.list[j] > x;
+        if (above < num) out[above] = x;
+    }
+    for (uint32_t i = n + threadIdx.x; i < num; i += kBeamThreads) out[i] = 0;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <class T> __device__ __forceinline__ float element(const uint4& v, int i) { return to_f32(reinterpret_cast<const T*>(&v)[i]); }
+
+// 16 bytes that start `shift` bytes into the 32 of a and b; shift is the same for the row
+__device__ __forceinline__ uint4 joined(const uint4& a, const uint4& b, uint32_t shift) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const uint32_t words = shift / 4, bits = 8 * (shift & 3);
+    uint32_t x[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) x[i] = words == 0 ? w[i] : words == 1 ? w[i + 1] : words == 2 ? w[i + 2] : w[i + 3];
+    return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits), __funnelshift_r(x[3], x[4], bits));
+}
+
+// kVecs 16-byte pieces a thread.  The pieces are counted from the row's first element, wherever in memory that is: equal rows give equal sums.
+template <class T, int kVecs>
+__global__ void __launch_bounds__(kBeamThreads, 4) rows_kernel(BeamArgs a) {
+    constexpr int v = kVecOf<T>;
+    __shared__ PickShared sh;
+    __shared__ float sh_max[kBeamWarps], sh_sum[kBeamWarps];
+    const uint32_t row = blockIdx.y, request = row / a.beams, beam = row - request * a.beams;
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    if (a.ended && a.ended[row]) return;
+    const T* x = static_cast<const T*>(a.logits) + (long long)request * a.request_stride + (long long)beam * a.beam_stride;
+    const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(x) & 15u);
+    const uint32_t base = blockIdx.x * (kBeamThreads * kVecs * v) + threadIdx.x * v;    // piece i: elements base + i * kBeamThreads * v on
+    uint4 raw[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const uint32_t at = base + i * (kBeamThreads * v);
+        const T* p = x + at;
+        if (shift == 0 && at + v <= a.vocab) {
+            raw[i] = __ldcs(reinterpret_cast<const uint4*>(p));
+        } else if (shift && at && at + 2 * v <= a.vocab) {           // the 32 aligned bytes around it lie inside the row
+            const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) - shift);
+            raw[i] = joined(q[0], q[1], shift);
+        } else {
+            T e[v];
+#pragma unroll
+            for (int k = 0; k < v; ++k) e[k] = at + k < a.vocab ? p[k] : from_f32<T>(-INFINITY);
+            raw[i] = *reinterpret_cast<const uint4*>(e);
+        }
+    }
+    // the pieces' maxima, and the sum against the thread's own maximum.  NaN is passed over here and shows in the sum.
+    float tops[kVecs], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        tops[i] = element<T>(raw[i], 0);
+#pragma unroll
+        for (int k = 1; k < v; ++k) tops[i] = fmaxf(tops[i], element<T>(raw[i], k));
+        top = fmaxf(top, tops[i]);
+    }
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int k = 0; k < v; ++k) sum[k & 3] += exp2_fast((element<T>(raw[i], k) - ref) * 1.44269504088896340736f);
+    float total = (sum[0] + sum[1]) + (sum[2] + sum[3]), most = top;
+    if (total != total) most = INFINITY;                             // NaN or +infinity: the row has no probabilities
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    if (lane == 0) sh_max[wid] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kBeamWarps; ++w) most = fmaxf(most, sh_max[w]);
+    total = top == -INFINITY ? 0.0f : total * exp2_fast((top - most) * 1.44269504088896340736f);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
+    if (lane == 0) sh_sum[wid] = total;
+    const size_t part = (size_t)row * a.splits + blockIdx.x;
+    // A number that some of the thread's candidates reaches: its maximum at the last place of the first piece that holds it.
+    unsigned long long best = 0;
+    if (top > -INFINITY)
+#pragma unroll
+        for (int i = kVecs - 1; i >= 0; --i)
+            if (tops[i] == top) best = candidate(top, base + i * (kBeamThreads * v) + v - 1);
+    pick_best(sh, best, a.num, a.keys + part * a.num, [&](unsigned long long bound, auto put) {
+        const float least = unordered((uint32_t)(bound >> 32));      // NaN for a bound below all numbers
+        if (top < least) return;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (tops[i] < least) continue;
+#pragma unroll
+            for (int k = 0; k < v; ++k) {
+                const float e = element<T>(raw[i], k);
+                const unsigned long long c = candidate(e, base + i * (kBeamThreads * v) + k);
+                if (c >= bound && e > -INFINITY) put(c);
+            }
+        }
+    });
+    if (threadIdx.x == 0) {                                          // pick_best has barriers between
+        total = 0.0f;
+        for (int w = 0; w < kBeamWarps; ++w) total += sh_sum[w];
+        a.sums[part] = make_float2(most, total);
+    }
+}
+
+// ---- the requests' picks -----------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned long long ordered64(double x) {
+    const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
+    return b ^ ((unsigned long long)((long long)b >> 63) | 0x8000000000000000ull);
+}
+
+// Candidates in order of (value in 64 bits, row, token): `order` is the complement of the last two, and value 0 is none.
+struct Candidate {
+    unsigned long long value, order;
+};
+__device__ __forceinline__ bool over(const Candidate& x, const Candidate& y) { return x.value > y.value || (x.value == y.value && x.order > y.order); }
+
+constexpr int kPickThreads = 256;
+struct PickList {
+    Candidate list[kList], bound;
+    uint32_t count;
+};
+
+// The num-th of the first n of a list, n >= num, becomes the bound: each counts those above it.
+__device__ __forceinline__ void bound_of(PickList& sh, uint32_t n, uint32_t num) {
+    for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
+        const Candidate x = sh.list[i];
+        uint32_t above = 0, same = 0;                                // those that are none are all the same
+        for (uint32_t j = 0; j < n; ++j) {
+            above += over(sh.list[j], x);
+            same += sh.list[j].value == x.value && sh.list[j].order == x.order;
+        }
+        if (above < num && above + same >= num) sh.bound = x;
+    }
+}
+
+__global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
+    extern __shared__ double of_row[];                               // [beams][3]: score (NaN: no candidates), largest logit, log of the sum
+    __shared__ PickList sh;
+    grid_dependency_wait();
+    const uint32_t request = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    for (uint32_t b = wid; b < a.beams; b += kPickThreads / 32) {
+        const uint32_t row = request * a.beams + b;
+        const double score = a.scores[row];
+        const bool live = score < INFINITY && score > -INFINITY;     // false for NaN
+        double valid = __longlong_as_double(0x7ff8000000000000ll);
+        if (a.ended && a.ended[row]) {
+            if (live) valid = score;
+        } else {
+            float most = -INFINITY;
+            for (uint32_t s = lane; s < a.splits; s += 32) most = fmaxf(most, a.sums[(size_t)row * a.splits + s].x);
+#pragma unroll
+            for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            double total = 0.0;
+            for (uint32_t s = lane; s < a.splits; s += 32) {
+                const float2 p = a.sums[(size_t)row * a.splits + s];
+                if (p.y > 0.0f) total += (double)p.y * exp((double)p.x - (double)most);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
+            if (live && most < INFINITY && most > -INFINITY) valid = score;
+            if (lane == 0) {
+                of_row[3 * b + 1] = most;
+                of_row[3 * b + 2] = log(total);
+            }
+        }
+        if (lane == 0) of_row[3 * b] = valid;
+    }
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    const uint32_t lists = a.beams * a.splits, entries = lists * a.num;
+    auto entry = [&](uint32_t list, uint32_t at) {
+        const uint32_t b = list / a.splits, row = request * a.beams + b;
+        const double score = of_row[3 * b];
+        Candidate c = {0, 0};
+        if (score != score) return c;
+        if (a.ended && a.ended[row]) {                               // goes on as it is, with the padding token
+            if (list == b * a.splits && at == 0) c = {ordered64(score), ~((unsigned long long)b << 32 | a.pad)};
+            return c;
+        }
+        const unsigned long long key = a.keys[((size_t)request * lists + list) * a.num + at];
+        if (key) {                                                   // the difference first: logits may be of any size
+            const double value = score + ((double)unordered((uint32_t)(key >> 32)) - of_row[3 * b + 1] - of_row[3 * b + 2]);
+            c = {ordered64(value), ~((unsigned long long)b << 32 | (uint32_t)~(uint32_t)key)};
+        }
+        return c;
+    };
+    // A bound: the num-th of the leading entries of (some of) the lists, at least num of them.  Then as in pick_best.
+    const uint32_t deep = (a.num + lists - 1) / lists, some = min(lists, (uint32_t)kPickThreads) * deep;   // deep > 1: fewer lists than num
+    for (uint32_t i = threadIdx.x; i < some; i += kPickThreads) sh.list[i] = entry(i / deep, i % deep);
+    __syncthreads();
+    bound_of(sh, some, a.num);
+    __syncthreads();
+    while (true) {
+        const Candidate bound = sh.bound;
+        for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
+            const Candidate c = entry(i / a.num, i % a.num);
+            if (c.value && !over(bound, c)) {
+                const uint32_t at = atomicAdd(&sh.count, 1u);
+                if (at < kList) sh.list[at] = c;
+            }
+        }
+        __syncthreads();
+        if (sh.count <= kList) break;
+        __syncthreads();
+        if (threadIdx.x == 0) sh.count = 0;
+        bound_of(sh, kList, a.num);
+        __syncthreads();
+    }
+    const uint32_t n = sh.count;
+    for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
+        const Candidate x = sh.list[i];
+        uint32_t above = 0;
+        for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
+        if (above < a.num) {
+            const size_t to = (size_t)request * a.num + above;
+            const unsigned long long bits = x.value & 0x8000000000000000ull ? x.value ^ 0x8000000000000000ull : ~x.value, order = ~x.order;
+            a.scores_out[to] = (float)__longlong_as_double((long long)bits);
+            a.parent_out[to] = (int32_t)(request * a.beams + (uint32_t)(order >> 32));
+            a.token_out[to] = (int32_t)(uint32_t)order;
+        }
+    }
+    for (uint32_t i = n + threadIdx.x; i < a.num; i += kPickThreads) {
+        const size_t to = (size_t)request * a.num + i;
+        a.scores_out[to] = -INFINITY;
+        a.parent_out[to] = a.token_out[to] = -1;
+    }
+}
+
+struct BeamShape {
+    uint32_t splits;
+    bool large;
+    size_t keys, bytes;
+};
+// Parts of 8 pieces a thread, or of 2 where those would leave SMs without a block.
+static BeamShape beam_shape(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type) {
+    BeamShape s;
+    const unsigned long long rows = (unsigned long long)requests * beams, one = (unsigned long long)kBeamThreads * 16 / size_of_type(type);
+    const unsigned long long eight = (vocab + 8 * one - 1) / (8 * one), two = (vocab + 2 * one - 1) / (2 * one);
+    s.large = rows * eight >= 2ull * (unsigned long long)sm_count();
+    s.splits = (uint32_t)(s.large ? eight : two);
+    s.keys = (size_t)rows * s.splits * num * sizeof(unsigned long long);
+    s.bytes = (s.keys + (size_t)rows * s.splits * sizeof(float2) + 255) / 256 * 256;
+    return s;
+}
+static bool beam_valid(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type) {
+    return beams > 0 && beams <= 256 && vocab > 0 && vocab <= 1u << 24 && num > 0 && num <= (uint32_t)kMostNum && known_type(type) &&
+           (unsigned long long)requests * beams <= 65535u;
+}
+
+template <class T> static int launch_rows(const BeamArgs& a, bool large, cudaStream_t st) {
+    void (*k)(BeamArgs) = large ? rows_kernel<T, 8> : rows_kernel<T, 2>;
+    return launch("beam_rows", k, dim3(a.splits, a.requests * a.beams), dim3(kBeamThreads), 0, st, false, a);
+}
+
+}  // namespace roomie
+
+using namespace roomie;
+
+extern "C" size_t roomie_beam_workspace_bytes(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type) {
+    if (requests == 0 || !beam_valid(requests, beams, vocab, num, type)) return 0;
+    return beam_shape(requests, beams, vocab, num, type).bytes;
+}
+
+extern "C" int roomie_beam_select(const void* logits, int32_t type, int64_t request_stride, int64_t beam_stride, uint32_t requests, uint32_t beams,
+                                  uint32_t vocab, const float* scores, const uint8_t* ended, uint32_t pad, uint32_t num, float* scores_out,
+                                  int32_t* parent_out, int32_t* token_out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!beam_valid(requests, beams, vocab, num, type) || pad > 0x7fffffffu) return ROOMIE_ERR_INVALID_ARG;
+    if (requests == 0) return ROOMIE_OK;
+    if (!logits || !scores || !scores_out || !parent_out || !token_out || reinterpret_cast<uintptr_t>(logits) % size_of_type(type)) return ROOMIE_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ROOMIE_ERR_INVALID_ARG;
+    const BeamShape s = beam_shape(requests, beams, vocab, num, type);
+    if (workspace_bytes < s.bytes) return ROOMIE_ERR_CAPACITY;
+    BeamArgs a = {};
+    a.logits = logits; a.request_stride = request_stride; a.beam_stride = beam_stride;
+    a.scores = scores; a.ended = ended;
+    a.requests = requests; a.beams = beams; a.vocab = vocab; a.num = num; a.pad = pad; a.splits = s.splits;
+    a.keys = static_cast<unsigned long long*>(workspace);
+    a.sums = reinterpret_cast<float2*>(static_cast<char*>(workspace) + s.keys);
+    a.scores_out = scores_out; a.parent_out = parent_out; a.token_out = token_out;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int rc = type == ROOMIE_F32 ? launch_rows<float>(a, s.large, st)
+             : type == ROOMIE_F16 ? launch_rows<__half>(a, s.large, st) : launch_rows<__nv_bfloat16>(a, s.large, st);
+    if (rc != ROOMIE_OK) return rc;
+    return launch("beam_pick", pick_kernel, dim3(requests), dim3(kPickThreads), 3 * beams * sizeof(double), st, true, a);
+}

@@ -25,6 +25,7 @@ EXPORTS = [
     "roomie_rope_frequencies", "roomie_rope", "roomie_qk_norm_rope", "roomie_qk_norm_rope_grad", "roomie_qk_norm_rope_workspace_bytes",
     "roomie_kv_workspace_bytes", "roomie_kv_append", "roomie_kv_attention",
     "roomie_kv_reserve", "roomie_kv_fork", "roomie_kv_free", "roomie_kv_copy", "roomie_kv_compact",
+    "roomie_beam_workspace_bytes", "roomie_beam_select",
     "roomie_record_enable", "roomie_record_read",
 ]
 
@@ -88,6 +89,9 @@ def _load():
     dll.roomie_kv_free.argtypes = [p, p, u32, p]
     dll.roomie_kv_copy.argtypes = [p, p, p, p, u32, p]
     dll.roomie_kv_compact.argtypes = [p, p, p, p, p, C.c_size_t, p]
+    dll.roomie_beam_workspace_bytes.restype = C.c_size_t
+    dll.roomie_beam_workspace_bytes.argtypes = [u32, u32, u32, u32, C.c_int32]
+    dll.roomie_beam_select.argtypes = [p, C.c_int32, C.c_int64, C.c_int64, u32, u32, u32, p, p, u32, u32, p, p, p, p, C.c_size_t, p]
     dll.roomie_record_enable.argtypes = [u32]
     dll.roomie_record_read.argtypes = [p, u32, p]
     return dll

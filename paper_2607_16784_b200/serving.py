@@ -435,6 +435,45 @@ def kv_compact(cache: KVCache, *, refs_out=None, pages_out=None, used_out=None, 
                                   workspace.numel(), _stream(cache.k)), "roomie_kv_compact")
 
 
+def beam_workspace(requests, beams, vocab, num, dtype=torch.float32, device="cuda"):
+    """Device scratch for beam_select calls of this shape; keep it and pass it to each of them."""
+    kind = _TYPES.get(dtype)
+    size = 0 if kind is None else int(_dll.roomie_beam_workspace_bytes(int(requests), int(beams), int(vocab), int(num), kind))
+    if size == 0:
+        raise ValueError("beam shape outside the library's limits (requests * beams up to 65535, beams up to 256, vocab up to 2^24, num up to 128)")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+@_on_stream
+def beam_select(logits, scores, num, *, ended=None, pad=0, out=None, workspace=None):
+    """roomie_beam_select: logits [requests, beams, vocab] and the beams' scores (float32 [requests, beams]) to the `num` best continuations of
+    each request: (scores float32, parent int32, token int32), each [requests, num].  parent is the row r * beams + b that a continuation comes
+    from: what kv_reorder takes.  `ended` (bool [requests, beams]): beams that go on as they are, with the token `pad`.  `out`: tensors for the three
+    results.  For serving: no gradient passes through."""
+    kind, stride = _TYPES.get(logits.dtype), logits.stride()
+    if kind is None or len(stride) != 3 or not logits.is_cuda or (stride[2] != 1 and logits.shape[2] > 1):
+        raise ValueError("logits: a [requests, beams, vocab] CUDA tensor of float32, float16 or bfloat16 whose last dimension is contiguous")
+    requests, beams, vocab = logits.shape
+    shape = (requests, beams)
+    if tuple(scores.shape) != shape or scores.dtype != torch.float32 or not scores.is_contiguous():
+        raise ValueError("scores: a contiguous float32 tensor [requests, beams]")
+    if ended is not None and (tuple(ended.shape) != shape or ended.dtype not in (torch.bool, torch.uint8) or not ended.is_contiguous()):
+        raise ValueError("ended: a contiguous bool tensor [requests, beams]")
+    if out is None:
+        new = scores.new_empty
+        out = (new((requests, num)), new((requests, num), dtype=torch.int32), new((requests, num), dtype=torch.int32))
+    elif len(out) != 3 or any(tuple(t.shape) != (requests, num) or not t.is_contiguous() or t.dtype != k
+                              for t, k in zip(out, (torch.float32, torch.int32, torch.int32))):
+        raise ValueError("out: contiguous tensors [requests, num] of float32, int32 and int32")
+    if workspace is None and requests:
+        workspace = beam_workspace(requests, beams, vocab, num, logits.dtype, logits.device)
+    _here(logits.get_device(), scores, ended, workspace, *out)
+    _check(_dll.roomie_beam_select(logits.data_ptr(), kind, stride[0], stride[1], requests, beams, vocab, scores.data_ptr(), _ptr(ended), pad, num,
+                                   out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                   _stream(logits)), "roomie_beam_select")
+    return out
+
+
 @contextmanager
 def record_launches(capacity=4096):
     """Notes the serving operators' launches inside the block (roomie_record_*).  Yields a list that is filled when the block

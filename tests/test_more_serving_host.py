@@ -43,3 +43,18 @@ def test_norm_gradient_refusals():
                 dict(dwk=FAKE + 1, kind=1), dict(ws=None), dict(ws=FAKE + 2), dict(kind=7)):
         assert call(**bad) == -1, bad
     assert call(room=room - 1) == -4
+
+
+def test_beam_sizes_and_refusals():
+    size = dll.roomie_beam_workspace_bytes
+    assert size(4, 4, 32000, 8, 2) > 0 and size(4, 4, 32000, 8, 2) % 256 == 0 and size(4, 4, 32000, 16, 2) > size(4, 4, 32000, 8, 2)
+    for bad in ((0, 4, 100, 8, 2), (4, 0, 100, 8, 2), (4, 257, 100, 8, 2), (4, 4, 0, 8, 2), (4, 4, (1 << 24) + 1, 8, 2), (4, 4, 100, 0, 2), (4, 4, 100, 129, 2),
+                (4, 4, 100, 8, 3), (16384, 4, 100, 8, 2)):
+        assert size(*bad) == 0, bad
+    need = size(4, 4, 100, 8, 2)
+    def call(logits=FAKE, kind=2, requests=4, beams=4, vocab=100, scores=FAKE, pad=0, num=8, out=(FAKE, FAKE, FAKE), ws=FAKE, room=need):
+        return dll.roomie_beam_select(logits, kind, 400, 100, requests, beams, vocab, scores, None, pad, num, *out, ws, room, None)
+    for bad in (dict(logits=None), dict(logits=FAKE + 1), dict(kind=4), dict(beams=0), dict(vocab=0), dict(scores=None), dict(pad=1 << 31), dict(num=0), dict(num=129),
+                dict(out=(None, FAKE, FAKE)), dict(out=(FAKE, None, FAKE)), dict(out=(FAKE, FAKE, None)), dict(ws=None), dict(ws=FAKE + 64)):
+        assert call(**bad) == -1, bad
+    assert call(room=need - 1) == -4 and call(requests=0) == 0
