@@ -519,6 +519,10 @@ int roomie_kv_attention(const roomie_kv_cache *cache /* host */, uint32_t layer,
  *   fork     child children[i] (empty) becomes a copy of parents[i]: whole pages are shared, a part-filled last page is
  *            copied, codes and scales; parents are taken as they were before the call;
  *   free     the sequences become empty; their pages lose a reference;
+ *   reorder  sequence seqs[i] becomes what sequence seqs[parents[i]] was before the call (parents[i] in [0, n), repeated or left out at will;
+ *            -1: empty), in place: whole pages are shared; a part-filled last page goes to the first child, the others get copies, in the lowest
+ *            pages that are free once those without a child have been given up.  All or nothing: where a sequence is named twice, an index or length is out
+ *            of range, a page is not one or has too few references, or the free pages do not suffice, nothing changes but the status;
  *   copy     page src_pages[i] of src to page dst_pages[i] of dst, codes and scales of all layers (n pairs; the caches
  *            agree in layers, page_tokens, kv_heads, head_dim, format and layout; no page may be written twice, or both
  *            read and written); tables and counts are left alone;
@@ -531,10 +535,25 @@ int roomie_kv_reserve(const roomie_kv_cache *cache /* host */, const int32_t *se
 int roomie_kv_fork(const roomie_kv_cache *cache /* host */, const int32_t *parents, const int32_t *children, uint32_t n,
                    void *workspace, size_t workspace_bytes, void *stream);
 int roomie_kv_free(const roomie_kv_cache *cache /* host */, const int32_t *seqs, uint32_t n, void *stream);
+int roomie_kv_reorder(const roomie_kv_cache *cache /* host */, const int32_t *seqs, const int32_t *parents, uint32_t n, void *workspace,
+                      size_t workspace_bytes, void *stream);
 int roomie_kv_copy(const roomie_kv_cache *src /* host */, const int32_t *src_pages, const roomie_kv_cache *dst /* host */,
                    const int32_t *dst_pages, uint32_t n, void *stream);
 int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out, int32_t *pages_out, int32_t *used_out,
                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* Cuts the sequences that are longer than `keep` tokens to that length.  Each layer and head keeps a set of its own: the first `first` tokens, the
+ * last `recent`, and of the others the keep - first - recent with the largest weight (equal ones: the earlier; NaN: below all), moved together in
+ * their order.  weight [layers][max_seqs][kv_heads][max_pages * page_tokens] is what roomie_kv_weights wrote; weight_out (the same shape, weight
+ * itself or apart from it) gets the kept tokens' weights, then zeros up to the old length; rows of sequences that stay as they are are not written.
+ *   Each page and head gets the scale that append would give its values (a power of two); codes whose scale stays move as they are, others are
+ * rescaled in float32 and rounded once.  A page that another sequence holds too is replaced by a free one, pages behind the kept tokens lose a
+ * reference.  Requests are served in order while the pages that were free before the call suffice; others change nothing and set
+ * ROOMIE_FLAG_KV_FULL.  A sequence named again, or one with a table entry that is no page, is left as it is and reported.
+ *   Lengths are no longer positions afterwards: rotate with positions of one's own (roomie_rope, roomie_qk_norm_rope) and append without `rope`.
+ * first + recent <= keep, keep > 0; max_pages * page_tokens at most 2^20.  Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
+int roomie_kv_evict(const roomie_kv_cache *cache /* host */, const int32_t *seqs, uint32_t n, const float *weight, uint32_t keep, uint32_t first,
+                    uint32_t recent, float *weight_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* One step of beam search: of each request's beams * vocab continuations the `num` with the largest scores[r][b] + logit[v] - log sum exp(logit),
  * in order, equal ones by (beam, token).  logits: element (r, b, v) at r * request_stride + b * beam_stride + v (strides in elements, any

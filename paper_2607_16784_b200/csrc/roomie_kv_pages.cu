@@ -1,5 +1,5 @@
 // Page operations of the 8-bit cache: reserve, fork, free, copy, compact.
-#include "roomie_kv.cuh"
+#include "roomie_kv_pages.cuh"
 
 namespace roomie {
 
@@ -110,96 +110,7 @@ static uint32_t copy_blocks(const CopyArgs& a, unsigned long long pairs) {
     return (uint32_t)(units < 1 ? 1 : units < full ? units : full);
 }
 
-// ---- a block's view of the free pages ----------------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
-
-// exclusive prefix sum over the block of one value a thread; `total` for all.  sh: kPlanWarps values.
-template <class V> __device__ __forceinline__ V block_exclusive(V x, V& total, V* sh) {
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    V incl = x;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const V up = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += up;
-    }
-    __syncthreads();
-    if (lane == 31) sh[wid] = incl;
-    __syncthreads();
-    if (wid == 0) {
-        V w = sh[lane];
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const V up = __shfl_up_sync(0xffffffffu, w, d);
-            if (lane >= d) w += up;
-        }
-        sh[lane] = w;
-    }
-    __syncthreads();
-    total = sh[kPlanWarps - 1];
-    return (wid ? sh[wid - 1] : V(0)) + incl - x;
-}
-
-// Writes the lowest `want` free pages to list, ascending; returns how many there are.
-constexpr int kScan = 16;                                     // counts a thread looks at in one trip
-__device__ uint32_t lowest_free(const int32_t* refs, uint32_t num_pages, uint32_t want, int32_t* list, uint32_t* sh) {
-    uint32_t found = 0;
-    for (uint32_t base = 0; base < num_pages && found < want; base += kPlanThreads * kScan) {
-        const uint32_t p0 = base + threadIdx.x * kScan;
-        uint32_t free = 0;
-        if (p0 + kScan <= num_pages && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
-#pragma unroll
-            for (int e = 0; e < kScan / 4; ++e) {
-                const int4 r = *reinterpret_cast<const int4*>(refs + p0 + 4 * e);
-                free |= ((r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3) << (4 * e);
-            }
-        } else {
-            for (int e = 0; e < kScan; ++e)
-                if (p0 + e < num_pages && refs[p0 + e] == 0) free |= 1u << e;
-        }
-        uint32_t all;
-        uint32_t at = found + block_exclusive((uint32_t)__popc(free), all, sh);
-        while (free && at < want) {
-            list[at++] = (int32_t)(p0 + __ffs(free) - 1);
-            free &= free - 1;
-        }
-        found += all;
-    }
-    return min(found, want);
-}
-
 // ---- reserve and fork --------------------------------------------------------------------------------------------------
-struct TableView {
-    int32_t *refs, *pages, *length;
-    uint32_t* status;
-    uint32_t num_pages, max_seqs, max_pages, page_shift;
-};
-__device__ __forceinline__ bool slot_ok(const TableView& t, int32_t s) { return s >= 0 && (uint32_t)s < t.max_seqs; }
-__device__ __forceinline__ int32_t length_of(const TableView& t, int32_t s) {      // -1: not a sequence or not a length
-    if (!slot_ok(t, s)) return -1;
-    const int32_t n = t.length[s];
-    return n >= 0 && (unsigned long long)n <= ((unsigned long long)t.max_pages << t.page_shift) ? n : -1;
-}
-__device__ __forceinline__ uint32_t pages_of(const TableView& t, uint32_t tokens) {
-    return (tokens + (1u << t.page_shift) - 1) >> t.page_shift;
-}
-
-// One block.  need[i] = pages request i wants (0 for one that is refused, with state[i] = -1); afterwards first[i] is where its
-// pages begin in list, and the return value is how many of list exist.  Sums are 64 bits wide: what is asked for may be any multiple of
-// what there is.
-__device__ uint32_t serve(const TableView& t, uint32_t n, const int32_t* need, int32_t* first, int32_t* list, uint32_t limit, uint32_t* sh) {
-    __shared__ unsigned long long sums[kPlanWarps];
-    unsigned long long carry = 0;
-    for (uint32_t base = 0; base < n; base += kPlanThreads) {
-        const uint32_t i = base + threadIdx.x;
-        unsigned long long all;
-        const unsigned long long x = i < n ? (uint32_t)need[i] : 0u;
-        const unsigned long long at = carry + block_exclusive(x, all, sums);
-        if (i < n) first[i] = (int32_t)min(at, 0x7fffffffull);
-        carry += all;
-    }
-    return lowest_free(t.refs, t.num_pages, (uint32_t)min(carry, (unsigned long long)limit), list, sh);
-}
-
 // Workspace of n requests: need, first (n words each), the list of free pages (num_pages), refused (n).
 __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(TableView t, const int32_t* seqs, const int32_t* want, uint32_t n,
                                                                int32_t* ws) {
@@ -360,6 +271,140 @@ __global__ void __launch_bounds__(128) free_kernel(TableView t, const int32_t* s
     }
 }
 
+// ---- reorder -----------------------------------------------------------------------------------------------------------
+// Workspace of n sequences: 16 words, the first of them the widest row in use (-1: the call changes nothing); length, children, first child,
+// src, dst, the list of free pages (n words each), and the claims of max_seqs slots.
+struct ReorderView {
+    int32_t *widest, *len, *count, *first, *src, *dst, *list, *owner;
+};
+__host__ __device__ __forceinline__ ReorderView reorder_view(int32_t* ws, uint32_t n) {
+    int32_t* at = ws + 16;
+    return {ws, at, at + n, at + 2 * (size_t)n, at + 3 * (size_t)n, at + 4 * (size_t)n, at + 5 * (size_t)n, at + 6 * (size_t)n};
+}
+constexpr uint32_t kReorderMost = 8192;                           // sequences of a call: a column of their rows fits shared memory
+
+// The pages of the sequences whose number of holders changes, by a warp each: `f(page, change)`.  A whole page has a holder for each child instead
+// of one; the part-filled last page goes to the first child, and is given up when there is none.
+template <class F> __device__ __forceinline__ void held_pages(const TableView& t, const int32_t* seqs, uint32_t n, const ReorderView& v, F f) {
+    const uint32_t lane = threadIdx.x & 31;
+    for (uint32_t p = threadIdx.x >> 5; p < n; p += kPlanWarps) {
+        const int32_t len = v.len[p], children = v.count[p];
+        if (len <= 0 || children == 1) continue;
+        const uint32_t held = pages_of(t, (uint32_t)len), whole = (uint32_t)len >> t.page_shift;
+        const int32_t* row = t.pages + (size_t)seqs[p] * t.max_pages;
+        for (uint32_t e = lane; e < held; e += 32) f(row[e], e < whole ? children - 1 : children ? 0 : -1);
+    }
+}
+
+__global__ void __launch_bounds__(kPlanThreads) reorder_plan_kernel(TableView t, const int32_t* seqs, const int32_t* parents, uint32_t n, int32_t* ws) {
+    __shared__ uint32_t sh[kPlanWarps], widest;
+    const ReorderView v = reorder_view(ws, n);
+    const uint32_t inside = (1u << t.page_shift) - 1;
+    if (threadIdx.x == 0) widest = 0;
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        if (slot_ok(t, seqs[i])) v.owner[seqs[i]] = 0x7fffffff;
+        v.count[i] = 0;
+        v.first[i] = 0x7fffffff;
+        v.src[i] = v.dst[i] = -1;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads)
+        if (slot_ok(t, seqs[i])) atomicMin(v.owner + seqs[i], (int32_t)i);
+    __syncthreads();
+    uint32_t bad = 0;
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int32_t p = parents[i];
+        v.len[i] = length_of(t, seqs[i]);
+        if (v.len[i] < 0 || v.owner[seqs[i]] != (int32_t)i || p < -1 || p >= (int32_t)n) {
+            bad |= ROOMIE_FLAG_KV_SEQUENCE;
+        } else if (p >= 0) {
+            atomicAdd(v.count + p, 1);
+            atomicMin(v.first + p, (int32_t)i);
+        }
+    }
+    bool refused = __syncthreads_or(bad) != 0;
+    if (!refused) {
+        held_pages(t, seqs, n, v, [&](int32_t id, int32_t change) {
+            if (id < 0 || (uint32_t)id >= t.num_pages) bad |= ROOMIE_FLAG_KV_PAGE;
+            else if (change) atomicAdd(t.refs + id, change);
+        });
+        __syncthreads();
+        held_pages(t, seqs, n, v, [&](int32_t id, int32_t) {
+            if (id >= 0 && (uint32_t)id < t.num_pages && t.refs[id] < 0) bad |= ROOMIE_FLAG_KV_PAGE;
+        });
+        const bool broken = __syncthreads_or(bad) != 0;
+        // copies of part-filled pages, in order, to the lowest pages that are free now
+        uint32_t copies = 0;
+        for (uint32_t base = 0; base < n; base += kPlanThreads) {
+            const uint32_t i = base + threadIdx.x;
+            const int32_t p = i < n ? parents[i] : -1;
+            const uint32_t copy = p >= 0 && v.len[p] > 0 && ((uint32_t)v.len[p] & inside) && v.first[p] != (int32_t)i;
+            uint32_t all;
+            const uint32_t at = copies + block_exclusive(copy, all, sh);
+            if (copy) v.dst[i] = (int32_t)at;
+            copies += all;
+        }
+        const uint32_t found = broken ? 0u : lowest_free(t.refs, t.num_pages, copies, v.list, sh);
+        __syncthreads();
+        refused = broken || found < copies;
+        if (refused) {                                            // as it was
+            if (!broken) bad |= ROOMIE_FLAG_KV_FULL;
+            held_pages(t, seqs, n, v, [&](int32_t id, int32_t change) {
+                if (id >= 0 && (uint32_t)id < t.num_pages && change) atomicSub(t.refs + id, change);
+            });
+        }
+    }
+    if (bad) kv_flag(t.status, bad);
+    __syncthreads();
+    if (refused) {
+        if (threadIdx.x == 0) *v.widest = -1;
+        return;
+    }
+    for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int32_t p = parents[i];
+        t.length[seqs[i]] = p < 0 ? 0 : v.len[p];
+        atomicMax(&widest, pages_of(t, (uint32_t)v.len[i]));
+        if (v.dst[i] >= 0) {
+            v.src[i] = t.pages[(size_t)seqs[p] * t.max_pages + ((uint32_t)v.len[p] >> t.page_shift)];
+            v.dst[i] = v.list[v.dst[i]];
+            t.refs[v.dst[i]] = 1;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *v.widest = (int32_t)widest;
+}
+
+// The first blocks: columns of the table, `columns` of them at a time: a column's entries depend on nothing but the same column.  The rest: the
+// part-filled pages.
+__global__ void __launch_bounds__(256) reorder_move_kernel(TableView t, const int32_t* seqs, const int32_t* parents, uint32_t n, int32_t* ws, uint32_t columns,
+                                                           uint32_t table_blocks, CopyArgs copy) {
+    extern __shared__ int32_t was[];                              // [n][columns]
+    grid_dependency_wait();                                       // the plan; this kernel's start overlaps its end
+    const ReorderView v = reorder_view(ws, n);
+    const int32_t widest = *v.widest;
+    if (widest < 0) return;
+    if (blockIdx.x >= table_blocks) {
+        copy_pages(copy, blockIdx.x - table_blocks, gridDim.x - table_blocks);
+        return;
+    }
+    const uint32_t entries = n * columns, c = threadIdx.x % columns;       // `columns` divides the block
+    for (uint32_t c0 = blockIdx.x * columns; c0 < (uint32_t)widest; c0 += table_blocks * columns) {
+        const uint32_t e = c0 + c;
+        for (uint32_t x = threadIdx.x; x < entries; x += 256)
+            if (e < t.max_pages) was[x] = t.pages[(size_t)seqs[x / columns] * t.max_pages + e];
+        __syncthreads();
+        for (uint32_t x = threadIdx.x; x < entries; x += 256) {
+            const uint32_t i = x / columns;
+            const int32_t p = parents[i], fresh = v.dst[i], len = p < 0 ? 0 : v.len[p];
+            if (p == (int32_t)i && fresh < 0) continue;
+            const uint32_t held = pages_of(t, (uint32_t)len);
+            if (e < max(held, pages_of(t, (uint32_t)v.len[i])))
+                t.pages[(size_t)seqs[i] * t.max_pages + e] = e >= held ? -1 : e + 1 == held && fresh >= 0 ? fresh : was[(uint32_t)p * columns + c];
+        }
+        __syncthreads();
+    }
+}
+
 // ---- compact -----------------------------------------------------------------------------------------------------------
 // which of the kScan pages from p0 on are in use
 __device__ __forceinline__ uint32_t used_mask(const int32_t* refs, uint32_t p0, uint32_t num_pages) {
@@ -440,23 +485,9 @@ __global__ void __launch_bounds__(256) compact_move_kernel(TableView t, const in
     }
 }
 
-static TableView table_view(const roomie_kv_cache* c) {
-    const uint32_t shift = c->page_tokens == 16 ? 4 : c->page_tokens == 32 ? 5 : c->page_tokens == 64 ? 6 : 7;
-    return {c->refs, c->pages, c->length, c->status, c->num_pages, c->max_seqs, c->max_pages, shift};
-}
-
 size_t kv_pages_bytes(const roomie_kv_cache* c) {
     const size_t words = 16 + 4 * (size_t)c->num_pages + 8 * (size_t)c->max_seqs;
     return (words * sizeof(int32_t) + 255) / 256 * 256;
-}
-
-static int check_workspace(const roomie_kv_cache* c, const void* ws, size_t bytes) {
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return ROOMIE_ERR_INVALID_ARG;
-    return bytes < roomie_kv_workspace_bytes(c) ? ROOMIE_ERR_CAPACITY : ROOMIE_OK;
-}
-// the attention call's part of a workspace comes first (its counters have to stay zero), the page operations' behind it
-static int32_t* page_scratch(const roomie_kv_cache* c, void* ws) {
-    return reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kv_attention_bytes(c));
 }
 
 }  // namespace roomie
@@ -495,6 +526,28 @@ extern "C" int roomie_kv_fork(const roomie_kv_cache* cache, const int32_t* paren
     copy.n = n; copy.src = ws + 2 * (size_t)n; copy.dst = ws + 3 * (size_t)n;
     return launch("kv_fork_move", fork_move_kernel, dim3(n + copy_blocks(copy, n)), dim3(256), 0, st, true, t, parents, children, n,
                   ws, copy);
+}
+
+extern "C" int roomie_kv_reorder(const roomie_kv_cache* cache, const int32_t* seqs, const int32_t* parents, uint32_t n, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+    if (kv_check(cache) != ROOMIE_OK) return ROOMIE_ERR_INVALID_ARG;
+    if (n == 0) return ROOMIE_OK;
+    if (!seqs || !parents || n > cache->max_seqs || n > kReorderMost) return ROOMIE_ERR_INVALID_ARG;
+    int rc = check_workspace(cache, workspace, workspace_bytes);
+    if (rc != ROOMIE_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int32_t* ws = page_scratch(cache, workspace);
+    const TableView t = table_view(cache);
+    rc = launch("kv_reorder_plan", reorder_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, false, t, seqs, parents, n, ws);
+    if (rc != ROOMIE_OK) return rc;
+    const ReorderView v = reorder_view(ws, n);
+    CopyArgs copy = copy_args(cache, cache);
+    copy.n = n; copy.src = v.src; copy.dst = v.dst;
+    uint32_t columns = 32;                                        // at most 32 KB of shared memory
+    while (columns > 1 && n * columns > kReorderMost) columns /= 2;
+    const uint32_t all = (cache->max_pages + columns - 1) / columns, table_blocks = all < 148 ? all : 148;
+    return launch("kv_reorder_move", reorder_move_kernel, dim3(table_blocks + copy_blocks(copy, n)), dim3(256), (size_t)n * columns * sizeof(int32_t), st, true, t,
+                  seqs, parents, n, ws, columns, table_blocks, copy);
 }
 
 extern "C" int roomie_kv_free(const roomie_kv_cache* cache, const int32_t* seqs, uint32_t n, void* stream) {

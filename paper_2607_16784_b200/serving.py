@@ -295,6 +295,10 @@ class KVCache:
         scratch[:16384].zero_()                          # ROOMIE_KV_WORKSPACE_ZEROED
         return scratch
 
+    def key_weights(self):
+        """Zeros for the weights that kv_weights gathers: float32 [layers, max_seqs, kv_heads, max_pages * page_tokens]."""
+        return torch.zeros((self.layers, self.max_seqs, self.kv_heads, self.max_pages * self.page_tokens), dtype=torch.float32, device=self.k.device)
+
     def status_flags(self) -> int:
         """Synchronises and returns the sticky ROOMIE_FLAG_KV_* bits."""
         return int(self.status.item()) & 0xFFFFFFFF
@@ -304,6 +308,11 @@ class KVCache:
         if f:
             names = [n for b, n in ((8, "WAIT_TIMEOUT"), (16, "KV_PAGE"), (32, "KV_SEQUENCE"), (64, "KV_NONFINITE"), (128, "KV_FULL")) if f & b]
             raise RoomieError("cache status flags set: " + "|".join(names))
+
+
+def _key_weights(cache, t, what):
+    if tuple(t.shape) != (cache.layers, cache.max_seqs, cache.kv_heads, cache.max_pages * cache.page_tokens) or t.dtype != torch.float32 or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous float32 tensor [layers, max_seqs, kv_heads, max_pages * page_tokens] (cache.key_weights())")
 
 
 def _scratch(cache, workspace):
@@ -406,6 +415,34 @@ def kv_free(cache: KVCache, seqs):
     seqs = _ids(seqs, "seqs")
     _here(cache.index, seqs)
     _check(_dll.roomie_kv_free(cache.ref, seqs.data_ptr(), seqs.numel(), _stream(cache.k)), "roomie_kv_free")
+
+
+@_on_stream
+def kv_reorder(cache: KVCache, seqs, parents, *, workspace=None):
+    """roomie_kv_reorder: sequence seqs[i] becomes what seqs[parents[i]] was (parents: indexes into seqs, as beam_select returns them; -1: empty)."""
+    seqs = _ids(seqs, "seqs")
+    parents = _ids(parents.reshape(-1) if isinstance(parents, torch.Tensor) else np.reshape(parents, -1), "parents", seqs.numel())
+    _here(cache.index, seqs, parents, workspace)
+    workspace = _scratch(cache, workspace)
+    _check(_dll.roomie_kv_reorder(cache.ref, seqs.data_ptr(), parents.data_ptr(), seqs.numel(), workspace.data_ptr(), workspace.numel(),
+                                  _stream(cache.k)), "roomie_kv_reorder")
+
+
+@_on_stream
+def kv_evict(cache: KVCache, seqs, weight, keep, *, first=0, recent=0, weight_out=None, workspace=None):
+    """roomie_kv_evict: sequences longer than `keep` tokens keep, for each layer and head, their `first` first and `recent` last tokens and the heaviest
+    of the others by `weight` (float32 [layers, max_seqs, kv_heads, max_pages * page_tokens]).  weight_out None: weight itself is updated.  Returns it."""
+    seqs = _ids(seqs, "seqs")
+    weight_out = weight if weight_out is None else weight_out
+    _key_weights(cache, weight, "weight")
+    _key_weights(cache, weight_out, "weight_out")
+    if min(keep, first, recent) < 0:
+        raise ValueError("keep, first, recent: 0 or more")
+    _here(cache.index, seqs, weight, weight_out, workspace)
+    workspace = _scratch(cache, workspace)
+    _check(_dll.roomie_kv_evict(cache.ref, seqs.data_ptr(), seqs.numel(), weight.data_ptr(), keep, first, recent, weight_out.data_ptr(), workspace.data_ptr(),
+                                workspace.numel(), _stream(cache.k)), "roomie_kv_evict")
+    return weight_out
 
 
 @_on_stream

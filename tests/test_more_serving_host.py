@@ -58,3 +58,36 @@ def test_beam_sizes_and_refusals():
                 dict(out=(None, FAKE, FAKE)), dict(out=(FAKE, None, FAKE)), dict(out=(FAKE, FAKE, None)), dict(ws=None), dict(ws=FAKE + 64)):
         assert call(**bad) == -1, bad
     assert call(room=need - 1) == -4 and call(requests=0) == 0
+
+
+def cache(**kw):
+    d = dict(layers=2, num_pages=100, page_tokens=32, kv_heads=4, head_dim=128, format=0, layout=0, max_seqs=8, max_pages=16,
+             k=FAKE, v=FAKE + (1 << 30), layer_stride=100 * 4 * 32 * 128, page_stride=4 * 32 * 128, k_scale=FAKE, v_scale=FAKE,
+             refs=FAKE, pages=FAKE, length=FAKE, status=FAKE)
+    d.update(kw)
+    return serving._KVCache(**d)
+
+
+def room(**kw):
+    return dll.roomie_kv_workspace_bytes(C.byref(cache(**kw)))
+
+
+def test_reorder_refusals():
+    def call(c=cache(), seqs=FAKE, parents=FAKE, n=2, ws=FAKE, size=room()):
+        return dll.roomie_kv_reorder(C.byref(c), seqs, parents, n, ws, size, None)
+    for bad in (dict(c=cache(head_dim=24)), dict(c=cache(refs=None)), dict(seqs=None), dict(parents=None), dict(n=9), dict(ws=None), dict(ws=FAKE + 8)):
+        assert call(**bad) == -1, bad
+    big = dict(max_seqs=10000)
+    assert call(c=cache(**big), n=8193, size=room(**big)) == -1
+    assert call(size=room() - 1) == -4 and call(n=0, seqs=None) == 0
+
+
+def test_evict_refusals():
+    def call(c=cache(), seqs=FAKE, n=2, weight=FAKE, keep=100, first=4, recent=50, out=FAKE, ws=FAKE, size=room()):
+        return dll.roomie_kv_evict(C.byref(c), seqs, n, weight, keep, first, recent, out, ws, size, None)
+    for bad in (dict(c=cache(page_tokens=48)), dict(seqs=None), dict(weight=None), dict(out=None), dict(weight=FAKE + 2), dict(out=FAKE + 1), dict(n=9), dict(keep=0),
+                dict(keep=1 << 31), dict(keep=53), dict(first=0xffffffff, recent=0xffffffff), dict(ws=None), dict(ws=FAKE + 8)):
+        assert call(**bad) == -1, bad
+    wide = dict(max_pages=(1 << 15) + 1)
+    assert call(c=cache(**wide), size=room(**wide)) == -1
+    assert call(size=room() - 1) == -4 and call(n=0) == 0
