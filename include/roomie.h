@@ -542,6 +542,19 @@ int roomie_kv_copy(const roomie_kv_cache *src /* host */, const int32_t *src_pag
 int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out, int32_t *pages_out, int32_t *used_out,
                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* What the cached keys have received: for each key j of each sequence of the call and each key head, the sum over the call's rows that see it, of
+ * all query heads of that key head, of exp(scale * q k_j - lse).  Rows, positions and windows are those of roomie_kv_attention, whose lse
+ * [rows][q_heads] (float32) of the same q, scale and window this takes; so a row's shares add up to 1.
+ *   weight [layers][max_seqs][kv_heads][max_pages * page_tokens] float32: the sums are added to what is there for the sequence's earlier tokens, and
+ * replace it for the call's own ones (which have received nothing before); with `fresh`, for all its tokens.  What lies behind a sequence's length
+ * is not touched.  A key on a page that is none receives nothing.
+ *   Float32 sums of products of the codes with q (bfloat16 queries: as float16 against the row's largest, which leaves their bits but below
+ * 2^-14 of it).  A NaN reaches the keys that its row sees, or the key whose code it is; not others.  The same call gives the same bits.
+ * q: F16 or BF16.  Errors: INVALID_ARG, CUDA. */
+int roomie_kv_weights(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs, const int32_t *q_offset,
+                      uint32_t rows, uint32_t q_heads, const roomie_rows *q, const float *lse, float scale, uint32_t window, int fresh, float *weight,
+                      void *stream);
+
 /* Cuts the sequences that are longer than `keep` tokens to that length.  Each layer and head keeps a set of its own: the first `first` tokens, the
  * last `recent`, and of the others the keep - first - recent with the largest weight (equal ones: the earlier; NaN: below all), moved together in
  * their order.  weight [layers][max_seqs][kv_heads][max_pages * page_tokens] is what roomie_kv_weights wrote; weight_out (the same shape, weight

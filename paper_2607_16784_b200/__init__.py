@@ -17,6 +17,6 @@ from .roomie import (  # noqa: F401
 )
 from .shard import partition_pairs, combine_shards, pair_matrix_sharded  # noqa: F401,E402
 from .serving import (  # noqa: F401,E402
-    RopeTable, KVCache, rope_frequencies, rope, qk_norm_rope, kv_append, kv_attention, kv_reserve, kv_fork, kv_free, kv_copy, kv_compact, kv_reorder, kv_evict,
+    RopeTable, KVCache, rope_frequencies, rope, qk_norm_rope, kv_append, kv_attention, kv_reserve, kv_fork, kv_free, kv_copy, kv_compact, kv_reorder, kv_weights, kv_evict,
     beam_select, beam_workspace, record_launches, profile_columns,
 )

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libroomie.so")
 SOURCES = ["roomie_api.cu", "roomie_library.cu", "roomie_pairs.cu", "roomie_place.cu", "roomie_optimal.cu",
            "roomie_serving.cu", "roomie_norm.cu", "roomie_beam.cu", "roomie_kv_append.cu", "roomie_kv_attention.cu", "roomie_kv_prompt.cu",
-           "roomie_kv_pages.cu", "roomie_kv_evict.cu"]
+           "roomie_kv_pages.cu", "roomie_kv_evict.cu", "roomie_kv_weights.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--fmad=true", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

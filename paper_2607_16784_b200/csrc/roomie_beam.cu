@@ -129,11 +129,6 @@ __device__ __forceinline__ void pick_best(PickShared& sh, unsigned long long bes
     for (uint32_t i = n + threadIdx.x; i < num; i += kBeamThreads) out[i] = 0;
 }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 template <class T> __device__ __forceinline__ float element(const uint4& v, int i) { return to_f32(reinterpret_cast<const T*>(&v)[i]); }
 
 // 16 bytes that start `shift` bytes into the 32 of a and b; shift is the same for the row

@@ -61,27 +61,6 @@ struct FewRows {
     static constexpr int kSmem = kRing * kAttnWarps > kMeet ? kRing * kAttnWarps : kMeet;
 };
 
-// Where 16-byte chunk `chunk` of row `row` of a step lies: chunks are exchanged so that neither the keys' reads (8 lanes: two rows, four
-// chunks) nor the values' (four rows, two chunks) meet in a bank.
-template <int DP> __device__ __forceinline__ uint32_t code_at(uint32_t row, uint32_t chunk) {
-    if constexpr (DP >= 128) return row * DP + ((chunk ^ (row & 7)) << 4);
-    const uint32_t line = row >> 1;                                // two rows of 64 bytes
-    return line * 128 + ((((row & 1) * 4 + chunk) ^ ((line & 3) << 1)) << 4);
-}
-// N words from a span that starts at byte `first` of a row
-template <int DP, int N> __device__ __forceinline__ void read_span(uint32_t* to, const uint8_t* side, uint32_t row, uint32_t first) {
-    if constexpr (N >= 4) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(side + code_at<DP>(row, first / 16 + i / 4));
-            to[i] = x.x; to[i + 1] = x.y; to[i + 2] = x.z; to[i + 3] = x.w;
-        }
-    } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(side + code_at<DP>(row, first / 16) + (first & 8));
-        to[0] = x.x; to[1] = x.y;
-    }
-}
-
 template <class T> __device__ __forceinline__ float load_elem(const T* p) { return to_f32(*p); }
 
 template <int DP, int NT, int kFormat, class T>

@@ -51,12 +51,6 @@ __device__ __forceinline__ void one_reference(float& m, float& l, float& up, flo
 // The first key that a row at `position` sees.  Rows may lie before the sequence, and a window be as wide as its type: neither wraps here.
 __device__ __forceinline__ int first_seen(int position, uint32_t window) { return max(max(position + 1, 0) - (int)window, 0); }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 __device__ __forceinline__ float log2_fast(float x) {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -99,6 +93,27 @@ template <int kFormat> __device__ __forceinline__ void codes_to_f16(uint32_t w, 
         const __half2 y = __hsub2(reinterpret_cast<const __half2&>(h), reinterpret_cast<const __half2&>(bias));
         lo = reinterpret_cast<const uint32_t&>(x);
         hi = reinterpret_cast<const uint32_t&>(y);
+    }
+}
+
+// Where 16-byte chunk `chunk` of row `row` of a step lies: chunks are exchanged so that neither the keys' reads (8 lanes: two rows, four
+// chunks) nor the values' (four rows, two chunks) meet in a bank.
+template <int DP> __device__ __forceinline__ uint32_t code_at(uint32_t row, uint32_t chunk) {
+    if constexpr (DP >= 128) return row * DP + ((chunk ^ (row & 7)) << 4);
+    const uint32_t line = row >> 1;                                // two rows of 64 bytes
+    return line * 128 + ((((row & 1) * 4 + chunk) ^ ((line & 3) << 1)) << 4);
+}
+// N words from a span that starts at byte `first` of a row
+template <int DP, int N> __device__ __forceinline__ void read_span(uint32_t* to, const uint8_t* side, uint32_t row, uint32_t first) {
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(side + code_at<DP>(row, first / 16 + i / 4));
+            to[i] = x.x; to[i + 1] = x.y; to[i + 2] = x.z; to[i + 3] = x.w;
+        }
+    } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(side + code_at<DP>(row, first / 16) + (first & 8));
+        to[0] = x.x; to[1] = x.y;
     }
 }
 

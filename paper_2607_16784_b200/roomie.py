@@ -25,7 +25,7 @@ EXPORTS = [
     "roomie_rope_frequencies", "roomie_rope", "roomie_qk_norm_rope", "roomie_qk_norm_rope_grad", "roomie_qk_norm_rope_workspace_bytes",
     "roomie_kv_workspace_bytes", "roomie_kv_append", "roomie_kv_attention",
     "roomie_kv_reserve", "roomie_kv_fork", "roomie_kv_free", "roomie_kv_copy", "roomie_kv_compact",
-    "roomie_kv_reorder", "roomie_kv_evict",
+    "roomie_kv_reorder", "roomie_kv_weights", "roomie_kv_evict",
     "roomie_beam_workspace_bytes", "roomie_beam_select",
     "roomie_record_enable", "roomie_record_read",
 ]
@@ -88,6 +88,7 @@ def _load():
     dll.roomie_kv_reserve.argtypes = [p, p, p, u32, p, C.c_size_t, p]
     dll.roomie_kv_fork.argtypes = [p, p, p, u32, p, C.c_size_t, p]
     dll.roomie_kv_reorder.argtypes = [p, p, p, u32, p, C.c_size_t, p]
+    dll.roomie_kv_weights.argtypes = [p, u32, p, u32, p, u32, u32, p, p, C.c_float, u32, C.c_int, p, p]
     dll.roomie_kv_evict.argtypes = [p, p, u32, p, u32, u32, u32, p, p, C.c_size_t, p]
     dll.roomie_kv_free.argtypes = [p, p, u32, p]
     dll.roomie_kv_copy.argtypes = [p, p, p, p, u32, p]

@@ -429,6 +429,28 @@ def kv_reorder(cache: KVCache, seqs, parents, *, workspace=None):
 
 
 @_on_stream
+def kv_weights(cache: KVCache, seqs, q, lse, weight, q_offset=None, *, layer=0, scale=None, window=0, fresh=False):
+    """roomie_kv_weights: adds to `weight` (cache.key_weights()) what the rows of q give to the keys of their sequences: q, q_offset, scale and window as in
+    kv_attention, lse what it returned.  The call's own tokens start from nothing; with `fresh` all of the sequences' do.  Returns weight."""
+    rows, heads, d = q.shape
+    if d != cache.head_dim or heads % cache.kv_heads:
+        raise ValueError("q: [rows, q_heads, head_dim] with q_heads a multiple of the cache's kv_heads")
+    if tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse: a contiguous float32 tensor [rows, q_heads]")
+    _key_weights(cache, weight, "weight")
+    seqs = _ids(seqs, "seqs")
+    n = seqs.shape[0]
+    if q_offset is not None:
+        q_offset = _ids(q_offset, "q_offset", n + 1)
+    elif rows != n:
+        raise ValueError("without q_offset every sequence brings one row")
+    _here(cache.index, seqs, q_offset, q, lse, weight)
+    _check(_dll.roomie_kv_weights(cache.ref, layer, seqs.data_ptr(), n, None if q_offset is None else q_offset.data_ptr(), rows, heads, _rows(q, "q"),
+                                  lse.data_ptr(), d ** -0.5 if scale is None else scale, window, fresh, weight.data_ptr(), _stream(q)), "roomie_kv_weights")
+    return weight
+
+
+@_on_stream
 def kv_evict(cache: KVCache, seqs, weight, keep, *, first=0, recent=0, weight_out=None, workspace=None):
     """roomie_kv_evict: sequences longer than `keep` tokens keep, for each layer and head, their `first` first and `recent` last tokens and the heaviest
     of the others by `weight` (float32 [layers, max_seqs, kv_heads, max_pages * page_tokens]).  weight_out None: weight itself is updated.  Returns it."""

@@ -91,3 +91,13 @@ def test_evict_refusals():
     wide = dict(max_pages=(1 << 15) + 1)
     assert call(c=cache(**wide), size=room(**wide)) == -1
     assert call(size=room() - 1) == -4 and call(n=0) == 0
+
+
+def test_weights_refusals():
+    def call(c=cache(), layer=0, seqs=FAKE, n=2, offset=None, count=2, heads=8, q=rows(), lse=FAKE, scale=0.1, window=0, weight=FAKE):
+        return dll.roomie_kv_weights(C.byref(c), layer, seqs, n, offset, count, heads, q, lse, scale, window, 0, weight, None)
+    for bad in (dict(c=cache(head_dim=24)), dict(layer=5), dict(seqs=None), dict(count=3), dict(heads=0), dict(heads=6), dict(q=rows(kind=0)), dict(q=None),
+                dict(lse=None), dict(lse=FAKE + 2), dict(weight=None), dict(weight=FAKE + 1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
+                dict(scale=float("nan")), dict(window=1 << 31)):
+        assert call(**bad) == -1, bad
+    assert call(n=0, count=0) == 0 and call(count=0) == 0
