@@ -24,96 +24,9 @@
 // V's codes, and the softmax total sum exp2(s - M) is the sum of each page's w times 1 / vs.  So neither costs an instruction an
 // element, and the operands stay exact.  (Value scales beyond kNear: the total is summed apart.)
 #include "roomie_kv_attention.cuh"
+#include "roomie_tc.cuh"
 
 namespace roomie {
-
-// ---- tensor memory and matrix instructions ---------------------------------------------------------------------------------
-__device__ __forceinline__ void tmem_alloc(uint32_t* at, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(at)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-}
-__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-// Operands in shared memory are given by the low halves of their descriptors; the high half is the same for all (kOperandHigh).
-constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
-template <bool kAdd> __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tmov.b64 x, {%1, %4};\n\tmov.b64 y, {%2, %4};\n\tsetp.ne.u32 p, %5, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "n"(kOperandHigh), "n"((int)kAdd)
-                 : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tmov.b64 y, {%2, %4};\n\tsetp.ne.u32 p, %5, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "n"(kOperandHigh),
-                 "r"((uint32_t)add)
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* x) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]),
-          "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]), "=r"(x[18]),
-          "=r"(x[19]), "=r"(x[20]), "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]), "=r"(x[27]),
-          "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
-        : "r"(at));
-}
-__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t* x) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]),
-                   "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
-                 : "r"(at));
-}
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* x) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
-        "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]),
-        "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]),
-        "r"(x[21]), "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]),
-        "r"(x[31])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* x) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(x[0]),
-        "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]),
-        "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15])
-        : "memory");
-}
-// The wait names the registers of the load before it: nothing that uses them may be moved in front of it.
-__device__ __forceinline__ void tmem_wait16(uint32_t* x) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]),
-          "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15])::"memory");
-}
-__device__ __forceinline__ void tmem_wait32(uint32_t* x) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]),
-          "+r"(x[8]), "+r"(x[9]), "+r"(x[10]), "+r"(x[11]), "+r"(x[12]), "+r"(x[13]), "+r"(x[14]), "+r"(x[15]),
-          "+r"(x[16]), "+r"(x[17]), "+r"(x[18]), "+r"(x[19]), "+r"(x[20]), "+r"(x[21]), "+r"(x[22]), "+r"(x[23]),
-          "+r"(x[24]), "+r"(x[25]), "+r"(x[26]), "+r"(x[27]), "+r"(x[28]), "+r"(x[29]), "+r"(x[30]), "+r"(x[31])::"memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-
-// Shared-memory operand: rows of 128 bytes (64 float16), 16-byte chunks exchanged by chunk ^ (row & 7) within groups of 8 rows
-// (1024 bytes apart).  `lbo`: distance of the next 64 columns where the operand's columns are the contiguous direction.
-__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t lbo) { return (at & 0x3ffffu) >> 4 | (lbo >> 4) << 16; }
-// float16 operands, float32 accumulator, 128 rows, n columns; `columns_contiguous`: of the second operand
-__host__ __device__ constexpr uint32_t instruction(uint32_t n, bool columns_contiguous) {
-    return 1u << 4 | (columns_contiguous ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
-}
-
-template <int kN> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
-template <int kN> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN)); }
 
 // ---- shape ------------------------------------------------------------------------------------------------------------------
 constexpr int kKeys = 128;                          // keys of a step
@@ -300,23 +213,6 @@ struct PromptShared {
     float q_scale[2][256];                          // of a row, segments in turn: 2^e of its float16 form times scale * log2(e)
     uint32_t tmem, last, failed;
 };
-
-// By a whole warp, with one answer.  The instruction itself suspends the warp for up to the hint (20 us); a wait that runs out after
-// 2^16 of them (about a second) ends the block: the flag makes its other waits give up too.  Kept to a few instructions: the roles'
-// loops have to fit the instruction caches together.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, PromptShared& sh) {
-    const uint32_t at = smem_addr(bar);
-#pragma unroll 1
-    for (uint32_t spin = 0; spin < 65536u; ++spin) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(at), "r"(parity) : "memory");
-        if (__all_sync(0xffffffffu, ok != 0)) return true;
-        if (*reinterpret_cast<volatile uint32_t*>(&sh.failed)) return false;
-    }
-    *reinterpret_cast<volatile uint32_t*>(&sh.failed) = 1u;
-    return false;
-}
 
 // 16 codes to two 16-byte chunks of float16
 template <int kFormat> __device__ __forceinline__ void widen(const uint4& c, uint4& x, uint4& y) {
@@ -506,11 +402,6 @@ __device__ __forceinline__ void look_up(const AttnArgs& a, PromptShared& sh, Wal
 // The whole warp goes through the loop, so that what does not depend on the lane stays in uniform registers; one elected lane issues.
 // (A single thread's branch around all of it took 280 cycles an instruction, this some 80; the instructions themselves have 32 and 64,
 // so one warp for both tiles was what the step waited for.)
-__device__ __forceinline__ bool elected() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
-    return p != 0;
-}
 template <int DP>
 __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uint32_t t) {
     using P = Prompt<DP>;
@@ -580,27 +471,6 @@ __device__ __forceinline__ void issue(PromptShared& sh, uint8_t* smem, const uin
 }
 
 // ---- one row's share of a step -----------------------------------------------------------------------------------------------------
-// two float32 at a time
-__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ void split(uint64_t p, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));

@@ -2,7 +2,9 @@
 // exp(scale * ks[page] * q_i.k_j - lse_i).
 //
 // Every key's sum is one thread's (or one warp's, in a fixed order): nothing is joined, and a call repeats bit for bit.
+#include <type_traits>
 #include "roomie_kv_attention.cuh"
+#include "roomie_tc.cuh"
 
 namespace roomie {
 
@@ -10,6 +12,7 @@ struct WeightArgs {
     KvView c;
     const int32_t *seqs, *q_offset;
     uint32_t num_seqs, rows, q_heads, group;
+    unsigned long long group_inverse;                // 2^64 / group + 1, 0 for a group of 1
     const void* q;
     long long q_token, q_head;
     const float* lse;                                // [rows][q_heads]
@@ -297,19 +300,343 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
     }
 }
 
+// ---- many rows a key head ----------------------------------------------------------------------------------------------------------
+// Products on the fifth-generation tensor cores, transposed: S^T = K q^T with 128 keys as the accumulator's rows, so that a thread owns a key: it
+// reads its key's products with 64 query rows after the other from tensor memory and adds up their exponentials.  Nothing is exchanged between
+// threads, and a key's scale is a factor of its thread.
+//
+// A block has 256 keys of one (sequence, key head) at a time, two tiles.  Warpgroups 0 and 1 turn their tile's codes into operands (of q's type:
+// exact), then take the exponentials; in warpgroup 2 one warp issues the products and three bring the queries, 64 rows at a time, by asynchronous
+// copies.  While the exponentials of 64 rows are taken, the products of the next are under way.
+constexpr int kManyThreads = 384, kManyRows = 64, kManyKeys = 256, kLoaders = 96;
+
+template <int DP> struct Many {
+    static constexpr int kSlabs = DP / 64;                          // 64-column slabs of an operand
+    static constexpr uint32_t kKeySlab = 128 * 128, kKeyOperand = kSlabs * kKeySlab;          // bytes: 128 keys
+    static constexpr uint32_t kRowSlab = kManyRows * 128, kRowOperand = kSlabs * kRowSlab;    // 64 query rows
+    static constexpr uint32_t kSmem = 2 * kKeyOperand + 2 * kRowOperand + 1024;
+    static constexpr int kPerSm = DP > 128 ? 1 : 2;
+};
+struct ManyShared {
+    uint64_t k_full, q_full[4], q_empty[2], s_full[2], s_empty[2], drain;
+    __align__(16) float lse[4][kManyRows];           // of the rows, negated and in powers of two; -infinity: no row
+    long long at[2][8];                              // of 16 keys each: bytes from the pool's start to them, -1: none
+    float ks[2][8];
+    WeightSeq seq[kManyThreads / 3];
+    unsigned long long sum[kManyThreads / 32];
+    uint32_t tmem, failed;
+};
+
+struct ManyUnit {                                    // 256 keys of a (sequence, head), and the rows that see some of them
+    uint32_t seq, head, k0, row0, row1;
+};
+__device__ __forceinline__ ManyUnit many_unit(const WeightArgs& a, const ManyShared& sh, uint32_t here, unsigned long long at) {
+    uint32_t lo = 0, hi = here;                      // the last one of those that begin at or before `at`: it is not empty
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (sh.seq[mid].first <= at) lo = mid;
+        else hi = mid;
+    }
+    const WeightSeq& s = sh.seq[lo];
+    ManyUnit u;
+    const uint32_t inside = (uint32_t)(at - s.first);
+    u.seq = lo;
+    u.head = inside / s.steps;
+    u.k0 = (s.step0 + inside - u.head * s.steps) * kManyKeys;
+    const long long start = (long long)s.length - s.count, last = min(u.k0 + kManyKeys, s.length) - 1ll;
+    const long long t0 = max(0ll, (long long)u.k0 - start), t1 = a.window ? min((long long)s.count, last + a.window - start) : (long long)s.count;
+    u.row0 = (uint32_t)t0 * a.group;
+    u.row1 = t1 > t0 ? (uint32_t)t1 * a.group : u.row0;
+    return u;
+}
+
+// 16 codes to two 16-byte chunks of T
+template <int kFormat, class T> __device__ __forceinline__ void widen_to(const uint4& c, uint4& x, uint4& y) {
+    codes_to_f16<kFormat>(c.x, x.x, x.y);
+    codes_to_f16<kFormat>(c.y, x.z, x.w);
+    codes_to_f16<kFormat>(c.z, y.x, y.y);
+    codes_to_f16<kFormat>(c.w, y.z, y.w);
+    if constexpr (sizeof(T) == 2 && !std::is_same<T, __half>::value) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t& w = i < 4 ? (&x.x)[i] : (&y.x)[i - 4];
+            const float2 f = __half22float2(reinterpret_cast<const __half2&>(w));
+            const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+            w = reinterpret_cast<const uint32_t&>(b);
+        }
+    }
+}
+
+template <int DP, int kFormat, class T>
+__device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block) {
+    using M = Many<DP>;
+    constexpr int kPerRow = DP / 16, kRowStep = 128 / kPerRow;      // 16-code pieces of a key; piece e of a thread: key row0 + e * kRowStep
+    const KvView& kv = a.c;
+    const uint32_t tile = threadIdx.x >> 7, tid = threadIdx.x & 127, lanes = (threadIdx.x & 96) << 16;
+    const uint32_t piece = tid % kPerRow, row0 = tid / kPerRow;
+    // the odd slabs store their second chunk first: the eight lanes of a store then hit different banks
+    const uint32_t slab = piece / 4, swap = slab & 1, chunk = (piece & 3) * 2;
+    uint8_t* to0 = smem + tile * M::kKeyOperand + slab * M::kKeySlab + row0 * 128 + (((chunk + swap) ^ (row0 & 7)) << 4);
+    const uint32_t to1 = (((chunk + 1 - swap) ^ (row0 & 7)) << 4) - (((chunk + swap) ^ (row0 & 7)) << 4);
+    for (; at < end; at += gridDim.x) {
+        const ManyUnit u = many_unit(a, sh, here, at);
+        const WeightSeq& s = sh.seq[u.seq];
+        const int start = (int)s.length - (int)s.count;
+        const uint32_t key0 = u.k0 + 128 * tile, key = key0 + tid;
+        const bool mine = key < s.length;
+        float* weight = a.weight + ((size_t)s.slot * kv.heads + u.head) * a.max_tokens + key;
+        const float old = mine && !a.fresh && key + s.count < s.length ? *weight : 0.0f;
+        float total = 0.0f;
+        if (u.row1 > u.row0) {
+            if (tid < 8) {                                           // pages of 16 keys each
+                const uint32_t k = key0 + 16 * tid, low = a.window ? (uint32_t)first_seen(start, a.window) : 0u;
+                int32_t id = -1;
+                if (k < s.length && k + 16 > low) {
+                    id = __ldg(kv.pages + (size_t)s.slot * kv.max_pages + (k >> kv.page_shift));
+                    if ((uint32_t)id >= kv.num_pages) {
+                        kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
+                        id = -1;
+                    }
+                }
+                sh.at[tile][tid] = id < 0 ? -1ll : (long long)id * kv.page_stride + (long long)(k & (kv.page_tokens - 1)) * kv.token_step;
+                sh.ks[tile][tid] = id < 0 ? 0.0f : __ldg(kv.k_scale + (size_t)id * kv.heads + u.head);
+            }
+            if (tile) asm volatile("bar.sync 2, 128;" ::: "memory");
+            else asm volatile("bar.sync 1, 128;" ::: "memory");
+            const uint8_t* pool = kv.k + (long long)u.head * kv.head_step + 16 * piece;
+            uint4 c[kPerRow];
+#pragma unroll
+            for (int e = 0; e < kPerRow; ++e) {
+                const uint32_t row = row0 + e * kRowStep;
+                const long long from = sh.at[tile][row >> 4];
+                c[e] = make_uint4(0, 0, 0, 0);
+                if (from >= 0 && 16 * piece < kv.dim && key0 + row < s.length)
+                    c[e] = __ldg(reinterpret_cast<const uint4*>(pool + from + (long long)(row & 15) * kv.token_step));
+            }
+            const bool there = sh.at[tile][tid >> 4] >= 0;
+            const float f = sh.ks[tile][tid >> 4] * a.scale_log2;
+#pragma unroll
+            for (int e = 0; e < kPerRow; ++e) {
+                uint4 x, y;
+                widen_to<kFormat, T>(c[e], x, y);
+                uint8_t* to = to0 + e * kRowStep * 128;
+                *reinterpret_cast<uint4*>(to) = swap ? y : x;
+                *reinterpret_cast<uint4*>(to + to1) = swap ? x : y;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.k_full);
+            // the rows that see this key: [lo, hi)
+            const long long first = max(0ll, (long long)key - start), past = a.window ? min((long long)s.count, (long long)key + a.window - start) : (long long)s.count;
+            const uint32_t lo = (uint32_t)min(first, (long long)s.count) * a.group, hi = past > 0 ? (uint32_t)past * a.group : 0u;
+            const uint64_t f2 = pair(f, f);
+            uint64_t sum[2] = {0, 0};
+            for (uint32_t rb = u.row0; rb < u.row1; rb += kManyRows, ++block) {
+                const uint32_t side = block & 1, s_at = sh.tmem + tile * 128 + side * 64 + lanes;
+                if (!warp_wait(&sh.q_full[block & 3], (block >> 2) & 1, sh) || !warp_wait(&sh.s_full[side], (block >> 1) & 1, sh)) return;
+                tc_fence_after();
+                const bool cut = __any_sync(0xffffffffu, lo > rb || hi < min(rb + kManyRows, u.row1));
+                const ulonglong2* minus = reinterpret_cast<const ulonglong2*>(sh.lse[block & 3]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[32];
+                    tmem_load32(s_at + 32 * h, x);
+                    tmem_wait32(x);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const ulonglong2 m = minus[8 * h + e / 4];
+#pragma unroll
+                        for (int o = 0; o < 4; o += 2) {
+                            float v, w;
+                            split(fma2(pair(x[e + o], x[e + o + 1]), f2, o ? m.y : m.x), v, w);
+                            if (cut) {
+                                const uint32_t row = rb + 32 * h + e + o;
+                                if (row < lo || row >= hi) v = -INFINITY;
+                                if (row + 1 < lo || row + 1 >= hi) w = -INFINITY;
+                            }
+                            sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
+                        }
+                    }
+                }
+                tc_fence_before();
+                mbar_arrive(&sh.s_empty[side]);                      // the columns are read, and so is this block's place in sh.lse
+            }
+            float even, odd;
+            split(add2(sum[0], sum[1]), even, odd);
+            if (there) total = even + odd;
+        }
+        if (mine) *weight = old + total;
+    }
+}
+
+template <int DP, class T>
+__device__ __forceinline__ void many_issue(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block,
+                                           uint32_t& units) {
+    using M = Many<DP>;
+    const uint32_t k0 = operand(smem_addr(smem), 16), q0 = operand(smem_addr(smem) + 2 * M::kKeyOperand, 16), tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
+    constexpr uint32_t kS = instruction(kManyRows, false) | (std::is_same<T, __half>::value ? 0u : 1u << 7 | 1u << 10);     // both operands bfloat16
+    for (; at < end; at += gridDim.x) {
+        const ManyUnit u = many_unit(a, sh, here, at);
+        const uint32_t row0 = __shfl_sync(0xffffffffu, u.row0, 0), row1 = __shfl_sync(0xffffffffu, u.row1, 0);
+        if (row0 >= row1) continue;
+        if (!warp_wait(&sh.k_full, units & 1, sh)) return;
+        ++units;
+        for (uint32_t rb = row0; rb < row1; rb += kManyRows, ++block) {
+            const uint32_t side = block & 1;
+            if (!warp_wait(&sh.q_full[block & 3], (block >> 2) & 1, sh)) return;
+            if (block >= 2 && !warp_wait(&sh.s_empty[side], ((block >> 1) - 1) & 1, sh)) return;
+            tc_fence_after();
+            const uint32_t q = q0 + side * (M::kRowOperand >> 4);
+            if (elected()) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t k = k0 + t * (M::kKeyOperand >> 4), to = tm + t * 128 + side * 64;
+                    mma_ss<false>(to, k, q, kS);
+#pragma unroll
+                    for (int i = 1; i < DP / 16; ++i)
+                        mma_ss<true>(to, k + (((i / 4) * M::kKeySlab + (i % 4) * 32) >> 4), q + (((i / 4) * M::kRowSlab + (i % 4) * 32) >> 4), kS);
+                }
+                tc_commit(&sh.s_full[side]);
+                tc_commit(&sh.q_empty[side]);
+            }
+            __syncwarp();
+        }
+    }
+}
+
+template <int DP, class T>
+__device__ __forceinline__ void many_queries(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block) {
+    using M = Many<DP>;
+    constexpr uint32_t kChunks = DP / 8;                             // 16-byte chunks of a row
+    const uint32_t tid = threadIdx.x - (kManyThreads - kLoaders);
+    uint8_t* stages = smem + 2 * M::kKeyOperand;
+    for (; at < end; at += gridDim.x) {
+        const ManyUnit u = many_unit(a, sh, here, at);
+        const WeightSeq& s = sh.seq[u.seq];
+        for (uint32_t rb = u.row0; rb < u.row1; rb += kManyRows, ++block) {
+            const uint32_t side = block & 1;
+            if (block >= 2 && !warp_wait(&sh.q_empty[side], ((block >> 1) - 1) & 1, sh)) return;
+            uint8_t* stage = stages + side * M::kRowOperand;
+            for (uint32_t x = tid; x < kManyRows * kChunks; x += kLoaders) {
+                const uint32_t r = x / kChunks, c = x % kChunks, row = rb + r, tok = a.group_inverse ? (uint32_t)__umul64hi(row, a.group_inverse) : row;
+                const bool there = row < u.row1 && 8 * c < a.c.dim;
+                const T* q = static_cast<const T*>(a.q);
+                if (there) q += (long long)(s.row + tok) * a.q_token + (long long)(u.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
+                uint8_t* to = stage + (c >> 3) * M::kRowSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+                if (a.q_aligned) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(q), "r"(there ? 16u : 0u) : "memory");
+                } else {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(q);
+                    if (there)
+                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                    *reinterpret_cast<uint4*>(to) = v;
+                }
+            }
+            if (tid < kManyRows) {
+                const uint32_t row = rb + tid, tok = a.group_inverse ? (uint32_t)__umul64hi(row, a.group_inverse) : row;
+                float minus = -INFINITY;
+                if (row < u.row1) minus = -kLog2e * a.lse[(size_t)(s.row + tok) * a.q_heads + u.head * a.group + row - tok * a.group];
+                sh.lse[block & 3][tid] = minus;
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.q_full[block & 3]);
+        }
+    }
+}
+
+template <int DP, int kFormat, class T>
+__global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_kernel(WeightArgs a) {
+    constexpr uint32_t kSeqs = kManyThreads / 3;
+    extern __shared__ uint8_t raw[];
+    __shared__ ManyShared sh;
+    uint8_t* smem = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        mbar_init(&sh.k_full, 256);
+        for (int i = 0; i < 4; ++i) mbar_init(&sh.q_full[i], kLoaders);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.q_empty[i], 1);
+            mbar_init(&sh.s_full[i], 1);
+            mbar_init(&sh.s_empty[i], 256);
+        }
+        mbar_init(&sh.drain, 1);
+        sh.failed = 0;
+    }
+    if (wid == 8) tmem_alloc(&sh.tmem, 256);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    uint32_t block = 0, units = 0;                                   // of this block, each role in step with the others
+    unsigned long long before = 0;                                   // units of the sequences so far
+    for (uint32_t base = 0; base < a.num_seqs; base += kSeqs) {
+        const uint32_t here = min(a.num_seqs - base, kSeqs);
+        __syncthreads();
+        unsigned long long mine = 0;
+        WeightSeq w = {};
+        if (threadIdx.x < here) {
+            const KvSeq s = kv_seq(a.c, a.seqs, a.q_offset, a.rows, base + threadIdx.x, blockIdx.x == 0);
+            w.slot = s.slot; w.row = s.row; w.count = s.count; w.length = s.length;
+            const uint32_t low = a.fresh ? 0u : a.window ? min((uint32_t)first_seen((int)s.length - (int)s.count, a.window), s.length) : 0u;
+            w.step0 = low / kManyKeys;
+            w.steps = s.count ? (s.length + kManyKeys - 1) / kManyKeys - w.step0 : 0u;
+            mine = (unsigned long long)w.steps * a.c.heads;
+        }
+        unsigned long long upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += up;
+        }
+        if (lane == 31) sh.sum[wid] = upto;
+        __syncthreads();
+        unsigned long long total = 0;
+        for (uint32_t x = 0; x < kManyThreads / 32; ++x) {
+            if (x < wid) upto += sh.sum[x];
+            total += sh.sum[x];
+        }
+        w.first = upto - mine;
+        if (threadIdx.x < here) sh.seq[threadIdx.x] = w;
+        __syncthreads();
+        // units go round the blocks
+        const unsigned long long turn = before % gridDim.x, at = blockIdx.x >= turn ? blockIdx.x - turn : blockIdx.x + gridDim.x - turn;
+        before += total;
+        if (wid < 8) many_sums<DP, kFormat, T>(a, sh, smem, here, at, total, block);
+        else if (wid == 8) many_issue<DP, T>(a, sh, smem, here, at, total, block, units);
+        else many_queries<DP, T>(a, sh, smem, here, at, total, block);
+        __syncwarp();
+    }
+    if (wid == 8) {
+        if (elected()) tc_commit(&sh.drain);                         // whatever was issued has ended before the memory is given back
+        __syncwarp();
+        warp_wait(&sh.drain, 0, sh);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0 && sh.failed) kv_flag(a.c.status, ROOMIE_FLAG_WAIT_TIMEOUT);
+    if (wid == 8) tmem_free(sh.tmem, 256);
+}
+
+template <int DP, int kFormat, class T> static int launch_many_weights(const WeightArgs& a, cudaStream_t st) {
+    return launch("kv_weights", many_weights_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count() * Many<DP>::kPerSm), dim3(kManyThreads), Many<DP>::kSmem, st, false, a);
+}
+
 template <int DP, int NT, int kFormat, class T> static int launch_few_weights(const WeightArgs& a, cudaStream_t st) {
     return launch("kv_weights", few_weights_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * 3), dim3(kWeightThreads), FewWeights<DP>::kSmem, st, false, a);
 }
-template <int DP, int kFormat, class T> static int weight_rows(const WeightArgs& a, bool eight, cudaStream_t st) {
-    return eight ? launch_few_weights<DP, 1, kFormat, T>(a, st) : launch_few_weights<DP, 2, kFormat, T>(a, st);
+enum class Rows { eight, sixteen, many };
+template <int DP, int kFormat, class T> static int weight_rows(const WeightArgs& a, Rows rows, cudaStream_t st) {
+    if (rows == Rows::many) return launch_many_weights<DP, kFormat, T>(a, st);
+    return rows == Rows::eight ? launch_few_weights<DP, 1, kFormat, T>(a, st) : launch_few_weights<DP, 2, kFormat, T>(a, st);
 }
-template <int kFormat, class T> static int weight_dims(const WeightArgs& a, bool eight, cudaStream_t st) {
-    if (a.c.dim <= 64) return weight_rows<64, kFormat, T>(a, eight, st);
-    if (a.c.dim <= 128) return weight_rows<128, kFormat, T>(a, eight, st);
-    return weight_rows<256, kFormat, T>(a, eight, st);
+template <int kFormat, class T> static int weight_dims(const WeightArgs& a, Rows rows, cudaStream_t st) {
+    if (a.c.dim <= 64) return weight_rows<64, kFormat, T>(a, rows, st);
+    if (a.c.dim <= 128) return weight_rows<128, kFormat, T>(a, rows, st);
+    return weight_rows<256, kFormat, T>(a, rows, st);
 }
-template <class T> static int weight_format(const WeightArgs& a, bool eight, cudaStream_t st) {
-    return a.c.format == ROOMIE_KV_E4M3 ? weight_dims<ROOMIE_KV_E4M3, T>(a, eight, st) : weight_dims<ROOMIE_KV_INT8, T>(a, eight, st);
+template <class T> static int weight_format(const WeightArgs& a, Rows rows, cudaStream_t st) {
+    return a.c.format == ROOMIE_KV_E4M3 ? weight_dims<ROOMIE_KV_E4M3, T>(a, rows, st) : weight_dims<ROOMIE_KV_INT8, T>(a, rows, st);
 }
 
 }  // namespace roomie
@@ -329,15 +656,18 @@ extern "C" int roomie_kv_weights(const roomie_kv_cache* cache, uint32_t layer, c
     a.c = kv_view(cache, layer);
     a.seqs = seqs; a.q_offset = q_offset; a.num_seqs = num_seqs; a.rows = rows;
     a.q_heads = q_heads; a.group = q_heads / cache->kv_heads;
+    a.group_inverse = a.group > 1 ? ~0ull / a.group + 1 : 0;
     a.q = q->data; a.q_token = q->token_stride; a.q_head = q->head_stride;
     a.lse = lse;
     a.max_tokens = cache->max_pages * cache->page_tokens;
+    if ((unsigned long long)cache->kv_heads * (a.max_tokens / 256 + 1) > 0xffffffffull) return ROOMIE_ERR_INVALID_ARG;
     a.weight = weight + (size_t)layer * cache->max_seqs * cache->kv_heads * a.max_tokens;
     a.window = window;
     a.scale_log2 = scale * kLog2e;
     a.q_aligned = rows_aligned16(*q, rows, q_heads);
     a.fresh = fresh != 0;
-    const bool eight = (unsigned long long)rows * a.group <= 8ull * num_seqs;
+    const unsigned long long all = (unsigned long long)rows * a.group;
+    const Rows kind = all <= 8ull * num_seqs ? Rows::eight : all <= 16ull * num_seqs ? Rows::sixteen : Rows::many;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return q->type == ROOMIE_F16 ? weight_format<__half>(a, eight, st) : weight_format<__nv_bfloat16>(a, eight, st);
+    return q->type == ROOMIE_F16 ? weight_format<__half>(a, kind, st) : weight_format<__nv_bfloat16>(a, kind, st);
 }
