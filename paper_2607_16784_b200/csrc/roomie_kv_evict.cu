@@ -1,24 +1,26 @@
 // Eviction from the paged 8-bit cache: every layer and head keeps `keep` tokens - the first ones, the last ones and those that have received the most
 // weight - moved together in their order.
+#include "roomie_kv_attention.cuh"
 #include "roomie_kv_pages.cuh"
 
 namespace roomie {
 
 // ---- the plan: which pages the kept tokens go to ---------------------------------------------------------------------------------------
 // Workspace of n requests: length (-1: nothing is done), need, first, blocks that are done (n words each), the claims of max_seqs slots, the list
-// of free pages (num_pages).
+// of free pages and the pages that they replace (num_pages each).
 struct EvictView {
-    int32_t *len, *need, *first, *done, *owner, *list;
+    int32_t *len, *need, *first, *done, *owner, *list, *replaced;
 };
-__host__ __device__ __forceinline__ EvictView evict_view(int32_t* ws, uint32_t n, uint32_t max_seqs) {
-    return {ws, ws + n, ws + 2 * (size_t)n, ws + 3 * (size_t)n, ws + 4 * (size_t)n, ws + 4 * (size_t)n + max_seqs};
+__host__ __device__ __forceinline__ EvictView evict_view(int32_t* ws, uint32_t n, uint32_t max_seqs, uint32_t num_pages) {
+    int32_t* list = ws + 4 * (size_t)n + max_seqs;
+    return {ws, ws + n, ws + 2 * (size_t)n, ws + 3 * (size_t)n, ws + 4 * (size_t)n, list, list + num_pages};
 }
 
-// While the call runs, a page of the kept part that another sequence holds too stands in the table as its complement: its tokens go to a page of the
-// list.  The last block of a sequence puts the new pages into the table, gives up the old ones and sets the length.
+// While the call runs, a page of the kept part that another sequence holds too stands in the table as the complement of its place in the list.
+// The last block of a sequence puts the new pages into the table, gives up the old ones and sets the length.
 __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(TableView t, const int32_t* seqs, uint32_t n, uint32_t keep, int32_t* ws) {
     __shared__ uint32_t sh[kPlanWarps];
-    const EvictView v = evict_view(ws, n, t.max_seqs);
+    const EvictView v = evict_view(ws, n, t.max_seqs, t.num_pages);
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, now = pages_of(t, keep);
     uint32_t bad = 0;
     for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads)
@@ -70,8 +72,18 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(TableView t, c
             continue;
         }
         int32_t* row = t.pages + (size_t)seqs[i] * t.max_pages;
-        for (uint32_t e = lane; e < now; e += 32)
-            if (t.refs[row[e]] > 1) row[e] = ~row[e];
+        uint32_t at = (uint32_t)v.first[i];
+        for (uint32_t base = 0; base < now; base += 32) {
+            const uint32_t e = base + lane;
+            const bool shared = e < now && t.refs[row[e]] > 1;
+            const uint32_t votes = __ballot_sync(0xffffffffu, shared);
+            if (shared) {
+                const uint32_t place = at + __popc(votes & ((1u << lane) - 1));
+                v.replaced[place] = row[e];
+                row[e] = ~(int32_t)place;
+            }
+            at += __popc(votes);
+        }
     }
     if (bad) kv_flag(t.status, bad);
 }
@@ -81,8 +93,6 @@ struct EvictArgs {
     KvView c;                                       // of layer 0
     long long layer_stride;
     uint32_t layers, n, keep, first, recent, max_tokens;
-    uint32_t pieces, piece_inverse;                 // 16-byte pieces of a token, and 2^20 / pieces + 1
-    uint32_t pages;                                 // of a round
     const int32_t* seqs;
     int32_t* ws;
     const float* weight;
@@ -92,14 +102,14 @@ struct EvictArgs {
 
 // A block has one (sequence, layer, head), keys and values alike.
 //
-// Selection: the smallest kept weight by its bits, 11, 11 and 10 at a time, from histograms in shared memory; then a bit for each token and the
-// number of kept ones in front of each 128.
+// Selection: the smallest kept weight by its bits, 11, 11 and 10 at a time, from histograms in shared memory, where the first kCached weights'
+// bits lie too; then a bit for each token and the number of kept ones in front of each 128.
 //
-// Move: rounds of up to 256 tokens, in order.  A round's codes are read into registers (16 pieces of 16 bytes a thread: four warps have
-// the keys, four the values), the pages' largest magnitudes are found, and behind a barrier the codes are written.  A token never moves up,
-// so what a round writes was read by it or a round before, and no round after it reads there: tokens move inside their own pages.  Where the tokens of
-// the next round come from is looked up while this round's codes arrive.
-constexpr int kEvictThreads = 256, kEvictWarps = kEvictThreads / 32, kRoundTokens = 256, kPiecesEach = 16;
+// Move: rounds of 128 tokens, in order.  A warp has the keys or the values of 32 of them: a lane looks up where one token comes from, then each token's
+// 16-byte pieces are read by kLanes neighbouring lanes, all at once, into registers; the next round's tokens are looked up meanwhile.  Behind the one
+// barrier of a round, when the pages' largest magnitudes are known, the codes are written.  A token never moves up, so what a round writes was read by it
+// or a round before, and no round after it reads there: tokens move inside their own pages.
+constexpr int kEvictThreads = 256, kEvictWarps = kEvictThreads / 32, kCached = 8192;
 
 // One thread, after a barrier of its block: what the block read of the table comes before the count, what it writes there behind it.
 __device__ __forceinline__ uint32_t count_done(int32_t* counter) {
@@ -109,15 +119,9 @@ __device__ __forceinline__ uint32_t count_done(int32_t* counter) {
     return before;
 }
 
-struct Origin {                                     // of a token of a round
-    long long at;                                   // bytes from the pool's start; -1: there is none
-    float ks, vs;
-};
 struct EvictShared {
     uint32_t hist[2048];
-    Origin origin[3][kRoundTokens];                 // rounds in turn: one that is read, one that is filled, one that may still be read
-    int32_t target[3][16];                          // the pages that a round's tokens go to
-    uint32_t amax[3][2][16];                        // rounds in turn, side, page: bits of the largest magnitude
+    uint32_t amax[3][2][8];                         // rounds in turn, side, page: bits of the largest magnitude
     uint32_t part[kEvictWarps];
     uint32_t digit, left, ties, last;
 };
@@ -130,9 +134,10 @@ __device__ __forceinline__ uint32_t weight_bits(float x) {
 }
 
 // The largest magnitude of 16 codes.  Codes of e4m3 are in the order of their magnitudes but for the sign (NaN, 0x7f, counts as the largest value).
+// Pairs of bytes are compared by the upper one: as they are, and shifted up by one.
 template <int kFormat> __device__ __forceinline__ float largest_of(const uint4& x) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t even = 0, odd = 0;
+    uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t m;
@@ -142,17 +147,40 @@ template <int kFormat> __device__ __forceinline__ float largest_of(const uint4& 
             const uint32_t sign = (w[i] >> 7) & 0x01010101u;
             m = (w[i] ^ (sign * 0xffu)) + sign;                     // -128 becomes 128: no byte carries
         }
-        even = __vmaxu2(even, m & 0x00ff00ffu);
-        odd = __vmaxu2(odd, (m >> 8) & 0x00ff00ffu);
+        most = __vmaxu2(most, __vmaxu2(m, m << 8));
     }
-    even = __vmaxu2(even, odd);
-    uint32_t most = max(even & 0xffffu, even >> 16);
+    most = max(most >> 24, (most >> 8) & 0xffu);
     if constexpr (kFormat == ROOMIE_KV_E4M3) return kv_value((uint8_t)min(most, 0x7eu), ROOMIE_KV_E4M3);
     return (float)most;
 }
 
-// 16 codes of scale `from` to codes of the power of two whose inverse is `inverse`
-template <int kFormat> __device__ __forceinline__ uint4 rescaled(const uint4& x, float from, float inverse) {
+// 16 codes times `ratio`, a power of two from 2^-15 to 2^7, rounded to codes.  In float16 code and product are exact: the only rounding is that to
+// the code.
+template <int kFormat> __device__ __forceinline__ uint4 multiplied(const uint4& x, float ratio) {
+    uint4 y;
+    const uint32_t* w = &x.x;
+    uint32_t* o = &y.x;
+    const __half2 r = __float2half2_rn(ratio);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t lo, hi;
+        codes_to_f16<kFormat>(w[i], lo, hi);
+        if constexpr (kFormat == ROOMIE_KV_E4M3) {
+            const __half2 a = __hmul2(reinterpret_cast<const __half2&>(lo), r), b = __hmul2(reinterpret_cast<const __half2&>(hi), r);
+            asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+                : "=r"(o[i]) : "r"(reinterpret_cast<const uint32_t&>(a)), "r"(reinterpret_cast<const uint32_t&>(b)));
+        } else {
+            // added to 1536 the product is rounded to a whole number, whose two's complement is the low byte
+            const __half2 magic = __float2half2_rn(1536.0f);
+            const __half2 a = __hfma2(reinterpret_cast<const __half2&>(lo), r, magic), b = __hfma2(reinterpret_cast<const __half2&>(hi), r, magic);
+            o[i] = __byte_perm(reinterpret_cast<const uint32_t&>(a), reinterpret_cast<const uint32_t&>(b), 0x6420);
+        }
+    }
+    return y;
+}
+
+// 16 codes of scale `from`, any number, to codes of the scale whose inverse is `inverse`, a power of two
+template <int kFormat> __device__ __noinline__ uint4 rescaled(uint4 x, float from, float inverse) {
     uint4 y;
     const uint32_t* w = &x.x;
     uint32_t* o = &y.x;
@@ -169,14 +197,17 @@ template <int kFormat> __device__ __forceinline__ uint4 rescaled(const uint4& x,
     return y;
 }
 
-template <int kFormat>
-__global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
-    extern __shared__ uint32_t bits[];              // a bit for each of max_tokens, 1: kept; then how many are kept in front of each 128
+// kLanes: the least power of two that is at least a token's pieces; also the pieces of a lane.
+template <int kFormat, int kLanes>
+__global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_kernel(EvictArgs a) {
+    constexpr uint32_t kTokens = 128, kSpan = 32 / kLanes;           // of a round; of a warp's load
+    extern __shared__ uint32_t bits[];              // a bit for each of max_tokens, 1: kept; then how many are kept in front of each 128; then the
+                                                    // bits of the first weights
     __shared__ EvictShared sh;
     grid_dependency_wait();                         // the plan; this kernel's start overlaps its end
     const KvView& c = a.c;
     const uint32_t head = blockIdx.x % c.heads, rest = blockIdx.x / c.heads, layer = rest % a.layers, i = rest / a.layers;
-    const EvictView v = evict_view(a.ws, a.n, c.max_seqs);
+    const EvictView v = evict_view(a.ws, a.n, c.max_seqs, c.num_pages);
     const int32_t length = v.len[i];
     if (length < 0) return;
     const uint32_t tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, len = (uint32_t)length, keep = a.keep;
@@ -188,7 +219,12 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
     // ---- selection among [first, end) of `quota` ----
     const uint32_t end = len - a.recent, quota = keep - a.first - a.recent;
     uint32_t least = 0, left = quota, ties = 0;     // kept: those above `least`, and the first `left` of the `ties` that equal it
+    uint32_t* ahead = bits + (a.max_tokens + 31) / 32;
+    uint32_t* cached = ahead + (a.max_tokens + 127) / 128;
+    auto bits_at = [&](uint32_t p) { return p < kCached ? cached[p] : weight_bits(weight[p]); };
     if (quota) {
+#pragma unroll 8
+        for (uint32_t p = tid; p < min(end, (uint32_t)kCached); p += kEvictThreads) cached[p] = weight_bits(weight[p]);
 #pragma unroll 1
         for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {       // digits [21, 32), [10, 21), [0, 10)
             for (uint32_t b = tid; b < 2048; b += kEvictThreads) sh.hist[b] = 0;
@@ -196,7 +232,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
             const uint32_t digits = shift ? 0x7ffu : 0x3ffu, above = shift == 21 ? 0u : shift == 10 ? 21u : 10u;
 #pragma unroll 4
             for (uint32_t p = a.first + tid; p < end; p += kEvictThreads) {
-                const uint32_t b = weight_bits(weight[p]);
+                const uint32_t b = bits_at(p);
                 if (above == 0 || b >> above == least >> above) atomicAdd(&sh.hist[(b >> shift) & digits], 1u);
             }
             __syncthreads();
@@ -232,7 +268,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
     auto look = [&](uint32_t w, bool& over, bool& same) {
         const uint32_t p = 32 * w + lane;
         const bool middle = p >= a.first && p < end;
-        const uint32_t b = middle && quota ? weight_bits(weight[p]) : 0u;
+        const uint32_t b = middle && quota ? bits_at(p) : 0u;
         over = p < len && (!middle || (quota && b > least));
         same = middle && quota && b == least;
     };
@@ -264,7 +300,6 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
     __syncthreads();
     // kept ones in front of each four words
     const uint32_t fours = (words + 3) / 4, run = (fours + kEvictThreads - 1) / kEvictThreads;
-    uint32_t* ahead = bits + (a.max_tokens + 31) / 32;
     {
         auto of = [&](uint32_t f) {
             uint32_t n = 0;
@@ -288,96 +323,100 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
             before += of(f);
         }
     }
-    if (tid < 96) (&sh.amax[0][0][0])[tid] = 0;
+    if (tid < 48) (&sh.amax[0][0][0])[tid] = 0;
     __syncthreads();
 
     // ---- move ----
     const int32_t* table = c.pages + (size_t)slot * c.max_pages;
-    const uint32_t now = (keep + c.page_tokens - 1) >> c.page_shift;
-    uint32_t fresh = (uint32_t)v.first[i];          // of the first warp: how many of the list's pages are taken, from the call's first on
-    const size_t scale_row = (size_t)layer * c.num_pages * c.heads + head;
-    const uint32_t tokens = a.pages * c.page_tokens, rounds = (keep + tokens - 1) / tokens;    // tokens of a round, at most 256
-    float moved = 0.0f;                             // the weight of this thread's token of the next round
-    auto origins = [&](uint32_t round) {
-        const uint32_t rank = round * tokens + tid;
-        if (wid == 0) {
-            const uint32_t e = round * a.pages + lane;
-            const int32_t id = lane < a.pages && e < now ? table[e] : 0;
-            const uint32_t votes = __ballot_sync(0xffffffffu, id < 0);
-            if (lane < a.pages) sh.target[round % 3][lane] = id < 0 ? v.list[fresh + __popc(votes & ((1u << lane) - 1))] : id;
-            fresh += __popc(votes);
-        }
-        if (tid >= tokens) return;
-        Origin o = {-1, 0.0f, 0.0f};
-        if (rank < keep) {
-            uint32_t lo = 0, hi = fours;            // ahead[lo] <= rank < ahead[hi]
-            while (hi - lo > 1) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (ahead[mid] <= rank) lo = mid;
-                else hi = mid;
-            }
-            uint32_t skip = rank - ahead[lo], w = 4 * lo;
-            for (uint32_t n; skip >= (n = __popc(bits[w])); ++w) skip -= n;
-            uint32_t b = bits[w];
-            for (; skip; --skip) b &= b - 1;
-            const uint32_t p = 32 * w + __ffs(b) - 1;
-            int32_t id = table[p >> c.page_shift];
-            if (id < 0) id = ~id;
-            o.at = (long long)id * c.page_stride + (long long)(p & (c.page_tokens - 1)) * c.token_step;
-            o.ks = c.k_scale[scale_row + (size_t)id * c.heads];
-            o.vs = c.v_scale[scale_row + (size_t)id * c.heads];
-            moved = weight[p];
-        }
-        sh.origin[round % 3][tid] = o;
-    };
-    origins(0);
-    __syncthreads();
-    const uint32_t side = wid >> 2, piece0 = (wid & 3) * 32 + lane;
+    const uint32_t now = (keep + c.page_tokens - 1) >> c.page_shift, rounds = (keep + kTokens - 1) / kTokens;
+    const uint32_t side = wid >> 2, own = 32 * (wid & 3) + lane;     // this lane's token of a round
     uint8_t* pool = (side ? c.v : c.k) + (long long)layer * a.layer_stride + (long long)head * c.head_step;
-    float* scales = (side ? c.v_scale : c.k_scale) + scale_row;
-    const uint32_t pieces = tokens * a.pieces;      // of a side and round: at most 2048
-    for (uint32_t round = 0; round < rounds; ++round) {
-        const Origin* from = sh.origin[round % 3];
-        uint32_t* amax = sh.amax[round % 3][side];
-        uint4 x[kPiecesEach];
-        float scale[kPiecesEach];
-        const float was = moved;
-#pragma unroll
-        for (int e = 0; e < kPiecesEach; ++e) {
-            const uint32_t f = piece0 + e * 128, token = (f * a.piece_inverse) >> 20;
-            scale[e] = -1.0f;
-            if (f < pieces && from[token].at >= 0) {
-                x[e] = *reinterpret_cast<const uint4*>(pool + from[token].at + 16 * (f - token * a.pieces));
-                scale[e] = side ? from[token].vs : from[token].ks;
-            }
+    float* scales = (side ? c.v_scale : c.k_scale) + (size_t)layer * c.num_pages * c.heads + head;
+    long long from = -1;                            // of this lane's token: bytes from the pool's start, its page's scale, its weight
+    float scale = 0.0f, heavy = 0.0f;
+    auto look_up = [&](uint32_t round) {
+        const uint32_t rank = round * kTokens + own;
+        from = -1;
+        if (rank >= keep) return;
+        uint32_t lo = 0, hi = fours;                // ahead[lo] <= rank < ahead[hi]
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (ahead[mid] <= rank) lo = mid;
+            else hi = mid;
         }
-        if (round + 1 < rounds) origins(round + 1);
+        uint32_t skip = rank - ahead[lo], w = 4 * lo;
+        for (uint32_t n; skip >= (n = __popc(bits[w])); ++w) skip -= n;
+        uint32_t b = bits[w];
+        for (; skip; --skip) b &= b - 1;
+        const uint32_t p = 32 * w + __ffs(b) - 1;
+        int32_t id = table[p >> c.page_shift];
+        if (id < 0) id = v.replaced[~id];
+        from = (long long)id * c.page_stride + (long long)(p & (c.page_tokens - 1)) * c.token_step;
+        scale = scales[(size_t)id * c.heads];
+        if (side == 0) heavy = weight[p];
+    };
+    const uint32_t piece = lane & (kLanes - 1), sub = lane / kLanes;  // load e: token e * kSpan + sub of the warp's
+    const bool real = 16 * piece < c.dim, two = c.page_tokens == 16;  // two: the warp's tokens lie in two pages
+    look_up(0);
+    for (uint32_t round = 0; round < rounds; ++round) {
+        uint4 x[kLanes];
 #pragma unroll
-        for (int e = 0; e < kPiecesEach; ++e) {
-            const uint32_t f = piece0 + e * 128, token = (f * a.piece_inverse) >> 20, page = token >> c.page_shift;
-            const float m = scale[e] >= 0.0f ? largest_of<kFormat>(x[e]) * scale[e] : 0.0f;
-            if (f - lane >= pieces) break;          // the same for the warp
-            if (c.page_tokens * a.pieces % 32 == 0) {
-                const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
-                if (lane == 0 && most) atomicMax(amax + page, most);
-            } else if (f < pieces) {
-                atomicMax(amax + page, __float_as_uint(m));
-            }
+        for (int e = 0; e < kLanes; ++e) {
+            const long long at = __shfl_sync(0xffffffffu, from, e * kSpan + sub);
+            x[e] = make_uint4(0, 0, 0, 0);
+            if (at >= 0 && real) x[e] = __ldcs(reinterpret_cast<const uint4*>(pool + at + 16 * piece));
+        }
+        const bool there = from >= 0;
+        const float was = there ? scale : 0.0f, carried = heavy;
+        if (round + 1 < rounds) look_up(round + 1);
+        uint32_t* amax = sh.amax[round % 3][side];
+        const uint32_t page = own >> c.page_shift;                    // of this lane's token, in the round
+        float most[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < kLanes; ++e) {
+            const float m = largest_of<kFormat>(x[e]) * __shfl_sync(0xffffffffu, was, e * kSpan + sub);
+            if (kLanes == 1) most[lane >> 4] = m;
+            else most[2 * e / kLanes] = fmaxf(most[2 * e / kLanes], m);
+        }
+        if (!two) most[0] = fmaxf(most[0], most[1]);
+        {
+            const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(most[0]));
+            if (lane == 0) atomicMax(amax + page, m);
+        }
+        if (two) {
+            const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(most[1]));
+            if (lane == 16) atomicMax(amax + page, m);
         }
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kPiecesEach; ++e) {
-            const uint32_t f = piece0 + e * 128, token = (f * a.piece_inverse) >> 20, page = token >> c.page_shift;
-            if (scale[e] < 0.0f) continue;
-            const int exponent = kv_scale_exponent(__uint_as_float(amax[page]), kFormat);
-            const float unit = pow2f(exponent);
-            const int32_t id = sh.target[round % 3][page];
-            uint8_t* to = pool + (long long)id * c.page_stride + (long long)(token & (c.page_tokens - 1)) * c.token_step + 16 * (f - token * a.pieces);
-            *reinterpret_cast<uint4*>(to) = scale[e] == unit ? x[e] : rescaled<kFormat>(x[e], scale[e], pow2f(-exponent));
-            if ((token & (c.page_tokens - 1)) == 0 && f == token * a.pieces) scales[(size_t)id * c.heads] = unit;
+        // where this lane's token goes, and by what its codes are multiplied: a power of two near 1, or else (negative) their scale
+        const int exponent = kv_scale_exponent(__uint_as_float(amax[page]), kFormat);
+        const uint32_t target = round * (kTokens >> c.page_shift) + page;
+        int32_t id = target < now ? table[target] : 0;
+        if (id < 0) id = v.list[~id];
+        const long long base = (long long)id * c.page_stride;
+        float ratio = was * pow2f(-exponent);
+        if ((__float_as_uint(ratio) & 0x7fffffu) != 0 || ratio < 0x1p-15f || ratio > 0x1p7f) ratio = -was;
+        if (there) {
+            if (side == 0) weight_out[round * kTokens + own] = carried;
+            if ((own & (c.page_tokens - 1)) == 0) scales[(size_t)id * c.heads] = pow2f(exponent);
         }
-        if (tid < tokens && round * tokens + tid < keep) weight_out[round * tokens + tid] = was;
-        if (tid < 32) (&sh.amax[(round + 2) % 3][0][0])[tid] = 0;    // read before this round's barrier, written behind the next one's
+        const uint32_t known = __ballot_sync(0xffffffffu, there);
+        const long long base0 = __shfl_sync(0xffffffffu, base, 0), base1 = __shfl_sync(0xffffffffu, base, 16);
+        const int exponent0 = __shfl_sync(0xffffffffu, exponent, 0), exponent1 = __shfl_sync(0xffffffffu, exponent, 16);
+#pragma unroll
+        for (int e = 0; e < kLanes; ++e) {
+            const uint32_t t = e * kSpan + sub;
+            const float r = __shfl_sync(0xffffffffu, ratio, t);
+            if (!(known >> t & 1) || !real) continue;
+            if (r > 0.0f) {
+                if (r != 1.0f) x[e] = multiplied<kFormat>(x[e], r);
+            } else {
+                x[e] = rescaled<kFormat>(x[e], -r, pow2f(-(t < 16 ? exponent0 : exponent1)));
+            }
+            const uint32_t inside = (32 * (wid & 3) + t) & (c.page_tokens - 1);
+            __stcs(reinterpret_cast<uint4*>(pool + (t < 16 ? base0 : base1) + (long long)inside * c.token_step + 16 * piece), x[e]);
+        }
+        if (tid < 16) (&sh.amax[(round + 2) % 3][0][0])[tid] = 0;    // read before this round's barrier, written behind the next one's
     }
     for (uint32_t p = keep + tid; p < len; p += kEvictThreads) weight_out[p] = 0.0f;
 
@@ -388,27 +427,26 @@ __global__ void __launch_bounds__(kEvictThreads, 2) evict_kernel(EvictArgs a) {
     if (!sh.last) return;
     const uint32_t held = (len + c.page_tokens - 1) >> c.page_shift;
     int32_t* entries = a.pages_out + (size_t)slot * c.max_pages;
-    if (wid == 0) {
-        fresh = (uint32_t)v.first[i];
-        for (uint32_t base = 0; base < held; base += 32) {
-            const uint32_t e = base + lane;
-            const int32_t id = e < held ? entries[e] : 0;
-            const bool replaced = e < now && id < 0;
-            const uint32_t votes = __ballot_sync(0xffffffffu, replaced);
-            if (e < held && (replaced || e >= now)) {
-                int32_t* count = a.refs + (replaced ? ~id : id);
-                if (atomicSub(count, 1) <= 0) {
-                    atomicAdd(count, 1);
-                    kv_flag(c.status, ROOMIE_FLAG_KV_PAGE);
-                }
-                const int32_t to = replaced ? v.list[fresh + __popc(votes & ((1u << lane) - 1))] : -1;
-                if (replaced) a.refs[to] = 1;
-                entries[e] = to;
-            }
-            fresh += __popc(votes);
+    for (uint32_t e = tid; e < held; e += kEvictThreads) {
+        const int32_t id = entries[e];
+        if (id >= 0 && e < now) continue;
+        int32_t* count = a.refs + (id < 0 ? v.replaced[~id] : id);
+        if (atomicSub(count, 1) <= 0) {
+            atomicAdd(count, 1);
+            kv_flag(c.status, ROOMIE_FLAG_KV_PAGE);
         }
-        if (lane == 0) a.length[slot] = (int32_t)keep;
+        const int32_t to = id < 0 ? v.list[~id] : -1;
+        if (id < 0) a.refs[to] = 1;
+        entries[e] = to;
     }
+    if (tid == 0) a.length[slot] = (int32_t)keep;
+}
+template <int kFormat> static void (*evict_kernel_for(const roomie_kv_cache* c))(EvictArgs) {
+    const uint32_t pieces = c->head_dim / 16;
+    if (pieces == 1) return evict_kernel<kFormat, 1>;
+    if (pieces == 2) return evict_kernel<kFormat, 2>;
+    if (pieces <= 4) return evict_kernel<kFormat, 4>;
+    return pieces <= 8 ? evict_kernel<kFormat, 8> : evict_kernel<kFormat, 16>;
 }
 
 }  // namespace roomie
@@ -431,17 +469,12 @@ extern "C" int roomie_kv_evict(const roomie_kv_cache* cache, const int32_t* seqs
     a.c = kv_view(cache, 0);
     a.layer_stride = cache->layer_stride;
     a.layers = cache->layers; a.n = n; a.keep = keep; a.first = first; a.recent = recent; a.max_tokens = (uint32_t)tokens;
-    a.pieces = cache->head_dim / 16;
-    a.piece_inverse = (1u << 20) / a.pieces + 1;
-    const uint32_t most = 2048 / (cache->page_tokens * a.pieces);                  // pages whose pieces fit the block's registers
-    a.pages = most < kRoundTokens / cache->page_tokens ? most : kRoundTokens / cache->page_tokens;
     a.seqs = seqs; a.ws = page_scratch(cache, workspace);
     a.weight = weight; a.weight_out = weight_out;
     a.refs = cache->refs; a.pages_out = cache->pages; a.length = cache->length;
     rc = launch("kv_evict_plan", evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, false, table_view(cache), seqs, n, keep, a.ws);
     if (rc != ROOMIE_OK) return rc;
-    const size_t smem = ((tokens + 31) / 32 + (tokens + 127) / 128) * sizeof(uint32_t);
-    const uint32_t blocks = n * cache->layers * cache->kv_heads;
-    return launch("kv_evict", cache->format == ROOMIE_KV_E4M3 ? evict_kernel<ROOMIE_KV_E4M3> : evict_kernel<ROOMIE_KV_INT8>, dim3(blocks), dim3(kEvictThreads), smem, st,
-                  true, a);
+    const size_t smem = ((tokens + 31) / 32 + (tokens + 127) / 128 + (tokens < kCached ? tokens : kCached)) * sizeof(uint32_t);
+    void (*k)(EvictArgs) = cache->format == ROOMIE_KV_E4M3 ? evict_kernel_for<ROOMIE_KV_E4M3>(cache) : evict_kernel_for<ROOMIE_KV_INT8>(cache);
+    return launch("kv_evict", k, dim3(n * cache->layers * cache->kv_heads), dim3(kEvictThreads), smem, st, true, a);
 }

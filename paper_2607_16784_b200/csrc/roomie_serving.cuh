@@ -13,7 +13,7 @@ void record_begin(const char* name, const void* fn, unsigned long long blocks, u
                   cudaStream_t st);
 void record_end(cudaStream_t st);
 
-int allow_smem(const void* fn, size_t bytes);   // more than 48 KB of dynamic shared memory for a kernel
+int allow_smem(const void* fn, size_t bytes);   // so much dynamic shared memory for a kernel that may need more than 48 KB in all
 
 // With `overlap` the kernel may start while the launch before it on the stream drains; it then waits for that launch's
 // results itself (grid_dependency_wait) before it reads or writes anything another kernel touches.
@@ -21,7 +21,7 @@ template <class... KArgs, class... Args>
 int launch(const char* name, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool overlap,
            Args... args) {
     const void* fn = reinterpret_cast<const void*>(kernel);
-    if (smem > 48 * 1024) {
+    if (smem > 16 * 1024) {                           // 48 KB less what a kernel has of its own, at most 32
         const int rc = allow_smem(fn, smem);
         if (rc != ROOMIE_OK) return rc;
     }
