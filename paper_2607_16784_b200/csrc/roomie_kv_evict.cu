@@ -109,7 +109,7 @@ struct EvictArgs {
 // 16-byte pieces are read by kLanes neighbouring lanes, all at once, into registers; the next round's tokens are looked up meanwhile.  Behind the one
 // barrier of a round, when the pages' largest magnitudes are known, the codes are written.  A token never moves up, so what a round writes was read by it
 // or a round before, and no round after it reads there: tokens move inside their own pages.
-constexpr int kEvictThreads = 256, kEvictWarps = kEvictThreads / 32, kCached = 8192;
+constexpr int kEvictThreads = 512, kEvictWarps = kEvictThreads / 32, kCached = 8192;
 
 // One thread, after a barrier of its block: what the block read of the table comes before the count, what it writes there behind it.
 __device__ __forceinline__ uint32_t count_done(int32_t* counter) {
@@ -121,7 +121,7 @@ __device__ __forceinline__ uint32_t count_done(int32_t* counter) {
 
 struct EvictShared {
     uint32_t hist[2048];
-    uint32_t amax[3][2][8];                         // rounds in turn, side, page: bits of the largest magnitude
+    uint32_t amax[3][2][kEvictWarps];                        // rounds in turn, side, page: bits of the largest magnitude
     uint32_t part[kEvictWarps];
     uint32_t digit, left, ties, last;
 };
@@ -147,7 +147,7 @@ template <int kFormat> __device__ __forceinline__ float largest_of(const uint4& 
             const uint32_t sign = (w[i] >> 7) & 0x01010101u;
             m = (w[i] ^ (sign * 0xffu)) + sign;                     // -128 becomes 128: no byte carries
         }
-        most = __vmaxu2(most, __vmaxu2(m, m << 8));
+        most = __vimax3_u16x2(most, m, m << 8);
     }
     most = max(most >> 24, (most >> 8) & 0xffu);
     if constexpr (kFormat == ROOMIE_KV_E4M3) return kv_value((uint8_t)min(most, 0x7eu), ROOMIE_KV_E4M3);
@@ -199,8 +199,8 @@ template <int kFormat> __device__ __noinline__ uint4 rescaled(uint4 x, float fro
 
 // kLanes: the least power of two that is at least a token's pieces; also the pieces of a lane.
 template <int kFormat, int kLanes>
-__global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_kernel(EvictArgs a) {
-    constexpr uint32_t kTokens = 128, kSpan = 32 / kLanes;           // of a round; of a warp's load
+__global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 1 : 2) evict_kernel(EvictArgs a) {
+    constexpr uint32_t kTokens = 16 * kEvictWarps, kSpan = 32 / kLanes;           // of a round; of a warp's load
     extern __shared__ uint32_t bits[];              // a bit for each of max_tokens, 1: kept; then how many are kept in front of each 128; then the
                                                     // bits of the first weights
     __shared__ EvictShared sh;
@@ -236,10 +236,11 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
                 if (above == 0 || b >> above == least >> above) atomicAdd(&sh.hist[(b >> shift) & digits], 1u);
             }
             __syncthreads();
-            // eight digits a thread, from the top: the one in which the left-th lies
+            // some digits a thread, from the top: the one in which the left-th lies
+            constexpr uint32_t kDigits = 2048 / kEvictThreads;
             uint32_t mine = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) mine += sh.hist[2047 - 8 * tid - k];
+            for (uint32_t k = 0; k < kDigits; ++k) mine += sh.hist[2047 - kDigits * tid - k];
             uint32_t upto = mine;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
             uint32_t before = upto - mine;
             for (uint32_t w = 0; w < wid; ++w) before += sh.part[w];
             if (before < left && left <= before + mine) {
-                uint32_t k = 2047 - 8 * tid;
+                uint32_t k = 2047 - kDigits * tid;
                 while (before + sh.hist[k] < left) before += sh.hist[k--];
                 sh.digit = k;
                 sh.left = left - before;
@@ -323,14 +324,16 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
             before += of(f);
         }
     }
-    if (tid < 48) (&sh.amax[0][0][0])[tid] = 0;
+    if (tid < 6 * kEvictWarps) (&sh.amax[0][0][0])[tid] = 0;
     __syncthreads();
 
     // ---- move ----
     const int32_t* table = c.pages + (size_t)slot * c.max_pages;
     const uint32_t now = (keep + c.page_tokens - 1) >> c.page_shift, rounds = (keep + kTokens - 1) / kTokens;
-    const uint32_t side = wid >> 2, own = 32 * (wid & 3) + lane;     // this lane's token of a round
-    uint8_t* pool = (side ? c.v : c.k) + (long long)layer * a.layer_stride + (long long)head * c.head_step;
+    const uint32_t side = wid / (kEvictWarps / 2), mine = 32 * (wid % (kEvictWarps / 2)), own = mine + lane;     // this lane's token of a round
+    const uint32_t piece = lane & (kLanes - 1), sub = lane / kLanes;  // load e: token e * kSpan + sub of the warp's
+    const bool real = 16 * piece < c.dim, two = c.page_tokens == 16;  // two: the warp's tokens lie in two pages
+    uint8_t* pool = (side ? c.v : c.k) + (long long)layer * a.layer_stride + (long long)head * c.head_step + (real ? 16 * piece : 0);
     float* scales = (side ? c.v_scale : c.k_scale) + (size_t)layer * c.num_pages * c.heads + head;
     long long from = -1;                            // of this lane's token: bytes from the pool's start, its page's scale, its weight
     float scale = 0.0f, heavy = 0.0f;
@@ -346,25 +349,29 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
         }
         uint32_t skip = rank - ahead[lo], w = 4 * lo;
         for (uint32_t n; skip >= (n = __popc(bits[w])); ++w) skip -= n;
-        uint32_t b = bits[w];
-        for (; skip; --skip) b &= b - 1;
-        const uint32_t p = 32 * w + __ffs(b) - 1;
+        uint32_t b = bits[w], p = 32 * w;
+#pragma unroll
+        for (int half = 16; half > 0; half /= 2) {  // the skip-th set bit
+            const uint32_t n = __popc(b & ((1u << half) - 1));
+            if (skip >= n) {
+                skip -= n;
+                b >>= half;
+                p += half;
+            }
+        }
         int32_t id = table[p >> c.page_shift];
         if (id < 0) id = v.replaced[~id];
         from = (long long)id * c.page_stride + (long long)(p & (c.page_tokens - 1)) * c.token_step;
         scale = scales[(size_t)id * c.heads];
         if (side == 0) heavy = weight[p];
     };
-    const uint32_t piece = lane & (kLanes - 1), sub = lane / kLanes;  // load e: token e * kSpan + sub of the warp's
-    const bool real = 16 * piece < c.dim, two = c.page_tokens == 16;  // two: the warp's tokens lie in two pages
     look_up(0);
     for (uint32_t round = 0; round < rounds; ++round) {
         uint4 x[kLanes];
 #pragma unroll
         for (int e = 0; e < kLanes; ++e) {
-            const long long at = __shfl_sync(0xffffffffu, from, e * kSpan + sub);
-            x[e] = make_uint4(0, 0, 0, 0);
-            if (at >= 0 && real) x[e] = __ldcs(reinterpret_cast<const uint4*>(pool + at + 16 * piece));
+            const long long at = __shfl_sync(0xffffffffu, max(from, 0ll), e * kSpan + sub);   // some token where there is none: it counts as 0
+            x[e] = __ldcs(reinterpret_cast<const uint4*>(pool + at));
         }
         const bool there = from >= 0;
         const float was = there ? scale : 0.0f, carried = heavy;
@@ -378,6 +385,7 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
             if (kLanes == 1) most[lane >> 4] = m;
             else most[2 * e / kLanes] = fmaxf(most[2 * e / kLanes], m);
         }
+        if (!real) most[0] = most[1] = 0.0f;
         if (!two) most[0] = fmaxf(most[0], most[1]);
         {
             const uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(most[0]));
@@ -393,7 +401,6 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
         const uint32_t target = round * (kTokens >> c.page_shift) + page;
         int32_t id = target < now ? table[target] : 0;
         if (id < 0) id = v.list[~id];
-        const long long base = (long long)id * c.page_stride;
         float ratio = was * pow2f(-exponent);
         if ((__float_as_uint(ratio) & 0x7fffffu) != 0 || ratio < 0x1p-15f || ratio > 0x1p7f) ratio = -was;
         if (there) {
@@ -401,22 +408,29 @@ __global__ void __launch_bounds__(kEvictThreads, kLanes == 16 ? 2 : 4) evict_ker
             if ((own & (c.page_tokens - 1)) == 0) scales[(size_t)id * c.heads] = pow2f(exponent);
         }
         const uint32_t known = __ballot_sync(0xffffffffu, there);
-        const long long base0 = __shfl_sync(0xffffffffu, base, 0), base1 = __shfl_sync(0xffffffffu, base, 16);
-        const int exponent0 = __shfl_sync(0xffffffffu, exponent, 0), exponent1 = __shfl_sync(0xffffffffu, exponent, 16);
+        const int exponent0 = __shfl_sync(0xffffffffu, exponent, 0), exponent1 = __shfl_sync(0xffffffffu, exponent, 31);
+        // the first token's page, and with `two` the last one's
+        const int32_t last = __shfl_sync(0xffffffffu, id, 31);
+        id = __shfl_sync(0xffffffffu, id, 0);
+        uint8_t* to = pool + (long long)id * c.page_stride + (long long)((mine + sub) & (c.page_tokens - 1)) * c.token_step;
+        const long long step = (long long)kSpan * c.token_step;
+        if (two && kLanes == 1 && sub >= 16) to += (long long)(last - id) * c.page_stride;
 #pragma unroll
         for (int e = 0; e < kLanes; ++e) {
             const uint32_t t = e * kSpan + sub;
             const float r = __shfl_sync(0xffffffffu, ratio, t);
-            if (!(known >> t & 1) || !real) continue;
-            if (r > 0.0f) {
-                if (r != 1.0f) x[e] = multiplied<kFormat>(x[e], r);
-            } else {
-                x[e] = rescaled<kFormat>(x[e], -r, pow2f(-(t < 16 ? exponent0 : exponent1)));
+            if (kLanes > 1 && e == kLanes / 2 && two) to += (long long)(last - id) * c.page_stride - 16ll * c.token_step;
+            if ((known >> t & 1) && real) {
+                if (r > 0.0f) {
+                    if (r != 1.0f) x[e] = multiplied<kFormat>(x[e], r);
+                } else {
+                    x[e] = rescaled<kFormat>(x[e], -r, pow2f(-(t < 16 ? exponent0 : exponent1)));
+                }
+                __stcs(reinterpret_cast<uint4*>(to), x[e]);
             }
-            const uint32_t inside = (32 * (wid & 3) + t) & (c.page_tokens - 1);
-            __stcs(reinterpret_cast<uint4*>(pool + (t < 16 ? base0 : base1) + (long long)inside * c.token_step + 16 * piece), x[e]);
+            to += step;
         }
-        if (tid < 16) (&sh.amax[(round + 2) % 3][0][0])[tid] = 0;    // read before this round's barrier, written behind the next one's
+        if (tid < 2 * kEvictWarps) (&sh.amax[(round + 2) % 3][0][0])[tid] = 0;    // read before this round's barrier, written behind the next one's
     }
     for (uint32_t p = keep + tid; p < len; p += kEvictThreads) weight_out[p] = 0.0f;
 
