@@ -34,11 +34,12 @@ template <int DP> struct FewWeights {
     static constexpr int kGroups = DP > 128 ? 1 : 2;                // 16-key groups of a step
     static constexpr int kStep = 16 * kGroups;
     static constexpr int kSide = kStep * DP;                        // bytes of a step's keys
-    static constexpr int kStages = 16384 / kSide;                   // 16 KB a warp
+    static constexpr int kStages = 12288 / kSide;                   // 12 KB a warp
     static constexpr int kStage = kSide + kStep * 4 + 16;           // codes, the keys' old weights, the groups' scales
     static constexpr int kRing = kStages * kStage;
     static constexpr int kSmem = kRing * kWeightWarps;
 };
+template <int DP, int NT> constexpr int kWeightBlocks = DP > 128 && NT > 1 ? 3 : 4;      // of an SM: 16 warps with 128 registers a thread, but for these
 
 struct WeightSeq {                                   // a sequence of the call, as its warps need it
     unsigned long long first;                        // flat index of its first step
@@ -46,7 +47,7 @@ struct WeightSeq {                                   // a sequence of the call, 
 };
 
 template <int DP, int NT, int kFormat, class T>
-__global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightArgs a) {
+__global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_weights_kernel(WeightArgs a) {
     using F = FewWeights<DP>;
     constexpr int G = F::kGroups, KW = DP / 16, KS = DP / 16, kStages = F::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -95,80 +96,107 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) seq = max(seq, __shfl_xor_sync(0xffffffffu, seq, d));
 
-        // ---- copies: a place of its own in the flat order, some steps ahead ----
+        // ---- two places in the flat order: of the products, and some steps ahead of the copies ----
         struct Place {
-            uint32_t seq, head, step;
-            unsigned long long left;                                // steps of the warp's share from here on
+            uint32_t seq, head, steps;                              // steps: of this (sequence, head) from here on
+            unsigned long long left;                                // of the warp's share
+            int key, length;                                        // first key of the step; the sequence's length
         };
         const unsigned long long inside = at - sh_seq[seq].first;
-        Place now = {seq, (uint32_t)(inside / sh_seq[seq].steps), (uint32_t)(inside % sh_seq[seq].steps), end - at}, next = now;
-        auto go_on = [&](Place& p) {
+        Place now;
+        now.seq = seq;
+        now.head = (uint32_t)(inside / sh_seq[seq].steps);
+        now.left = end - at;
+        {
+            const uint32_t step = (uint32_t)(inside - (unsigned long long)now.head * sh_seq[seq].steps);
+            now.steps = sh_seq[seq].steps - step;
+            now.key = (int)(sh_seq[seq].step0 + step) * F::kStep;
+            now.length = (int)sh_seq[seq].length;
+        }
+        Place next = now;
+        auto go_on = [&](Place& p) {                                // true: another (sequence, head)
             --p.left;
-            if (++p.step < sh_seq[p.seq].steps) return;
-            p.step = 0;
-            if (++p.head < kv.heads) return;
-            p.head = 0;
-            if (p.left) do ++p.seq; while (sh_seq[p.seq].steps == 0);
+            p.key += F::kStep;
+            if (--p.steps || !p.left) return false;
+            if (++p.head == kv.heads) {
+                p.head = 0;
+                do ++p.seq; while (sh_seq[p.seq].steps == 0);
+            }
+            p.steps = sh_seq[p.seq].steps;
+            p.key = (int)sh_seq[p.seq].step0 * F::kStep;
+            p.length = (int)sh_seq[p.seq].length;
+            return true;
+        };
+        constexpr int kChunks = DP / 16, kRowsPer = 32 / kChunks, kLoads = 16 / kRowsPer;      // of a group: row0 + i * kRowsPer
+        const uint32_t chunk = lane % kChunks, row0 = lane / kChunks;
+        const bool real = 16 * chunk < kv.dim;
+        const uint32_t ring_at = smem_addr(ring), place0 = code_at<DP>(row0, chunk);
+        const int32_t* table;                                       // of the copies' (sequence, head)
+        const uint8_t* codes;
+        const float *was, *scales;
+        int low, known;                                             // keys before `low` no row sees; those before `known` have received something before
+        auto enter = [&] {
+            const WeightSeq& s = sh_seq[next.seq];
+            const int start = (int)s.length - (int)s.count;
+            table = kv.pages + (size_t)s.slot * kv.max_pages;
+            codes = kv.k + (long long)next.head * kv.head_step + (real ? 16 * chunk : 0) + (long long)row0 * kv.token_step;
+            was = a.weight + ((size_t)s.slot * kv.heads + next.head) * a.max_tokens;
+            scales = kv.k_scale + next.head;
+            low = a.window ? first_seen(start, a.window) : 0;
+            known = a.fresh ? 0 : start;
         };
         int32_t page[G];
-        auto get_pages = [&] {                                      // of the place that is copied next
-#pragma unroll
-            for (int g = 0; g < G; ++g) page[g] = -1;
-            if (!next.left) return;
-            const WeightSeq& s = sh_seq[next.seq];
-            const uint32_t k0 = (s.step0 + next.step) * F::kStep;
-            const int start = (int)s.length - (int)s.count;
-            const uint32_t low = a.window ? (uint32_t)first_seen(start, a.window) : 0u;
+        auto get_pages = [&] {                                      // of the step that is copied next
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const uint32_t k = k0 + 16 * g;
-                if (k >= s.length || k + 16 <= low) continue;
-                const int32_t id = __ldg(kv.pages + (size_t)s.slot * kv.max_pages + (k >> kv.page_shift));
-                page[g] = id;
-                if ((uint32_t)id >= kv.num_pages) {
-                    if (lane == 0) kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
-                    page[g] = -1;
+                const int k = next.key + 16 * g;
+                page[g] = -1;
+                if (next.left && k < next.length && k + 16 > low) {
+                    page[g] = __ldg(table + (k >> kv.page_shift));
+                    if ((uint32_t)page[g] >= kv.num_pages) {
+                        if (lane == 0) kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
+                        page[g] = -1;
+                    }
                 }
             }
         };
-        constexpr int kChunks = DP / 16, kRowsPer = 32 / kChunks, kLoads = F::kStep / kRowsPer;
-        const uint32_t chunk = lane % kChunks, row0 = lane / kChunks;
-        auto copy_step = [&](int stage) {                           // of `next`, which moves on
+        auto copy_step = [&](uint32_t to) {                         // of `next`, which moves on
             if (next.left) {
-                const WeightSeq& s = sh_seq[next.seq];
-                const uint32_t k0 = (s.step0 + next.step) * F::kStep, to = smem_addr(ring + stage * F::kStage);
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const uint32_t row = row0 + i * kRowsPer, key = k0 + row;
-                    const int g = i * kRowsPer / 16;                // (kRowsPer divides 16)
-                    const uint32_t n = page[g] >= 0 && 16 * chunk < kv.dim && key < s.length ? 16u : 0u;   // the rest becomes zeros
-                    const uint8_t* p = kv.k + (long long)max(page[g], 0) * kv.page_stride + (long long)next.head * kv.head_step +
-                                       (long long)(key & (kv.page_tokens - 1)) * kv.token_step + 16 * chunk;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + code_at<DP>(row, chunk)), "l"(n ? p : kv.k), "r"(n) : "memory");
+                for (int g = 0; g < G; ++g) {
+                    const int k = next.key + 16 * g;
+                    const uint8_t* p = codes + (long long)max(page[g], 0) * kv.page_stride + (long long)(k & (int)(kv.page_tokens - 1)) * kv.token_step;
+                    const int rows = page[g] >= 0 && real ? next.length - k - (int)row0 : 0;   // the rest becomes zeros
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) {
+                        // row r of a step lies at code_at(r): rows kRowsPer apart differ in the chunks' exchange by those bits
+                        const uint32_t d = (DP >= 128 ? place0 ^ ((kRowsPer * i & 7) << 4) : place0) + (16 * g + kRowsPer * i) * DP;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + d), "l"(p), "r"(i * kRowsPer < rows ? 16u : 0u) : "memory");
+                        p += kRowsPer * kv.token_step;
+                    }
                 }
                 if (lane < F::kStep) {
-                    const uint32_t key = k0 + lane;
-                    const float* p = a.weight + ((size_t)s.slot * kv.heads + next.head) * a.max_tokens + key;
-                    const uint32_t n = !a.fresh && key + s.count < s.length ? 4u : 0u;      // the call's own keys have received nothing before
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + F::kSide + 4 * lane), "l"(n ? p : a.weight), "r"(n) : "memory");
+                    const int k = next.key + lane;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + F::kSide + 4 * lane), "l"(k < known ? was + k : was), "r"(k < known ? 4u : 0u)
+                                 : "memory");
                 }
-                float* scales = reinterpret_cast<float*>(ring + stage * F::kStage + F::kSide + 4 * F::kStep);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     if (lane == g) {
-                        if (page[g] < 0) scales[g] = -1.0f;         // no page
+                        const uint32_t d = to + F::kSide + 4 * F::kStep + 4 * g;
+                        if (page[g] < 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(d), "f"(-1.0f) : "memory");       // no page
                         else
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(scales + g)),
-                                         "l"(kv.k_scale + (size_t)page[g] * kv.heads + next.head) : "memory");
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(scales + (size_t)page[g] * kv.heads) : "memory");
                     }
-                go_on(next);
+                if (go_on(next)) enter();
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
+        enter();
         get_pages();
 #pragma unroll 1
         for (int i = 0; i < kStages; ++i) {
-            copy_step(i);
+            copy_step(ring_at + i * F::kStage);
             get_pages();
         }
 
@@ -176,8 +204,11 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
         uint32_t qf[NT][KS][2];
         float qscale[NT][2], lse2[NT][2];
         int see_hi[NT][2], see_lo[NT][2];                           // rows 2c and 2c + 1 of each eight see keys [lo, hi)
+        int all_hi, all_lo;                                         // every row of the tile sees [all_lo, all_hi)
         auto load_queries = [&](const WeightSeq& s, uint32_t head, uint32_t first_row) {
             const uint32_t rows = s.count * a.group;
+            all_hi = 0x7fffffff;
+            all_lo = 0;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const uint32_t row = first_row + t * 8 + r, tok = row / a.group;
@@ -225,36 +256,46 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
                     const int pos = start + (int)(rc / a.group);
                     see_hi[t][n] = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
                     see_lo[t][n] = a.window ? first_seen(pos, a.window) : 0;
+                    if (rc >= rows) lse2[t][n] = INFINITY;          // takes no part, whether its keys are looked at one by one or not
+                    else {
+                        all_hi = min(all_hi, see_hi[t][n]);
+                        all_lo = max(all_lo, see_lo[t][n]);
+                    }
                 }
+            }
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) {
+                all_hi = min(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, d));
+                all_lo = max(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, d));
             }
         };
 
-        uint32_t q_seq = 0xffffffffu, q_head = 0;
+        bool fresh_queries = true;
         int stage = 0;
+        float* weight = a.weight + ((size_t)sh_seq[now.seq].slot * kv.heads + now.head) * a.max_tokens;
+        uint32_t rows = sh_seq[now.seq].count * a.group;
+        const uint32_t place = 16 * (c >> 1) + 8 * (c & 1) + r;     // a key's rows lie in four lanes; lane c writes key r + 8 * (c & 1) of group c >> 1
         while (now.left) {
-            const WeightSeq& s = sh_seq[now.seq];
-            const uint32_t rows = s.count * a.group, k0 = (s.step0 + now.step) * F::kStep;
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             __syncwarp();
             const uint8_t* side = ring + stage * F::kStage;
             const float* old = reinterpret_cast<const float*>(side + F::kSide);
             float ks[G], sum[G][2];
+            bool pages = true;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 ks[g] = old[F::kStep + g];
+                pages = pages && ks[g] >= 0.0f;
                 sum[g][0] = sum[g][1] = 0.0f;
             }
             for (uint32_t first_row = 0; first_row < rows; first_row += 8 * NT) {
-                if (rows > 8 * NT || now.seq != q_seq || now.head != q_head) {
-                    load_queries(s, now.head, first_row);
-                    q_seq = now.seq;
-                    q_head = now.head;
-                }
+                if (fresh_queries) load_queries(sh_seq[now.seq], now.head, first_row);
+                fresh_queries = rows > 8 * NT;
+                float sc[G][NT][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    float sc[NT][4];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.0f;
+                    for (int t = 0; t < NT; ++t) sc[g][t][0] = sc[g][t][1] = sc[g][t][2] = sc[g][t][3] = 0.0f;
                     uint32_t kr[2][KW];
                     read_span<DP, KW>(kr[0], side, 16 * g + r, c * (DP / 4));
                     read_span<DP, KW>(kr[1], side, 16 * g + r + 8, c * (DP / 4));
@@ -264,20 +305,29 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
                         codes_to_f16<kFormat>(kr[0][i], a0, a2);
                         codes_to_f16<kFormat>(kr[1][i], a1, a3);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16816(sc[t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
+                        for (int t = 0; t < NT; ++t) mma16816(sc[g][t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
                     }
-                    // sc[e] is key r + 8 * (e >> 1) of the group, row 2c + (e & 1)
+                }
+                // sc[e] is key r + 8 * (e >> 1) of the group, row 2c + (e & 1)
+                const bool whole = pages && now.key >= all_lo && now.key + F::kStep <= all_hi;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int n = e & 1, k = (int)k0 + 16 * g + 8 * (e >> 1) + r;
-                            const float p = exp2_fast(fmaf(sc[t][e], qscale[t][n] * ks[g], -lse2[t][n]));
-                            if (k < see_hi[t][n] && k >= see_lo[t][n] && !(ks[g] < 0.0f)) sum[g][e >> 1] += p;
+                        for (int n = 0; n < 2; ++n) {
+                            const float f = qscale[t][n] * ks[g];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float x = fmaf(sc[g][t][2 * h + n], f, -lse2[t][n]);
+                                if (!whole) {
+                                    const int k = now.key + 16 * g + 8 * h + r;
+                                    if (k >= see_hi[t][n] || k < see_lo[t][n] || ks[g] < 0.0f) x = -INFINITY;
+                                }
+                                sum[g][h] += exp2_fast(x);
+                            }
                         }
-                }
             }
-            // a key's rows lie in four lanes; lane c writes key r + 8 * (c & 1) of group c >> 1
             float mine = 0.0f;
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -288,13 +338,17 @@ __global__ void __launch_bounds__(kWeightThreads, 3) few_weights_kernel(WeightAr
                     x += __shfl_xor_sync(0xffffffffu, x, 2);
                     if (c == 2 * g + h) mine = x;
                 }
-            const uint32_t place = 16 * (c >> 1) + 8 * (c & 1) + r, key = k0 + place;
-            if (c < 2 * G && key < s.length) a.weight[((size_t)s.slot * kv.heads + now.head) * a.max_tokens + key] = old[place] + mine;
+            const int key = now.key + (int)place;
+            if (c < 2 * G && key < now.length) weight[key] = old[place] + mine;
             __syncwarp();                                           // the stage is read
-            copy_step(stage);
+            copy_step(ring_at + stage * F::kStage);
             get_pages();
             if (++stage == kStages) stage = 0;
-            go_on(now);
+            if (go_on(now)) {
+                fresh_queries = true;
+                weight = a.weight + ((size_t)sh_seq[now.seq].slot * kv.heads + now.head) * a.max_tokens;
+                rows = sh_seq[now.seq].count * a.group;
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     }
@@ -623,7 +677,7 @@ template <int DP, int kFormat, class T> static int launch_many_weights(const Wei
 }
 
 template <int DP, int NT, int kFormat, class T> static int launch_few_weights(const WeightArgs& a, cudaStream_t st) {
-    return launch("kv_weights", few_weights_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * 3), dim3(kWeightThreads), FewWeights<DP>::kSmem, st, false, a);
+    return launch("kv_weights", few_weights_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * kWeightBlocks<DP, NT>), dim3(kWeightThreads), FewWeights<DP>::kSmem, st, false, a);
 }
 enum class Rows { eight, sixteen, many };
 template <int DP, int kFormat, class T> static int weight_rows(const WeightArgs& a, Rows rows, cudaStream_t st) {
