@@ -2,6 +2,7 @@
 // exp(scale * ks[page] * q_i.k_j - lse_i).
 //
 // Every key's sum is one thread's (or one warp's, in a fixed order): nothing is joined, and a call repeats bit for bit.
+#include <cuda.h>
 #include <type_traits>
 #include "roomie_kv_attention.cuh"
 #include "roomie_tc.cuh"
@@ -12,7 +13,8 @@ struct WeightArgs {
     KvView c;
     const int32_t *seqs, *q_offset;
     uint32_t num_seqs, rows, q_heads, group;
-    unsigned long long group_inverse;                // 2^64 / group + 1, 0 for a group of 1
+    uint32_t block_tokens, block_heads;              // of a block of rows: 32 / group and group, or 1 and 32
+    int32_t tensor_copies;
     const void* q;
     long long q_token, q_head;
     const float* lse;                                // [rows][q_heads]
@@ -356,33 +358,36 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
 
 // ---- many rows a key head ----------------------------------------------------------------------------------------------------------
 // Products on the fifth-generation tensor cores, transposed: S^T = K q^T with 128 keys as the accumulator's rows, so that a thread owns a key: it
-// reads its key's products with 64 query rows after the other from tensor memory and adds up their exponentials.  Nothing is exchanged between
-// threads, and a key's scale is a factor of its thread.
+// reads its key's products with 32 query rows after the other from tensor memory and adds up their exponentials.  Nothing is exchanged between
+// threads, and a key's scale is a factor of its thread.  The keys are the operand that stays: widened to q's type (exactly) they lie in tensor
+// memory too, so that a product reads only the queries from shared memory.
 //
-// A block has 256 keys of one (sequence, key head) at a time, two tiles.  Warpgroups 0 and 1 turn their tile's codes into operands (of q's type:
-// exact), then take the exponentials; in warpgroup 2 one warp issues the products and three bring the queries, 64 rows at a time, by asynchronous
-// copies.  While the exponentials of 64 rows are taken, the products of the next are under way.
-constexpr int kManyThreads = 384, kManyRows = 64, kManyKeys = 256, kLoaders = 96;
+// A block has 128 keys of one (sequence, key head) at a time.  Warps 0 to 3 widen the codes and take the exponentials; warp 4 issues the products;
+// warp 5 brings the queries, up to 32 rows at a time, by tensor copies (rows that are not aligned to 16 bytes: by hand), warp 6 the codes of the next keys
+// by asynchronous copies.  Four blocks share an SM (two with heads of more than 128): while one waits or widens, the others keep the
+// special-function units busy.  A block of rows is whole tokens of the group, or part of one where the group has more than 32 heads.
+constexpr int kManyThreads = 224, kManyRows = 32, kManyKeys = 128, kManySeqs = 128;
+constexpr int kQueryStages = 4;                      // of 32 rows
+constexpr int kLseStages = 8;                        // the exponentials lag the products by at most two blocks, and the queries are at most four ahead of these
 
 template <int DP> struct Many {
-    static constexpr int kSlabs = DP / 64;                          // 64-column slabs of an operand
-    static constexpr uint32_t kKeySlab = 128 * 128, kKeyOperand = kSlabs * kKeySlab;          // bytes: 128 keys
-    static constexpr uint32_t kRowSlab = kManyRows * 128, kRowOperand = kSlabs * kRowSlab;    // 64 query rows
-    static constexpr uint32_t kSmem = 2 * kKeyOperand + 2 * kRowOperand + 1024;
-    static constexpr int kPerSm = DP > 128 ? 1 : 2;
+    static constexpr uint32_t kCodes = kManyKeys * DP;              // bytes: codes of 128 keys
+    static constexpr uint32_t kRowSlab = kManyRows * 128, kRowOperand = DP / 64 * kRowSlab;   // 64-column slabs of 32 query rows
+    static constexpr uint32_t kSmem = kCodes + kQueryStages * kRowOperand + 1024;
+    static constexpr uint32_t kColumns = DP > 128 ? 256 : 128;      // of tensor memory: two S of 32, then the keys' DP / 2
+    static constexpr int kPerSm = DP > 128 ? 2 : 4;
 };
 struct ManyShared {
-    uint64_t k_full, q_full[4], q_empty[2], s_full[2], s_empty[2], drain;
-    __align__(16) float lse[4][kManyRows];           // of the rows, negated and in powers of two; -infinity: no row
-    long long at[2][8];                              // of 16 keys each: bytes from the pool's start to them, -1: none
-    float ks[2][8];
-    WeightSeq seq[kManyThreads / 3];
+    uint64_t codes_full, codes_empty, k_full, q_full[kQueryStages], q_empty[kQueryStages], s_full[2], s_empty[2], drain;
+    __align__(16) float lse[kLseStages][kManyRows];  // of the rows, negated and in powers of two; -infinity: no row
+    float ks[8];                                     // of 16 keys each; -1: no page
+    WeightSeq seq[kManySeqs];
     unsigned long long sum[kManyThreads / 32];
     uint32_t tmem, failed;
 };
 
-struct ManyUnit {                                    // 256 keys of a (sequence, head), and the rows that see some of them
-    uint32_t seq, head, k0, row0, row1;
+struct ManyUnit {                                    // 128 keys of a (sequence, head), and the tokens whose rows see some of them
+    uint32_t seq, head, k0, t0, t1;
 };
 __device__ __forceinline__ ManyUnit many_unit(const WeightArgs& a, const ManyShared& sh, uint32_t here, unsigned long long at) {
     uint32_t lo = 0, hi = here;                      // the last one of those that begin at or before `at`: it is not empty
@@ -399,232 +404,284 @@ __device__ __forceinline__ ManyUnit many_unit(const WeightArgs& a, const ManySha
     u.k0 = (s.step0 + inside - u.head * s.steps) * kManyKeys;
     const long long start = (long long)s.length - s.count, last = min(u.k0 + kManyKeys, s.length) - 1ll;
     const long long t0 = max(0ll, (long long)u.k0 - start), t1 = a.window ? min((long long)s.count, last + a.window - start) : (long long)s.count;
-    u.row0 = (uint32_t)t0 * a.group;
-    u.row1 = t1 > t0 ? (uint32_t)t1 * a.group : u.row0;
+    u.t0 = (uint32_t)t0;
+    u.t1 = t1 > t0 ? (uint32_t)t1 : u.t0;
     return u;
 }
+// The unit's blocks of rows: tokens [t, t + tokens), heads [h, h + heads) of the group; f(t, h).  false from f ends it.
+template <class F> __device__ __forceinline__ bool row_blocks(const WeightArgs& a, uint32_t t0, uint32_t t1, F f) {
+    for (uint32_t t = t0; t < t1; t += a.block_tokens)
+        for (uint32_t h = 0; h < a.group; h += a.block_heads)
+            if (!f(t, h)) return false;
+    return true;
+}
 
-// 16 codes to two 16-byte chunks of T
-template <int kFormat, class T> __device__ __forceinline__ void widen_to(const uint4& c, uint4& x, uint4& y) {
-    codes_to_f16<kFormat>(c.x, x.x, x.y);
-    codes_to_f16<kFormat>(c.y, x.z, x.w);
-    codes_to_f16<kFormat>(c.z, y.x, y.y);
-    codes_to_f16<kFormat>(c.w, y.z, y.w);
-    if constexpr (sizeof(T) == 2 && !std::is_same<T, __half>::value) {
+// 16 codes to eight pairs of T
+template <int kFormat, class T> __device__ __forceinline__ void widen_to(const uint4& c, uint32_t* x) {
+    codes_to_f16<kFormat>(c.x, x[0], x[1]);
+    codes_to_f16<kFormat>(c.y, x[2], x[3]);
+    codes_to_f16<kFormat>(c.z, x[4], x[5]);
+    codes_to_f16<kFormat>(c.w, x[6], x[7]);
+    if constexpr (!std::is_same<T, __half>::value) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            uint32_t& w = i < 4 ? (&x.x)[i] : (&y.x)[i - 4];
-            const float2 f = __half22float2(reinterpret_cast<const __half2&>(w));
+            const float2 f = __half22float2(reinterpret_cast<const __half2&>(x[i]));
             const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
-            w = reinterpret_cast<const uint32_t&>(b);
+            x[i] = reinterpret_cast<const uint32_t&>(b);
         }
     }
 }
 
+// Where piece `piece` of key `row` lies among the codes: exchanged so that the 8 lanes of an access hit different banks, by rows in the reading, by
+// pieces in the writing.
+template <int DP> __device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t piece) {
+    if constexpr (DP == 64) return row * 64 + ((piece ^ (row >> 1 & 3)) << 4);
+    return row * DP + ((piece ^ (row & 7)) << 4);
+}
+
+// warps 0 to 3
 template <int DP, int kFormat, class T>
-__device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block) {
-    using M = Many<DP>;
-    constexpr int kPerRow = DP / 16, kRowStep = 128 / kPerRow;      // 16-code pieces of a key; piece e of a thread: key row0 + e * kRowStep
+__device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, const uint8_t* codes, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block,
+                                          uint32_t& units) {
     const KvView& kv = a.c;
-    const uint32_t tile = threadIdx.x >> 7, tid = threadIdx.x & 127, lanes = (threadIdx.x & 96) << 16;
-    const uint32_t piece = tid % kPerRow, row0 = tid / kPerRow;
-    // the odd slabs store their second chunk first: the eight lanes of a store then hit different banks
-    const uint32_t slab = piece / 4, swap = slab & 1, chunk = (piece & 3) * 2;
-    uint8_t* to0 = smem + tile * M::kKeyOperand + slab * M::kKeySlab + row0 * 128 + (((chunk + swap) ^ (row0 & 7)) << 4);
-    const uint32_t to1 = (((chunk + 1 - swap) ^ (row0 & 7)) << 4) - (((chunk + swap) ^ (row0 & 7)) << 4);
+    const uint32_t tid = threadIdx.x, tm = sh.tmem + ((tid & 96) << 16);
     for (; at < end; at += gridDim.x) {
         const ManyUnit u = many_unit(a, sh, here, at);
         const WeightSeq& s = sh.seq[u.seq];
         const int start = (int)s.length - (int)s.count;
-        const uint32_t key0 = u.k0 + 128 * tile, key = key0 + tid;
+        const uint32_t key = u.k0 + tid;
         const bool mine = key < s.length;
         float* weight = a.weight + ((size_t)s.slot * kv.heads + u.head) * a.max_tokens + key;
         const float old = mine && !a.fresh && key + s.count < s.length ? *weight : 0.0f;
         float total = 0.0f;
-        if (u.row1 > u.row0) {
-            if (tid < 8) {                                           // pages of 16 keys each
-                const uint32_t k = key0 + 16 * tid, low = a.window ? (uint32_t)first_seen(start, a.window) : 0u;
-                int32_t id = -1;
-                if (k < s.length && k + 16 > low) {
-                    id = __ldg(kv.pages + (size_t)s.slot * kv.max_pages + (k >> kv.page_shift));
-                    if ((uint32_t)id >= kv.num_pages) {
-                        kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
-                        id = -1;
-                    }
-                }
-                sh.at[tile][tid] = id < 0 ? -1ll : (long long)id * kv.page_stride + (long long)(k & (kv.page_tokens - 1)) * kv.token_step;
-                sh.ks[tile][tid] = id < 0 ? 0.0f : __ldg(kv.k_scale + (size_t)id * kv.heads + u.head);
-            }
-            if (tile) asm volatile("bar.sync 2, 128;" ::: "memory");
-            else asm volatile("bar.sync 1, 128;" ::: "memory");
-            const uint8_t* pool = kv.k + (long long)u.head * kv.head_step + 16 * piece;
-            uint4 c[kPerRow];
+        if (u.t1 > u.t0) {
+            if (!warp_wait(&sh.codes_full, units & 1, sh)) return;
+            ++units;
+            const float ks = sh.ks[tid >> 4], f = ks * a.scale_log2;
 #pragma unroll
-            for (int e = 0; e < kPerRow; ++e) {
-                const uint32_t row = row0 + e * kRowStep;
-                const long long from = sh.at[tile][row >> 4];
-                c[e] = make_uint4(0, 0, 0, 0);
-                if (from >= 0 && 16 * piece < kv.dim && key0 + row < s.length)
-                    c[e] = __ldg(reinterpret_cast<const uint4*>(pool + from + (long long)(row & 15) * kv.token_step));
-            }
-            const bool there = sh.at[tile][tid >> 4] >= 0;
-            const float f = sh.ks[tile][tid >> 4] * a.scale_log2;
+            for (int h = 0; h < DP / 64; ++h) {                      // 64 elements at a time: 32 columns
+                uint32_t x[32];
 #pragma unroll
-            for (int e = 0; e < kPerRow; ++e) {
-                uint4 x, y;
-                widen_to<kFormat, T>(c[e], x, y);
-                uint8_t* to = to0 + e * kRowStep * 128;
-                *reinterpret_cast<uint4*>(to) = swap ? y : x;
-                *reinterpret_cast<uint4*>(to + to1) = swap ? x : y;
+                for (int e = 0; e < 4; ++e) widen_to<kFormat, T>(*reinterpret_cast<const uint4*>(codes + piece_at<DP>(tid, 4 * h + e)), x + 8 * e);
+                tmem_store32(tm + 2 * kManyRows + 32 * h, x);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.codes_empty);
+            tmem_wait_st();
+            tc_fence_before();
             mbar_arrive(&sh.k_full);
-            // the rows that see this key: [lo, hi)
-            const long long first = max(0ll, (long long)key - start), past = a.window ? min((long long)s.count, (long long)key + a.window - start) : (long long)s.count;
-            const uint32_t lo = (uint32_t)min(first, (long long)s.count) * a.group, hi = past > 0 ? (uint32_t)past * a.group : 0u;
+            // the tokens that see this key: [lo, hi)
+            const int lo = max((int)key - start, 0), hi = a.window ? (int)min((long long)s.count, (long long)key + a.window - start) : (int)s.count;
             const uint64_t f2 = pair(f, f);
             uint64_t sum[2] = {0, 0};
-            for (uint32_t rb = u.row0; rb < u.row1; rb += kManyRows, ++block) {
-                const uint32_t side = block & 1, s_at = sh.tmem + tile * 128 + side * 64 + lanes;
-                if (!warp_wait(&sh.q_full[block & 3], (block >> 2) & 1, sh) || !warp_wait(&sh.s_full[side], (block >> 1) & 1, sh)) return;
+            const bool done = row_blocks(a, u.t0, u.t1, [&](uint32_t t, uint32_t h) {
+                const uint32_t side = block & 1;
+                if (!warp_wait(&sh.s_full[side], (block >> 1) & 1, sh)) return false;
                 tc_fence_after();
-                const bool cut = __any_sync(0xffffffffu, lo > rb || hi < min(rb + kManyRows, u.row1));
-                const ulonglong2* minus = reinterpret_cast<const ulonglong2*>(sh.lse[block & 3]);
+                uint32_t x[32];
+                tmem_load32(tm + side * kManyRows, x);
+                // of the block's columns, those that this key is to be weighed by: [c0, c1)
+                const int tokens = (int)min(a.block_tokens, u.t1 - t), c0 = min(max(lo - (int)t, 0), (int)a.block_tokens) * (int)a.block_heads;
+                int c1 = min(max(hi - (int)t, 0), tokens) * (int)a.block_heads;
+                if (a.block_tokens == 1) c1 = min(c1, (int)(a.group - h));            // a part of the group's heads
+                const bool cut = __any_sync(0xffffffffu, c0 > 0 || c1 < (int)(a.block_tokens * a.block_heads));
+                const ulonglong2* minus = reinterpret_cast<const ulonglong2*>(sh.lse[block & (kLseStages - 1)]);
+                tmem_wait32(x);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t x[32];
-                    tmem_load32(s_at + 32 * h, x);
-                    tmem_wait32(x);
+                for (int e = 0; e < 32; e += 4) {
+                    const ulonglong2 m = minus[e / 4];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const ulonglong2 m = minus[8 * h + e / 4];
-#pragma unroll
-                        for (int o = 0; o < 4; o += 2) {
-                            float v, w;
-                            split(fma2(pair(x[e + o], x[e + o + 1]), f2, o ? m.y : m.x), v, w);
-                            if (cut) {
-                                const uint32_t row = rb + 32 * h + e + o;
-                                if (row < lo || row >= hi) v = -INFINITY;
-                                if (row + 1 < lo || row + 1 >= hi) w = -INFINITY;
-                            }
-                            sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
+                    for (int o = 0; o < 4; o += 2) {
+                        float v, w;
+                        split(fma2(pair(x[e + o], x[e + o + 1]), f2, o ? m.y : m.x), v, w);
+                        if (cut) {
+                            if (e + o < c0 || e + o >= c1) v = -INFINITY;
+                            if (e + o + 1 < c0 || e + o + 1 >= c1) w = -INFINITY;
                         }
+                        sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
                     }
                 }
                 tc_fence_before();
-                mbar_arrive(&sh.s_empty[side]);                      // the columns are read, and so is this block's place in sh.lse
-            }
+                mbar_arrive(&sh.s_empty[side]);                      // the columns are read
+                ++block;
+                return true;
+            });
+            if (!done) return;
             float even, odd;
             split(add2(sum[0], sum[1]), even, odd);
-            if (there) total = even + odd;
+            if (!(ks < 0.0f)) total = even + odd;
         }
         if (mine) *weight = old + total;
     }
 }
 
+// warp 4
 template <int DP, class T>
-__device__ __forceinline__ void many_issue(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block,
-                                           uint32_t& units) {
+__device__ __forceinline__ void many_issue(const WeightArgs& a, ManyShared& sh, const uint8_t* queries, uint32_t here, unsigned long long at, unsigned long long end,
+                                           uint32_t& block, uint32_t& units) {
     using M = Many<DP>;
-    const uint32_t k0 = operand(smem_addr(smem), 16), q0 = operand(smem_addr(smem) + 2 * M::kKeyOperand, 16), tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
+    const uint32_t q0 = operand(smem_addr(queries), 16), tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
     constexpr uint32_t kS = instruction(kManyRows, false) | (std::is_same<T, __half>::value ? 0u : 1u << 7 | 1u << 10);     // both operands bfloat16
     for (; at < end; at += gridDim.x) {
         const ManyUnit u = many_unit(a, sh, here, at);
-        const uint32_t row0 = __shfl_sync(0xffffffffu, u.row0, 0), row1 = __shfl_sync(0xffffffffu, u.row1, 0);
-        if (row0 >= row1) continue;
+        const uint32_t t0 = __shfl_sync(0xffffffffu, u.t0, 0), t1 = __shfl_sync(0xffffffffu, u.t1, 0);
+        if (t0 >= t1) continue;
         if (!warp_wait(&sh.k_full, units & 1, sh)) return;
         ++units;
-        for (uint32_t rb = row0; rb < row1; rb += kManyRows, ++block) {
-            const uint32_t side = block & 1;
-            if (!warp_wait(&sh.q_full[block & 3], (block >> 2) & 1, sh)) return;
-            if (block >= 2 && !warp_wait(&sh.s_empty[side], ((block >> 1) - 1) & 1, sh)) return;
+        const bool done = row_blocks(a, t0, t1, [&](uint32_t, uint32_t) {
+            const uint32_t side = block & 1, stage = block & (kQueryStages - 1);
+            if (!warp_wait(&sh.q_full[stage], block / kQueryStages & 1, sh)) return false;
+            if (block >= 2 && !warp_wait(&sh.s_empty[side], ((block >> 1) - 1) & 1, sh)) return false;
             tc_fence_after();
-            const uint32_t q = q0 + side * (M::kRowOperand >> 4);
+            const uint32_t q = q0 + stage * (M::kRowOperand >> 4), to = tm + side * kManyRows, k = tm + 2 * kManyRows;
             if (elected()) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint32_t k = k0 + t * (M::kKeyOperand >> 4), to = tm + t * 128 + side * 64;
-                    mma_ss<false>(to, k, q, kS);
-#pragma unroll
-                    for (int i = 1; i < DP / 16; ++i)
-                        mma_ss<true>(to, k + (((i / 4) * M::kKeySlab + (i % 4) * 32) >> 4), q + (((i / 4) * M::kRowSlab + (i % 4) * 32) >> 4), kS);
-                }
+                for (int i = 0; i < DP / 16; ++i) mma_ts(to, k + 8 * i, q + (((i / 4) * M::kRowSlab + (i % 4) * 32) >> 4), kS, i > 0);
                 tc_commit(&sh.s_full[side]);
-                tc_commit(&sh.q_empty[side]);
+                tc_commit(&sh.q_empty[stage]);
+                mbar_arrive(&sh.s_full[side]);                       // and hands on what came with q_full: the rows' lse
             }
             __syncwarp();
-        }
+            ++block;
+            return true;
+        });
+        if (!done) return;
     }
 }
 
+// warp 5.  The rows of a block are asked for when those kQueryStages before it have been read by their product.
 template <int DP, class T>
-__device__ __forceinline__ void many_queries(const WeightArgs& a, ManyShared& sh, uint8_t* smem, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block) {
+__device__ __forceinline__ void many_queries(const WeightArgs& a, const CUtensorMap* map, ManyShared& sh, uint8_t* queries, uint32_t here, unsigned long long at,
+                                             unsigned long long end, uint32_t& block) {
     using M = Many<DP>;
-    constexpr uint32_t kChunks = DP / 8;                             // 16-byte chunks of a row
-    const uint32_t tid = threadIdx.x - (kManyThreads - kLoaders);
-    uint8_t* stages = smem + 2 * M::kKeyOperand;
+    const uint32_t lane = threadIdx.x & 31, token = lane / a.block_heads, head = lane - token * a.block_heads;      // of the lane's row in a block
+    const bool inside = token < a.block_tokens;
     for (; at < end; at += gridDim.x) {
         const ManyUnit u = many_unit(a, sh, here, at);
         const WeightSeq& s = sh.seq[u.seq];
-        for (uint32_t rb = u.row0; rb < u.row1; rb += kManyRows, ++block) {
-            const uint32_t side = block & 1;
-            if (block >= 2 && !warp_wait(&sh.q_empty[side], ((block >> 1) - 1) & 1, sh)) return;
-            uint8_t* stage = stages + side * M::kRowOperand;
-            for (uint32_t x = tid; x < kManyRows * kChunks; x += kLoaders) {
-                const uint32_t r = x / kChunks, c = x % kChunks, row = rb + r, tok = a.group_inverse ? (uint32_t)__umul64hi(row, a.group_inverse) : row;
-                const bool there = row < u.row1 && 8 * c < a.c.dim;
-                const T* q = static_cast<const T*>(a.q);
-                if (there) q += (long long)(s.row + tok) * a.q_token + (long long)(u.head * a.group + row - tok * a.group) * a.q_head + 8 * c;
-                uint8_t* to = stage + (c >> 3) * M::kRowSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-                if (a.q_aligned) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(q), "r"(there ? 16u : 0u) : "memory");
-                } else {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    const unsigned short* h = reinterpret_cast<const unsigned short*>(q);
-                    if (there)
-                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                    *reinterpret_cast<uint4*>(to) = v;
+        const float* lse = a.lse + (size_t)(s.row + token) * a.q_heads + u.head * a.group + head;
+        auto minus_at = [&](uint32_t t, uint32_t h) {
+            return inside && t + token < u.t1 && h + head < a.group ? -kLog2e * lse[(size_t)t * a.q_heads + h] : -INFINITY;
+        };
+        float next = u.t0 < u.t1 ? minus_at(u.t0, 0) : 0.0f;
+        const bool done = row_blocks(a, u.t0, u.t1, [&](uint32_t t, uint32_t h) {
+            const uint32_t stage = block & (kQueryStages - 1);
+            const float minus = next;
+            const uint32_t h2 = h + a.block_heads < a.group ? h + a.block_heads : 0u, t2 = h2 ? t : t + a.block_tokens;
+            if (t2 < u.t1) next = minus_at(t2, h2);                   // one block ahead
+            if (block >= kQueryStages && !warp_wait(&sh.q_empty[stage], (block / kQueryStages - 1) & 1, sh)) return false;
+            uint8_t* to = queries + stage * M::kRowOperand;
+            sh.lse[block & (kLseStages - 1)][lane] = minus;
+            if (a.tensor_copies) {
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive_expect(&sh.q_full[stage], DP / 64 * 128 * a.block_heads * a.block_tokens);
+#pragma unroll
+                    for (int i = 0; i < DP / 64; ++i)
+                        asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                                         smem_addr(to + i * M::kRowSlab)),
+                                     "l"(map), "r"(64 * i), "r"(u.head * a.group + h), "r"(s.row + t), "r"(smem_addr(&sh.q_full[stage]))
+                                     : "memory");
                 }
+            } else {                                                  // a lane has a row
+                const bool there = inside && t + token < u.t1 && h + head < a.group;
+                const T* q = static_cast<const T*>(a.q) + (there ? (long long)(s.row + t + token) * a.q_token + (long long)(u.head * a.group + h + head) * a.q_head : 0ll);
+                for (uint32_t c = 0; c < DP / 8; ++c) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    const unsigned short* e = reinterpret_cast<const unsigned short*>(q) + 8 * c;
+                    if (there && 8 * c < a.c.dim)
+                        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+                    *reinterpret_cast<uint4*>(to + (c >> 3) * M::kRowSlab + lane * 128 + (((c & 7) ^ (lane & 7)) << 4)) = v;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.q_full[stage]);
             }
-            if (tid < kManyRows) {
-                const uint32_t row = rb + tid, tok = a.group_inverse ? (uint32_t)__umul64hi(row, a.group_inverse) : row;
-                float minus = -INFINITY;
-                if (row < u.row1) minus = -kLog2e * a.lse[(size_t)(s.row + tok) * a.q_heads + u.head * a.group + row - tok * a.group];
-                sh.lse[block & 3][tid] = minus;
+            ++block;
+            return true;
+        });
+        if (!done) return;
+    }
+}
+
+// warp 6
+template <int DP>
+__device__ __forceinline__ void many_codes(const WeightArgs& a, ManyShared& sh, uint8_t* codes, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& units) {
+    constexpr uint32_t kPieces = DP / 16, kPass = 32 / kPieces;       // 16-byte pieces of a key; keys of a pass: they divide 16
+    const KvView& kv = a.c;
+    const uint32_t lane = threadIdx.x & 31, piece = lane % kPieces, r0 = lane / kPieces;
+    const bool real = 16 * piece < kv.dim;
+    for (; at < end; at += gridDim.x) {
+        const ManyUnit u = many_unit(a, sh, here, at);
+        if (u.t0 >= u.t1) continue;
+        const WeightSeq& s = sh.seq[u.seq];
+        const uint32_t low = a.window ? (uint32_t)first_seen((int)s.length - (int)s.count, a.window) : 0u;
+        long long from = -1;                                          // of the lane's 16 keys (lanes 0 to 7): bytes from the pool's start
+        float ks = -1.0f;
+        const uint32_t k = u.k0 + 16 * lane;
+        if (lane < 8 && k < s.length && k + 16 > low) {
+            const int32_t id = __ldg(kv.pages + (size_t)s.slot * kv.max_pages + (k >> kv.page_shift));
+            if ((uint32_t)id < kv.num_pages) {
+                from = (long long)id * kv.page_stride + (long long)(k & (kv.page_tokens - 1)) * kv.token_step;
+                ks = __ldg(kv.k_scale + (size_t)id * kv.heads + u.head);
+            } else {
+                kv_flag(kv.status, ROOMIE_FLAG_KV_PAGE);
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(&sh.q_full[block & 3]);
         }
+        if (units && !warp_wait(&sh.codes_empty, (units - 1) & 1, sh)) return;
+        ++units;
+        if (lane < 8) sh.ks[lane] = ks;
+        const uint8_t* pool = kv.k + (long long)u.head * kv.head_step + (real ? 16 * piece : 0);
+#pragma unroll 1
+        for (uint32_t g = 0; g < 8; ++g) {
+            const long long base = __shfl_sync(0xffffffffu, from, g);
+            const uint8_t* p = pool + max(base, 0ll) + (long long)r0 * kv.token_step;
+            const uint32_t keys = base >= 0 && real ? s.length - (u.k0 + 16 * g) : 0u;       // (a group with a page begins before the end)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; r += kPass) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(codes + piece_at<DP>(16 * g + r + r0, piece))), "l"(p),
+                             "r"(r + r0 < keys ? 16u : 0u) : "memory");
+                p += kPass * kv.token_step;
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        mbar_arrive(&sh.codes_full);
     }
 }
 
 template <int DP, int kFormat, class T>
-__global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_kernel(WeightArgs a) {
-    constexpr uint32_t kSeqs = kManyThreads / 3;
+__global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_kernel(WeightArgs a, const __grid_constant__ CUtensorMap map) {
+    using M = Many<DP>;
     extern __shared__ uint8_t raw[];
     __shared__ ManyShared sh;
-    uint8_t* smem = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
+    uint8_t* queries = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
+    uint8_t* codes = queries + kQueryStages * M::kRowOperand;
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        mbar_init(&sh.k_full, 256);
-        for (int i = 0; i < 4; ++i) mbar_init(&sh.q_full[i], kLoaders);
-        for (int i = 0; i < 2; ++i) {
+        mbar_init(&sh.codes_full, 32);
+        mbar_init(&sh.codes_empty, 128);
+        mbar_init(&sh.k_full, 128);
+        for (int i = 0; i < kQueryStages; ++i) {
+            mbar_init(&sh.q_full[i], 1);
             mbar_init(&sh.q_empty[i], 1);
-            mbar_init(&sh.s_full[i], 1);
-            mbar_init(&sh.s_empty[i], 256);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.s_full[i], 2);
+            mbar_init(&sh.s_empty[i], 128);
         }
         mbar_init(&sh.drain, 1);
         sh.failed = 0;
     }
-    if (wid == 8) tmem_alloc(&sh.tmem, 256);
+    if (wid == 4) tmem_alloc(&sh.tmem, M::kColumns);
+    // rows of a block that hold none stay zero
+    for (uint32_t x = threadIdx.x; x < kQueryStages * M::kRowOperand / 16; x += kManyThreads) reinterpret_cast<uint4*>(queries)[x] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     uint32_t block = 0, units = 0;                                   // of this block, each role in step with the others
     unsigned long long before = 0;                                   // units of the sequences so far
-    for (uint32_t base = 0; base < a.num_seqs; base += kSeqs) {
-        const uint32_t here = min(a.num_seqs - base, kSeqs);
+    for (uint32_t base = 0; base < a.num_seqs; base += kManySeqs) {
+        const uint32_t here = min(a.num_seqs - base, (uint32_t)kManySeqs);
         __syncthreads();
         unsigned long long mine = 0;
         WeightSeq w = {};
@@ -655,12 +712,13 @@ __global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_k
         // units go round the blocks
         const unsigned long long turn = before % gridDim.x, at = blockIdx.x >= turn ? blockIdx.x - turn : blockIdx.x + gridDim.x - turn;
         before += total;
-        if (wid < 8) many_sums<DP, kFormat, T>(a, sh, smem, here, at, total, block);
-        else if (wid == 8) many_issue<DP, T>(a, sh, smem, here, at, total, block, units);
-        else many_queries<DP, T>(a, sh, smem, here, at, total, block);
+        if (wid < 4) many_sums<DP, kFormat, T>(a, sh, codes, here, at, total, block, units);
+        else if (wid == 4) many_issue<DP, T>(a, sh, queries, here, at, total, block, units);
+        else if (wid == 5) many_queries<DP, T>(a, &map, sh, queries, here, at, total, block);
+        else many_codes<DP>(a, sh, codes, here, at, total, units);
         __syncwarp();
     }
-    if (wid == 8) {
+    if (wid == 4) {
         if (elected()) tc_commit(&sh.drain);                         // whatever was issued has ended before the memory is given back
         __syncwarp();
         warp_wait(&sh.drain, 0, sh);
@@ -669,11 +727,33 @@ __global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_k
     __syncthreads();
     tc_fence_after();
     if (threadIdx.x == 0 && sh.failed) kv_flag(a.c.status, ROOMIE_FLAG_WAIT_TIMEOUT);
-    if (wid == 8) tmem_free(sh.tmem, 256);
+    if (wid == 4) tmem_free(sh.tmem, M::kColumns);
 }
 
-template <int DP, int kFormat, class T> static int launch_many_weights(const WeightArgs& a, cudaStream_t st) {
-    return launch("kv_weights", many_weights_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count() * Many<DP>::kPerSm), dim3(kManyThreads), Many<DP>::kSmem, st, false, a);
+// The queries as (dim, head, token) for tensor copies of 64 elements of a block's heads and tokens.  false: copied by hand.
+static bool queries_map(const WeightArgs& a, bool half, CUtensorMap* map) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
+        return reinterpret_cast<Encode>(f);
+    }();
+    const long long most = 1ll << 39;
+    if (!encode || !a.q_aligned || (a.q_heads > 1 && (a.q_head <= 0 || a.q_head >= most / 2)) || (a.rows > 1 && (a.q_token <= 0 || a.q_token >= most / 2))) return false;
+    // a stride that no step takes still has to be a legal one
+    const cuuint64_t dims[3] = {a.c.dim, a.q_heads, a.rows};
+    const cuuint64_t strides[2] = {2 * (cuuint64_t)(a.q_heads > 1 ? a.q_head : (long long)a.c.dim), 2 * (cuuint64_t)(a.rows > 1 ? a.q_token : (long long)a.c.dim)};
+    const cuuint32_t box[3] = {64, a.block_heads, a.block_tokens}, steps[3] = {1, 1, 1};
+    return encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP, int kFormat, class T> static int launch_many_weights(WeightArgs a, cudaStream_t st) {
+    CUtensorMap map = {};
+    a.tensor_copies = queries_map(a, std::is_same<T, __half>::value, &map);
+    return launch("kv_weights", many_weights_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count() * Many<DP>::kPerSm), dim3(kManyThreads), Many<DP>::kSmem, st, false, a, map);
 }
 
 template <int DP, int NT, int kFormat, class T> static int launch_few_weights(const WeightArgs& a, cudaStream_t st) {
@@ -710,11 +790,12 @@ extern "C" int roomie_kv_weights(const roomie_kv_cache* cache, uint32_t layer, c
     a.c = kv_view(cache, layer);
     a.seqs = seqs; a.q_offset = q_offset; a.num_seqs = num_seqs; a.rows = rows;
     a.q_heads = q_heads; a.group = q_heads / cache->kv_heads;
-    a.group_inverse = a.group > 1 ? ~0ull / a.group + 1 : 0;
+    a.block_heads = a.group < kManyRows ? a.group : kManyRows;
+    a.block_tokens = kManyRows / a.block_heads;
     a.q = q->data; a.q_token = q->token_stride; a.q_head = q->head_stride;
     a.lse = lse;
     a.max_tokens = cache->max_pages * cache->page_tokens;
-    if ((unsigned long long)cache->kv_heads * (a.max_tokens / 256 + 1) > 0xffffffffull) return ROOMIE_ERR_INVALID_ARG;
+    if ((unsigned long long)cache->kv_heads * (a.max_tokens / kManyKeys + 1) > 0xffffffffull) return ROOMIE_ERR_INVALID_ARG;
     a.weight = weight + (size_t)layer * cache->max_seqs * cache->kv_heads * a.max_tokens;
     a.window = window;
     a.scale_log2 = scale * kLog2e;

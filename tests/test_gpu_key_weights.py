@@ -113,6 +113,28 @@ def test_weights_of_long_chunks(torch, rm, dim, page, layout, fmt, dtype):
     check(torch, rm, cache, [1, 0], [257, 40], 2, dtype, view="odd", window=100)
 
 
+@pytest.mark.parametrize("group", [1, 3, 7, 20, 32, 33, 48, 70])
+@pytest.mark.parametrize("view", ["whole", "odd"])
+@pytest.mark.parametrize("window", [0, 30])
+def test_weights_of_any_group(torch, rm, group, view, window):
+    """Blocks of rows hold whole tokens of a group, or a part of a large one."""
+    cache = make_cache(torch, rm, [300, 40, 129], page=16, heads=2, dim=64)
+    check(torch, rm, cache, [0, 1, 2], [60, 40, 1], 2 * group, "f16", window=window, view=view)
+
+
+def test_weights_of_broadcast_queries(torch, rm):
+    """Strides of zero, of tokens and of heads."""
+    cache = make_cache(torch, rm, [200], page=16, heads=2, dim=64)
+    q = torch.randn(40, 8, 64, device="cuda").half()
+    for view in (q[:1].expand(40, 8, 64), q[:, :1].expand(40, 8, 64)):
+        whole = view.contiguous()
+        _, lse = rm.kv_attention(cache, [0], whole, [0, 40])
+        got, want = cache.key_weights(), cache.key_weights()
+        rm.kv_weights(cache, [0], view, lse, got, [0, 40])
+        rm.kv_weights(cache, [0], whole, lse, want, [0, 40])
+        assert torch.equal(got, want) and float(want.sum()) > 0
+
+
 @pytest.mark.parametrize("news,count", [(1, 300), (3, 150), (40, 50)])
 def test_weights_of_many_sequences(torch, rm, news, count):
     rng = np.random.default_rng(count)
