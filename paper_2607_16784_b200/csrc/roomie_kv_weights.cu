@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
 // special-function units busy.  A block of rows is whole tokens of the group, or part of one where the group has more than 32 heads.
 constexpr int kManyThreads = 224, kManyRows = 32, kManyKeys = 128, kManySeqs = 128;
 constexpr int kQueryStages = 4;                      // of 32 rows
-constexpr int kLseStages = 8;                        // the exponentials lag the products by at most two blocks, and the queries are at most four ahead of these
+constexpr int kLseStages = 8;                        // the queries are at most four blocks ahead of the products, and these at most three of the exponentials
 
 template <int DP> struct Many {
     static constexpr uint32_t kCodes = kManyKeys * DP;              // bytes: codes of 128 keys
@@ -473,35 +473,49 @@ __device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, c
             const int lo = max((int)key - start, 0), hi = a.window ? (int)min((long long)s.count, (long long)key + a.window - start) : (int)s.count;
             const uint64_t f2 = pair(f, f);
             uint64_t sum[2] = {0, 0};
+            // 16 columns at a time: while their exponentials are taken the next 16 come, of this block or the next
+            uint32_t x[2][16];
+            if (!warp_wait(&sh.s_full[block & 1], (block >> 1) & 1, sh)) return;
+            tc_fence_after();
+            tmem_load16(tm + (block & 1) * kManyRows, x[0]);
             const bool done = row_blocks(a, u.t0, u.t1, [&](uint32_t t, uint32_t h) {
                 const uint32_t side = block & 1;
-                if (!warp_wait(&sh.s_full[side], (block >> 1) & 1, sh)) return false;
-                tc_fence_after();
-                uint32_t x[32];
-                tmem_load32(tm + side * kManyRows, x);
                 // of the block's columns, those that this key is to be weighed by: [c0, c1)
                 const int tokens = (int)min(a.block_tokens, u.t1 - t), c0 = min(max(lo - (int)t, 0), (int)a.block_tokens) * (int)a.block_heads;
                 int c1 = min(max(hi - (int)t, 0), tokens) * (int)a.block_heads;
                 if (a.block_tokens == 1) c1 = min(c1, (int)(a.group - h));            // a part of the group's heads
                 const bool cut = __any_sync(0xffffffffu, c0 > 0 || c1 < (int)(a.block_tokens * a.block_heads));
                 const ulonglong2* minus = reinterpret_cast<const ulonglong2*>(sh.lse[block & (kLseStages - 1)]);
-                tmem_wait32(x);
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const ulonglong2 m = minus[e / 4];
-#pragma unroll
-                    for (int o = 0; o < 4; o += 2) {
-                        float v, w;
-                        split(fma2(pair(x[e + o], x[e + o + 1]), f2, o ? m.y : m.x), v, w);
-                        if (cut) {
-                            if (e + o < c0 || e + o >= c1) v = -INFINITY;
-                            if (e + o + 1 < c0 || e + o + 1 >= c1) w = -INFINITY;
+                for (int half = 0; half < 2; ++half) {
+                    tmem_wait16(x[half]);
+                    if (half == 0) {
+                        tmem_load16(tm + side * kManyRows + 16, x[1]);
+                    } else {
+                        tc_fence_before();
+                        mbar_arrive(&sh.s_empty[side]);              // the columns are read
+                        if (h + a.block_heads < a.group || t + a.block_tokens < u.t1) {
+                            if (!warp_wait(&sh.s_full[side ^ 1], ((block + 1) >> 1) & 1, sh)) return false;
+                            tc_fence_after();
+                            tmem_load16(tm + (side ^ 1) * kManyRows, x[0]);
                         }
-                        sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const ulonglong2 m = minus[4 * half + e / 4];
+#pragma unroll
+                        for (int o = 0; o < 4; o += 2) {
+                            float v, w;
+                            split(fma2(pair(x[half][e + o], x[half][e + o + 1]), f2, o ? m.y : m.x), v, w);
+                            if (cut) {
+                                const int c = 16 * half + e + o;
+                                if (c < c0 || c >= c1) v = -INFINITY;
+                                if (c + 1 < c0 || c + 1 >= c1) w = -INFINITY;
+                            }
+                            sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
+                        }
                     }
                 }
-                tc_fence_before();
-                mbar_arrive(&sh.s_empty[side]);                      // the columns are read
                 ++block;
                 return true;
             });
