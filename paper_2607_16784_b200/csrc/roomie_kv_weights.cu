@@ -439,6 +439,24 @@ template <int DP> __device__ __forceinline__ uint32_t piece_at(uint32_t row, uin
     return row * DP + ((piece ^ (row & 7)) << 4);
 }
 
+// Adds the exponentials of 16 products to two pairs of sums; cut: of columns [c0, c1) alone.
+template <bool kCut> __device__ __forceinline__ void weigh16(const uint32_t* x, const ulonglong2* minus, uint64_t f2, int c0, int c1, uint64_t* sum) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const ulonglong2 m = minus[e / 4];
+#pragma unroll
+        for (int o = 0; o < 4; o += 2) {
+            float v, w;
+            split(fma2(pair(x[e + o], x[e + o + 1]), f2, o ? m.y : m.x), v, w);
+            if (kCut) {
+                if (e + o < c0 || e + o >= c1) v = -INFINITY;
+                if (e + o + 1 < c0 || e + o + 1 >= c1) w = -INFINITY;
+            }
+            sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
+        }
+    }
+}
+
 // warps 0 to 3
 template <int DP, int kFormat, class T>
 __device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, const uint8_t* codes, uint32_t here, unsigned long long at, unsigned long long end, uint32_t& block,
@@ -500,21 +518,8 @@ __device__ __forceinline__ void many_sums(const WeightArgs& a, ManyShared& sh, c
                             tmem_load16(tm + (side ^ 1) * kManyRows, x[0]);
                         }
                     }
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const ulonglong2 m = minus[4 * half + e / 4];
-#pragma unroll
-                        for (int o = 0; o < 4; o += 2) {
-                            float v, w;
-                            split(fma2(pair(x[half][e + o], x[half][e + o + 1]), f2, o ? m.y : m.x), v, w);
-                            if (cut) {
-                                const int c = 16 * half + e + o;
-                                if (c < c0 || c >= c1) v = -INFINITY;
-                                if (c + 1 < c0 || c + 1 >= c1) w = -INFINITY;
-                            }
-                            sum[o / 2] = add2(sum[o / 2], pair(exp2_fast(v), exp2_fast(w)));
-                        }
-                    }
+                    if (cut) weigh16<true>(x[half], minus + 4 * half, f2, c0 - 16 * half, c1 - 16 * half, sum);
+                    else weigh16<false>(x[half], minus + 4 * half, f2, 0, 0, sum);
                 }
                 ++block;
                 return true;
