@@ -4,6 +4,7 @@
 //
 // Two launches.  rows_kernel: a block takes a part of a row that its threads hold in registers: the part's maximum and sum of exponentials, and
 // its `num` best logits in order.  pick_kernel: a block for each request adds the parts' sums up in 64 bits and picks from their lists.
+#include <type_traits>
 #include "roomie_serving.cuh"
 
 namespace roomie {
@@ -30,106 +31,139 @@ __device__ __forceinline__ unsigned long long candidate(float x, uint32_t token)
 
 constexpr int kBeamThreads = 256, kBeamWarps = kBeamThreads / 32, kMostNum = 128;
 constexpr int kList = 1024;                         // candidates that a block looks at closely
+// Of a list that ran over, so many are enough for a bound that leaves a fourth or less: each is compared with each.
+__device__ __forceinline__ uint32_t sample_of(uint32_t num) { return max(4 * num, 256u); }
 
-// sorts R numbers a lane, descending over (register, lane)
-template <int R> __device__ __forceinline__ void sort_warp(unsigned long long* x) {
-    const uint32_t lane = threadIdx.x & 31;
+// Values that were widened before are widened again: kept, they would take four times the registers.
+template <int kVecs> __device__ __forceinline__ void as_they_are(uint4* raw) {
 #pragma unroll
-    for (int size = 2; size <= 32 * R; size *= 2)
+    for (int i = 0; i < kVecs; ++i) asm volatile("" : "+r"(raw[i].x), "+r"(raw[i].y), "+r"(raw[i].z), "+r"(raw[i].w));
+}
+// the largest of a piece, NaN passed over
+template <class T> __device__ __forceinline__ float largest(const uint4& raw) {
+    if constexpr (sizeof(T) == 4) {
+        return fmaxf(fmaxf(__uint_as_float(raw.x), __uint_as_float(raw.y)), fmaxf(__uint_as_float(raw.z), __uint_as_float(raw.w)));
+    } else {
+        using Two = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const Two* e = reinterpret_cast<const Two*>(&raw);
+        const Two m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
+        return fmaxf(to_f32(m.x), to_f32(m.y));
+    }
+}
+template <class T> __device__ __forceinline__ float element(const uint4& v, int i) { return to_f32(reinterpret_cast<const T*>(&v)[i]); }
+
+constexpr int kHits = 512;                          // pieces that may hold a candidate
+struct PickShared {
+    unsigned long long list[kList], bound;
+    uint4 hit[kHits];
+    uint32_t hit_at[kHits], hits, count;
+};
+
+// The `num` best candidates of the block's pieces, in order, to out[0, num); 0 where there are fewer.  Piece i of a thread: elements base + i * step
+// on, the largest of them tops[i].
+//
+// A bound that leaves few: the threads are 8, 16 or 32 groups (at least num) of neighbours, and the least of the groups' best is reached once in each -
+// of numbers in no order about groups * log(groups) are as large; for more than 32, the num-th of the threads' best.  The pieces that may hold such a one are put into shared memory, where a thread looks at
+// one element of them; candidates are listed, and each counts those above it.  (Divergent threads that looked through their own pieces took 4000 to
+// 18000 cycles of a block's 15000 to 25000.)  Should the pieces or the list run over, as with rows of one number, the threads do go through their own, and the
+// num-th of a full list is a higher bound.
+template <class T, int kVecs>
+__device__ __forceinline__ void pick_best(PickShared& sh, const uint4* raw, const float* tops, float top, uint32_t base, uint32_t num, unsigned long long* out) {
+    constexpr int v = kVecOf<T>;
+    constexpr uint32_t step = kBeamThreads * v;
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    // a number that some of the thread's candidates reaches: its maximum at the last place of the first piece that holds it
+    unsigned long long best = 0;
+    if (top > -INFINITY)
 #pragma unroll
-        for (int step = size / 2; step > 0; step /= 2) {
-            if (step >= 32) {
+        for (int i = kVecs - 1; i >= 0; --i)
+            if (tops[i] == top) best = candidate(top, base + i * step + v - 1);
+    unsigned long long bound;
+    if (threadIdx.x == 0) sh.count = sh.hits = 0;
+    if (num <= 32) {
+        const uint32_t wide = num <= 8 ? 32u : num <= 16 ? 16u : 8u;  // threads of a group
 #pragma unroll
-                for (int i = 0; i < R; ++i)
-                    if (!(i & (step / 32))) {
-                        const int j = i | (step / 32);
-                        const bool up = (i * 32) & size;
-                        if ((x[i] < x[j]) != up) {
-                            const unsigned long long t = x[i];
-                            x[i] = x[j];
-                            x[j] = t;
-                        }
-                    }
-            } else {
+        for (uint32_t d = 1; d < 32; d *= 2) {                        // the largest of a group, then the least of a warp's groups
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, d);
+            if ((other > best) == (d < wide)) best = other;
+        }
+        if (lane == 0) sh.list[wid] = best;
+        __syncthreads();
+        bound = sh.list[0];
 #pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    const unsigned long long other = __shfl_xor_sync(0xffffffffu, x[i], step);
-                    const bool up = ((i * 32 + lane) & size) != 0, low = !(lane & step);
-                    x[i] = (low != up) == (x[i] > other) ? x[i] : other;
-                }
+        for (int w = 1; w < kBeamWarps; ++w) bound = min(bound, sh.list[w]);
+    } else {                                                          // the num-th of the threads' best (0 where fewer have one)
+        sh.list[threadIdx.x] = best;
+        if (threadIdx.x == 0) sh.bound = 0;
+        __syncthreads();
+        uint32_t above = 0;
+#pragma unroll 8
+        for (uint32_t j = 0; j < kBeamThreads; ++j) above += sh.list[j] > best;
+        if (above == num - 1) sh.bound = best;                        // one thread, but for 0
+        __syncthreads();
+        bound = sh.bound;
+    }
+    bound = max(bound, 1ull);
+    auto put = [&](float e, uint32_t token) {
+        const unsigned long long c = candidate(e, token);
+        if (c >= bound && e > -INFINITY) {
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < kList) sh.list[at] = c;
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+        if (tops[i] > -INFINITY && candidate(tops[i], base + i * step) >= bound) {
+            const uint32_t at = atomicAdd(&sh.hits, 1u);
+            if (at < kHits) {
+                sh.hit[at] = raw[i];
+                sh.hit_at[at] = base + i * step;
             }
         }
-}
-
-// The `num` largest of the numbers that each thread offers, in order, to out[0, num); 0 where there are fewer.  offer(bound, put) calls put for
-// each of the thread's numbers that is at least `bound`; best: the thread's largest (0: none).  Numbers other than 0 differ.
-//
-// A bound that leaves few: at least `num` numbers are as large as the num-th of the threads' (or neighbouring threads') largest.  What is above it
-// is listed, and each listed number counts those above it.  Should the list run over, the num-th of the listed ones is a higher bound.
-struct PickShared {
-    unsigned long long best[kMostNum], list[kList], bound;
-    uint32_t count;
-};
-template <class Offer>
-__device__ __forceinline__ void pick_best(PickShared& sh, unsigned long long best, uint32_t num, unsigned long long* out, Offer offer) {
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    // the largest of 2 (up to 128 wanted), or 8 (up to 32) neighbouring threads
-    const uint32_t wide = num <= 32 ? 8u : 2u, groups = kBeamThreads / wide;
-    for (uint32_t d = 1; d < wide; d *= 2) {
-        const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, d);
-        if (other > best) best = other;
+    __syncthreads();
+    const uint32_t hits = sh.hits;                                    // (behind this barrier nobody reads the best any more)
+    if (hits <= kHits) {
+        for (uint32_t x = threadIdx.x; x < hits * v; x += kBeamThreads)
+            put(to_f32(reinterpret_cast<const T*>(&sh.hit[x / v])[x % v]), sh.hit_at[x / v] + x % v);
+        __syncthreads();
     }
-    __syncthreads();
-    if ((lane & (wide - 1)) == 0) sh.best[threadIdx.x / wide] = best;
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
-    if (wid == 0) {
-        if (groups == 32) {
-            unsigned long long x[1] = {sh.best[lane]};
-            sort_warp<1>(x);
-            if (lane == num - 1) sh.bound = x[0];
-        } else {
-            unsigned long long x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = sh.best[32 * i + lane];
-            sort_warp<4>(x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (32 * i + lane == num - 1) sh.bound = x[i];
+    while (hits > kHits || sh.count > kList) {
+        if (hits <= kHits || sh.count > kList) {                      // a list that ran over
+            const uint32_t sample = sample_of(num);
+            for (uint32_t i = threadIdx.x; i < sample; i += kBeamThreads) {
+                const unsigned long long x = sh.list[i];
+                uint32_t above = 0;
+#pragma unroll 8
+                for (uint32_t j = 0; j < sample; ++j) above += sh.list[j] > x;
+                if (above == num - 1) sh.bound = x;
+            }
+            __syncthreads();
+            bound = sh.bound;
+            if (threadIdx.x == 0) sh.count = 0;
+            __syncthreads();
         }
-    }
-    __syncthreads();
-    while (true) {
-        const unsigned long long bound = sh.bound > 0 ? sh.bound : 1ull;
-        offer(bound, [&](unsigned long long x) {
-            const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < kList) sh.list[at] = x;
-        });
-        __syncthreads();
-        const uint32_t n = sh.count;
-        if (n <= kList) break;
-        // rank num - 1 of the listed
-        __syncthreads();
-        if (threadIdx.x == 0) sh.count = 0;
-        for (uint32_t i = threadIdx.x; i < kList; i += kBeamThreads) {
-            const unsigned long long x = sh.list[i];
-            uint32_t above = 0;
-            for (uint32_t j = 0; j < kList; ++j) above += sh.list[j] > x;
-            if (above == num - 1) sh.bound = x;
+#pragma unroll 1
+        for (int i = 0; i < kVecs; ++i) {
+            uint4 piece = raw[0];
+#pragma unroll
+            for (int j = 1; j < kVecs; ++j)
+                if (j == i) piece = raw[j];
+#pragma unroll
+            for (int k = 0; k < v; ++k) put(element<T>(piece, k), base + i * step + k);
         }
         __syncthreads();
+        if (sh.count <= kList) break;
     }
     const uint32_t n = sh.count;
     for (uint32_t i = threadIdx.x; i < n; i += kBeamThreads) {
         const unsigned long long x = sh.list[i];
         uint32_t above = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) above += sh.list[j] > x;
         if (above < num) out[above] = x;
     }
     for (uint32_t i = n + threadIdx.x; i < num; i += kBeamThreads) out[i] = 0;
 }
-
-template <class T> __device__ __forceinline__ float element(const uint4& v, int i) { return to_f32(reinterpret_cast<const T*>(&v)[i]); }
 
 // 16 bytes that start `shift` bytes into the 32 of a and b; shift is the same for the row
 __device__ __forceinline__ uint4 joined(const uint4& a, const uint4& b, uint32_t shift) {
@@ -139,6 +173,30 @@ __device__ __forceinline__ uint4 joined(const uint4& a, const uint4& b, uint32_t
 #pragma unroll
     for (int i = 0; i < 5; ++i) x[i] = words == 0 ? w[i] : words == 1 ? w[i + 1] : words == 2 ? w[i + 2] : w[i + 3];
     return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits), __funnelshift_r(x[3], x[4], bits));
+}
+
+// Elements [at, at + 16 bytes) of a row of any alignment, -infinity behind its end.
+template <class T> __device__ __forceinline__ uint4 piece_of(const T* x, uint32_t at, uint32_t vocab, uint32_t shift) {
+    constexpr int v = kVecOf<T>;
+    const T* p = x + at;
+    if (shift == 0 && at + v <= vocab) return __ldcs(reinterpret_cast<const uint4*>(p));
+    if (shift && at && at + 2 * v <= vocab) {                         // the 32 aligned bytes around it lie inside the row
+        const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) - shift);
+        return joined(q[0], q[1], shift);
+    }
+    uint4 y;
+    uint32_t* w = &y.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = at + i < vocab ? reinterpret_cast<const uint32_t*>(p)[i] : 0xff800000u;
+        } else {
+            const uint32_t none = std::is_same<T, __half>::value ? 0xfc00u : 0xff80u;
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+            w[i] = (at + 2 * i < vocab ? h[2 * i] : none) | (at + 2 * i + 1 < vocab ? (uint32_t)h[2 * i + 1] : none) << 16;
+        }
+    }
+    return y;
 }
 
 // kVecs 16-byte pieces a thread.  The pieces are counted from the row's first element, wherever in memory that is: equal rows give equal sums.
@@ -154,37 +212,28 @@ __global__ void __launch_bounds__(kBeamThreads, 4) rows_kernel(BeamArgs a) {
     const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(x) & 15u);
     const uint32_t base = blockIdx.x * (kBeamThreads * kVecs * v) + threadIdx.x * v;    // piece i: elements base + i * kBeamThreads * v on
     uint4 raw[kVecs];
+    if (shift == 0 && (blockIdx.x + 1) * (kBeamThreads * kVecs * v) <= a.vocab) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const uint32_t at = base + i * (kBeamThreads * v);
-        const T* p = x + at;
-        if (shift == 0 && at + v <= a.vocab) {
-            raw[i] = __ldcs(reinterpret_cast<const uint4*>(p));
-        } else if (shift && at && at + 2 * v <= a.vocab) {           // the 32 aligned bytes around it lie inside the row
-            const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) - shift);
-            raw[i] = joined(q[0], q[1], shift);
-        } else {
-            T e[v];
+        for (int i = 0; i < kVecs; ++i) raw[i] = __ldcs(reinterpret_cast<const uint4*>(x + base + i * (kBeamThreads * v)));
+    } else {
 #pragma unroll
-            for (int k = 0; k < v; ++k) e[k] = at + k < a.vocab ? p[k] : from_f32<T>(-INFINITY);
-            raw[i] = *reinterpret_cast<const uint4*>(e);
-        }
+        for (int i = 0; i < kVecs; ++i) raw[i] = piece_of(x, base + i * (kBeamThreads * v), a.vocab, shift);
     }
     // the pieces' maxima, and the sum against the thread's own maximum.  NaN is passed over here and shows in the sum.
     float tops[kVecs], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        tops[i] = element<T>(raw[i], 0);
-#pragma unroll
-        for (int k = 1; k < v; ++k) tops[i] = fmaxf(tops[i], element<T>(raw[i], k));
+        tops[i] = largest<T>(raw[i]);
         top = fmaxf(top, tops[i]);
     }
+    as_they_are<kVecs>(raw);
     const float ref = top == -INFINITY ? 0.0f : top;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
 #pragma unroll
         for (int k = 0; k < v; ++k) sum[k & 3] += exp2_fast((element<T>(raw[i], k) - ref) * 1.44269504088896340736f);
+    as_they_are<kVecs>(raw);
     float total = (sum[0] + sum[1]) + (sum[2] + sum[3]), most = top;
     if (total != total) most = INFINITY;                             // NaN or +infinity: the row has no probabilities
 #pragma unroll
@@ -198,26 +247,7 @@ __global__ void __launch_bounds__(kBeamThreads, 4) rows_kernel(BeamArgs a) {
     for (int d = 1; d < 32; d *= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
     if (lane == 0) sh_sum[wid] = total;
     const size_t part = (size_t)row * a.splits + blockIdx.x;
-    // A number that some of the thread's candidates reaches: its maximum at the last place of the first piece that holds it.
-    unsigned long long best = 0;
-    if (top > -INFINITY)
-#pragma unroll
-        for (int i = kVecs - 1; i >= 0; --i)
-            if (tops[i] == top) best = candidate(top, base + i * (kBeamThreads * v) + v - 1);
-    pick_best(sh, best, a.num, a.keys + part * a.num, [&](unsigned long long bound, auto put) {
-        const float least = unordered((uint32_t)(bound >> 32));      // NaN for a bound below all numbers
-        if (top < least) return;
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (tops[i] < least) continue;
-#pragma unroll
-            for (int k = 0; k < v; ++k) {
-                const float e = element<T>(raw[i], k);
-                const unsigned long long c = candidate(e, base + i * (kBeamThreads * v) + k);
-                if (c >= bound && e > -INFINITY) put(c);
-            }
-        }
-    });
+    pick_best<T, kVecs>(sh, raw, tops, top, base, a.num, a.keys + part * a.num);
     if (threadIdx.x == 0) {                                          // pick_best has barriers between
         total = 0.0f;
         for (int w = 0; w < kBeamWarps; ++w) total += sh_sum[w];
@@ -248,6 +278,7 @@ __device__ __forceinline__ void bound_of(PickList& sh, uint32_t n, uint32_t num)
     for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
         const Candidate x = sh.list[i];
         uint32_t above = 0, same = 0;                                // those that are none are all the same
+#pragma unroll 4
         for (uint32_t j = 0; j < n; ++j) {
             above += over(sh.list[j], x);
             same += sh.list[j].value == x.value && sh.list[j].order == x.order;
@@ -307,32 +338,35 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
         }
         return c;
     };
-    // A bound: the num-th of the leading entries of (some of) the lists, at least num of them.  Then as in pick_best.
-    const uint32_t deep = (a.num + lists - 1) / lists, some = min(lists, (uint32_t)kPickThreads) * deep;   // deep > 1: fewer lists than num
+    // A bound: the num-th of the leading entries of (some of) the lists, about four times num of them: what it leaves is little more than num.
+    // (With num of them it left so many of 32 lists of 64 that the call took 330 us.)  Then as in pick_best.
+    const uint32_t deep = min((4 * a.num + lists - 1) / lists, a.num), some = min(lists, (uint32_t)kPickThreads) * deep;   // deep > 1: lists < 4 num <= 512
     for (uint32_t i = threadIdx.x; i < some; i += kPickThreads) sh.list[i] = entry(i / deep, i % deep);
     __syncthreads();
     bound_of(sh, some, a.num);
     __syncthreads();
+    const uint32_t room = sample_of(a.num);                           // more than so many: another bound
     while (true) {
         const Candidate bound = sh.bound;
         for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
             const Candidate c = entry(i / a.num, i % a.num);
             if (c.value && !over(bound, c)) {
                 const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < kList) sh.list[at] = c;
+                if (at < room) sh.list[at] = c;
             }
         }
         __syncthreads();
-        if (sh.count <= kList) break;
+        if (sh.count <= room) break;
         __syncthreads();
         if (threadIdx.x == 0) sh.count = 0;
-        bound_of(sh, kList, a.num);
+        bound_of(sh, room, a.num);
         __syncthreads();
     }
     const uint32_t n = sh.count;
     for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
         const Candidate x = sh.list[i];
         uint32_t above = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
         if (above < a.num) {
             const size_t to = (size_t)request * a.num + above;
