@@ -32,45 +32,7 @@ template <int kBytes> struct RawOf { using type = uint4; };
 template <> struct RawOf<8> { using type = uint2; };
 template <> struct RawOf<4> { using type = uint32_t; };
 template <> struct RawOf<2> { using type = uint16_t; };
-
-template <class T, int kV> __device__ __forceinline__ void load_chunk(const T* p, bool on, float* x) {
-    using Raw = typename RawOf<kV * (int)sizeof(T)>::type;
-    if (on) {
-        const Raw raw = *reinterpret_cast<const Raw*>(p);
-        const T* e = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-        for (int i = 0; i < kV; ++i) x[i] = to_f32(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kV; ++i) x[i] = 0.0f;
-    }
-}
-template <class T, int kV> __device__ __forceinline__ void store_chunk(T* p, bool on, const float* x) {
-    using Raw = typename RawOf<kV * (int)sizeof(T)>::type;
-    if (!on) return;
-    Raw raw;
-    T* e = reinterpret_cast<T*>(&raw);
-#pragma unroll
-    for (int i = 0; i < kV; ++i) e[i] = from_f32<T>(x[i]);
-    *reinterpret_cast<Raw*>(p) = raw;
-}
-__device__ __forceinline__ float load_weight(const void* w, int32_t type, uint32_t at) {
-    if (!w) return 1.0f;
-    if (type == ROOMIE_F32) return static_cast<const float*>(w)[at];
-    if (type == ROOMIE_F16) return __half2float(static_cast<const __half*>(w)[at]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(w)[at]);
-}
-
-// x[0, kV) and x[kV, 2 kV) are a unit's chunks; with interleaved pairs, neighbours turn together
-template <int kV, bool kPairs> __device__ __forceinline__ void turn_unit(float* x, const float2* cs, float sign) {
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        const int a = kPairs ? 2 * i : i, b = kPairs ? 2 * i + 1 : i + kV;
-        const float u = x[a], v = x[b], s = cs[i].y * sign;
-        x[a] = __fsub_rn(__fmul_rn(u, cs[i].x), __fmul_rn(v, s));
-        x[b] = __fadd_rn(__fmul_rn(v, cs[i].x), __fmul_rn(u, s));
-    }
-}
+template <class T, int kV> using Raw = typename RawOf<kV * (int)sizeof(T)>::type;
 
 // What a thread knows of its unit: where its chunks lie, and whether they are there and turn.
 struct Unit {
@@ -88,123 +50,316 @@ template <int kV, bool kPairs> __device__ __forceinline__ Unit unit_of(const Nor
     return u;
 }
 
+// A unit's 2 kV elements as two vectors whose i-th elements turn together (where the unit turns), two float32 a register pair.  A vector of one
+// element is a pair whose second is 0.
+template <int kV> constexpr int kTwos = (kV + 1) / 2;
+template <int kV> struct Elements {
+    uint64_t a[kTwos<kV>], b[kTwos<kV>];
+};
+// from a unit's elements as they lie in memory, and back
+template <int kV, bool kPairs> __device__ __forceinline__ Elements<kV> vectors(const float* x) {
+    Elements<kV> v;
+#pragma unroll
+    for (int i = 0; i < kTwos<kV>; ++i) {
+        if constexpr (kV == 1) {
+            v.a[0] = pair(x[0], 0.0f);
+            v.b[0] = pair(x[1], 0.0f);
+        } else if constexpr (kPairs) {
+            v.a[i] = pair(x[4 * i], x[4 * i + 2]);
+            v.b[i] = pair(x[4 * i + 1], x[4 * i + 3]);
+        } else {
+            v.a[i] = pair(x[2 * i], x[2 * i + 1]);
+            v.b[i] = pair(x[kV + 2 * i], x[kV + 2 * i + 1]);
+        }
+    }
+    return v;
+}
+template <int kV, bool kPairs> __device__ __forceinline__ void scalars(const Elements<kV>& v, float* x) {
+#pragma unroll
+    for (int i = 0; i < kTwos<kV>; ++i) {
+        float none;
+        if constexpr (kV == 1) {
+            split(v.a[0], x[0], none);
+            split(v.b[0], x[1], none);
+        } else if constexpr (kPairs) {
+            split(v.a[i], x[4 * i], x[4 * i + 2]);
+            split(v.b[i], x[4 * i + 1], x[4 * i + 3]);
+        } else {
+            split(v.a[i], x[2 * i], x[2 * i + 1]);
+            split(v.b[i], x[kV + 2 * i], x[kV + 2 * i + 1]);
+        }
+    }
+}
+template <class T, int kV> struct Loaded {
+    Raw<T, kV> a, b;
+};
+template <class T, int kV> __device__ __forceinline__ Loaded<T, kV> load_unit(const T* p, const Unit& u) {
+    Loaded<T, kV> r = {};
+    if (u.on) r.a = *reinterpret_cast<const Raw<T, kV>*>(p + u.a);
+    if (u.two) r.b = *reinterpret_cast<const Raw<T, kV>*>(p + u.b);
+    return r;
+}
+template <class T, int kV, bool kPairs> __device__ __forceinline__ Elements<kV> widened(const Loaded<T, kV>& r) {
+    float x[2 * kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        x[i] = to_f32(reinterpret_cast<const T*>(&r.a)[i]);
+        x[kV + i] = to_f32(reinterpret_cast<const T*>(&r.b)[i]);
+    }
+    return vectors<kV, kPairs>(x);
+}
+template <class T, int kV, bool kPairs> __device__ __forceinline__ void store_unit(T* p, const Unit& u, const Elements<kV>& v) {
+    float x[2 * kV];
+    scalars<kV, kPairs>(v, x);
+    Loaded<T, kV> r;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        reinterpret_cast<T*>(&r.a)[i] = from_f32<T>(x[i]);
+        reinterpret_cast<T*>(&r.b)[i] = from_f32<T>(x[kV + i]);
+    }
+    if (u.on) *reinterpret_cast<Raw<T, kV>*>(p + u.a) = r.a;
+    if (u.two) *reinterpret_cast<Raw<T, kV>*>(p + u.b) = r.b;
+}
+template <int kV, bool kPairs> __device__ __forceinline__ Elements<kV> load_weights(const void* w, int32_t type, const Unit& u) {
+    float x[2 * kV];
+#pragma unroll
+    for (int i = 0; i < 2 * kV; ++i) {
+        const uint32_t at = i < kV ? u.a + i : u.b + i - kV;
+        const bool there = i < kV ? u.on : u.two;
+        x[i] = !there ? 0.0f : !w ? 1.0f : type == ROOMIE_F32 ? static_cast<const float*>(w)[at]
+               : type == ROOMIE_F16 ? __half2float(static_cast<const __half*>(w)[at]) : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[at]);
+    }
+    return vectors<kV, kPairs>(x);
+}
+// cosines and sines of a unit's pairs; 1 and 0 where it does not turn
+template <int kV> __device__ __forceinline__ Elements<kV> turns_of(const NormArgs& n, uint32_t unit, const Unit& u, int32_t position) {
+    float2 cs[2 * kTwos<kV>];
+#pragma unroll
+    for (int i = 0; i < 2 * kTwos<kV>; ++i)
+        cs[i] = u.turn && i < kV ? rope_turn(n.rope.frequency[unit * kV + i], position, n.rope.amplitude) : make_float2(1.0f, 0.0f);
+    Elements<kV> v;
+#pragma unroll
+    for (int i = 0; i < kTwos<kV>; ++i) {
+        v.a[i] = pair(cs[2 * i].x, cs[2 * i + 1].x);
+        v.b[i] = pair(cs[2 * i].y, cs[2 * i + 1].y);
+    }
+    return v;
+}
+__device__ __forceinline__ uint64_t both(float x) { return pair(x, x); }
+__device__ __forceinline__ uint64_t minus(uint64_t x) { return x ^ 0x8000000080000000ull; }
+template <int kV> __device__ __forceinline__ void multiply(Elements<kV>& v, float f) {
+#pragma unroll
+    for (int i = 0; i < kTwos<kV>; ++i) {
+        v.a[i] = mul2(v.a[i], both(f));
+        v.b[i] = mul2(v.b[i], both(f));
+    }
+}
+template <int kV> __device__ __forceinline__ uint64_t dot(const Elements<kV>& v, const Elements<kV>& w, uint64_t sum) {
+#pragma unroll
+    for (int i = 0; i < kTwos<kV>; ++i) sum = fma2(v.b[i], w.b[i], fma2(v.a[i], w.a[i], sum));
+    return sum;
+}
+
 // The sum over the lanes of a row.
-__device__ __forceinline__ float row_sum(float x, uint32_t lanes, uint32_t mask) {
-    for (uint32_t d = lanes / 2; d > 0; d >>= 1) x += __shfl_xor_sync(mask, x, d);
+__device__ __forceinline__ float row_sum(uint64_t twos, uint32_t lanes, uint32_t mask) {
+    float x, y;
+    split(twos, x, y);
+    x += y;
+#pragma unroll
+    for (uint32_t d = 16; d > 0; d >>= 1)
+        if (d < lanes) x += __shfl_xor_sync(mask, x, d);
     return x;
 }
 
 // Squares of values above 2^64 leave float32: such a row is taken times 2^-80.
 constexpr float kLess = 8.271806125530277e-25f;
 
-template <class T, int kV, int kPer, bool kPairs, bool kGrad>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs n) {
-    extern __shared__ float sums[];                                  // backward: [head groups of the block][dim]
-    const uint32_t lane = threadIdx.x & 31, first = lane & ~(n.lanes - 1);
-    const uint32_t mask = n.lanes == 32 ? 0xffffffffu : ((1u << n.lanes) - 1) << first;
-    const uint32_t all = n.side[0].groups + n.side[1].groups;
-    const uint32_t flat = blockIdx.x * (kNormThreads / n.lanes) + threadIdx.x / n.lanes, slot = flat / all;
-    uint32_t group = flat - slot * all;
-    const bool second = group >= n.side[0].groups;
-    if (second) group -= n.side[0].groups;
-    const NormSide& s = n.side[second];
+// What a warp's threads know of their place: its lanes of a row, its head group and side.
+struct Place {
+    uint32_t first, mask, slot, group, all;
+    bool second;
+};
+__device__ __forceinline__ Place place_of(const NormArgs& n) {
+    Place p;
+    const uint32_t lane = threadIdx.x & 31;
+    p.first = lane & ~(n.lanes - 1);
+    p.mask = n.lanes == 32 ? 0xffffffffu : ((1u << n.lanes) - 1) << p.first;
+    p.all = n.side[0].groups + n.side[1].groups;
+    const uint32_t flat = blockIdx.x * (kNormThreads / n.lanes) + threadIdx.x / n.lanes;
+    p.slot = flat / p.all;
+    p.group = flat - p.slot * p.all;
+    p.second = p.group >= n.side[0].groups;
+    if (p.second) p.group -= n.side[0].groups;
+    return p;
+}
+
+// Bound by memory, and near it by instructions: two float32 an instruction, weights and turns multiplied once for all heads of a thread, the next head's
+// row under way (16384 tokens x 40 heads x 128 in bf16, 336 MB: 77 us, 4340 GB/s; each element on its own: 101).  Six blocks an SM; the spills that this
+// takes lie in front of the loop over heads (without a limit, 125 registers and four blocks: 95 us; 8-byte chunks: 125).
+template <class T, int kV, int kPer, bool kPairs>
+__global__ void __launch_bounds__(kNormThreads, 6) norm_kernel(NormArgs n) {
+    const Place p = place_of(n);
+    if (p.slot >= n.slots) return;
+    const NormSide s = p.second ? n.side[1] : n.side[0];
     Unit u[kPer];
-    float w[kPer][2 * kV], dw[kPer][2 * kV];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        u[k] = unit_of<kV, kPairs>(n, lane - first + k * n.lanes);
+    for (int k = 0; k < kPer; ++k) u[k] = unit_of<kV, kPairs>(n, (threadIdx.x & 31) - p.first + k * n.lanes);
+    const long long x_step = s.groups * s.x_head, y_step = s.groups * s.y_head;
+    for (uint32_t token = p.slot; token < n.tokens; token += n.slots) {
+        const T* x = static_cast<const T*>(s.x) + (long long)token * s.x_token + (long long)p.group * s.x_head;
+        T* y = static_cast<T*>(s.y) + (long long)token * s.y_token + (long long)p.group * s.y_head;
+        Loaded<T, kV> next[kPer];
 #pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            w[k][i] = u[k].on ? load_weight(s.w, n.weight_type, u[k].a + i) : 0.0f;
-            w[k][kV + i] = u[k].two ? load_weight(s.w, n.weight_type, u[k].b + i) : 0.0f;
-            if (kGrad) dw[k][i] = dw[k][kV + i] = 0.0f;
-        }
-    }
-    if (slot < n.slots)
-        for (uint32_t token = slot; token < n.tokens; token += n.slots) {
-            float2 cs[kPer][kV];
+        for (int k = 0; k < kPer; ++k) next[k] = load_unit<T, kV>(x, u[k]);
+        // y_a = x_a own.a - x_b cross.b, y_b = x_b own.b + x_a cross.a, each with r
+        const int32_t position = n.rope.rot ? n.positions[token] : 0;
+        Elements<kV> own[kPer], cross[kPer];
 #pragma unroll
-            for (int k = 0; k < kPer; ++k)
-                if (u[k].turn)
+        for (int k = 0; k < kPer; ++k) {
+            const Elements<kV> w = load_weights<kV, kPairs>(s.w, n.weight_type, u[k]);
+            const Elements<kV> turn = turns_of<kV>(n, (threadIdx.x & 31) - p.first + k * n.lanes, u[k], position);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i)
-                        cs[k][i] = rope_turn(n.rope.frequency[(lane - first + k * n.lanes) * kV + i], n.positions[token], n.rope.amplitude);
-            for (uint32_t head = group; head < s.heads; head += s.groups) {
-                const T* px = static_cast<const T*>(s.x) + (long long)token * s.x_token + (long long)head * s.x_head;
-                const T* pg = static_cast<const T*>(s.g) + (long long)token * s.g_token + (long long)head * s.g_head;
-                T* py = static_cast<T*>(s.y) + (long long)token * s.y_token + (long long)head * s.y_head;
-                float x[kPer][2 * kV], g[kPer][2 * kV];
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    load_chunk<T, kV>(px + u[k].a, u[k].on, x[k]);
-                    load_chunk<T, kV>(px + u[k].b, u[k].two, x[k] + kV);
-                    if (kGrad) {
-                        load_chunk<T, kV>(pg + u[k].a, u[k].on, g[k]);
-                        load_chunk<T, kV>(pg + u[k].b, u[k].two, g[k] + kV);
-                    }
-                }
-                if (kGrad) {
-#pragma unroll
-                    for (int k = 0; k < kPer; ++k)
-                        if (u[k].turn) turn_unit<kV, kPairs>(g[k], cs[k], -1.0f);
-                }
-                float r, less = 1.0f, along = 0.0f;
-                while (true) {
-                    float square = 0.0f;
-                    along = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < kPer; ++k)
-#pragma unroll
-                        for (int i = 0; i < 2 * kV; ++i) {
-                            square = fmaf(x[k][i], x[k][i], square);
-                            if (kGrad) along = fmaf(g[k][i] * w[k][i], x[k][i], along);
-                        }
-                    square = row_sum(square, n.lanes, mask);
-                    if (kGrad) along = row_sum(along, n.lanes, mask);
-                    r = __frsqrt_rn(fmaf(square, n.inverse_dim, n.eps * less * less));
-                    if (less != 1.0f || square != INFINITY) break;   // the same in all lanes of the row
-                    less = kLess;
-#pragma unroll
-                    for (int k = 0; k < kPer; ++k)
-#pragma unroll
-                        for (int i = 0; i < 2 * kV; ++i) x[k][i] *= kLess;
-                }
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    if (kGrad) {
-                        const float mean = along * r * n.inverse_dim;
-#pragma unroll
-                        for (int i = 0; i < 2 * kV; ++i) {
-                            const float unit = x[k][i] * r;
-                            dw[k][i] = fmaf(g[k][i], unit, dw[k][i]);
-                            x[k][i] = r * less * (g[k][i] * w[k][i] - unit * mean);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2 * kV; ++i) x[k][i] = x[k][i] * r * w[k][i];
-                        if (u[k].turn) turn_unit<kV, kPairs>(x[k], cs[k], 1.0f);
-                    }
-                    store_chunk<T, kV>(py + u[k].a, u[k].on, x[k]);
-                    store_chunk<T, kV>(py + u[k].b, u[k].two, x[k] + kV);
-                }
+            for (int i = 0; i < kTwos<kV>; ++i) {
+                own[k].a[i] = mul2(turn.a[i], w.a[i]);
+                own[k].b[i] = mul2(turn.a[i], w.b[i]);
+                cross[k].a[i] = mul2(turn.b[i], w.a[i]);
+                cross[k].b[i] = minus(mul2(turn.b[i], w.b[i]));
             }
         }
-    if (!kGrad) return;
+        for (uint32_t head = p.group; head < s.heads; head += s.groups) {
+            Elements<kV> v[kPer];
+            uint64_t sum = 0;
+            x += x_step;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                v[k] = widened<T, kV, kPairs>(next[k]);
+                if (head + s.groups < s.heads) next[k] = load_unit<T, kV>(x, u[k]);     // the next head's
+                sum = dot<kV>(v[k], v[k], sum);
+            }
+            float square = row_sum(sum, n.lanes, p.mask), eps = n.eps;
+            if (square == INFINITY) {                                 // the same in all lanes of the row
+                sum = 0;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    multiply<kV>(v[k], kLess);
+                    sum = dot<kV>(v[k], v[k], sum);
+                }
+                square = row_sum(sum, n.lanes, p.mask);
+                eps *= kLess * kLess;
+            }
+            const float r = rsqrtf(fmaf(square, n.inverse_dim, eps));
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                multiply<kV>(v[k], r);
+                Elements<kV> z;
+#pragma unroll
+                for (int i = 0; i < kTwos<kV>; ++i) {
+                    z.a[i] = fma2(v[k].a[i], own[k].a[i], mul2(v[k].b[i], cross[k].b[i]));
+                    z.b[i] = fma2(v[k].b[i], own[k].b[i], mul2(v[k].a[i], cross[k].a[i]));
+                }
+                store_unit<T, kV, kPairs>(y, u[k], z);
+            }
+            y += y_step;
+        }
+    }
+}
+
+template <class T, int kV, int kPer, bool kPairs>
+__global__ void __launch_bounds__(kNormThreads, 4) norm_grad_kernel(NormArgs n) {
+    extern __shared__ float sums[];                                  // [head groups of the block][dim]
+    const Place p = place_of(n);
+    const NormSide s = p.second ? n.side[1] : n.side[0];
+    Unit u[kPer];
+    Elements<kV> w[kPer], dw[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        u[k] = unit_of<kV, kPairs>(n, (threadIdx.x & 31) - p.first + k * n.lanes);
+        w[k] = load_weights<kV, kPairs>(s.w, n.weight_type, u[k]);
+        dw[k] = {};
+    }
+    const long long x_step = s.groups * s.x_head, g_step = s.groups * s.g_head, y_step = s.groups * s.y_head;
+    if (p.slot < n.slots)
+        for (uint32_t token = p.slot; token < n.tokens; token += n.slots) {
+            const T* x = static_cast<const T*>(s.x) + (long long)token * s.x_token + (long long)p.group * s.x_head;
+            const T* g = static_cast<const T*>(s.g) + (long long)token * s.g_token + (long long)p.group * s.g_head;
+            T* y = static_cast<T*>(s.y) + (long long)token * s.y_token + (long long)p.group * s.y_head;
+            const int32_t position = n.rope.rot ? n.positions[token] : 0;
+            Elements<kV> turn[kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) turn[k] = turns_of<kV>(n, (threadIdx.x & 31) - p.first + k * n.lanes, u[k], position);
+            for (uint32_t head = p.group; head < s.heads; head += s.groups) {
+                Elements<kV> v[kPer], back[kPer];                     // the rows, and their gradients turned back
+                uint64_t sum = 0, along = 0;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    const Loaded<T, kV> lx = load_unit<T, kV>(x, u[k]), lg = load_unit<T, kV>(g, u[k]);
+                    v[k] = widened<T, kV, kPairs>(lx);
+                    const Elements<kV> d = widened<T, kV, kPairs>(lg);
+#pragma unroll
+                    for (int i = 0; i < kTwos<kV>; ++i) {
+                        back[k].a[i] = fma2(d.a[i], turn[k].a[i], mul2(d.b[i], turn[k].b[i]));
+                        back[k].b[i] = fma2(d.b[i], turn[k].a[i], minus(mul2(d.a[i], turn[k].b[i])));
+                    }
+                }
+                auto sums_of = [&] {
+                    sum = along = 0;
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) {
+                        sum = dot<kV>(v[k], v[k], sum);
+#pragma unroll
+                        for (int i = 0; i < kTwos<kV>; ++i)
+                            along = fma2(mul2(back[k].a[i], w[k].a[i]), v[k].a[i], fma2(mul2(back[k].b[i], w[k].b[i]), v[k].b[i], along));
+                    }
+                };
+                sums_of();
+                float square = row_sum(sum, n.lanes, p.mask), eps = n.eps, less = 1.0f;
+                if (square == INFINITY) {                             // the same in all lanes of the row
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) multiply<kV>(v[k], kLess);
+                    sums_of();
+                    square = row_sum(sum, n.lanes, p.mask);
+                    less = kLess;
+                    eps *= kLess * kLess;
+                }
+                const float r = rsqrtf(fmaf(square, n.inverse_dim, eps));
+                const uint64_t mean = both(-row_sum(along, n.lanes, p.mask) * r * n.inverse_dim);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    multiply<kV>(v[k], r);
+                    Elements<kV> d;
+#pragma unroll
+                    for (int i = 0; i < kTwos<kV>; ++i) {
+                        dw[k].a[i] = fma2(back[k].a[i], v[k].a[i], dw[k].a[i]);
+                        dw[k].b[i] = fma2(back[k].b[i], v[k].b[i], dw[k].b[i]);
+                        d.a[i] = fma2(v[k].a[i], mean, mul2(back[k].a[i], w[k].a[i]));
+                        d.b[i] = fma2(v[k].b[i], mean, mul2(back[k].b[i], w[k].b[i]));
+                    }
+                    multiply<kV>(d, r * less);
+                    store_unit<T, kV, kPairs>(y, u[k], d);
+                }
+                x += x_step;
+                g += g_step;
+                y += y_step;
+            }
+        }
     // the block's sums, head group after head group
     const uint32_t mine = threadIdx.x / n.lanes, here = kNormThreads / n.lanes;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
+    for (int k = 0; k < kPer; ++k) {
+        float d[2 * kV];
+        scalars<kV, kPairs>(dw[k], d);
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            if (u[k].on) sums[mine * n.dim + u[k].a + i] = dw[k][i];
-            if (u[k].two) sums[mine * n.dim + u[k].b + i] = dw[k][kV + i];
+            if (u[k].on) sums[mine * n.dim + u[k].a + i] = d[i];
+            if (u[k].two) sums[mine * n.dim + u[k].b + i] = d[kV + i];
         }
+    }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < 2 * n.dim; d += kNormThreads) {
         const uint32_t side = d >= n.dim, at = d - side * n.dim;
         float total = 0.0f;
         for (uint32_t i = 0; i < here; ++i) {
-            const uint32_t f = (blockIdx.x * here + i) % all;
+            const uint32_t f = (blockIdx.x * here + i) % p.all;
             if ((f >= n.side[0].groups) == (side != 0)) total += sums[i * n.dim + at];
         }
         n.partial[(size_t)blockIdx.x * 2 * n.dim + d] = total;
@@ -238,7 +393,9 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
 constexpr uint32_t kNormBlocksPerSm = 8;             // at most: the backward pass leaves a row of sums for each
 
 template <class T, int kV, int kPer, bool kGrad> static int launch_norm(NormArgs n, uint32_t blocks, size_t smem, cudaStream_t st) {
-    void (*k)(NormArgs) = n.rope.interleaved ? norm_kernel<T, kV, kPer, true, kGrad> : norm_kernel<T, kV, kPer, false, kGrad>;
+    void (*k)(NormArgs);
+    if (kGrad) k = n.rope.interleaved ? norm_grad_kernel<T, kV, kPer, true> : norm_grad_kernel<T, kV, kPer, false>;
+    else k = n.rope.interleaved ? norm_kernel<T, kV, kPer, true> : norm_kernel<T, kV, kPer, false>;
     return launch(kGrad ? "qk_norm_rope_grad" : "qk_norm_rope", k, dim3(blocks), dim3(kNormThreads), smem, st, false, n);
 }
 
@@ -257,11 +414,12 @@ template <class T, bool kGrad> static int run_norm(NormArgs n, uint32_t align, u
     n.units = n.rope.rot / 2 / v + ((n.dim - n.rope.rot) / v + 1) / 2;
     n.lanes = 1;
     while (n.lanes < n.units && n.lanes < 32) n.lanes *= 2;
-    // head groups as rope's: four heads or more a thread, unless there are too few rows to fill the GPU
+    // Head groups: a thread's weights and turns cost as much as some heads, so it should have eight heads or more (16384 tokens x 40 heads: 77 us, with four
+    // 83, with sixteen 85), unless there are too few rows to fill the GPU.
     const unsigned long long one = (unsigned long long)n.tokens * n.lanes;
     for (NormSide& s : n.side) {
-        unsigned long long g = (4096ull * sms + one - 1) / one, few = 256ull * sms / one;
-        if (g > s.heads / 4) g = s.heads / 4;
+        unsigned long long g = (2048ull * sms + one - 1) / one, few = 256ull * sms / one;
+        if (g > s.heads / 8) g = s.heads / 8;
         if (g < few) g = few;
         if (g > s.heads) g = s.heads;
         if (kGrad && g > (unsigned long long)sms * kNormBlocksPerSm) g = (unsigned long long)sms * kNormBlocksPerSm;   // all groups fit the grid below

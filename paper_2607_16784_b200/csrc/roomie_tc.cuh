@@ -1,6 +1,6 @@
 // Tensor memory, the fifth-generation matrix instructions and what kernels that use them share.
 #pragma once
-#include "roomie_common.cuh"
+#include "roomie_serving.cuh"
 
 namespace roomie {
 
@@ -98,27 +98,6 @@ __device__ __forceinline__ bool elected() {
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
     return p != 0;
 }
-// two float32 at a time
-__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ void split(uint64_t p, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // By a whole warp, with one answer.  The instruction itself suspends the warp for up to the hint (20 us); a wait that runs out after
 // 2^16 of them (about a second) ends the block: the flag makes its other waits give up too.  Kept to a few instructions: the roles'
 // loops have to fit the instruction caches together.

@@ -222,20 +222,42 @@ class _NormTurn(torch.autograd.Function):
         return qk_norm_rope(q, k, positions, table, q_weight, k_weight, eps=eps)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, gq, gk):
-        q, k, positions, q_weight, k_weight = ctx.saved_tensors
-        unit = lambda g: g if g is None or g.stride(2) == 1 else g.clone(memory_format=torch.contiguous_format)
-        gq, gk = unit(gq), unit(gk) if k is not None else None
-        n, d, at, kind, (hq, qw), (hk, kw) = _norm_sides(q, k, q_weight, k_weight, positions, ctx.table, gq, gk)
-        dq, dk = _norm_out(q, None, "q"), _norm_out(k, None, "k")
-        dqw, dkw = (torch.empty_like(w) if w is not None and need else None for w, need in ((q_weight, ctx.needs_input_grad[4]), (k_weight, ctx.needs_input_grad[5])))
-        scratch = torch.empty(int(_dll.roomie_qk_norm_rope_workspace_bytes(d)), dtype=torch.uint8, device=q.device)
-        _check(_dll.roomie_qk_norm_rope_grad(ctx.table.ref if ctx.table is not None else None, ctx.eps, n, d, at, kind, hq, _rows(q, "q"), qw, _rows(gq, "gq"),
-                                             _rows(dq, "dq"), _ptr(dqw), hk, _rows(k, "k") if hk else None, kw, _rows(gk, "gk") if hk else None,
-                                             _rows(dk, "dk") if hk else None, _ptr(dkw), scratch.data_ptr(), scratch.numel(), _stream(q)),
-               "roomie_qk_norm_rope_grad")
+        need = ctx.needs_input_grad
+        back = _NormBack.apply if torch.is_grad_enabled() else _norm_back
+        dq, dk, dqw, dkw = back(*ctx.saved_tensors, gq, gk, ctx.table, ctx.eps, need[4], need[5])
         return dq, dk, None, None, dqw, dkw, None
+
+
+def _norm_back(q, k, positions, q_weight, k_weight, gq, gk, table, eps, need_qw, need_kw):
+    """Gradients of q, k and the weights (None where there is none); the forward call has checked its arguments."""
+    n, hq, d = q.shape
+    hk = 0 if k is None else k.shape[1]
+    unit = lambda g: g if g.stride(2) == 1 else g.clone(memory_format=torch.contiguous_format)
+    gq, gk = unit(gq), unit(gk) if hk else None
+    _here(q.get_device(), gq, gk)
+    new = torch.empty_like
+    dq, dk = new(q, memory_format=torch.contiguous_format), None if k is None else new(k, memory_format=torch.contiguous_format)
+    dqw, dkw = new(q_weight) if need_qw else None, new(k_weight) if need_kw else None
+    kind = 0 if q_weight is None and k_weight is None else _TYPES[(k_weight if q_weight is None else q_weight).dtype]
+    scratch = torch.empty(int(_dll.roomie_qk_norm_rope_workspace_bytes(d)), dtype=torch.uint8, device=q.device)
+    at = lambda t: None if t is None else t.data_ptr()
+    _check(_dll.roomie_qk_norm_rope_grad(table.ref if table is not None else None, eps, n, d, at(positions), kind, hq, _rows(q, "q"), at(q_weight), _rows(gq, "gq"),
+                                         _rows(dq, "dq"), at(dqw), hk, _rows(k, "k") if hk else None, at(k_weight), _rows(gk, "gk") if hk else None,
+                                         _rows(dk, "dk") if hk else None, at(dkw), scratch.data_ptr(), scratch.numel(), _stream(q)), "roomie_qk_norm_rope_grad")
+    return dq, dk, dqw, dkw
+
+
+class _NormBack(torch.autograd.Function):
+    """The gradients where they are recorded for a second derivative, which there is not."""
+
+    @staticmethod
+    def forward(ctx, *args):
+        return _norm_back(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("qk_norm_rope can be differentiated once")
 
 
 class KVCache:
