@@ -287,12 +287,26 @@ constexpr uint32_t kReorderMost = 8192;                           // sequences o
 // of one; the part-filled last page goes to the first child, and is given up when there is none.
 template <class F> __device__ __forceinline__ void held_pages(const TableView& t, const int32_t* seqs, uint32_t n, const ReorderView& v, F f) {
     const uint32_t lane = threadIdx.x & 31;
-    for (uint32_t p = threadIdx.x >> 5; p < n; p += kPlanWarps) {
-        const int32_t len = v.len[p], children = v.count[p];
-        if (len <= 0 || children == 1) continue;
-        const uint32_t held = pages_of(t, (uint32_t)len), whole = (uint32_t)len >> t.page_shift;
-        const int32_t* row = t.pages + (size_t)seqs[p] * t.max_pages;
-        for (uint32_t e = lane; e < held; e += 32) f(row[e], e < whole ? children - 1 : children ? 0 : -1);
+    for (uint32_t base = threadIdx.x >> 5; base < n; base += 32 * kPlanWarps) {      // 32 sequences of a warp at a time: a lane asks for each
+        const uint32_t mine = base + lane * kPlanWarps;
+        const int32_t my_len = mine < n ? v.len[mine] : 0, my_children = mine < n ? v.count[mine] : 0, my_slot = mine < n ? seqs[mine] : 0;
+        for (uint32_t i = 0; i < 32 && base + i * kPlanWarps < n; ++i) {
+            const int32_t len = __shfl_sync(0xffffffffu, my_len, i), children = __shfl_sync(0xffffffffu, my_children, i);
+            const int32_t slot = __shfl_sync(0xffffffffu, my_slot, i);
+            if (len <= 0 || children == 1) continue;
+            const uint32_t held = pages_of(t, (uint32_t)len), whole = (uint32_t)len >> t.page_shift;
+            const int32_t* row = t.pages + (size_t)slot * t.max_pages;
+            for (uint32_t e0 = 0; e0 < held; e0 += 128) {                            // four entries of a lane under way
+                int32_t id[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) id[k] = e0 + 32 * k + lane < held ? row[e0 + 32 * k + lane] : 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t e = e0 + 32 * k + lane;
+                    if (e < held) f(id[k], e < whole ? children - 1 : children ? 0 : -1);
+                }
+            }
+        }
     }
 }
 

@@ -160,35 +160,14 @@ class _Turn(torch.autograd.Function):
 
 
 def _head_weight(w, dim, like, what):
-    """(pointer, type) of a weight [head_dim], or of none."""
-    if w is None:
-        return None, like
+    """(pointer, type) of a weight [head_dim]; like: the type of the other one."""
     kind = _TYPES.get(w.dtype)
     if kind is None or tuple(w.shape) != (dim,) or not w.is_contiguous() or not w.is_cuda or (like is not None and kind != like):
         raise ValueError(f"{what}: contiguous CUDA tensors [head_dim] of one type, float32, float16 or bfloat16")
     return w.data_ptr(), kind
 
 
-def _norm_sides(q, k, q_weight, k_weight, positions, table, *others):
-    """What both directions check: (tokens, head_dim, positions, type of the weights, [(heads, weight)] of the sides)."""
-    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
-        raise ValueError("q, k: [tokens, heads, head_dim] of one type")
-    if k is None and k_weight is not None:
-        raise ValueError("k_weight: without k there is nothing to scale")
-    n, _, d = q.shape
-    qw, kind = _head_weight(q_weight, d, None, "q_weight, k_weight")
-    kw, kind = _head_weight(k_weight, d, kind, "q_weight, k_weight")
-    if table is not None:
-        positions = _ids(positions, "positions", n)
-    _here(q.get_device() if table is None else table.index, q, k, q_weight, k_weight, positions if table is not None else None, *others)
-    return n, d, positions.data_ptr() if table is not None else None, kind or 0, (q.shape[1], qw), (0 if k is None else k.shape[1], kw)
-
-
 def _norm_out(x, out, what):
-    if x is None:
-        if out is not None:
-            raise ValueError(f"{what}: without its input there is nothing to write")
-        return None
     if out is None:
         return torch.empty_like(x, memory_format=torch.contiguous_format)
     if out.shape != x.shape or out.dtype != x.dtype:
@@ -201,16 +180,40 @@ def qk_norm_rope(q, k, positions, table: RopeTable | None, q_weight=None, k_weig
     """roomie_qk_norm_rope: q and k [tokens, heads, head_dim] (k may be None), each head divided by its root mean square, times its weight
     [head_dim] (None: ones), turned to `positions` (int32 [tokens]; table None: not turned).  Outputs may be the inputs.  Returns
     (q_out, k_out).  Without outputs given the call is differentiable, once, in q, k and the weights."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight, q_out, k_out)):
+    if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad) or
+                                    any(t is not None and t.requires_grad for t in (q_weight, k_weight, q_out, k_out))):
         if q_out is not None or k_out is not None:
             raise ValueError("q_out, k_out: not where a gradient is wanted")
         if table is not None:
             positions = _ids(positions, "positions")
         return _NormTurn.apply(q, k, positions if table is not None else None, table, q_weight, k_weight, eps)
-    n, d, at, kind, (hq, qw), (hk, kw) = _norm_sides(q, k, q_weight, k_weight, positions, table, q_out, k_out)
-    q_out, k_out = _norm_out(q, q_out, "q_out"), _norm_out(k, k_out, "k_out")
-    _check(_dll.roomie_qk_norm_rope(table.ref if table is not None else None, eps, n, d, at, kind, hq, _rows(q, "q"), qw, _rows(q_out, "q_out"), hk,
-                                    _rows(k, "k") if hk else None, kw, _rows(k_out, "k_out") if hk else None, _stream(q)), "roomie_qk_norm_rope")
+    cq = _rows(q, "q")
+    n, hq, d = q.shape
+    qw = kw = kind = None
+    if q_weight is not None:
+        qw, kind = _head_weight(q_weight, d, None, "q_weight, k_weight")
+    if k_weight is not None:
+        kw, kind = _head_weight(k_weight, d, kind, "q_weight, k_weight")
+    hk, ck, ko = 0, None, None
+    if k is not None:
+        hk = k.shape[1] if k.dim() == 3 else -1
+        if k.shape != (n, hk, d) or k.dtype != q.dtype:
+            raise ValueError("q, k: [tokens, heads, head_dim] of one type")
+    elif k_weight is not None or k_out is not None:
+        raise ValueError("k_weight, k_out: without k there is nothing to scale or to write")
+    at = ref = None
+    index = q.get_device()
+    if table is not None:
+        positions = _ids(positions, "positions", n)
+        at, ref, index = positions.data_ptr(), table.ref, table.index
+    _here(index, q, k, q_weight, k_weight, positions if at is not None else None, q_out, k_out)
+    q_out = _norm_out(q, q_out, "q_out")
+    if hk:
+        k_out = _norm_out(k, k_out, "k_out")
+        ck, ko = _rows(k, "k"), _rows(k_out, "k_out")
+    elif k is not None:
+        k_out = _norm_out(k, k_out, "k_out")
+    _check(_dll.roomie_qk_norm_rope(ref, eps, n, d, at, kind or 0, hq, cq, qw, _rows(q_out, "q_out"), hk, ck, kw, ko, _stream(q)), "roomie_qk_norm_rope")
     return q_out, k_out
 
 
