@@ -4,6 +4,9 @@
 //
 // Two launches.  rows_kernel: a block takes a part of a row that its threads hold in registers: the part's maximum and sum of exponentials, and
 // its `num` best logits in order.  pick_kernel: a block for each request adds the parts' sums up in 64 bits and picks from their lists.
+//
+// Bound by the logits' bytes, with the exponentials close behind (256 rows of 128256 in bf16, 66 MB: 10 us and 7.5 us of special-function time); it takes 21
+// us, of which a part's block spends some 2000 cycles on the loads, 3000 on the exponentials and 2500 on its barriers and its list, four blocks an SM.
 #include <type_traits>
 #include "roomie_serving.cuh"
 
@@ -388,12 +391,15 @@ struct BeamShape {
     bool large;
     size_t keys, bytes;
 };
-// Parts of 8 pieces a thread, or of 2 where those would leave SMs without a block.
+// Parts of 8 pieces a thread, or of 2 where those would leave more than half of the SMs without a block.  Both launches, us (bf16; rows x vocabulary):
+//      1 x 32000  1 x 128256  16 x 32000 | 16 x 128256  64 x 32000  64 x 128256  256 x 128256
+//   8  8.9        10.6        10.7       | 10.8         10.8        14.9         27.3
+//   2  8.5        9.4         9.9        | 17.3         11.4        23.9         49.6
 static BeamShape beam_shape(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type) {
     BeamShape s;
     const unsigned long long rows = (unsigned long long)requests * beams, one = (unsigned long long)kBeamThreads * 16 / size_of_type(type);
     const unsigned long long eight = (vocab + 8 * one - 1) / (8 * one), two = (vocab + 2 * one - 1) / (2 * one);
-    s.large = rows * eight >= 2ull * (unsigned long long)sm_count();
+    s.large = 2 * rows * eight >= (unsigned long long)sm_count();
     s.splits = (uint32_t)(s.large ? eight : two);
     s.keys = (size_t)rows * s.splits * num * sizeof(unsigned long long);
     s.bytes = (s.keys + (size_t)rows * s.splits * sizeof(float2) + 255) / 256 * 256;

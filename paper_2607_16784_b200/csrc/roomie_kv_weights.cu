@@ -29,7 +29,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // ---- few rows a key head -----------------------------------------------------------------------------------------------------------
 // As in attention over few rows: S^T = K q^T by 16x8x16 products, a lane's span of a key contiguous, every warp with steps of codes under way to its
 // own part of shared memory.  The flat order (sequence, head, step of keys) is cut into equal shares for the call's warps.  Bound by the bytes
-// of the codes.
+// of the codes: 64 sequences of up to 16384 keys (764 MB) take 145 us, 5280 GB/s; of up to 4096 (191 MB) 44, of which 10 are the way from the lengths over
+// the table to the first codes.  Instructions come next (some 450 of a warp for 32 keys): with places in the flat order worked out anew for each
+// step it took 60, with 12 warps an SM instead of 16 51.
 constexpr int kWeightWarps = 4, kWeightThreads = 32 * kWeightWarps;
 
 template <int DP> struct FewWeights {
@@ -41,15 +43,15 @@ template <int DP> struct FewWeights {
     static constexpr int kRing = kStages * kStage;
     static constexpr int kSmem = kRing * kWeightWarps;
 };
-template <int DP, int NT> constexpr int kWeightBlocks = DP > 128 && NT > 1 ? 3 : 4;      // of an SM: 16 warps with 128 registers a thread, but for these
+constexpr int kWeightBlocks = 4;                                    // of an SM: 16 warps with 128 registers a thread
 
 struct WeightSeq {                                   // a sequence of the call, as its warps need it
     unsigned long long first;                        // flat index of its first step
     uint32_t slot, row, count, length, step0, steps; // step0: a head's first step, of `steps`
 };
 
-template <int DP, int NT, int kFormat, class T>
-__global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_weights_kernel(WeightArgs a) {
+template <int DP, int kFormat, class T>
+__global__ void __launch_bounds__(kWeightThreads, kWeightBlocks) few_weights_kernel(WeightArgs a) {
     using F = FewWeights<DP>;
     constexpr int G = F::kGroups, KW = DP / 16, KS = DP / 16, kStages = F::kStages;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -202,67 +204,64 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
             get_pages();
         }
 
-        // ---- queries of a tile of rows: operand b of S^T, row r of each eight, dims as the lane's keys ----
-        uint32_t qf[NT][KS][2];
-        float qscale[NT][2], lse2[NT][2];
-        int see_hi[NT][2], see_lo[NT][2];                           // rows 2c and 2c + 1 of each eight see keys [lo, hi)
-        int all_hi, all_lo;                                         // every row of the tile sees [all_lo, all_hi)
+        // ---- queries of eight rows: operand b of S^T, row r of them, dims as the lane's keys ----
+        uint32_t qf[KS][2];
+        float qscale[2], lse2[2];
+        int see_hi[2], see_lo[2];                                   // rows 2c and 2c + 1 of the eight see keys [lo, hi)
+        int all_hi, all_lo;                                         // every one of the rows sees [all_lo, all_hi)
         auto load_queries = [&](const WeightSeq& s, uint32_t head, uint32_t first_row) {
             const uint32_t rows = s.count * a.group;
             all_hi = 0x7fffffff;
             all_lo = 0;
+            const uint32_t row = first_row + r, tok = row / a.group;
+            const bool on = row < rows;
+            const T* q = static_cast<const T*>(a.q);
+            if (on) q += (long long)(s.row + tok) * a.q_token + (long long)(head * a.group + row - tok * a.group) * a.q_head + c * (DP / 4);
+            float x[DP / 4], amax = 0.0f;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint32_t row = first_row + t * 8 + r, tok = row / a.group;
-                const bool on = row < rows;
-                const T* q = static_cast<const T*>(a.q);
-                if (on) q += (long long)(s.row + tok) * a.q_token + (long long)(head * a.group + row - tok * a.group) * a.q_head + c * (DP / 4);
-                float x[DP / 4], amax = 0.0f;
+            for (int d = 0; d < DP / 4; ++d) x[d] = 0.0f;
+            if (on) {
+                if (a.q_aligned) {
 #pragma unroll
-                for (int d = 0; d < DP / 4; ++d) x[d] = 0.0f;
-                if (on) {
-                    if (a.q_aligned) {
+                    for (int d = 0; d < DP / 4; d += 8)
+                        if (c * (DP / 4) + d < kv.dim) unpack<T>(*reinterpret_cast<const uint4*>(q + d), x + d);
+                } else {
 #pragma unroll
-                        for (int d = 0; d < DP / 4; d += 8)
-                            if (c * (DP / 4) + d < kv.dim) unpack<T>(*reinterpret_cast<const uint4*>(q + d), x + d);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < DP / 4; ++d)
-                            if (c * (DP / 4) + d < kv.dim) x[d] = to_f32(q[d]);
-                    }
+                    for (int d = 0; d < DP / 4; ++d)
+                        if (c * (DP / 4) + d < kv.dim) x[d] = to_f32(q[d]);
                 }
+            }
 #pragma unroll
-                for (int d = 0; d < DP / 4; ++d) amax = fmaxf(amax, fabsf(x[d]));
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-                // To float16 with the row's largest magnitude in [1, 2): exact for float16 and bfloat16 queries but for elements below
-                // 2^-14 of it, which lose at most 2^-25 of it.
-                int e = (int)(__float_as_uint(amax) >> 23) - 127;
-                e = max(min(e, 126), -126);
-                const float down = pow2f(-e);
+            for (int d = 0; d < DP / 4; ++d) amax = fmaxf(amax, fabsf(x[d]));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            // To float16 with the row's largest magnitude in [1, 2): exact for float16 and bfloat16 queries but for elements below
+            // 2^-14 of it, which lose at most 2^-25 of it.
+            int e = (int)(__float_as_uint(amax) >> 23) - 127;
+            e = max(min(e, 126), -126);
+            const float down = pow2f(-e);
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const __half2 lo = __floats2half2_rn(x[4 * i] * down, x[4 * i + 1] * down);
-                    const __half2 hi = __floats2half2_rn(x[4 * i + 2] * down, x[4 * i + 3] * down);
-                    qf[t][i][0] = reinterpret_cast<const uint32_t&>(lo);
-                    qf[t][i][1] = reinterpret_cast<const uint32_t&>(hi);
-                }
-                const float up = pow2f(e) * a.scale_log2;
-                const float own = on ? a.lse[(size_t)(s.row + tok) * a.q_heads + head * a.group + row - tok * a.group] * kLog2e : 0.0f;
-                const int start = (int)s.length - (int)s.count;
+            for (int i = 0; i < KS; ++i) {
+                const __half2 lo = __floats2half2_rn(x[4 * i] * down, x[4 * i + 1] * down);
+                const __half2 hi = __floats2half2_rn(x[4 * i + 2] * down, x[4 * i + 3] * down);
+                qf[i][0] = reinterpret_cast<const uint32_t&>(lo);
+                qf[i][1] = reinterpret_cast<const uint32_t&>(hi);
+            }
+            const float up = pow2f(e) * a.scale_log2;
+            const float own = on ? a.lse[(size_t)(s.row + tok) * a.q_heads + head * a.group + row - tok * a.group] * kLog2e : 0.0f;
+            const int start = (int)s.length - (int)s.count;
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    qscale[t][n] = __shfl_sync(0xffffffffu, up, (2 * c + n) * 4);
-                    lse2[t][n] = __shfl_sync(0xffffffffu, own, (2 * c + n) * 4);
-                    const uint32_t rc = first_row + t * 8 + 2 * c + n;
-                    const int pos = start + (int)(rc / a.group);
-                    see_hi[t][n] = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
-                    see_lo[t][n] = a.window ? first_seen(pos, a.window) : 0;
-                    if (rc >= rows) lse2[t][n] = INFINITY;          // takes no part, whether its keys are looked at one by one or not
-                    else {
-                        all_hi = min(all_hi, see_hi[t][n]);
-                        all_lo = max(all_lo, see_lo[t][n]);
-                    }
+            for (int n = 0; n < 2; ++n) {
+                qscale[n] = __shfl_sync(0xffffffffu, up, (2 * c + n) * 4);
+                lse2[n] = __shfl_sync(0xffffffffu, own, (2 * c + n) * 4);
+                const uint32_t rc = first_row + 2 * c + n;
+                const int pos = start + (int)(rc / a.group);
+                see_hi[n] = rc < rows ? max(min(pos + 1, (int)s.length), 0) : 0;
+                see_lo[n] = a.window ? first_seen(pos, a.window) : 0;
+                if (rc >= rows) lse2[n] = INFINITY;          // takes no part, whether its keys are looked at one by one or not
+                else {
+                    all_hi = min(all_hi, see_hi[n]);
+                    all_lo = max(all_lo, see_lo[n]);
                 }
             }
 #pragma unroll
@@ -290,14 +289,13 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
                 pages = pages && ks[g] >= 0.0f;
                 sum[g][0] = sum[g][1] = 0.0f;
             }
-            for (uint32_t first_row = 0; first_row < rows; first_row += 8 * NT) {
+            for (uint32_t first_row = 0; first_row < rows; first_row += 8) {
                 if (fresh_queries) load_queries(sh_seq[now.seq], now.head, first_row);
-                fresh_queries = rows > 8 * NT;
-                float sc[G][NT][4];
+                fresh_queries = rows > 8;                             // a chunk among single tokens
+                float sc[G][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) sc[g][t][0] = sc[g][t][1] = sc[g][t][2] = sc[g][t][3] = 0.0f;
+                    sc[g][0] = sc[g][1] = sc[g][2] = sc[g][3] = 0.0f;
                     uint32_t kr[2][KW];
                     read_span<DP, KW>(kr[0], side, 16 * g + r, c * (DP / 4));
                     read_span<DP, KW>(kr[1], side, 16 * g + r + 8, c * (DP / 4));
@@ -306,8 +304,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
                         uint32_t a0, a1, a2, a3;
                         codes_to_f16<kFormat>(kr[0][i], a0, a2);
                         codes_to_f16<kFormat>(kr[1][i], a1, a3);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16816(sc[g][t], a0, a1, a2, a3, qf[t][i][0], qf[t][i][1]);
+                        mma16816(sc[g], a0, a1, a2, a3, qf[i][0], qf[i][1]);
                     }
                 }
                 // sc[e] is key r + 8 * (e >> 1) of the group, row 2c + (e & 1)
@@ -315,20 +312,18 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                    for (int n = 0; n < 2; ++n) {
+                        const float f = qscale[n] * ks[g];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            const float f = qscale[t][n] * ks[g];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                float x = fmaf(sc[g][t][2 * h + n], f, -lse2[t][n]);
-                                if (!whole) {
-                                    const int k = now.key + 16 * g + 8 * h + r;
-                                    if (k >= see_hi[t][n] || k < see_lo[t][n] || ks[g] < 0.0f) x = -INFINITY;
-                                }
-                                sum[g][h] += exp2_fast(x);
+                        for (int h = 0; h < 2; ++h) {
+                            float x = fmaf(sc[g][2 * h + n], f, -lse2[n]);
+                            if (!whole) {
+                                const int k = now.key + 16 * g + 8 * h + r;
+                                if (k >= see_hi[n] || k < see_lo[n] || ks[g] < 0.0f) x = -INFINITY;
                             }
+                            sum[g][h] += exp2_fast(x);
                         }
+                    }
             }
             float mine = 0.0f;
 #pragma unroll
@@ -364,7 +359,11 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks<DP, NT>) few_wei
 //
 // A block has 128 keys of one (sequence, key head) at a time.  Warps 0 to 3 widen the codes and take the exponentials; warp 4 issues the products;
 // warp 5 brings the queries, up to 32 rows at a time, by tensor copies (rows that are not aligned to 16 bytes: by hand), warp 6 the codes of the next keys
-// by asynchronous copies.  Four blocks share an SM (two with heads of more than 128): while one waits or widens, the others keep the
+// by asynchronous copies.  What bounds it are the exponentials: 64 queries of 32 heads on 8 over four times up to 16384 keys, 87 million of them, are
+// 19 us of special-function time and take 50; 1024 queries 526 (310).  Some 1700 cycles go by for a block of 32 rows, 1024 of them exponentials of the
+// SM's four blocks, and 5000 for a unit's codes, widening and first product.  (Keys as shared-memory operands, 256 at a time, two blocks an SM: 63;
+// queries by asynchronous copies of two warps, 2400 cycles of instructions a block: 79.)
+// Four blocks share an SM (two with heads of more than 128): while one waits or widens, the others keep the
 // special-function units busy.  A block of rows is whole tokens of the group, or part of one where the group has more than 32 heads.
 constexpr int kManyThreads = 224, kManyRows = 32, kManyKeys = 128, kManySeqs = 128;
 constexpr int kQueryStages = 4;                      // of 32 rows
@@ -775,21 +774,17 @@ template <int DP, int kFormat, class T> static int launch_many_weights(WeightArg
     return launch("kv_weights", many_weights_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count() * Many<DP>::kPerSm), dim3(kManyThreads), Many<DP>::kSmem, st, false, a, map);
 }
 
-template <int DP, int NT, int kFormat, class T> static int launch_few_weights(const WeightArgs& a, cudaStream_t st) {
-    return launch("kv_weights", few_weights_kernel<DP, NT, kFormat, T>, dim3((uint32_t)sm_count() * kWeightBlocks<DP, NT>), dim3(kWeightThreads), FewWeights<DP>::kSmem, st, false, a);
+template <int DP, int kFormat, class T> static int weight_rows(const WeightArgs& a, bool many, cudaStream_t st) {
+    if (many) return launch_many_weights<DP, kFormat, T>(a, st);
+    return launch("kv_weights", few_weights_kernel<DP, kFormat, T>, dim3((uint32_t)sm_count() * kWeightBlocks), dim3(kWeightThreads), FewWeights<DP>::kSmem, st, false, a);
 }
-enum class Rows { eight, sixteen, many };
-template <int DP, int kFormat, class T> static int weight_rows(const WeightArgs& a, Rows rows, cudaStream_t st) {
-    if (rows == Rows::many) return launch_many_weights<DP, kFormat, T>(a, st);
-    return rows == Rows::eight ? launch_few_weights<DP, 1, kFormat, T>(a, st) : launch_few_weights<DP, 2, kFormat, T>(a, st);
+template <int kFormat, class T> static int weight_dims(const WeightArgs& a, bool many, cudaStream_t st) {
+    if (a.c.dim <= 64) return weight_rows<64, kFormat, T>(a, many, st);
+    if (a.c.dim <= 128) return weight_rows<128, kFormat, T>(a, many, st);
+    return weight_rows<256, kFormat, T>(a, many, st);
 }
-template <int kFormat, class T> static int weight_dims(const WeightArgs& a, Rows rows, cudaStream_t st) {
-    if (a.c.dim <= 64) return weight_rows<64, kFormat, T>(a, rows, st);
-    if (a.c.dim <= 128) return weight_rows<128, kFormat, T>(a, rows, st);
-    return weight_rows<256, kFormat, T>(a, rows, st);
-}
-template <class T> static int weight_format(const WeightArgs& a, Rows rows, cudaStream_t st) {
-    return a.c.format == ROOMIE_KV_E4M3 ? weight_dims<ROOMIE_KV_E4M3, T>(a, rows, st) : weight_dims<ROOMIE_KV_INT8, T>(a, rows, st);
+template <class T> static int weight_format(const WeightArgs& a, bool many, cudaStream_t st) {
+    return a.c.format == ROOMIE_KV_E4M3 ? weight_dims<ROOMIE_KV_E4M3, T>(a, many, st) : weight_dims<ROOMIE_KV_INT8, T>(a, many, st);
 }
 
 }  // namespace roomie
@@ -820,8 +815,12 @@ extern "C" int roomie_kv_weights(const roomie_kv_cache* cache, uint32_t layer, c
     a.scale_log2 = scale * kLog2e;
     a.q_aligned = rows_aligned16(*q, rows, q_heads);
     a.fresh = fresh != 0;
-    const unsigned long long all = (unsigned long long)rows * a.group;
-    const Rows kind = all <= 8ull * num_seqs ? Rows::eight : all <= 16ull * num_seqs ? Rows::sixteen : Rows::many;
+    // Which kernel, by the rows a sequence and key head (of a mixed call: their average).  32 query heads on 8, sequences of up to 4096 keys, 16 of them
+    // and 2 of them, us:
+    //   rows                  4        8         16        24        32       64
+    //   products by warps     16.1 8.0 18.3 10.3 26.6 15.6 88.8 21.6 110 25.6 209 45.9     (16 in one pass)
+    //   on tensor memory                         25.2 9.7  25.2 9.6  23.4 9.4 27.9 10.3
+    const bool many = (unsigned long long)rows * a.group > 8ull * num_seqs;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return q->type == ROOMIE_F16 ? weight_format<__half>(a, kind, st) : weight_format<__nv_bfloat16>(a, kind, st);
+    return q->type == ROOMIE_F16 ? weight_format<__half>(a, many, st) : weight_format<__nv_bfloat16>(a, many, st);
 }
