@@ -120,15 +120,34 @@ template <class T, int kV, bool kPairs> __device__ __forceinline__ void store_un
     if (u.on) *reinterpret_cast<Raw<T, kV>*>(p + u.a) = r.a;
     if (u.two) *reinterpret_cast<Raw<T, kV>*>(p + u.b) = r.b;
 }
+// kV weights in a row, 16 bytes at a time where they are aligned to that: a chunk starts at a multiple of kV.
+template <class W, int kV> __device__ __forceinline__ void weights_at(const W* w, float* x) {
+    if constexpr (kV * sizeof(W) >= 16) {
+        if ((reinterpret_cast<uintptr_t>(w) & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < kV; i += 16 / (int)sizeof(W)) {
+                const uint4 four = *reinterpret_cast<const uint4*>(w + i);
+#pragma unroll
+                for (int j = 0; j < 16 / (int)sizeof(W); ++j) x[i + j] = to_f32(reinterpret_cast<const W*>(&four)[j]);
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kV; ++i) x[i] = to_f32(w[i]);
+}
+template <class W, int kV> __device__ __forceinline__ void unit_weights(const void* w, const Unit& u, float* x) {
+    if (u.on) weights_at<W, kV>(static_cast<const W*>(w) + u.a, x);
+    if (u.two) weights_at<W, kV>(static_cast<const W*>(w) + u.b, x + kV);
+}
 template <int kV, bool kPairs> __device__ __forceinline__ Elements<kV> load_weights(const void* w, int32_t type, const Unit& u) {
     float x[2 * kV];
 #pragma unroll
-    for (int i = 0; i < 2 * kV; ++i) {
-        const uint32_t at = i < kV ? u.a + i : u.b + i - kV;
-        const bool there = i < kV ? u.on : u.two;
-        x[i] = !there ? 0.0f : !w ? 1.0f : type == ROOMIE_F32 ? static_cast<const float*>(w)[at]
-               : type == ROOMIE_F16 ? __half2float(static_cast<const __half*>(w)[at]) : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[at]);
-    }
+    for (int i = 0; i < 2 * kV; ++i) x[i] = !w && (i < kV ? u.on : u.two) ? 1.0f : 0.0f;
+    if (!w) return vectors<kV, kPairs>(x);
+    if (type == ROOMIE_F32) unit_weights<float, kV>(w, u, x);
+    else if (type == ROOMIE_F16) unit_weights<__half, kV>(w, u, x);
+    else unit_weights<__nv_bfloat16, kV>(w, u, x);
     return vectors<kV, kPairs>(x);
 }
 // cosines and sines of a unit's pairs; 1 and 0 where it does not turn
