@@ -215,6 +215,7 @@ __device__ __forceinline__ Place place_of(const NormArgs& n) {
 // Bound by memory, and near it by instructions: two float32 an instruction, weights and turns multiplied once for all heads of a thread, the next head's
 // row under way (16384 tokens x 40 heads x 128 in bf16, 336 MB: 77 us, 4340 GB/s; each element on its own: 101).  Six blocks an SM; the spills that this
 // takes lie in front of the loop over heads (without a limit, 125 registers and four blocks: 95 us; 8-byte chunks: 125).
+constexpr int kAhead = 3;
 template <class T, int kV, int kPer, bool kPairs>
 __global__ void __launch_bounds__(kNormThreads, 6) norm_kernel(NormArgs n) {
     const Place p = place_of(n);
@@ -224,12 +225,36 @@ __global__ void __launch_bounds__(kNormThreads, 6) norm_kernel(NormArgs n) {
 #pragma unroll
     for (int k = 0; k < kPer; ++k) u[k] = unit_of<kV, kPairs>(n, (threadIdx.x & 31) - p.first + k * n.lanes);
     const long long x_step = s.groups * s.x_head, y_step = s.groups * s.y_head;
+    // Chunks of 8 or 16 bytes come kAhead heads before they are needed, to a thread's own part of shared memory; smaller ones one head, to registers.
+    constexpr bool kRing = kPer == 1 && sizeof(Raw<T, kV>) >= 8;
+    __shared__ Raw<T, kV> ring[kRing ? kAhead + 1 : 1][2][kRing ? kNormThreads : 1];
+    auto fetch = [&](const T* from, bool there, int stage) {
+        if constexpr (kRing) {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ring[stage][0][threadIdx.x]);
+            if (there && u[0].on)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from + u[0].a), "n"((int)sizeof(Raw<T, kV>)) : "memory");
+            if (there && u[0].two)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + (uint32_t)(kNormThreads * sizeof(Raw<T, kV>))), "l"(from + u[0].b), "n"((int)sizeof(Raw<T, kV>)) : "memory");
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    if constexpr (kRing)
+#pragma unroll
+        for (int i = 0; i <= kAhead; ++i) {                          // what is not there stays 0
+            if (!u[0].on) ring[i][0][threadIdx.x] = {};
+            if (!u[0].two) ring[i][1][threadIdx.x] = {};
+        }
     for (uint32_t token = p.slot; token < n.tokens; token += n.slots) {
         const T* x = static_cast<const T*>(s.x) + (long long)token * s.x_token + (long long)p.group * s.x_head;
         T* y = static_cast<T*>(s.y) + (long long)token * s.y_token + (long long)p.group * s.y_head;
         Loaded<T, kV> next[kPer];
+        if constexpr (kRing) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) next[k] = load_unit<T, kV>(x, u[k]);
+            for (int i = 0; i < kAhead; ++i) fetch(x + i * x_step, p.group + i * s.groups < s.heads, i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) next[k] = load_unit<T, kV>(x, u[k]);
+        }
         // y_a = x_a own.a - x_b cross.b, y_b = x_b own.b + x_a cross.a, each with r
         const int32_t position = n.rope.rot ? n.positions[token] : 0;
         Elements<kV> own[kPer], cross[kPer];
@@ -245,14 +270,23 @@ __global__ void __launch_bounds__(kNormThreads, 6) norm_kernel(NormArgs n) {
                 cross[k].b[i] = minus(mul2(turn.b[i], w.b[i]));
             }
         }
+        int stage = 0;
         for (uint32_t head = p.group; head < s.heads; head += s.groups) {
             Elements<kV> v[kPer];
             uint64_t sum = 0;
+            if constexpr (kRing) {
+                fetch(x + kAhead * x_step, head + kAhead * s.groups < s.heads, (stage + kAhead) & kAhead);
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+                next[0].a = ring[stage][0][threadIdx.x];
+                next[0].b = ring[stage][1][threadIdx.x];
+                stage = (stage + 1) & kAhead;
+            }
             x += x_step;
 #pragma unroll
             for (int k = 0; k < kPer; ++k) {
                 v[k] = widened<T, kV, kPairs>(next[k]);
-                if (head + s.groups < s.heads) next[k] = load_unit<T, kV>(x, u[k]);     // the next head's
+                if constexpr (!kRing)
+                    if (head + s.groups < s.heads) next[k] = load_unit<T, kV>(x, u[k]);     // the next head's
                 sum = dot<kV>(v[k], v[k], sum);
             }
             float square = row_sum(sum, n.lanes, p.mask), eps = n.eps;
