@@ -212,12 +212,13 @@ __device__ __forceinline__ Place place_of(const NormArgs& n) {
     return p;
 }
 
-// Bound by memory, and near it by instructions: two float32 an instruction, weights and turns multiplied once for all heads of a thread, the next head's
-// row under way (16384 tokens x 40 heads x 128 in bf16, 336 MB: 77 us, 4340 GB/s; each element on its own: 101).  Six blocks an SM; the spills that this
-// takes lie in front of the loop over heads (without a limit, 125 registers and four blocks: 95 us; 8-byte chunks: 125).
+// Bound by memory: two float32 an instruction, weights and turns multiplied once for all heads of a thread, rows under way three heads ahead (16384 tokens
+// x 40 heads x 128 in bf16, 336 MB: 64 us, 5220 GB/s; the next head's row alone, in registers: 77; seven heads ahead: 87; each element on its own: 101).
+// Five blocks an SM; the spills that this takes lie in front of the loop over heads (six: 69 us, eight: 94; 8-byte chunks: 125).  Of smaller chunks six,
+// whose registers suffice (3001 tokens x 6 heads x 65: 18 us, with five 21).
 constexpr int kAhead = 3;
 template <class T, int kV, int kPer, bool kPairs>
-__global__ void __launch_bounds__(kNormThreads, 6) norm_kernel(NormArgs n) {
+__global__ void __launch_bounds__(kNormThreads, kV == 8 ? 5 : 6) norm_kernel(NormArgs n) {
     const Place p = place_of(n);
     if (p.slot >= n.slots) return;
     const NormSide s = p.second ? n.side[1] : n.side[0];
@@ -467,8 +468,8 @@ template <class T, bool kGrad> static int run_norm(NormArgs n, uint32_t align, u
     n.units = n.rope.rot / 2 / v + ((n.dim - n.rope.rot) / v + 1) / 2;
     n.lanes = 1;
     while (n.lanes < n.units && n.lanes < 32) n.lanes *= 2;
-    // Head groups: a thread's weights and turns cost as much as some heads, so it should have eight heads or more (16384 tokens x 40 heads: 77 us, with four
-    // 83, with sixteen 85), unless there are too few rows to fill the GPU.
+    // Head groups: a thread's weights and turns cost as much as some heads, so it should have eight heads or more (16384 tokens x 40 heads: with sixteen
+    // 2 us more; rows one head ahead: 77, with four heads 83), unless there are too few rows to fill the GPU.
     const unsigned long long one = (unsigned long long)n.tokens * n.lanes;
     for (NormSide& s : n.side) {
         unsigned long long g = (2048ull * sms + one - 1) / one, few = 256ull * sms / one;
