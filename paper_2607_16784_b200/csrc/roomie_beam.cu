@@ -130,8 +130,9 @@ __device__ __forceinline__ void pick_best(PickShared& sh, const uint4* raw, cons
             put(to_f32(reinterpret_cast<const T*>(&sh.hit[x / v])[x % v]), sh.hit_at[x / v] + x % v);
         __syncthreads();
     }
-    while (hits > kHits || sh.count > kList) {
-        if (hits <= kHits || sh.count > kList) {                      // a list that ran over
+    bool full = hits <= kHits && sh.count > kList;                    // the list ran over (the same for all threads: the count is at rest)
+    for (bool own = hits > kHits; own || full; own = false) {
+        if (full) {
             const uint32_t sample = sample_of(num);
             for (uint32_t i = threadIdx.x; i < sample; i += kBeamThreads) {
                 const unsigned long long x = sh.list[i];
@@ -155,7 +156,7 @@ __device__ __forceinline__ void pick_best(PickShared& sh, const uint4* raw, cons
             for (int k = 0; k < v; ++k) put(element<T>(piece, k), base + i * step + k);
         }
         __syncthreads();
-        if (sh.count <= kList) break;
+        full = sh.count > kList;
     }
     const uint32_t n = sh.count;
     for (uint32_t i = threadIdx.x; i < n; i += kBeamThreads) {

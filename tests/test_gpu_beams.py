@@ -3,6 +3,8 @@
 Picks are compared exactly wherever neighbouring candidates are further apart than what the sums of exponentials may be off: of n logits a
 thread adds at most 64 and a block 256 such sums in float32, and each exponential is off by 2^-22 and its argument by 2^-24 of at most 128:
 2^-17 + 2^-22 + 320 2^-24 of the sum at the very most, 3e-5 (SLACK; within a row the order is exact).  Scores: the same, and their own rounding."""
+import math
+
 import numpy as np
 import pytest
 
@@ -228,3 +230,19 @@ def test_beam_refusals(torch, rm):
             rm.beam_workspace(*bad)
     got = rm.beam_select(x[:0], s[:0], 4)
     assert all(tuple(t.shape) == (0, 4) for t in got)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("num", [1, 32, 33, 128])
+def test_beams_of_one_number_in_large_parts(torch, rm, dtype, num):
+    """Rows whose every piece may hold a candidate, enough of them for parts of eight pieces a thread: the same answer each time."""
+    requests, beams, vocab = 10, 3, 33333
+    x = torch.zeros(requests, beams, vocab, dtype=dtype_of(torch, dtype), device="cuda")
+    scores = torch.zeros(requests, beams, device="cuda")
+    for _ in range(20):
+        got = rm.beam_select(x, scores, num)
+        assert torch.equal(got[1].cpu(), (torch.arange(requests, dtype=torch.int32) * beams).unsqueeze(1).expand(-1, num))
+        assert torch.equal(got[2].cpu(), torch.arange(num, dtype=torch.int32).expand(requests, num))
+        assert (got[0].cpu().double() + math.log(vocab)).abs().max() <= 1e-5      # eps / 2 of 10.4 is 6e-7; sums of ones are exact
+    rising = (torch.arange(vocab, device="cuda") // 64).to(x.dtype).expand(requests, beams, vocab)
+    check(torch, rm, rising, scores, num)
