@@ -739,8 +739,11 @@ __global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_k
     if (wid == 4) {
         if (elected()) tc_commit(&sh.drain);                         // whatever was issued has ended before the memory is given back
         __syncwarp();
-        warp_wait(&sh.drain, 0, sh);
+        mbar_wait_bounded(&sh.drain, 0);
     }
+    if (wid == 5 && a.tensor_copies)                                  // nor does a block that gave up end before its copies: the last of each stage
+        for (uint32_t b = block > kQueryStages ? block - kQueryStages : 0; b < block; ++b) mbar_wait_bounded(&sh.q_full[b & (kQueryStages - 1)], b / kQueryStages & 1);
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
