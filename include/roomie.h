@@ -522,7 +522,7 @@ int roomie_kv_attention(const roomie_kv_cache *cache /* host */, uint32_t layer,
  *   reorder  sequence seqs[i] becomes what sequence seqs[parents[i]] was before the call (parents[i] in [0, n), repeated or left out at will;
  *            -1: empty), in place: whole pages are shared; a part-filled last page goes to the first child, the others get copies, in the lowest
  *            pages that are free once those without a child have been given up.  All or nothing: where a sequence is named twice, an index or length is out
- *            of range, a page is not one or has too few references, or the free pages do not suffice, nothing changes but the status;
+ *            of range, a page is not one or has too few references, or the free pages do not suffice, nothing changes but the status.  n is at most 8192;
  *   copy     page src_pages[i] of src to page dst_pages[i] of dst, codes and scales of all layers (n pairs; the caches
  *            agree in layers, page_tokens, kv_heads, head_dim, format and layout; no page may be written twice, or both
  *            read and written); tables and counts are left alone;
@@ -548,8 +548,8 @@ int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out
  *   weight [layers][max_seqs][kv_heads][max_pages * page_tokens] float32: the sums are added to what is there for the sequence's earlier tokens, and
  * replace it for the call's own ones (which have received nothing before); with `fresh`, for all its tokens.  What lies behind a sequence's length
  * is not touched.  A key on a page that is none receives nothing.
- *   Float32 sums of products of the codes with q (bfloat16 queries: as float16 against the row's largest, which leaves their bits but below
- * 2^-14 of it).  A NaN reaches the keys that its row sees, or the key whose code it is; not others.  The same call gives the same bits.
+ *   Float32 sums of products of the codes with q (up to 8 rows a sequence and key head on average, the queries as float16 against the row's largest, which leaves their bits but below
+ * 2^-14 of it; more rows as they are).  A NaN reaches the keys that its row sees, or the key whose code it is; not others.  The same call gives the same bits.
  * q: F16 or BF16.  Errors: INVALID_ARG, CUDA. */
 int roomie_kv_weights(const roomie_kv_cache *cache /* host */, uint32_t layer, const int32_t *seqs, uint32_t num_seqs, const int32_t *q_offset,
                       uint32_t rows, uint32_t q_heads, const roomie_rows *q, const float *lse, float scale, uint32_t window, int fresh, float *weight,
@@ -572,6 +572,7 @@ int roomie_kv_evict(const roomie_kv_cache *cache /* host */, const int32_t *seqs
  * in order, equal ones by (beam, token).  logits: element (r, b, v) at r * request_stride + b * beam_stride + v (strides in elements, any
  * alignment of the rows); scores, ended [requests][beams]; outputs [requests][num]: the score rounded to float32, the row r * beams + b it comes from
  * (what roomie_kv_reorder takes) and its token; -infinity, -1, -1 where there are fewer candidates.
+ * The outputs overlap nothing else of the call, except that scores_out may be scores where num == beams.
  *   A logit of -infinity is no candidate.  A beam whose score is not finite, or whose row holds NaN or +infinity, or nothing above -infinity, has none.
  *   A beam with ended != 0 (ended may be NULL) has one: itself, with its score and the token `pad`; its logits are not read.
  * Sums of exponentials are float32 over a thread's 8 to 64 logits and a block's threads, 64 bits from there on; scores are compared in 64 bits.
