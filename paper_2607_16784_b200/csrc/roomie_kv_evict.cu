@@ -105,7 +105,7 @@ struct EvictArgs {
 // Selection: the smallest kept weight by its bits, 11, 11 and 10 at a time, from histograms in shared memory, where the first kCached weights'
 // bits lie too; then a bit for each token and the number of kept ones in front of each 128.
 //
-// Move: rounds of 128 tokens, in order.  A warp has the keys or the values of 32 of them: a lane looks up where one token comes from, then each token's
+// Move: rounds of 256 tokens, in order.  A warp has the keys or the values of 32 of them: a lane looks up where one token comes from, then each token's
 // 16-byte pieces are read by kLanes neighbouring lanes, all at once, into registers; the next round's tokens are looked up meanwhile.  Behind the one
 // barrier of a round, when the pages' largest magnitudes are known, the codes are written.  A token never moves up, so what a round writes was read by it
 // or a round before, and no round after it reads there: tokens move inside their own pages.
