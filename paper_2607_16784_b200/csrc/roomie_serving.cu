@@ -49,18 +49,25 @@ static void record_drop(uint32_t made) {
 }
 
 // ---- large shared memory ---------------------------------------------------------------------------------------------
-// The attribute belongs to a function and a device and only ever grows here; a thread remembers what it has set, because setting it
+// The attribute belongs to a function and a device, for all threads of the process.  It is set to the most that there can be, once: were it set to
+// what a call needs, a small call would take it away from the large ones of other threads.  A thread remembers what it has set, because setting it
 // costs as much as half a launch.
 int allow_smem(const void* fn, size_t bytes) {
-    struct Set { const void* fn; int dev; size_t bytes; };
+    struct Set { const void* fn; int dev; size_t most; };
     static thread_local Set sets[64];
     int dev = 0;
     ROOMIE_CUDA_OK(cudaGetDevice(&dev));
     Set& s = sets[(reinterpret_cast<uintptr_t>(fn) >> 4) % 64];
-    if (s.fn == fn && s.dev == dev && s.bytes >= bytes) return ROOMIE_OK;
-    ROOMIE_CUDA_OK(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    s = {fn, dev, bytes};
-    return ROOMIE_OK;
+    if (s.fn != fn || s.dev != dev) {
+        int all = 0;
+        cudaFuncAttributes own;
+        ROOMIE_CUDA_OK(cudaDeviceGetAttribute(&all, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev));
+        ROOMIE_CUDA_OK(cudaFuncGetAttributes(&own, fn));
+        const size_t most = (size_t)all - own.sharedSizeBytes;
+        ROOMIE_CUDA_OK(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+        s = {fn, dev, most};
+    }
+    return bytes <= s.most ? ROOMIE_OK : check_cuda(cudaErrorInvalidValue);
 }
 
 // ---- rotary positions ------------------------------------------------------------------------------------------------
