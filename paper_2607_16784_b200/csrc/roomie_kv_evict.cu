@@ -491,9 +491,11 @@ extern "C" int roomie_kv_evict(const roomie_kv_cache* cache, const int32_t* seqs
     a.seqs = seqs; a.ws = page_scratch(cache, workspace);
     a.weight = weight; a.weight_out = weight_out;
     a.refs = cache->refs; a.pages_out = cache->pages; a.length = cache->length;
-    rc = launch("kv_evict_plan", evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, false, table_view(cache), seqs, n, keep, a.ws);
-    if (rc != ROOMIE_OK) return rc;
     const size_t smem = ((tokens + 31) / 32 + (tokens + 127) / 128 + (tokens < kCached ? tokens : kCached)) * sizeof(uint32_t);
     void (*k)(EvictArgs) = cache->format == ROOMIE_KV_E4M3 ? evict_kernel_for<ROOMIE_KV_E4M3>(cache) : evict_kernel_for<ROOMIE_KV_INT8>(cache);
+    rc = allow_smem(reinterpret_cast<const void*>(k), smem);      // before the plan, which marks entries of the table
+    if (rc != ROOMIE_OK) return rc;
+    rc = launch("kv_evict_plan", evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, false, table_view(cache), seqs, n, keep, a.ws);
+    if (rc != ROOMIE_OK) return rc;
     return launch("kv_evict", k, dim3(n * cache->layers * cache->kv_heads), dim3(kEvictThreads), smem, st, true, a);
 }

@@ -554,16 +554,19 @@ extern "C" int roomie_kv_reorder(const roomie_kv_cache* cache, const int32_t* se
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int32_t* ws = page_scratch(cache, workspace);
     const TableView t = table_view(cache);
+    uint32_t columns = 32;                                        // at most 32 KB of shared memory
+    while (columns > 1 && n * columns > kReorderMost) columns /= 2;
+    const size_t smem = (size_t)n * columns * sizeof(int32_t);
+    rc = allow_smem(reinterpret_cast<const void*>(reorder_move_kernel), smem);   // before the plan, which changes counts and lengths: all or nothing
+    if (rc != ROOMIE_OK) return rc;
     rc = launch("kv_reorder_plan", reorder_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, false, t, seqs, parents, n, ws);
     if (rc != ROOMIE_OK) return rc;
     const ReorderView v = reorder_view(ws, n);
     CopyArgs copy = copy_args(cache, cache);
     copy.n = n; copy.src = v.src; copy.dst = v.dst;
-    uint32_t columns = 32;                                        // at most 32 KB of shared memory
-    while (columns > 1 && n * columns > kReorderMost) columns /= 2;
     const uint32_t all = (cache->max_pages + columns - 1) / columns, table_blocks = all < 148 ? all : 148;
-    return launch("kv_reorder_move", reorder_move_kernel, dim3(table_blocks + copy_blocks(copy, n)), dim3(256), (size_t)n * columns * sizeof(int32_t), st, true, t,
-                  seqs, parents, n, ws, columns, table_blocks, copy);
+    return launch("kv_reorder_move", reorder_move_kernel, dim3(table_blocks + copy_blocks(copy, n)), dim3(256), smem, st, true, t, seqs, parents, n, ws, columns,
+                  table_blocks, copy);
 }
 
 extern "C" int roomie_kv_free(const roomie_kv_cache* cache, const int32_t* seqs, uint32_t n, void* stream) {

@@ -63,3 +63,15 @@ for big, small, call in ((256, 130, reorder), (8192, 700, evict)):
     assert a.submit(call, big).result() == 0
 assert fake.fake_refused() == 0 and fake.fake_launched() == 20
 """)
+
+
+def test_nothing_is_launched_where_the_second_kernel_cannot_be(python):
+    """A plan changes the cache: it is launched when nothing that can refuse the kernel behind it is left."""
+    python("""
+fake.fake_attributes_fail(1)
+for call in (lambda: reorder(256), lambda: reorder(3), lambda: evict(8192), lambda: evict(1)):
+    assert call() == -3 and fake.fake_launched() == 0             # ROOMIE_ERR_CUDA
+fake.fake_attributes_fail(0)
+for n, call in enumerate((lambda: reorder(256), lambda: reorder(3), lambda: evict(8192), lambda: evict(1))):
+    assert call() == 0 and fake.fake_launched() == 2 * n + 2
+""")
