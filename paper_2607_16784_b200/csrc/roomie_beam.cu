@@ -17,7 +17,8 @@ struct BeamArgs {
     long long request_stride, beam_stride;          // elements
     const float* scores;
     const uint8_t* ended;
-    uint32_t requests, beams, vocab, num, pad, splits;
+    uint32_t requests, beams, vocab, num, pad, splits, part;   // splits: parts of a row, of `part` elements each
+    int32_t type;
     unsigned long long* keys;                       // [rows][splits][num]
     float2* sums;                                   // [rows][splits] of maximum, sum of exp(x - maximum)
     float* scores_out;
@@ -271,11 +272,30 @@ struct Candidate {
 };
 __device__ __forceinline__ bool over(const Candidate& x, const Candidate& y) { return x.value > y.value || (x.value == y.value && x.order > y.order); }
 
-constexpr int kPickThreads = 256;
+constexpr int kPickThreads = 256, kPickWarps = kPickThreads / 32;
 struct PickList {
     Candidate list[kList], bound;
-    uint32_t count;
+    unsigned long long level;
+    uint32_t count, unsure, above, votes[kPickWarps];
 };
+
+// A beam's score, the largest logit of its row (or of nothing) and the logarithm of the row's sum, as the kernel has them for each beam.  A candidate's
+// value: the difference first, since logits may be of any size.
+__device__ __forceinline__ unsigned long long value_of(const double* of_beam, float logit) {
+    return ordered64(of_beam[0] + ((double)logit - of_beam[1] - of_beam[2]));
+}
+// Whether no other float32 near this logit has its value.
+__device__ __forceinline__ bool only_one(const double* of_beam, uint32_t logit, unsigned long long value) {
+    return value_of(of_beam, unordered(logit - 1)) < value && value_of(of_beam, unordered(logit + 1)) > value;
+}
+
+__device__ __forceinline__ void write_pick(const BeamArgs& a, uint32_t request, uint32_t at, unsigned long long value, uint32_t beam, uint32_t token) {
+    const size_t to = (size_t)request * a.num + at;
+    const unsigned long long bits = value & 0x8000000000000000ull ? value ^ 0x8000000000000000ull : ~value;
+    a.scores_out[to] = (float)__longlong_as_double((long long)bits);
+    a.parent_out[to] = (int32_t)(request * a.beams + beam);
+    a.token_out[to] = (int32_t)token;
+}
 
 // The num-th of the first n of a list, n >= num, becomes the bound: each counts those above it.
 __device__ __forceinline__ void bound_of(PickList& sh, uint32_t n, uint32_t num) {
@@ -291,7 +311,85 @@ __device__ __forceinline__ void bound_of(PickList& sh, uint32_t n, uint32_t num)
     }
 }
 
-__global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
+// The picks where lists may have been cut within candidates of one value.  Those above the num-th value are in the lists, fewer than num; of those that have
+// it the first by (beam, token) are looked for in the logits: in the parts whose best reaches it, of which 2 num at most are gone through, in order, up to the last one wanted.
+__device__ __noinline__ void pick_by_value(const BeamArgs& a, PickList& sh, const double* of_row, uint32_t request, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, lists = a.beams * a.splits;
+    for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
+        const Candidate x = sh.list[i];
+        uint32_t above = 0;
+        for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
+        if (above == a.num - 1) sh.level = x.value;
+    }
+    __syncthreads();
+    const unsigned long long level = sh.level;
+    for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
+        const Candidate x = sh.list[i];
+        if (x.value <= level) continue;
+        uint32_t above = 0;
+        for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
+        write_pick(a, request, above, x.value, (uint32_t)(~x.order >> 32), (uint32_t)~x.order);
+        atomicAdd(&sh.above, 1u);
+    }
+    __syncthreads();
+    uint32_t at = sh.above;                                          // the same in all threads, here and below
+    auto ended = [&](uint32_t b) { return a.ended && a.ended[request * a.beams + b]; };
+    for (uint32_t first = 0; first < lists && at < a.num; first += kPickThreads) {
+        const uint32_t mine = first + threadIdx.x, b = mine / a.splits;
+        bool look = false;
+        if (mine < lists && of_row[3 * b] == of_row[3 * b]) {
+            if (ended(b)) {
+                look = mine == b * a.splits && ordered64(of_row[3 * b]) == level;
+            } else {
+                const unsigned long long key = a.keys[((size_t)request * lists + mine) * a.num];
+                look = key && value_of(of_row + 3 * b, unordered((uint32_t)(key >> 32))) >= level;
+            }
+        }
+        const uint32_t votes = __ballot_sync(0xffffffffu, look);
+        __syncthreads();
+        if (lane == 0) sh.votes[wid] = votes;
+        __syncthreads();
+        uint32_t chosen[kPickWarps];
+#pragma unroll
+        for (int w = 0; w < kPickWarps; ++w) chosen[w] = sh.votes[w];
+#pragma unroll 1
+        for (uint32_t x = 0; x < kPickThreads && at < a.num; ++x) {
+            if (!(chosen[x >> 5] >> (x & 31) & 1)) continue;
+            const uint32_t beam = (first + x) / a.splits, split = first + x - beam * a.splits;
+            if (ended(beam)) {
+                if (threadIdx.x == 0) write_pick(a, request, at, level, beam, a.pad);
+                ++at;
+                continue;
+            }
+            const long long row = (long long)request * a.request_stride + (long long)beam * a.beam_stride;
+            const uint32_t end = min(a.vocab - split * a.part, a.part);
+            for (uint32_t t0 = 0; t0 < end && at < a.num; t0 += kPickThreads) {
+                const uint32_t token = split * a.part + t0 + threadIdx.x;
+                bool hit = false;
+                if (t0 + threadIdx.x < end) {
+                    const float logit = a.type == ROOMIE_F32 ? static_cast<const float*>(a.logits)[row + token]
+                                        : a.type == ROOMIE_F16 ? to_f32(static_cast<const __half*>(a.logits)[row + token])
+                                                               : to_f32(static_cast<const __nv_bfloat16*>(a.logits)[row + token]);
+                    hit = value_of(of_row + 3 * beam, logit) == level;
+                }
+                const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+                __syncthreads();
+                if (lane == 0) sh.votes[wid] = hits;
+                __syncthreads();
+                uint32_t to = at + __popc(hits & ((1u << lane) - 1));
+#pragma unroll
+                for (int w = 0; w < kPickWarps; ++w) {
+                    const uint32_t more = __popc(sh.votes[w]);
+                    if (w < (int)wid) to += more;
+                    at += more;
+                }
+                if (hit && to < a.num) write_pick(a, request, to, level, beam, token);
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ BeamArgs a) {
     extern __shared__ double of_row[];                               // [beams][3]: score (NaN: no candidates), largest logit, log of the sum
     __shared__ PickList sh;
     grid_dependency_wait();
@@ -323,7 +421,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
         }
         if (lane == 0) of_row[3 * b] = valid;
     }
-    if (threadIdx.x == 0) sh.count = 0;
+    if (threadIdx.x == 0) sh.count = sh.unsure = sh.above = 0;
     __syncthreads();
     const uint32_t lists = a.beams * a.splits, entries = lists * a.num;
     auto entry = [&](uint32_t list, uint32_t at) {
@@ -336,10 +434,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
             return c;
         }
         const unsigned long long key = a.keys[((size_t)request * lists + list) * a.num + at];
-        if (key) {                                                   // the difference first: logits may be of any size
-            const double value = score + ((double)unordered((uint32_t)(key >> 32)) - of_row[3 * b + 1] - of_row[3 * b + 2]);
-            c = {ordered64(value), ~((unsigned long long)b << 32 | (uint32_t)~(uint32_t)key)};
-        }
+        if (key) c = {value_of(of_row + 3 * b, unordered((uint32_t)(key >> 32))), ~((unsigned long long)b << 32 | (uint32_t)~(uint32_t)key)};
         return c;
     };
     // A bound: the num-th of the leading entries of (some of) the lists, about four times num of them: what it leaves is little more than num.
@@ -350,6 +445,14 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
     bound_of(sh, some, a.num);
     __syncthreads();
     const uint32_t room = sample_of(a.num);                           // more than so many: another bound
+    // Lists were cut by the logit.  Where a full one's last entry may be among the picked and other logits have its value (scores so large, or logits so small, that
+    // 64 bits do not tell them apart), elements that were cut may come before others by their token.
+    auto unsure_behind = [&](uint32_t list) {
+        const uint32_t b = list / a.splits, row = request * a.beams + b;
+        if (a.ended && a.ended[row]) return false;
+        const uint32_t logit = (uint32_t)(a.keys[((size_t)request * lists + list) * a.num + a.num - 1] >> 32);
+        return !only_one(of_row + 3 * b, logit, value_of(of_row + 3 * b, unordered(logit)));
+    };
     while (true) {
         const Candidate bound = sh.bound;
         for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
@@ -358,6 +461,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
                 const uint32_t at = atomicAdd(&sh.count, 1u);
                 if (at < room) sh.list[at] = c;
             }
+            if (c.value && i % a.num == a.num - 1 && c.value >= bound.value && unsure_behind(i / a.num)) sh.unsure = 1;
         }
         __syncthreads();
         if (sh.count <= room) break;
@@ -367,18 +471,16 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
         __syncthreads();
     }
     const uint32_t n = sh.count;
+    if (sh.unsure && n >= a.num) {                                   // (the same for all threads)
+        pick_by_value(a, sh, of_row, request, n);
+        return;
+    }
     for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
         const Candidate x = sh.list[i];
         uint32_t above = 0;
 #pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
-        if (above < a.num) {
-            const size_t to = (size_t)request * a.num + above;
-            const unsigned long long bits = x.value & 0x8000000000000000ull ? x.value ^ 0x8000000000000000ull : ~x.value, order = ~x.order;
-            a.scores_out[to] = (float)__longlong_as_double((long long)bits);
-            a.parent_out[to] = (int32_t)(request * a.beams + (uint32_t)(order >> 32));
-            a.token_out[to] = (int32_t)(uint32_t)order;
-        }
+        if (above < a.num) write_pick(a, request, above, x.value, (uint32_t)(~x.order >> 32), (uint32_t)~x.order);
     }
     for (uint32_t i = n + threadIdx.x; i < a.num; i += kPickThreads) {
         const size_t to = (size_t)request * a.num + i;
@@ -388,7 +490,7 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(BeamArgs a) {
 }
 
 struct BeamShape {
-    uint32_t splits;
+    uint32_t splits, part;
     bool large;
     size_t keys, bytes;
 };
@@ -403,6 +505,7 @@ static BeamShape beam_shape(uint32_t requests, uint32_t beams, uint32_t vocab, u
     s.large = 2 * rows * eight >= (unsigned long long)sm_count();
     s.splits = (uint32_t)(s.large ? eight : two);
     s.keys = (size_t)rows * s.splits * num * sizeof(unsigned long long);
+    s.part = (uint32_t)((s.large ? 8 : 2) * one);
     s.bytes = (s.keys + (size_t)rows * s.splits * sizeof(float2) + 255) / 256 * 256;
     return s;
 }
@@ -437,7 +540,8 @@ extern "C" int roomie_beam_select(const void* logits, int32_t type, int64_t requ
     BeamArgs a = {};
     a.logits = logits; a.request_stride = request_stride; a.beam_stride = beam_stride;
     a.scores = scores; a.ended = ended;
-    a.requests = requests; a.beams = beams; a.vocab = vocab; a.num = num; a.pad = pad; a.splits = s.splits;
+    a.requests = requests; a.beams = beams; a.vocab = vocab; a.num = num; a.pad = pad; a.splits = s.splits; a.part = s.part;
+    a.type = type;
     a.keys = static_cast<unsigned long long*>(workspace);
     a.sums = reinterpret_cast<float2*>(static_cast<char*>(workspace) + s.keys);
     a.scores_out = scores_out; a.parent_out = parent_out; a.token_out = token_out;
