@@ -132,7 +132,10 @@ __device__ __forceinline__ void pick_best(PickShared& sh, const uint4* raw, cons
         __syncthreads();
     }
     bool full = hits <= kHits && sh.count > kList;                    // the list ran over (the same for all threads: the count is at rest)
-    for (bool own = hits > kHits; own || full; own = false) {
+    // Each trip with a full list leaves out sample - num candidates or more, which is 128 at least.
+    constexpr uint32_t kTrips = step * kVecs / 128 + 2;
+    uint32_t trip = 0;
+    for (bool own = hits > kHits; (own || full) && trip < kTrips; own = false, ++trip) {
         if (full) {
             const uint32_t sample = sample_of(num);
             for (uint32_t i = threadIdx.x; i < sample; i += kBeamThreads) {
@@ -159,7 +162,7 @@ __device__ __forceinline__ void pick_best(PickShared& sh, const uint4* raw, cons
         __syncthreads();
         full = sh.count > kList;
     }
-    const uint32_t n = sh.count;
+    const uint32_t n = min(sh.count, (uint32_t)kList);
     for (uint32_t i = threadIdx.x; i < n; i += kBeamThreads) {
         const unsigned long long x = sh.list[i];
         uint32_t above = 0;
@@ -276,7 +279,7 @@ constexpr int kPickThreads = 256, kPickWarps = kPickThreads / 32;
 struct PickList {
     Candidate list[kList], bound;
     unsigned long long level;
-    uint32_t count, unsure, above, votes[kPickWarps];
+    uint32_t count, unsure, above, votes[kPickWarps], hist[256];
 };
 
 // A beam's score, the largest logit of its row (or of nothing) and the logarithm of the row's sum, as the kernel has them for each beam.  A candidate's
@@ -287,6 +290,21 @@ __device__ __forceinline__ unsigned long long value_of(const double* of_beam, fl
 // Whether no other float32 near this logit has its value.
 __device__ __forceinline__ bool only_one(const double* of_beam, uint32_t logit, unsigned long long value) {
     return value_of(of_beam, unordered(logit - 1)) < value && value_of(of_beam, unordered(logit + 1)) > value;
+}
+
+// Entry `at` of a list, a part of a beam's row.  keys: the request's.
+__device__ __forceinline__ Candidate entry_of(const BeamArgs& a, const double* of_row, uint32_t request, const unsigned long long* keys, uint32_t list, uint32_t at) {
+    const uint32_t b = list / a.splits, row = request * a.beams + b;
+    const double score = of_row[3 * b];
+    Candidate c = {0, 0};
+    if (score != score) return c;
+    if (a.ended && a.ended[row]) {                                   // goes on as it is, with the padding token
+        if (list == b * a.splits && at == 0) c = {ordered64(score), ~((unsigned long long)b << 32 | a.pad)};
+        return c;
+    }
+    const unsigned long long key = keys[(size_t)list * a.num + at];
+    if (key) c = {value_of(of_row + 3 * b, unordered((uint32_t)(key >> 32))), ~((unsigned long long)b << 32 | (uint32_t)~(uint32_t)key)};
+    return c;
 }
 
 __device__ __forceinline__ void write_pick(const BeamArgs& a, uint32_t request, uint32_t at, unsigned long long value, uint32_t beam, uint32_t token) {
@@ -311,24 +329,63 @@ __device__ __forceinline__ void bound_of(PickList& sh, uint32_t n, uint32_t num)
     }
 }
 
-// The picks where lists may have been cut within candidates of one value.  Those above the num-th value are in the lists, fewer than num; of those that have
-// it the first by (beam, token) are looked for in the logits: in the parts whose best reaches it, of which 2 num at most are gone through, in order, up to the last one wanted.
-__device__ __noinline__ void pick_by_value(const BeamArgs& a, PickList& sh, const double* of_row, uint32_t request, uint32_t n) {
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, lists = a.beams * a.splits;
+// The num-th value of all lists, eight bits at a time, becomes the level, and the list what lies above it: fewer than num.
+__device__ __noinline__ void find_level(const BeamArgs& a, PickList& sh, const double* of_row, uint32_t request) {
+    const uint32_t entries = a.beams * a.splits * a.num;
+    const unsigned long long* keys = a.keys + (size_t)request * entries;
+    unsigned long long level = 0;
+    uint32_t left = a.num;
+#pragma unroll 1
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        sh.hist[threadIdx.x] = 0;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
+            const unsigned long long x = entry_of(a, of_row, request, keys, i / a.num, i % a.num).value;
+            if (shift == 56 || x >> (shift + 8) == level >> (shift + 8)) atomicAdd(&sh.hist[x >> shift & 255], 1u);
+        }
+        __syncthreads();
+        uint32_t d = 255;                                            // the digit in which the left-th lies
+        for (; d > 0 && sh.hist[d] < left; --d) left -= sh.hist[d];
+        level |= (unsigned long long)d << shift;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        sh.level = level;
+        sh.count = 0;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
+        const Candidate c = entry_of(a, of_row, request, keys, i / a.num, i % a.num);
+        if (c.value > level) {
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < kList) sh.list[at] = c;                         // (always, unless another call writes to the lists meanwhile)
+        }
+    }
+    __syncthreads();
+}
+
+// The num-th of a list's n becomes the level.
+__device__ __forceinline__ void level_of(PickList& sh, uint32_t n, uint32_t num) {
     for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
         const Candidate x = sh.list[i];
         uint32_t above = 0;
         for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
-        if (above == a.num - 1) sh.level = x.value;
+        if (above == num - 1) sh.level = x.value;
     }
     __syncthreads();
+}
+
+// The picks from the num-th value, the level: those above it are among the list's n, fewer than num; of those that have it the first by (beam, token) are looked for
+// in the logits, in the parts whose best reaches it, of which 2 num at most are gone through, in order, up to the last one wanted.
+__device__ __noinline__ void pick_by_value(const BeamArgs& a, PickList& sh, const double* of_row, uint32_t request, uint32_t n) {
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, lists = a.beams * a.splits;
     const unsigned long long level = sh.level;
     for (uint32_t i = threadIdx.x; i < n; i += kPickThreads) {
         const Candidate x = sh.list[i];
         if (x.value <= level) continue;
         uint32_t above = 0;
         for (uint32_t j = 0; j < n; ++j) above += over(sh.list[j], x);
-        write_pick(a, request, above, x.value, (uint32_t)(~x.order >> 32), (uint32_t)~x.order);
+        if (above < a.num) write_pick(a, request, above, x.value, (uint32_t)(~x.order >> 32), (uint32_t)~x.order);
         atomicAdd(&sh.above, 1u);
     }
     __syncthreads();
@@ -421,22 +478,14 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
         }
         if (lane == 0) of_row[3 * b] = valid;
     }
-    if (threadIdx.x == 0) sh.count = sh.unsure = sh.above = 0;
+    if (threadIdx.x == 0) {
+        sh.count = sh.unsure = sh.above = 0;
+        sh.level = 0;
+    }
     __syncthreads();
     const uint32_t lists = a.beams * a.splits, entries = lists * a.num;
-    auto entry = [&](uint32_t list, uint32_t at) {
-        const uint32_t b = list / a.splits, row = request * a.beams + b;
-        const double score = of_row[3 * b];
-        Candidate c = {0, 0};
-        if (score != score) return c;
-        if (a.ended && a.ended[row]) {                               // goes on as it is, with the padding token
-            if (list == b * a.splits && at == 0) c = {ordered64(score), ~((unsigned long long)b << 32 | a.pad)};
-            return c;
-        }
-        const unsigned long long key = a.keys[((size_t)request * lists + list) * a.num + at];
-        if (key) c = {value_of(of_row + 3 * b, unordered((uint32_t)(key >> 32))), ~((unsigned long long)b << 32 | (uint32_t)~(uint32_t)key)};
-        return c;
-    };
+    const unsigned long long* keys = a.keys + (size_t)request * entries;
+    auto entry = [&](uint32_t list, uint32_t at) { return entry_of(a, of_row, request, keys, list, at); };
     // A bound: the num-th of the leading entries of (some of) the lists, about four times num of them: what it leaves is little more than num.
     // (With num of them it left so many of 32 lists of 64 that the call took 330 us.)  Then as in pick_best.
     const uint32_t deep = min((4 * a.num + lists - 1) / lists, a.num), some = min(lists, (uint32_t)kPickThreads) * deep;   // deep > 1: lists < 4 num <= 512
@@ -450,28 +499,40 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
     auto unsure_behind = [&](uint32_t list) {
         const uint32_t b = list / a.splits, row = request * a.beams + b;
         if (a.ended && a.ended[row]) return false;
-        const uint32_t logit = (uint32_t)(a.keys[((size_t)request * lists + list) * a.num + a.num - 1] >> 32);
+        const uint32_t logit = (uint32_t)(keys[(size_t)list * a.num + a.num - 1] >> 32);
         return !only_one(of_row + 3 * b, logit, value_of(of_row + 3 * b, unordered(logit)));
     };
-    while (true) {
+    // One trip as a rule.  A bound may leave out little, as where the best of many lists are the last ones: after a few trips the num-th value is found by its bits,
+    // in eight more (64 rising beams x 131072 words, 64 wanted: 2.3 ms, with nothing but trips 4.2; 256 x 128256 in float32, 128 wanted: 31, was 87).
+    constexpr uint32_t kTrips = 16;
+    for (uint32_t trip = 1;; ++trip) {
         const Candidate bound = sh.bound;
         for (uint32_t i = threadIdx.x; i < entries; i += kPickThreads) {
-            const Candidate c = entry(i / a.num, i % a.num);
-            if (c.value && !over(bound, c)) {
-                const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < room) sh.list[at] = c;
+            const uint32_t list = i / a.num, place = i - list * a.num;
+            const Candidate c = entry(list, place);
+            if (c.value && c.value >= bound.value) {
+                if (!over(bound, c)) {
+                    const uint32_t at = atomicAdd(&sh.count, 1u);
+                    if (at < room) sh.list[at] = c;
+                }
+                if (place == a.num - 1 && unsure_behind(list)) sh.unsure = 1;
             }
-            if (c.value && i % a.num == a.num - 1 && c.value >= bound.value && unsure_behind(i / a.num)) sh.unsure = 1;
         }
         __syncthreads();
-        if (sh.count <= room) break;
+        if (sh.count <= room || trip == kTrips) break;
         __syncthreads();
         if (threadIdx.x == 0) sh.count = 0;
         bound_of(sh, room, a.num);
         __syncthreads();
     }
     const uint32_t n = sh.count;
-    if (sh.unsure && n >= a.num) {                                   // (the same for all threads)
+    if (n > room) {                                                  // (the same for all threads, and below)
+        find_level(a, sh, of_row, request);
+        pick_by_value(a, sh, of_row, request, min(sh.count, (uint32_t)kList));
+        return;
+    }
+    if (sh.unsure && n >= a.num) {
+        level_of(sh, n, a.num);
         pick_by_value(a, sh, of_row, request, n);
         return;
     }

@@ -143,6 +143,14 @@ def test_beams_in_rising_order(torch, rm, beams, vocab, num):
     assert (mine - order.values[:num]).abs().max() < 2 * SLACK and len(set(zip(got[1][0].tolist(), got[2][0].tolist()))) == num
 
 
+@pytest.mark.parametrize("beams,vocab,num", [(256, 33000, 128), (200, 40000, 100), (256, 50, 128)])
+def test_beams_of_one_value_in_rising_order(torch, rm, beams, vocab, num):
+    """So far apart that the logits do not count: the last beam's lowest tokens, then those of the beam before it."""
+    x = torch.randn((2, beams, vocab), generator=torch.Generator().manual_seed(beams)).half().cuda()
+    scores = (torch.arange(-beams, 0).float() * 2.0 ** 90).expand(2, beams).contiguous().cuda()
+    check(torch, rm, x, scores, num)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_scores_updated_in_place(torch, rm, dtype):
     """scores_out may be scores where as many are wanted as there are beams."""
