@@ -522,7 +522,8 @@ int roomie_kv_attention(const roomie_kv_cache *cache /* host */, uint32_t layer,
  *   reorder  sequence seqs[i] becomes what sequence seqs[parents[i]] was before the call (parents[i] in [0, n), repeated or left out at will;
  *            -1: empty), in place: whole pages are shared; a part-filled last page goes to the first child, the others get copies, in the lowest
  *            pages that are free once those without a child have been given up.  All or nothing: where a sequence is named twice, an index or length is out
- *            of range, a page is not one or has too few references, or the free pages do not suffice, nothing changes but the status.  n is at most 8192;
+ *            of range, a sequence's page is not one or would afterwards count fewer holders than this sequence's children, or the free pages do not suffice,
+ *            nothing changes but the status.  n is at most 8192;
  *   copy     page src_pages[i] of src to page dst_pages[i] of dst, codes and scales of all layers (n pairs; the caches
  *            agree in layers, page_tokens, kv_heads, head_dim, format and layout; no page may be written twice, or both
  *            read and written); tables and counts are left alone;

@@ -283,9 +283,10 @@ __host__ __device__ __forceinline__ ReorderView reorder_view(int32_t* ws, uint32
 }
 constexpr uint32_t kReorderMost = 8192;                           // sequences of a call: a column of their rows fits shared memory
 
-// The pages of the sequences whose number of holders changes, by a warp each: `f(page, change)`.  A whole page has a holder for each child instead
-// of one; the part-filled last page goes to the first child, and is given up when there is none.
-template <class F> __device__ __forceinline__ void held_pages(const TableView& t, const int32_t* seqs, uint32_t n, const ReorderView& v, F f) {
+// The table's entries of the call's sequences, a sequence by a warp: `f(page, more)`, more: how many holders the page gets beyond the one that it has here.  A whole
+// page has one for each child; the part-filled last page goes to the first child, and is given up when there is none.  kChanging: of the sequences alone
+// where that changes anything.
+template <bool kChanging, class F> __device__ __forceinline__ void held_pages(const TableView& t, const int32_t* seqs, uint32_t n, const ReorderView& v, F f) {
     const uint32_t lane = threadIdx.x & 31;
     for (uint32_t base = threadIdx.x >> 5; base < n; base += 32 * kPlanWarps) {      // 32 sequences of a warp at a time: a lane asks for each
         const uint32_t mine = base + lane * kPlanWarps;
@@ -293,7 +294,7 @@ template <class F> __device__ __forceinline__ void held_pages(const TableView& t
         for (uint32_t i = 0; i < 32 && base + i * kPlanWarps < n; ++i) {
             const int32_t len = __shfl_sync(0xffffffffu, my_len, i), children = __shfl_sync(0xffffffffu, my_children, i);
             const int32_t slot = __shfl_sync(0xffffffffu, my_slot, i);
-            if (len <= 0 || children == 1) continue;
+            if (len <= 0 || (kChanging && children == 1)) continue;
             const uint32_t held = pages_of(t, (uint32_t)len), whole = (uint32_t)len >> t.page_shift;
             const int32_t* row = t.pages + (size_t)slot * t.max_pages;
             for (uint32_t e0 = 0; e0 < held; e0 += 128) {                            // four entries of a lane under way
@@ -311,7 +312,7 @@ template <class F> __device__ __forceinline__ void held_pages(const TableView& t
 }
 
 // One block, for the counts' sake: they are changed, looked at, and taken back where the whole does not fit.  Bound by latency: 32 x 8 beams of 2248
-// tokens take 18 us, most of it the two passes over the pages that change holders.
+// tokens take 20 us, most of it the pass over the pages that change holders and the one that looks at all.
 __global__ void __launch_bounds__(kPlanThreads) reorder_plan_kernel(TableView t, const int32_t* seqs, const int32_t* parents, uint32_t n, int32_t* ws) {
     __shared__ uint32_t sh[kPlanWarps], widest;
     const ReorderView v = reorder_view(ws, n);
@@ -340,13 +341,13 @@ __global__ void __launch_bounds__(kPlanThreads) reorder_plan_kernel(TableView t,
     }
     bool refused = __syncthreads_or(bad) != 0;
     if (!refused) {
-        held_pages(t, seqs, n, v, [&](int32_t id, int32_t change) {
-            if (id < 0 || (uint32_t)id >= t.num_pages) bad |= ROOMIE_FLAG_KV_PAGE;
-            else if (change) atomicAdd(t.refs + id, change);
+        held_pages<true>(t, seqs, n, v, [&](int32_t id, int32_t more) {
+            if (more && (uint32_t)id < t.num_pages) atomicAdd(t.refs + id, more);
         });
         __syncthreads();
-        held_pages(t, seqs, n, v, [&](int32_t id, int32_t) {
-            if (id >= 0 && (uint32_t)id < t.num_pages && t.refs[id] < 0) bad |= ROOMIE_FLAG_KV_PAGE;
+        // Every entry is a page, and counts for what this sequence hands on, so that none of them is among the free ones below.
+        held_pages<false>(t, seqs, n, v, [&](int32_t id, int32_t more) {
+            if ((uint32_t)id >= t.num_pages || t.refs[id] < more + 1) bad |= ROOMIE_FLAG_KV_PAGE;
         });
         const bool broken = __syncthreads_or(bad) != 0;
         // copies of part-filled pages, in order, to the lowest pages that are free now
@@ -365,8 +366,8 @@ __global__ void __launch_bounds__(kPlanThreads) reorder_plan_kernel(TableView t,
         refused = broken || found < copies;
         if (refused) {                                            // as it was
             if (!broken) bad |= ROOMIE_FLAG_KV_FULL;
-            held_pages(t, seqs, n, v, [&](int32_t id, int32_t change) {
-                if (id >= 0 && (uint32_t)id < t.num_pages && change) atomicSub(t.refs + id, change);
+            held_pages<true>(t, seqs, n, v, [&](int32_t id, int32_t more) {
+                if (more && (uint32_t)id < t.num_pages) atomicSub(t.refs + id, more);
             });
         }
     }
