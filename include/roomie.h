@@ -563,7 +563,7 @@ int roomie_kv_weights(const roomie_kv_cache *cache /* host */, uint32_t layer, c
  *   Each page and head gets the scale that append would give its values (a power of two); codes whose scale stays move as they are, others are
  * rescaled in float32 and rounded once.  A page that another sequence holds too is replaced by a free one, pages behind the kept tokens lose a
  * reference.  Requests are served in order while the pages that were free before the call suffice; others change nothing and set
- * ROOMIE_FLAG_KV_FULL.  A sequence named again, or one with a table entry that is no page, is left as it is and reported.
+ * ROOMIE_FLAG_KV_FULL.  A sequence named again, or one with a table entry that is no page or a free one, is left as it is and reported.
  *   Lengths are no longer positions afterwards: rotate with positions of one's own (roomie_rope, roomie_qk_norm_rope) and append without `rope`.
  * first + recent <= keep, keep > 0; max_pages * page_tokens at most 2^20.  Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
 int roomie_kv_evict(const roomie_kv_cache *cache /* host */, const int32_t *seqs, uint32_t n, const float *weight, uint32_t keep, uint32_t first,

@@ -42,9 +42,9 @@ __global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(TableView t, c
             bool broken = false;
             for (uint32_t e = lane; e < pages_of(t, (uint32_t)len); e += 32) {
                 const int32_t id = row[e];
-                const bool there = id >= 0 && (uint32_t)id < t.num_pages;
-                broken = broken || !there;
-                shared += e < now && there && t.refs[id] > 1;
+                const int32_t holders = id >= 0 && (uint32_t)id < t.num_pages ? t.refs[id] : 0;
+                broken = broken || holders < 1;                   // no page, or one that counts as free and may be handed out here
+                shared += e < now && holders > 1;
             }
             if (__any_sync(0xffffffffu, broken)) {
                 bad |= ROOMIE_FLAG_KV_PAGE;

@@ -1,8 +1,8 @@
-"""Reordering where the table or the counts are not what they should be, or the pages do not suffice: nothing is changed but the status."""
+"""Reordering and eviction where the table or the counts are not what they should be, or the pages do not suffice: nothing is changed but the status."""
 import numpy as np
 import pytest
 
-from test_gpu_bounded_cache import FLAG_PAGE, check_reorder, state, unchanged
+from test_gpu_bounded_cache import FLAG_PAGE, check_evict, check_reorder, state, unchanged
 from test_gpu_serving import make_cache
 
 pytestmark = pytest.mark.gpu
@@ -78,3 +78,11 @@ def test_reorder_takes_back_what_it_counted(torch, rm):
         rm.kv_free(cache, everyone)
         assert not cache.refs.any() and cache.status_flags() == 0
     assert full > 20 and served > 20
+
+
+def test_evict_leaves_a_sequence_whose_page_counts_as_free(torch, rm):
+    """Such a page may be handed out in the same call to another sequence: neither is the sequence cut, nor its counts changed."""
+    for entry in (0, 3, 9):
+        cache = make_cache(torch, rm, [160, 160, 160], page=16, slots=3, extra=16)
+        cache.refs[cache.pages[1, entry].item()] = 0
+        check_evict(torch, rm, cache, [0, 1, 2], 50, served=[0, 2], flags=FLAG_PAGE)
