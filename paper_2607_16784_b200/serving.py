@@ -77,6 +77,13 @@ def _here(index, *tensors):
     raise ValueError(f"all tensors of a call live on the current CUDA device ({device}), got one on {index}")
 
 
+def _u32(x, what):
+    """ctypes takes the low 32 bits of a number: 2^32 + 5 would become the call with 5."""
+    if not 0 <= x < 1 << 32:
+        raise ValueError(f"{what}: a number of at most 32 bits, not negative, got {x}")
+    return x
+
+
 def _on_stream(call):
     """With stream= given, what the binding itself allocates or copies is ordered on that stream too."""
     @functools.wraps(call)
@@ -94,8 +101,9 @@ def _stream(t):
 
 def rope_frequencies(rotary_dim, base=10000.0, factor=1.0, context=0, low_turns=1.0, high_turns=4.0):
     """roomie_rope_frequencies: turns per position in units of 2^-64, a host array uint64 [rotary_dim / 2]."""
-    out = np.empty(max(int(rotary_dim) // 2, 1), dtype=np.uint64)
-    _check(_dll.roomie_rope_frequencies(int(rotary_dim), float(base), float(factor), float(context), float(low_turns),
+    rotary_dim = _u32(max(int(rotary_dim), 0), "rotary_dim")
+    out = np.empty(max(rotary_dim // 2, 1), dtype=np.uint64)
+    _check(_dll.roomie_rope_frequencies(rotary_dim, float(base), float(factor), float(context), float(low_turns),
                                         float(high_turns), out.ctypes.data), "roomie_rope_frequencies")
     return out
 
@@ -349,7 +357,7 @@ def kv_append(cache: KVCache, seqs, k, v, q_offset=None, *, layer=0, rope: RopeT
     """roomie_kv_append: rows of k, v [rows, kv_heads, head_dim] become the last tokens of sequences `seqs` (rows
     q_offset[i]..q_offset[i+1] of sequence i; None: one row each), rotated when `rope` is given.  With `q` its rotated rows are
     returned in q_out (q itself, or its copy in q_out, without `rope`).  For serving: no gradient passes through."""
-    rows, d = k.shape[0], cache.head_dim
+    rows, d, layer = k.shape[0], cache.head_dim, _u32(layer, "layer")
     if k.shape[1:] != (cache.kv_heads, d) or k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k, v: [rows, kv_heads, head_dim] of one type")
     seqs = _ids(seqs, "seqs")
@@ -388,6 +396,7 @@ def kv_attention(cache: KVCache, seqs, q, q_offset=None, *, layer=0, scale=None,
     """roomie_kv_attention: q [rows, q_heads, head_dim] over the cached tokens of `seqs`.  Returns (out, lse); rows of no sequence are
     not written.  For serving: no gradient passes through."""
     rows, heads, d = q.shape
+    layer, window = _u32(layer, "layer"), _u32(window, "window")
     if d != cache.head_dim or heads % cache.kv_heads:
         raise ValueError("q: [rows, q_heads, head_dim] with q_heads a multiple of the cache's kv_heads")
     seqs = _ids(seqs, "seqs")
@@ -459,6 +468,7 @@ def kv_weights(cache: KVCache, seqs, q, lse, weight, q_offset=None, *, layer=0, 
     kv_attention, lse what it returned.  The call's own tokens start from nothing; with `fresh` all of the sequences' do.  A sequence is named once.
     Returns weight."""
     rows, heads, d = q.shape
+    layer, window = _u32(layer, "layer"), _u32(window, "window")
     if d != cache.head_dim or heads % cache.kv_heads:
         raise ValueError("q: [rows, q_heads, head_dim] with q_heads a multiple of the cache's kv_heads")
     if tuple(lse.shape) != (rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
@@ -484,8 +494,7 @@ def kv_evict(cache: KVCache, seqs, weight, keep, *, first=0, recent=0, weight_ou
     weight_out = weight if weight_out is None else weight_out
     _key_weights(cache, weight, "weight")
     _key_weights(cache, weight_out, "weight_out")
-    if min(keep, first, recent) < 0:
-        raise ValueError("keep, first, recent: 0 or more")
+    keep, first, recent = _u32(keep, "keep"), _u32(first, "first"), _u32(recent, "recent")
     _here(cache.index, seqs, weight, weight_out, workspace)
     workspace = _scratch(cache, workspace)
     _check(_dll.roomie_kv_evict(cache.ref, seqs.data_ptr(), seqs.numel(), weight.data_ptr(), keep, first, recent, weight_out.data_ptr(), workspace.data_ptr(),
@@ -522,8 +531,8 @@ def kv_compact(cache: KVCache, *, refs_out=None, pages_out=None, used_out=None, 
 
 def beam_workspace(requests, beams, vocab, num, dtype=torch.float32, device="cuda"):
     """Device scratch for beam_select calls of this shape; keep it and pass it to each of them."""
-    kind = _TYPES.get(dtype)
-    size = 0 if kind is None else int(_dll.roomie_beam_workspace_bytes(int(requests), int(beams), int(vocab), int(num), kind))
+    kind, sizes = _TYPES.get(dtype), [int(x) for x in (requests, beams, vocab, num)]
+    size = 0 if kind is None or not all(0 <= x < 1 << 32 for x in sizes) else int(_dll.roomie_beam_workspace_bytes(*sizes, kind))
     if size == 0:
         raise ValueError("beam shape outside the library's limits (requests * beams up to 65535, beams up to 256, vocab up to 2^24, num up to 128)")
     return torch.empty(size, dtype=torch.uint8, device=device)
@@ -539,7 +548,7 @@ def beam_select(logits, scores, num, *, ended=None, pad=0, out=None, workspace=N
     if kind is None or len(stride) != 3 or not logits.is_cuda or (stride[2] != 1 and logits.shape[2] > 1):
         raise ValueError("logits: a [requests, beams, vocab] CUDA tensor of float32, float16 or bfloat16 whose last dimension is contiguous")
     requests, beams, vocab = logits.shape
-    shape = (requests, beams)
+    shape, num, pad = (requests, beams), _u32(num, "num"), _u32(pad, "pad")
     if tuple(scores.shape) != shape or scores.dtype != torch.float32 or not scores.is_contiguous():
         raise ValueError("scores: a contiguous float32 tensor [requests, beams]")
     if ended is not None and (tuple(ended.shape) != shape or ended.dtype not in (torch.bool, torch.uint8) or not ended.is_contiguous()):
