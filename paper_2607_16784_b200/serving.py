@@ -11,6 +11,7 @@ from contextlib import contextmanager
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from .roomie import RoomieError, _check, _dll, _ptr
 
@@ -132,10 +133,18 @@ class RopeTable:
         self.ref = C.byref(self.c)
 
 
+def _no_tangent(call, *tensors):
+    """There are gradients, but no forward-mode derivatives: a result without the tangent that its inputs have would be a wrong one."""
+    # (outside of every level, which is as good as always, this is all: the number of the level is not public, without it every call asks)
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError(f"{call}: no forward-mode derivative")
+
+
 @_on_stream
 def rope(x, positions, table: RopeTable, *, inverse=False, out=None):
     """roomie_rope: x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); `inverse` is the gradient.
     `out` may be x itself.  Returns out.  Without `out` the call is differentiable in x."""
+    _no_tangent("rope", x)
     if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
         if out is not None:
             raise ValueError("out: not where a gradient is wanted")
@@ -188,6 +197,7 @@ def qk_norm_rope(q, k, positions, table: RopeTable | None, q_weight=None, k_weig
     """roomie_qk_norm_rope: q and k [tokens, heads, head_dim] (k may be None), each head divided by its root mean square, times its weight
     [head_dim] (None: ones), turned to `positions` (int32 [tokens]; table None: not turned).  Outputs may be the inputs.  Returns
     (q_out, k_out).  Without outputs given the call is differentiable, once, in q, k and the weights."""
+    _no_tangent("qk_norm_rope", q, k, q_weight, k_weight)
     if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad) or
                                     any(t is not None and t.requires_grad for t in (q_weight, k_weight, q_out, k_out))):
         if q_out is not None or k_out is not None:

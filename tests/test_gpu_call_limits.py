@@ -45,3 +45,28 @@ def test_numbers_past_32_bits(torch, rm):
     assert cache.status_flags() == 0 and torch.equal(w, old)
     for n in names:
         assert torch.equal(getattr(cache, n).view(torch.uint8), before[n].view(torch.uint8)), n
+
+
+def test_forward_mode_is_refused(torch, rm):
+    """A tangent that would be lost is an error; beside tensors without one the calls go on."""
+    import torch.autograd.forward_ad as fw
+    q, k = torch.randn(3, 4, 64, device="cuda"), torch.randn(3, 2, 64, device="cuda")
+    w, positions, table = torch.rand(64, device="cuda") + 0.5, torch.arange(3, dtype=torch.int32, device="cuda"), rm.RopeTable(64)
+    want, turned = rm.qk_norm_rope(q, k, positions, table, w, w), rm.rope(q, positions, table)
+    with fw.dual_level():
+        dual = lambda t: fw.make_dual(t, torch.ones_like(t))
+        for args in ((dual(q), k, positions, table, w, w), (q, dual(k), positions, table, w, w), (q, k, positions, table, dual(w), None), (q, k, positions, None, None, dual(w)),
+                     (dual(q.clone().requires_grad_()), k, positions, table, w, w)):
+            with pytest.raises(RuntimeError, match="forward"):
+                rm.qk_norm_rope(*args)
+        for x in (dual(q), dual(q.clone().requires_grad_())):
+            with pytest.raises(RuntimeError, match="forward"):
+                rm.rope(x, positions, table)
+        with torch.no_grad(), pytest.raises(RuntimeError, match="forward"):
+            rm.rope(dual(q), positions, table)
+        assert all(torch.equal(a, b) for a, b in zip(rm.qk_norm_rope(q, k, positions, table, w, w), want)) and torch.equal(rm.rope(q, positions, table), turned)
+    assert all(torch.equal(a, b) for a, b in zip(rm.qk_norm_rope(q, k, positions, table, w, w), want))
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(lambda x: rm.qk_norm_rope(x, k, positions, table, w, w)[0], (q,), (torch.ones_like(q),))
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(lambda x: rm.rope(x, positions, table), (q,), (torch.ones_like(q),))
