@@ -69,7 +69,8 @@ def search(requests, beams, prompt, steps, keep, q_heads=32, kv_heads=8, head_di
     read_out = (rand(q_heads * head_dim, vocab) * 0.2).to(torch.bfloat16)
     q_weight, k_weight = 1 + 0.1 * rand(head_dim), 1 + 0.1 * rand(head_dim)
     width = -(-max(prompt, keep + every) // page_tokens)
-    cache = rm.KVCache(total * (width + 1), page_tokens, kv_heads, head_dim, total, width)
+    # a cut replaces the pages that beams share, out of those that are free before it: as many again as the sequences hold
+    cache = rm.KVCache(2 * total * width, page_tokens, kv_heads, head_dim, total, width)
     workspace, table, weight = cache.workspace(), rm.RopeTable(head_dim), cache.key_weights()
 
     def step(slots, words, positions, lengths, offset, fresh):
