@@ -548,7 +548,8 @@ int roomie_kv_compact(const roomie_kv_cache *cache /* host */, int32_t *refs_out
  * [rows][q_heads] (float32) of the same q, scale and window this takes; so a row's shares add up to 1.
  *   weight [layers][max_seqs][kv_heads][max_pages * page_tokens] float32: the sums are added to what is there for the sequence's earlier tokens, and
  * replace it for the call's own ones (which have received nothing before); with `fresh`, for all its tokens.  What lies behind a sequence's length
- * is not touched.  A key on a page that is none receives nothing.  A sequence is named once in a call.
+ * is not touched.  A key on a page that is none receives nothing.  A sequence without rows in the call is left as it is, with `fresh` too; one
+ * named again is reported (ROOMIE_FLAG_KV_SEQUENCE) and its rows there give nothing.
  *   Float32 sums of products of the codes with q (up to 8 rows a sequence and key head on average, the queries as float16 against the row's largest, which leaves their bits but below
  * 2^-14 of it; more rows as they are).  A NaN reaches the keys that its row sees, or the key whose code it is; not others.  The same call gives the same bits.
  * q: F16 or BF16.  Errors: INVALID_ARG, CUDA. */

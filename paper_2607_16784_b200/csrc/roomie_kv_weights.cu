@@ -50,6 +50,39 @@ struct WeightSeq {                                   // a sequence of the call, 
     uint32_t slot, row, count, length, step0, steps; // step0: a head's first step, of `steps`
 };
 
+// Whether the call may name a sequence twice: a bit for each slot, or for each group of slots where there are more than bits.
+struct SlotBits {
+    uint32_t *bits, words;
+    __device__ __forceinline__ bool seen(uint32_t slot, uint32_t max_seqs) const {       // and from now on it is
+        const uint32_t bit = words * 32 >= max_seqs ? slot : slot % (words * 32);
+        return slot < max_seqs && (atomicOr(bits + bit / 32, 1u << (bit & 31)) >> (bit & 31) & 1);
+    }
+};
+// All threads of the block.  A call of one `batch` is asked about when its sequences have come anyway (a pass in front of them: 0.6 us), a longer one here.
+__device__ __forceinline__ bool maybe_twice(const WeightArgs& a, SlotBits& b, uint32_t batch) {
+    b.words = min(b.words, (a.c.max_seqs + 31) / 32);
+    for (uint32_t w = threadIdx.x; w < b.words; w += blockDim.x) b.bits[w] = 0;
+    if (a.num_seqs <= batch) return false;
+    __syncthreads();
+    bool twice = false;
+    for (uint32_t i = threadIdx.x; i < a.num_seqs; i += 8 * blockDim.x) {           // eight under way (2000 sequences: 6.5 us, one 8)
+        int32_t slot[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) slot[k] = i + k * blockDim.x < a.num_seqs ? a.seqs[i + k * blockDim.x] : -1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) twice |= b.seen((uint32_t)slot[k], a.c.max_seqs);
+    }
+    return __syncthreads_or(twice) != 0;
+}
+// ... and if so, whether an earlier one of the call is the same as the i-th.
+__device__ __forceinline__ bool named_before(const WeightArgs& a, uint32_t i, bool report) {
+    const int32_t slot = a.seqs[i];
+    bool before = false;
+    for (uint32_t j = 0; j < i && !before; ++j) before = a.seqs[j] == slot;
+    if (before && report) kv_flag(a.c.status, ROOMIE_FLAG_KV_SEQUENCE);
+    return before;
+}
+
 template <int DP, int kFormat, class T>
 __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks) few_weights_kernel(WeightArgs a) {
     using F = FewWeights<DP>;
@@ -61,6 +94,8 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks) few_weights_ker
     const KvView& kv = a.c;
     uint8_t* ring = smem + wid * F::kRing;
     const unsigned long long me = (unsigned long long)blockIdx.x * kWeightWarps + wid, all_warps = (unsigned long long)gridDim.x * kWeightWarps;
+    SlotBits slots = {reinterpret_cast<uint32_t*>(smem), F::kSmem / 4};
+    bool twice = maybe_twice(a, slots, kWeightThreads);
 
     for (uint32_t base = 0; base < a.num_seqs; base += kWeightThreads) {
         const uint32_t here = min(a.num_seqs - base, (uint32_t)kWeightThreads);
@@ -76,6 +111,8 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocks) few_weights_ker
             w.steps = s.count ? (s.length + F::kStep - 1) / F::kStep - w.step0 : 0u;
             mine = (unsigned long long)w.steps * kv.heads;
         }
+        if (a.num_seqs > 1 && a.num_seqs <= kWeightThreads) twice = __syncthreads_or(threadIdx.x < here && slots.seen((uint32_t)a.seqs[threadIdx.x], kv.max_seqs)) != 0;
+        if (twice && threadIdx.x < here && named_before(a, base + threadIdx.x, blockIdx.x == 0)) mine = w.steps = 0;
         unsigned long long upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -696,6 +733,8 @@ __global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_k
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    SlotBits slots = {reinterpret_cast<uint32_t*>(codes), M::kCodes / 4};
+    bool twice = maybe_twice(a, slots, kManySeqs);
     uint32_t block = 0, units = 0;                                   // of this block, each role in step with the others
     unsigned long long before = 0;                                   // units of the sequences so far
     for (uint32_t base = 0; base < a.num_seqs; base += kManySeqs) {
@@ -711,6 +750,8 @@ __global__ void __launch_bounds__(kManyThreads, Many<DP>::kPerSm) many_weights_k
             w.steps = s.count ? (s.length + kManyKeys - 1) / kManyKeys - w.step0 : 0u;
             mine = (unsigned long long)w.steps * a.c.heads;
         }
+        if (a.num_seqs > 1 && a.num_seqs <= kManySeqs) twice = __syncthreads_or(threadIdx.x < here && slots.seen((uint32_t)a.seqs[threadIdx.x], a.c.max_seqs)) != 0;
+        if (twice && threadIdx.x < here && named_before(a, base + threadIdx.x, blockIdx.x == 0)) mine = w.steps = 0;
         unsigned long long upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {

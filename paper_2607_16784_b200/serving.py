@@ -475,7 +475,7 @@ def kv_reorder(cache: KVCache, seqs, parents, *, workspace=None):
 @_on_stream
 def kv_weights(cache: KVCache, seqs, q, lse, weight, q_offset=None, *, layer=0, scale=None, window=0, fresh=False):
     """roomie_kv_weights: adds to `weight` (cache.key_weights()) what the rows of q give to the keys of their sequences: q, q_offset, scale and window as in
-    kv_attention, lse what it returned.  The call's own tokens start from nothing; with `fresh` all of the sequences' do.  A sequence is named once.
+    kv_attention, lse what it returned.  The call's own tokens start from nothing; with `fresh` all of the sequences' do.  A sequence named again is reported.
     Returns weight."""
     rows, heads, d = q.shape
     layer, window = _u32(layer, "layer"), _u32(window, "window")
