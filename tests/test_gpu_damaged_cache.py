@@ -80,6 +80,14 @@ def test_reorder_takes_back_what_it_counted(torch, rm):
     assert full > 20 and served > 20
 
 
+def test_reorder_into_pages_that_the_call_gives_back(torch, rm):
+    """In a full pool: a copy fits where a sequence ends, and nothing is changed where none does."""
+    cache = make_cache(torch, rm, [20, 17], page=16, extra=0, slots=3)
+    assert not check_reorder(torch, rm, cache, [0, 1, 2], [0, 1, 0])
+    assert check_reorder(torch, rm, cache, [0, 1, 2], [0, 0, 0])
+    assert int((cache.refs == 0).sum()) == 0 and int(cache.refs.max()) == 3
+
+
 def test_evict_leaves_a_sequence_whose_page_counts_as_free(torch, rm):
     """Such a page may be handed out in the same call to another sequence: neither is the sequence cut, nor its counts changed."""
     for entry in (0, 3, 9):
