@@ -577,7 +577,9 @@ int roomie_kv_evict(const roomie_kv_cache *cache /* host */, const int32_t *seqs
  * The outputs overlap nothing else of the call, except that scores_out may be scores where num == beams.
  *   A logit of -infinity is no candidate.  A beam whose score is not finite, or whose row holds NaN or +infinity, or nothing above -infinity, has none.
  *   A beam with ended != 0 (ended may be NULL) has one: itself, with its score and the token `pad`; its logits are not read.
- * Sums of exponentials are float32 over a thread's 8 to 64 logits and a block's threads, 64 bits from there on; scores are compared in 64 bits.
+ * Sums of exponentials are float32 over a thread's 8 to 64 logits and a block's threads, 64 bits from there on; scores are compared in 64 bits, equal ones among them
+ * whose logits differ.  So the order within a beam is exact; between beams it is that of scores which the sums may move by 3e-5 at most.  `ended` must not change
+ * while the call runs.
  * Limits: beams 1..256, vocab 1..2^24, num 1..128, requests * beams <= 65535.  workspace: roomie_beam_workspace_bytes of the same shape (0 where
  * it is outside these limits), 256-byte aligned, nothing in it is kept.  Errors: INVALID_ARG, CAPACITY (workspace), CUDA. */
 size_t roomie_beam_workspace_bytes(uint32_t requests, uint32_t beams, uint32_t vocab, uint32_t num, int32_t type);

@@ -29,7 +29,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // ---- few rows a key head -----------------------------------------------------------------------------------------------------------
 // As in attention over few rows: S^T = K q^T by 16x8x16 products, a lane's span of a key contiguous, every warp with steps of codes under way to its
 // own part of shared memory.  The flat order (sequence, head, step of keys) is cut into equal shares for the call's warps.  Bound by the bytes
-// of the codes: 64 sequences of up to 16384 keys (764 MB) take 145 us, 5280 GB/s; of up to 4096 (191 MB) 44, of which 10 are the way from the lengths over
+// of the codes: 64 sequences of up to 16384 keys (764 MB) take 145 us, 5280 GB/s; of up to 4096 (191 MB) 45, of which 10 are the way from the lengths over
 // the table to the first codes.  Instructions come next (some 450 of a warp for 32 keys): with places in the flat order worked out anew for each
 // step it took 60, with 12 warps an SM instead of 16 51.
 constexpr int kWeightWarps = 4, kWeightThreads = 32 * kWeightWarps;
